@@ -405,6 +405,151 @@ int ls_kv_commit_paged(const ls_desc *desc, const void *k_tree, const void *v_tr
                        const int32_t *block_table, int32_t bt_stride, int32_t page_size,
                        int32_t *new_prefix_lens, int32_t *err_flag, void *stream);
 
+/* ---- a step of new tokens into a paged cache ------------------------------------------- */
+
+/*
+ * What a serving program does before and between verification rounds (an extension beyond the
+ * paper, like the paged cache itself): it hands out pages for the new tokens of a step, rotates
+ * queries and keys by their positions, writes keys and values into the pages, and attends from
+ * the new tokens to everything their request has cached.  The tokens of all requests are packed
+ * one after the other: request b owns tokens cu_new[b] .. cu_new[b+1] - 1.  The pages are those
+ * that ls_hybrid_tree_attn_paged, ls_cache_attn_paged and ls_kv_commit_paged read and write.
+ */
+#define LS_MAX_STEP_BATCH 4096
+
+typedef struct {
+    int32_t batch;       /* 1 .. LS_MAX_STEP_BATCH */
+    int32_t n_tokens;    /* entries of slots / positions; 0: pages only, both are NULL */
+    int32_t page_size;   /* a power of two */
+    int32_t n_pages;     /* pages of the pool; n_pages * page_size <= 2^31 - 1 */
+    int32_t bt_stride;   /* entries per request of the block table */
+} ls_page_desc;
+
+/*
+ * Block tables, slots and positions of a step from the requests' lengths.  Request b has
+ * kv_lens[b] cached rows and new_lens[b] new ones; afterwards it holds
+ * ceil((kv_lens[b] + new_lens[b]) / page_size) pages, whatever pages_held[b] it held before
+ * (entries 0 .. pages_held[b] - 1 of its row of the block table).  So both lengths 0 end a
+ * request, and pages reserved for tokens that were not accepted go back by themselves.
+ *
+ *   Pages that a request gives back go on top of the stack of free pages, request after request
+ *   in order of their table entries; pages handed out then come from the top, request after
+ *   request, ascending in the table.  A request whose new pages are no longer there gets none
+ *   (the first one that does not fit, and every later one that needs a page).
+ *
+ *   kv_lens, new_lens, pages_held  DEVICE int32[batch], read
+ *   block_table     DEVICE int32[batch, bt_stride]; the entries of pages handed out are written
+ *   free_pages      DEVICE int32[n_pages]: the stack, free_count[0] entries, the last one on top;
+ *                   pages given back are written above them, nothing else is
+ *   free_count      DEVICE int32[1], read
+ *   new_pages_held  DEVICE int32[batch], out     new_free_count  DEVICE int32[1], out
+ *   cu_new          DEVICE int32[batch + 1], out: first token of each request, then their number
+ *   total_lens      DEVICE int32[batch], out: kv_lens[b] + new_lens[b]; 0 for a refused request
+ *                   (whose new rows then see nothing; its cached length is the caller's kv_lens)
+ *   slots           DEVICE int32[n_tokens], out: page * page_size + row in the page for every
+ *                   token; -1 for tokens of refused requests and past the last token
+ *   positions       DEVICE int32[n_tokens], out: kv_lens[b] + index among the new ones; 0 past the last token
+ *   err_flag        DEVICE int32[batch] or NULL, out: 0; 1 no page left; 2 lengths or pages_held
+ *                   negative or beyond the table, pages that do not cover kv_lens, or tokens beyond
+ *                   n_tokens.  A request with 1 or 2 keeps its pages; its tokens keep their place
+ *                   in cu_new (a negative new_lens counts as 0).
+ * bt_stride <= 2^18, bt_stride * page_size <= 2^31 - 1, n_tokens <= 2^30.
+ * Outputs must not alias inputs (other workgroups still read those), block_table and free_pages
+ * apart.  The same inputs give the same outputs, also when the call is repeated.  Page ids outside
+ * the pool give slot -1.
+ */
+int ls_page_plan(const ls_page_desc *desc, const int32_t *kv_lens, const int32_t *new_lens, const int32_t *pages_held,
+                 int32_t *block_table, int32_t *free_pages, const int32_t *free_count,
+                 int32_t *new_pages_held, int32_t *new_free_count, int32_t *cu_new, int32_t *total_lens,
+                 int32_t *slots, int32_t *positions, int32_t *err_flag, void *stream);
+
+#define LS_MAX_AXES 4
+
+typedef struct {
+    int32_t n_tokens;
+    int32_t n_q_heads, n_kv_heads;
+    int32_t head_dim;        /* 64 or 128 */
+    int32_t rotary_dim;      /* first elements of a head that are rotated: a multiple of 16, <= head_dim */
+    int32_t n_axes;          /* position axes, 1 .. LS_MAX_AXES */
+    int32_t sections[LS_MAX_AXES];  /* frequency pairs of each axis, in order; their sum is rotary_dim / 2 */
+    int32_t interleaved;     /* 0: pair i is elements i and i + rotary_dim/2; else 2i and 2i + 1 */
+    int32_t n_positions;     /* rows of cos_sin */
+    int32_t dtype;           /* ls_dtype of q, k, v and of what is written */
+    int32_t page_size;       /* (ls_rope_store_paged) a power of two */
+    int32_t n_pages;         /* (ls_rope_store_paged) n_pages * page_size <= 2^31 - 1 */
+    int64_t positions_stride;       /* between the axes of positions */
+    /* element strides: (token, head) axes; caches (page, head, row in the page) */
+    int64_t q_stride[2], k_stride[2], v_stride[2], qo_stride[2], ko_stride[2];
+    int64_t kc_stride[3], vc_stride[3];
+} ls_rope_desc;
+
+/*
+ * Rotary positions: pair i of a token's head, (x, y), becomes (x cos - y sin, x sin + y cos) with
+ *   cos = cos_sin[p, i], sin = cos_sin[p, rotary_dim/2 + i], p = positions[axis of pair i, token].
+ * With several axes (time, height and width of images and video among the text) the first
+ * sections[0] pairs go by the first axis, the next sections[1] by the second, and so on.  The
+ * arithmetic is fp32, rounded once.  Elements from rotary_dim on are copied.
+ *   q, q_out   DEVICE [n_tokens, n_q_heads, head_dim], rows 16-byte aligned; q_out may be q
+ *   k, k_out   DEVICE [n_tokens, n_kv_heads, head_dim]; k_out may be k; both NULL: queries alone (a draft
+ *              model's cross attention).  Tree nodes take this entry point: their rows stay beside the cache.
+ *   positions  DEVICE int32[n_axes, positions_stride]; clamped into [0, n_positions)
+ *   cos_sin    DEVICE float[n_positions, rotary_dim], 16-byte aligned, contiguous
+ */
+int ls_rope(const ls_rope_desc *desc, const void *q, const void *k, const int32_t *positions, const float *cos_sin,
+            void *q_out, void *k_out, void *stream);
+
+/*
+ * The same with the rotated keys and the values written into pages: token t goes to page
+ * slots[t] / page_size, row slots[t] % page_size.  A slot outside the pool (-1) writes nothing.
+ * No two tokens may have the same slot.
+ *   v          DEVICE [n_tokens, n_kv_heads, head_dim]
+ *   slots      DEVICE int32[n_tokens]
+ *   k_pages, v_pages  DEVICE, written in place; not overlapping the inputs
+ */
+int ls_rope_store_paged(const ls_rope_desc *desc, const void *q, const void *k, const void *v, const int32_t *positions,
+                        const float *cos_sin, const int32_t *slots, void *q_out, void *k_pages, void *v_pages, void *stream);
+
+typedef struct {
+    int32_t batch;           /* 1 .. LS_MAX_STEP_BATCH */
+    int32_t n_tokens;        /* rows of q and out */
+    int32_t max_new_len;     /* host-known upper bounds of a request's new tokens and of its rows; the closer */
+    int32_t max_kv_len;      /*   they are the better the kernels and the cut are chosen */
+    int32_t n_q_heads, n_kv_heads;
+    int32_t head_dim;        /* 64 or 128 */
+    int32_t dtype;           /* LS_BF16 or LS_F16 */
+    int32_t page_size;       /* a power of two >= 16 */
+    int32_t bt_stride;       /* entries per request of the block table; bt_stride * page_size >= max_kv_len */
+    int32_t window;          /* rows that a query sees, its own the last; 0: all up to its own */
+    float   softmax_scale;   /* 0 selects 1/sqrt(head_dim) */
+    int64_t q_stride[2], o_stride[2];        /* elements, (token, head) */
+    int64_t kc_stride[3], vc_stride[3];      /* elements, (page, head, row in the page) */
+} ls_chunk_desc;
+
+/* Bytes of DEVICE workspace that ls_chunk_attn_paged needs (256-byte aligned); depends on the current device's
+ * number of compute units, like ls_workspace_bytes. */
+int ls_chunk_workspace_bytes(const ls_chunk_desc *desc, size_t *bytes_out);
+
+/*
+ * Causal attention of the new tokens of a step over the paged cache, their own rows (already
+ * written) included.  Token i of request b, n = cu_new[b+1] - cu_new[b] new ones, stands at row
+ * p = kv_lens[b] - n + i and sees rows max(0, p - window + 1) .. p of the request.  One new token
+ * per request is a decoding step.
+ *   q, out       DEVICE dtype [n_tokens, n_q_heads, head_dim], rows 16-byte aligned; out must not overlap q or the pages
+ *   lse          DEVICE float [n_tokens, n_q_heads], contiguous: log-sum-exp of the scaled logits, natural log
+ *   block_table  DEVICE int32[batch, bt_stride], as for ls_hybrid_tree_attn_paged
+ *   cu_new       DEVICE int32[batch + 1], ascending; clamped into [0, n_tokens].  Tokens from
+ *                cu_new[batch] on, and those of a request past its first max_new_len, are not written.
+ *   kv_lens      DEVICE int32[batch], new rows included; clamped into [0, max_kv_len].  A token whose
+ *                row would be negative (a length of 0, say) sees nothing: zeros and lse = -inf.
+ *   workspace    DEVICE, >= ls_chunk_workspace_bytes(); contents are scratch, nothing in it has to start at zero
+ * Rows that a token does not see have no part in its result, also where they hold infinities or
+ * NaN; rows of a page past the request's length are never read as keys.  The same inputs give
+ * bit-identical outputs; a request's rounding may depend on the other requests' lengths.
+ */
+int ls_chunk_attn_paged(const ls_chunk_desc *desc, const void *q, const void *k_pages, const void *v_pages,
+                        const int32_t *block_table, const int32_t *cu_new, const int32_t *kv_lens,
+                        void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -47,6 +47,28 @@ class ls_desc(ctypes.Structure):
     ]
 
 
+LS_MAX_STEP_BATCH = 4096
+LS_MAX_AXES = 4
+
+
+class ls_page_desc(ctypes.Structure):
+    _fields_ = [(name, _i32) for name in ("batch", "n_tokens", "page_size", "n_pages", "bt_stride")]
+
+
+class ls_rope_desc(ctypes.Structure):
+    _fields_ = [(name, _i32) for name in ("n_tokens", "n_q_heads", "n_kv_heads", "head_dim", "rotary_dim", "n_axes")] + [
+        ("sections", _i32 * LS_MAX_AXES)] + [
+        (name, _i32) for name in ("interleaved", "n_positions", "dtype", "page_size", "n_pages")] + [
+        ("positions_stride", _i64)] + [(name, _i64 * 2) for name in ("q_stride", "k_stride", "v_stride", "qo_stride", "ko_stride")] + [
+        ("kc_stride", _i64 * 3), ("vc_stride", _i64 * 3)]
+
+
+class ls_chunk_desc(ctypes.Structure):
+    _fields_ = [(name, _i32) for name in ("batch", "n_tokens", "max_new_len", "max_kv_len", "n_q_heads", "n_kv_heads", "head_dim",
+                                          "dtype", "page_size", "bt_stride", "window")] + [
+        ("softmax_scale", _f32), ("q_stride", _i64 * 2), ("o_stride", _i64 * 2), ("kc_stride", _i64 * 3), ("vc_stride", _i64 * 3)]
+
+
 class LsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -92,15 +114,20 @@ def lib() -> ctypes.CDLL:
                                             _vp]
     L.ls_cache_attn_paged.argtypes = [dp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
     L.ls_kv_commit_paged.argtypes = [dp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp]
+    L.ls_page_plan.argtypes = [ctypes.POINTER(ls_page_desc)] + [_vp] * 14
+    L.ls_rope.argtypes = [ctypes.POINTER(ls_rope_desc)] + [_vp] * 7
+    L.ls_rope_store_paged.argtypes = [ctypes.POINTER(ls_rope_desc)] + [_vp] * 10
+    L.ls_chunk_workspace_bytes.argtypes = [ctypes.POINTER(ls_chunk_desc), ctypes.POINTER(_sz)]
+    L.ls_chunk_attn_paged.argtypes = [ctypes.POINTER(ls_chunk_desc)] + [_vp] * 9 + [_sz, _vp]
     for name in ("ls_validate_desc", "ls_validate_parents_host", "ls_prefix_num_splits", "ls_prefix_split_len",
                  "ls_workspace_bytes", "ls_workspace_error", "ls_hybrid_tree_attn", "ls_hybrid_tree_attn_single",
                  "ls_hybrid_tree_attn_static",
                  "ls_cache_attn", "ls_build_tree_mask",
                  "ls_prefix_attn_splitkv", "ls_tree_attn_masked", "ls_lse_merge", "ls_tree_accept_greedy",
                  "ls_kv_commit", "ls_hybrid_tree_attn_paged", "ls_cache_attn_paged",
-                 "ls_kv_commit_paged"):
+                 "ls_kv_commit_paged", "ls_chunk_workspace_bytes", *_STEP_CALLS):
         getattr(L, name).restype = ctypes.c_int
-    L.call = _device_calls(L, addresses=False)  # the functions below take tensors
+    L.call = _device_calls(L, addresses=False, names=_DEVICE_CALLS + _STEP_CALLS)  # the functions below take tensors
     _lib = L
     return L
 
@@ -109,6 +136,7 @@ _DEVICE_CALLS = ("ls_hybrid_tree_attn", "ls_hybrid_tree_attn_single", "ls_hybrid
                  "ls_hybrid_tree_attn_fused", "ls_hybrid_tree_attn_paged", "ls_workspace_init", "ls_cache_attn",
                  "ls_cache_attn_paged", "ls_build_tree_mask", "ls_prefix_attn_splitkv", "ls_tree_attn_masked",
                  "ls_lse_merge", "ls_tree_accept_greedy", "ls_kv_commit", "ls_kv_commit_paged")
+_STEP_CALLS = ("ls_page_plan", "ls_rope", "ls_rope_store_paged", "ls_chunk_attn_paged")  # a step of new tokens into a paged cache
 
 
 def _call_module(L):
@@ -131,9 +159,9 @@ def _call_module(L):
     return native
 
 
-def _device_calls(L, addresses=True):
+def _device_calls(L, addresses=True, names=_DEVICE_CALLS):
     """The device entry points of a loaded library as callables that take tensors (None, and integers if `addresses`) for
-    pointers and an ls_desc for its address."""
+    pointers and a descriptor for its address."""
     calls = types.SimpleNamespace()
     native = _call_module(L)
 
@@ -148,7 +176,7 @@ def _device_calls(L, addresses=True):
                         a if addresses and isinstance(a, int) else a.data_ptr() for kind, a in zip(kinds, args)])
         return call
 
-    for name in _DEVICE_CALLS:
+    for name in names:
         fn = getattr(L, name)
         setattr(calls, name, native.Caller(ctypes.cast(fn, _vp).value, name, addresses) if native else through_ctypes(fn))
     return calls
@@ -412,4 +440,97 @@ def ls_cache_attn_paged(desc, q, k_pages, v_pages, block_table, page_size, prefi
                                         prefix_lens, out, lse, workspace, _bytes(workspace), _stream(stream))
     if check:
         _check(st, "ls_cache_attn_paged")
+    return int(st)
+
+
+# ------------------------------------------------ a step of new tokens into a paged cache ----
+
+def _put_strides(field, t: torch.Tensor):
+    assert t.dim() == len(field) + 1 and t.stride(-1) == 1, "head_dim axis must be contiguous"
+    for a in range(len(field)):
+        field[a] = t.stride(a)
+
+
+def make_page_desc(block_table, n_tokens: int, page_size: int, n_pages: int) -> ls_page_desc:
+    """block_table: [batch, bt_stride], contiguous; n_tokens: entries of slots and positions (0: pages only)."""
+    assert block_table.is_contiguous()
+    return ls_page_desc(block_table.shape[0], int(n_tokens), int(page_size), int(n_pages), block_table.shape[1])
+
+
+def ls_page_plan(desc, kv_lens, new_lens, pages_held, block_table, free_pages, free_count, new_pages_held, new_free_count, cu_new,
+                 total_lens, slots=None, positions=None, err_flag=None, stream=None, check: bool = True) -> int:
+    """All tensors device int32: [batch], cu_new [batch + 1], block_table [batch, bt_stride], free_pages [n_pages],
+    free_count / new_free_count [1], slots / positions [n_tokens]."""
+    st = lib().call.ls_page_plan(desc, kv_lens, new_lens, pages_held, block_table, free_pages, free_count, new_pages_held,
+                                 new_free_count, cu_new, total_lens, slots, positions, err_flag, _stream(stream))
+    if check:
+        _check(st, "ls_page_plan")
+    return int(st)
+
+
+def make_rope_desc(q, k, v, q_out, k_out, k_pages, v_pages, positions, cos_sin, sections=None, interleaved=False) -> ls_rope_desc:
+    """q, k, v, q_out, k_out: [n_tokens, heads, head_dim]; k_pages, v_pages: [n_pages, n_kv_heads, page_size, head_dim] (any strides
+    but the last); positions: [n_axes, n_tokens]; cos_sin: [n_positions, rotary_dim]; sections: pairs per axis (one axis: all).
+    k, v, k_out and the pages may be None where the entry point does not take them."""
+    assert positions.dim() == 2 and positions.stride(1) == 1 and cos_sin.is_contiguous()
+    d = ls_rope_desc()
+    d.n_tokens, d.n_q_heads, d.head_dim = q.shape
+    d.n_kv_heads = k.shape[1] if k is not None else 1
+    d.rotary_dim, d.n_positions, d.n_axes = cos_sin.shape[1], cos_sin.shape[0], positions.shape[0]
+    sections = list(sections) if sections is not None else [d.rotary_dim // 2]
+    assert len(sections) == d.n_axes <= LS_MAX_AXES
+    d.sections[:len(sections)] = sections
+    d.interleaved, d.dtype, d.positions_stride = int(bool(interleaved)), _dtype_code(q), positions.stride(0)
+    for field, ten in ((d.q_stride, q), (d.k_stride, k if k is not None else q), (d.v_stride, v if v is not None else q), (d.qo_stride, q_out),
+                       (d.ko_stride, k_out if k_out is not None else q_out)):
+        _put_strides(field, ten)
+    if k_pages is not None:
+        d.n_pages, d.page_size = k_pages.shape[0], k_pages.shape[2]
+        _put_strides(d.kc_stride, k_pages)
+        _put_strides(d.vc_stride, v_pages)
+    return d
+
+
+def ls_rope(desc, q, k, positions, cos_sin, q_out, k_out, stream=None, check: bool = True) -> int:
+    st = lib().call.ls_rope(desc, q, k, positions, cos_sin, q_out, k_out, _stream(stream))
+    if check:
+        _check(st, "ls_rope")
+    return int(st)
+
+
+def ls_rope_store_paged(desc, q, k, v, positions, cos_sin, slots, q_out, k_pages, v_pages, stream=None, check: bool = True) -> int:
+    st = lib().call.ls_rope_store_paged(desc, q, k, v, positions, cos_sin, slots, q_out, k_pages, v_pages, _stream(stream))
+    if check:
+        _check(st, "ls_rope_store_paged")
+    return int(st)
+
+
+def make_chunk_desc(q, k_pages, v_pages, block_table, out, max_new_len: int, max_kv_len: int, window: int = 0,
+                    softmax_scale: float = 0.0) -> ls_chunk_desc:
+    """q, out: [n_tokens, n_q_heads, head_dim]; k_pages, v_pages: [n_pages, n_kv_heads, page_size, head_dim] (any strides but the
+    last); block_table: [batch, bt_stride], contiguous."""
+    assert block_table.is_contiguous()
+    d = ls_chunk_desc()
+    d.batch, d.bt_stride = block_table.shape
+    d.n_tokens, d.n_q_heads, d.head_dim = q.shape
+    d.n_kv_heads, d.page_size = k_pages.shape[1], k_pages.shape[2]
+    d.max_new_len, d.max_kv_len, d.window = int(max_new_len), int(max_kv_len), int(window)
+    d.dtype, d.softmax_scale = _dtype_code(q), float(softmax_scale)
+    for field, ten in ((d.q_stride, q), (d.o_stride, out), (d.kc_stride, k_pages), (d.vc_stride, v_pages)):
+        _put_strides(field, ten)
+    return d
+
+
+def ls_chunk_workspace_bytes(desc: ls_chunk_desc) -> int:
+    n = _sz(0)
+    _check(lib().ls_chunk_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)), "ls_chunk_workspace_bytes")
+    return int(n.value)
+
+
+def ls_chunk_attn_paged(desc, q, k_pages, v_pages, block_table, cu_new, kv_lens, out, lse, workspace, stream=None,
+                        check: bool = True) -> int:
+    st = lib().call.ls_chunk_attn_paged(desc, q, k_pages, v_pages, block_table, cu_new, kv_lens, out, lse, workspace,
+                                        _bytes(workspace), _stream(stream))
+    if check:
+        _check(st, "ls_chunk_attn_paged")
     return int(st)

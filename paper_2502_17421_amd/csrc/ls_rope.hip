@@ -1,0 +1,194 @@
+// Rotary positions of packed tokens, with the write of keys and values into pages.
+//
+// Pair (x, y) of a head becomes (x cos - y sin, x sin + y cos); the cosines and sines of a token are a row of a table (several
+// axes: pieces of several rows).  Products and differences in fp32, rounded once.
+//
+// A thread owns one unit of 16 elements of a token, 8 pairs, and goes through the token's heads: cosines and sines are read
+// once and stay in registers, queries, keys and values pass through once, 16 bytes a lane.  A rotated unit is two pieces of 8
+// elements rotary_dim/2 apart, or 16 neighbouring elements (interleaved).
+//
+// Bound by HBM for prompts, by latency for a few tokens.
+#include "ls_step.hpp"
+
+namespace ls {
+
+namespace {
+
+constexpr int NT = 256;   // threads per workgroup
+constexpr int BATCH = 4;  // heads whose loads are in flight together
+
+// 16-byte pieces of 8 elements
+template <typename T> constexpr int kPieces = sizeof(T) * 8 / 16;
+
+template <typename T> __device__ __forceinline__ void unpack(const uint4 (&raw)[kPieces<T>], float (&x)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float4 f = __builtin_bit_cast(float4, raw[i]);
+            x[4 * i] = f.x, x[4 * i + 1] = f.y, x[4 * i + 2] = f.z, x[4 * i + 3] = f.w;
+        }
+    } else {
+        const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            T lo, hi;
+            *(uint16_t *)&lo = (uint16_t)w[i];
+            *(uint16_t *)&hi = (uint16_t)(w[i] >> 16);
+            x[2 * i] = Elem<T>::load(&lo);
+            x[2 * i + 1] = Elem<T>::load(&hi);
+        }
+    }
+}
+
+template <typename T> __device__ __forceinline__ void pack(const float (&x)[8], uint4 (&raw)[kPieces<T>])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) raw[i] = __builtin_bit_cast(uint4, make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            T lo, hi;
+            Elem<T>::store(&lo, x[2 * i]);
+            Elem<T>::store(&hi, x[2 * i + 1]);
+            w[i] = (uint32_t) * (uint16_t *)&lo | (uint32_t) * (uint16_t *)&hi << 16;
+        }
+        raw[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// SLOTS: heads of a token in work at a time (threads per token: SLOTS * D / 16)
+template <typename T, int D, int SLOTS, bool INTERLEAVED>
+__global__ void __launch_bounds__(NT)
+rope_kernel(RopeArgs a)
+{
+    constexpr int UNITS = D / 16;
+    constexpr int PIECES = kPieces<T>;
+    constexpr int TOKENS = NT / (UNITS * SLOTS);  // per workgroup
+    const int unit = threadIdx.x % UNITS;
+    const int head0 = threadIdx.x / UNITS % SLOTS;
+    const int t = blockIdx.x * TOKENS + threadIdx.x / (UNITS * SLOTS);
+    if (t >= a.n_tokens) return;
+
+    // this unit's cosines and sines
+    const bool rotates = unit * 8 < a.pairs;
+    float cs[8], sn[8];
+    if (rotates) {
+        const int i0 = unit * 8;
+        int axis = 0;
+        while (axis + 1 < a.n_axes && i0 >= a.axis_end[axis]) ++axis;
+        auto row_of = [&](int x) {
+            int p = a.positions[x * a.positions_stride + t];
+            p = p < 0 ? 0 : (p < a.n_positions ? p : a.n_positions - 1);
+            return a.cos_sin + (int64_t)p * (2 * a.pairs);
+        };
+        if (i0 + 8 <= a.axis_end[axis]) {
+            const float *row = row_of(axis) + i0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float4 c = *(const float4 *)(row + 4 * i), s = *(const float4 *)(row + a.pairs + 4 * i);
+                cs[4 * i] = c.x, cs[4 * i + 1] = c.y, cs[4 * i + 2] = c.z, cs[4 * i + 3] = c.w;
+                sn[4 * i] = s.x, sn[4 * i + 1] = s.y, sn[4 * i + 2] = s.z, sn[4 * i + 3] = s.w;
+            }
+        } else {  // an axis ends inside the unit
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                while (axis + 1 < a.n_axes && i0 + i >= a.axis_end[axis]) ++axis;
+                const float *row = row_of(axis) + i0 + i;
+                cs[i] = row[0];
+                sn[i] = row[a.pairs];
+            }
+        }
+    }
+    // byte offsets of the unit's two pieces of 8 elements
+    const int at0 = (int)sizeof(T) * (rotates && !INTERLEAVED ? 8 * unit : 16 * unit);
+    const int at1 = (int)sizeof(T) * (rotates && !INTERLEAVED ? 8 * unit + a.pairs : 16 * unit + 8);
+
+    int32_t slot = a.slots ? a.slots[t] : 0;
+    const bool stored = !a.slots || (uint32_t)slot < (uint32_t)a.n_slots;
+    const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
+    const int64_t k_dst = a.slots ? page * a.ko_s[0] + row * a.ko_s[2] : t * a.ko_s[0];
+    const int64_t v_dst = page * a.vo_s[0] + row * a.vo_s[2];
+    const int n_k = a.k ? a.n_kv_heads : 0, n_v = a.v ? a.n_kv_heads : 0;
+    const int last_k = a.n_q_heads + n_k, n_heads = last_k + n_v;  // queries, then keys, then values
+
+    for (int h0 = head0; h0 < n_heads; h0 += BATCH * SLOTS) {
+        uint4 raw[BATCH][2][PIECES];
+        uint8_t *dst[BATCH];
+        bool turn[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int h = h0 + i * SLOTS;
+            dst[i] = nullptr;
+            if (h >= n_heads) continue;
+            const uint8_t *src;
+            if (h < a.n_q_heads) {
+                src = a.q + t * a.q_s[0] + h * a.q_s[1];
+                dst[i] = a.q_out + t * a.qo_s[0] + h * a.qo_s[1];
+            } else if (h < last_k) {
+                src = a.k + t * a.k_s[0] + (h - a.n_q_heads) * a.k_s[1];
+                dst[i] = stored ? a.k_out + k_dst + (h - a.n_q_heads) * a.ko_s[1] : nullptr;
+            } else {
+                src = a.v + t * a.v_s[0] + (h - last_k) * a.v_s[1];
+                dst[i] = stored ? a.v_out + v_dst + (h - last_k) * a.vo_s[1] : nullptr;
+            }
+            turn[i] = rotates && h < last_k;
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) {
+                raw[i][0][j] = *(const uint4 *)(src + at0 + 16 * j);
+                raw[i][1][j] = *(const uint4 *)(src + at1 + 16 * j);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (!dst[i]) continue;
+            if (turn[i]) {
+                float x[2][8], y[2][8];
+                unpack<T>(raw[i][0], x[0]);
+                unpack<T>(raw[i][1], x[1]);
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                    // pair p of the unit: elements p of both pieces, or 2p and 2p + 1 of the two in a row
+                    const int e0 = INTERLEAVED ? (2 * p) / 8 : 0, i0 = INTERLEAVED ? (2 * p) % 8 : p;
+                    const int e1 = INTERLEAVED ? e0 : 1, i1 = INTERLEAVED ? i0 + 1 : p;
+                    y[e0][i0] = x[e0][i0] * cs[p] - x[e1][i1] * sn[p];
+                    y[e1][i1] = x[e0][i0] * sn[p] + x[e1][i1] * cs[p];
+                }
+                pack<T>(y[0], raw[i][0]);
+                pack<T>(y[1], raw[i][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) {
+                *(uint4 *)(dst[i] + at0 + 16 * j) = raw[i][0][j];
+                *(uint4 *)(dst[i] + at1 + 16 * j) = raw[i][1][j];
+            }
+        }
+    }
+}
+
+template <typename T, int D, int SLOTS> hipError_t launch_form(const RopeArgs &a, hipStream_t stream)
+{
+    constexpr int TOKENS = NT / (D / 16 * SLOTS);
+    const dim3 grid((a.n_tokens + TOKENS - 1) / TOKENS);
+    if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, D, SLOTS, true>), grid, dim3(NT), 0, stream, a);
+    else hipLaunchKernelGGL((rope_kernel<T, D, SLOTS, false>), grid, dim3(NT), 0, stream, a);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_type(const RopeArgs &a, int head_dim, hipStream_t stream)
+{
+    return head_dim == 128 ? launch_form<T, 128, 8>(a, stream) : launch_form<T, 64, 16>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream)
+{
+    if (dtype == LS_BF16) return launch_type<uint16_t>(a, head_dim, stream);
+    if (dtype == LS_F16) return launch_type<half_t>(a, head_dim, stream);
+    return launch_type<float>(a, head_dim, stream);
+}
+
+}  // namespace ls

@@ -1,0 +1,43 @@
+// What the host side and the kernels of a serving step share (page plan, rotary positions, attention of new tokens).
+#pragma once
+
+#include "ls_internal.hpp"
+
+namespace ls {
+
+struct PagePlanArgs {
+    const int32_t *kv_lens, *new_lens, *pages_held, *free_count;
+    int32_t *block_table, *free_pages;
+    int32_t *new_pages_held, *new_free_count, *cu_new, *total_lens, *slots, *positions, *err_flag;
+    int32_t batch, n_tokens, page_shift, n_pages, bt_stride;
+};
+
+// Strides in bytes, (token, head) and (page, head, row).
+struct RopeArgs {
+    const uint8_t *q, *k, *v;       // k == nullptr: queries alone; v == nullptr: k goes to k_out
+    uint8_t *q_out, *k_out, *v_out; // k_out, v_out: the pages if slots != nullptr
+    const int32_t *positions, *slots;
+    const float *cos_sin;
+    int64_t positions_stride;
+    int64_t q_s[2], k_s[2], v_s[2], qo_s[2], ko_s[3], vo_s[3];
+    int32_t n_tokens, n_q_heads, n_kv_heads, pairs, n_axes, interleaved, n_positions, page_shift, n_slots;
+    int32_t axis_end[LS_MAX_AXES];  // first pair past each axis
+};
+
+// Strides in bytes.
+struct ChunkArgs {
+    const uint8_t *q, *k_pages, *v_pages;
+    const int32_t *block_table, *cu_new, *kv_lens;
+    uint8_t *out;
+    float *lse;
+    int64_t q_s[2], o_s[2], kc_s[3], vc_s[3];
+    int32_t batch, n_tokens, max_new_len, max_kv_len, n_q_heads, n_kv_heads, group, page_shift, bt_stride, window;
+    FastDiv by_group, by_kv_heads;
+    float scale_log2;
+};
+
+hipError_t launch_page_plan(const PagePlanArgs &a, hipStream_t stream);
+hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream);
+hipError_t launch_chunk_attn(const ChunkArgs &a, int dtype, int head_dim, hipStream_t stream);
+
+}  // namespace ls

@@ -1,6 +1,6 @@
 // Calls into the C ABI of include/ls_attn.h from Python: Caller(address, name, addresses) is a callable whose arguments are
 // those of the entry point, a tensor or None (or, if `addresses`, an integer address) where it takes a pointer, the stream's
-// handle, the ls_desc structure where it takes one.
+// handle, the descriptor structure where it takes one.
 // It returns the status.  A call with 13 arguments that is refused at once takes 0.14 us of the host, through ctypes 1.2; a program
 // that accepts a path and commits its rows, two calls bound by the host, takes 9.1 us a round instead of 10.75.
 #define PY_SSIZE_T_CLEAN
@@ -19,16 +19,20 @@
 namespace {
 
 // An argument as the C function takes it; false: a Python error is set.
-bool convert(PyObject *obj, const ls_desc *&value, bool)
+template <typename T> bool descriptor(PyObject *obj, const T *&value, const char *expected)
 {
     Py_buffer view;
     if (PyObject_GetBuffer(obj, &view, PyBUF_SIMPLE) != 0) return false;
-    const bool fits = view.len == (Py_ssize_t)sizeof(ls_desc);
-    value = (const ls_desc *)view.buf;  // lives as long as the structure, which the caller holds
+    const bool fits = view.len == (Py_ssize_t)sizeof(T);
+    value = (const T *)view.buf;  // lives as long as the structure, which the caller holds
     PyBuffer_Release(&view);
-    if (!fits) PyErr_SetString(PyExc_TypeError, "expected an ls_desc");
+    if (!fits) PyErr_SetString(PyExc_TypeError, expected);
     return fits;
 }
+bool convert(PyObject *obj, const ls_desc *&value, bool) { return descriptor(obj, value, "expected an ls_desc"); }
+bool convert(PyObject *obj, const ls_page_desc *&value, bool) { return descriptor(obj, value, "expected an ls_page_desc"); }
+bool convert(PyObject *obj, const ls_rope_desc *&value, bool) { return descriptor(obj, value, "expected an ls_rope_desc"); }
+bool convert(PyObject *obj, const ls_chunk_desc *&value, bool) { return descriptor(obj, value, "expected an ls_chunk_desc"); }
 
 bool integer(PyObject *obj, unsigned long long &value)  // wraps around like a C conversion
 {
@@ -106,7 +110,8 @@ const Entry kEntries[] = {
     LS_ENTRY(ls_hybrid_tree_attn_fused), LS_ENTRY(ls_hybrid_tree_attn_paged), LS_ENTRY(ls_workspace_init),
     LS_ENTRY(ls_cache_attn), LS_ENTRY(ls_cache_attn_paged), LS_ENTRY(ls_build_tree_mask), LS_ENTRY(ls_prefix_attn_splitkv),
     LS_ENTRY(ls_tree_attn_masked), LS_ENTRY(ls_lse_merge), LS_ENTRY(ls_tree_accept_greedy), LS_ENTRY(ls_kv_commit),
-    LS_ENTRY(ls_kv_commit_paged),
+    LS_ENTRY(ls_kv_commit_paged), LS_ENTRY(ls_page_plan), LS_ENTRY(ls_rope), LS_ENTRY(ls_rope_store_paged),
+    LS_ENTRY(ls_chunk_attn_paged),
 };
 
 struct Caller {
