@@ -88,21 +88,6 @@ Problem make_problem(const ls_desc &d, const void *q, const void *kc, const void
     return p;
 }
 
-int compute_units()
-{
-    static int cached = 0;
-    if (cached) return cached;
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) == hipSuccess &&
-        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
-        cached = n;
-    else {
-        (void)hipGetLastError();
-        return 256;  // MI355X; not cached so a later call with a device present asks again
-    }
-    return cached;
-}
-
 // The first bytes of every workspace are the arrival counters of the single-launch call, at a
 // place that does not depend on the problem: one ls_workspace_init serves every later call.
 constexpr size_t kArrivalBytes = (size_t)kMaxArrivalCounters * kCounterWords * sizeof(uint64_t);

@@ -4,10 +4,30 @@
 // max(0, p - window + 1) .. p.  The n * G query rows that share a KV head (G query heads a KV head) are ordered token
 // first, row r = token r / G, head r % G, so that what a row sees grows with r.
 //
-// One wave per 32 query rows of a request and KV head; it walks the rows they see in tiles of 32 keys.
-//   S^T = K Q^T, softmax with a running maximum, O^T += V^T P^T   (operand layouts: ls_mfma.hpp)
-// so a lane holds 16 scores of ONE query row, and the numerators go from the accumulators of the first product to the operand of the
-// second without leaving the lane.
+// Two forms of work, in one launch, because a step mixes them.  Keys go in tiles of 32:
+//   row blocks    up to 256 query rows of a request and KV head; eight waves of 32 rows share the tiles, which four of them copy
+//                 into rings in LDS.  Bound by the matrix cores: 512 flops per byte of a tile.
+//   few rows      requests with at most 32 rows per KV head (single tokens); the eight waves hold the same rows and take
+//                 every eighth tile each, without barriers, and are merged at the end.  Bound by HBM.
+// Both take about the same time per tile while the chip is full (1.0 and 0.75 us), so work is counted in tiles.
+//
+// Which piece a workgroup takes is worked out on the device, from the lengths, by every wave for itself: a program has
+// them there, and the host knows upper bounds only.  A block of more tiles than a compute unit's share of all tiles is cut into
+// pieces along the keys, whose partial rows (fp32, with the running maximum and sum) a second kernel merges.  Pieces
+// go out longest first, since the hardware deals them as compute units become free.  The workgroups of one KV head are 8
+// apart at least where there are 8 heads, so an XCD sees one head and its L2 holds the tiles that its workgroups share.
+//
+// Products (operand layouts: ls_mfma.hpp).  S^T = K Q^T, so a lane holds 16 scores of ONE query row, and the numerators go
+// from the accumulators to the operand of O^T = V^T P^T by a pack to 16 bits, which the row sum does not take part in.
+//
+// Softmax state of a row: reference exponent m (raw scores) and l, the sum of exp2((s - m) c), c = scale * log2(e).  Any m
+// gives the same result, so the row blocks only raise it when a step's sum leaves the range of the operand type.
+//
+// Masks.  A tile that every row of a wave sees whole has none; in the others scores are replaced by -inf.  Infinite or NaN
+// values of an unseen row would still come through the product as 0 * inf: in the tiles that some row does not see whole
+// they are replaced by zeros, and put into the rows that see them at the end.
+#include <type_traits>
+
 #include "ls_mfma.hpp"
 #include "ls_step.hpp"
 
@@ -15,158 +35,1131 @@ namespace ls {
 
 namespace {
 
-constexpr int TK = 32;  // keys per tile
+constexpr int TK = 32;            // keys per tile
+constexpr int NW = 8;             // waves per workgroup
+constexpr int NL = 4;             // of which copy the tiles of a row block
+constexpr int ROWS = NW * 32;     // query rows per row block
+constexpr int FEW = 32;           // rows per KV head up to which the waves split the keys
+constexpr int PD = 3;             // requests (a K and a V tile) in flight of a row block
+constexpr int KS = PD + 3, VS = PD + 4;  // stages of its rings
+constexpr int PAGES = 512;        // page ids of a row block in LDS, a ring of two halves
+constexpr int kMinSplit = 24;     // a row block's pieces have at least so many tiles
+constexpr int kFewWhole = 48, kFewSplit = 16;  // few rows: up to so many tiles in one piece; fewest of a piece
+constexpr float kLazy = 8.f;      // the reference exponent is raised when a score exceeds it by 2^8
+template <bool F16> constexpr float kSumCap = F16 ? 0x1p15f : 0x1p40f;  // largest sum of a step's numerators without raising it
+
+template <int D> constexpr int kTileBytes = TK * D * 2;
+template <int D> constexpr int kLds = 2 * NW * kTileBytes<D> + PAGES * 4 + 16;
+static_assert(KS + VS + 2 <= 2 * NW, "two stages beyond the rings, for the query rows of the last two waves");
+
+// ---- which piece --------------------------------------------------------------------------------
+
+// What the pieces are made of: one request.
+struct Request {
+    int32_t first, n, kv;  // first token, new tokens, rows
+    int32_t rows;          // query rows per KV head
+    int32_t blocks, tiles; // row blocks, and the tiles of the longest
+    float work;            // tiles of all of them, about
+};
+
+// Pieces of a request: each of its blocks is cut into `cut`.  Before it in the order of the requests: `slot` partial
+// blocks, `entry` blocks that are cut.
+struct Cut {
+    int32_t cut, slot, entry;
+};
+
+__device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
+
+// First tile and tiles of block k.
+__device__ __forceinline__ int2 block_tiles(const ChunkArgs &a, const Request &q, int k)
+{
+    const int top = (k + 1) * ROWS < q.rows ? (k + 1) * ROWS : q.rows;
+    const int place0 = q.kv - q.n;
+    const int hi = place0 + (int)a.by_group.div((uint32_t)(top - 1)) + 1;
+    int lo = a.window > 0 ? place0 + (int)a.by_group.div((uint32_t)(k * ROWS)) - a.window + 1 : 0;
+    lo = lo > 0 ? lo : 0;
+    return hi > lo ? make_int2(lo / TK, (hi + TK - 1) / TK - lo / TK) : make_int2(0, 0);
+}
+
+__device__ __forceinline__ Request load_request(const ChunkArgs &a, int b)
+{
+    Request q{0, 0, 0, 0, 0, 0, 0.f};
+    if (b >= a.batch) return q;
+    int first = a.cu_new[b], end = a.cu_new[b + 1], kv = a.kv_lens[b];
+    first = first < 0 ? 0 : (first > a.n_tokens ? a.n_tokens : first);
+    end = end < first ? first : (end > a.n_tokens ? a.n_tokens : end);
+    q.first = first;
+    q.n = end - first;
+    q.kv = kv < 0 ? 0 : (kv > a.max_kv_len ? a.max_kv_len : kv);
+    q.rows = (q.n < a.max_new_len ? q.n : a.max_new_len) * a.group;
+    q.blocks = div_up(q.rows, ROWS);
+    if (q.blocks > 0) {
+        const int t0 = block_tiles(a, q, 0).y, t1 = block_tiles(a, q, q.blocks - 1).y;
+        q.tiles = t0 > t1 ? t0 : t1;
+        q.work = 0.5f * (float)q.blocks * (float)(t0 + t1);
+    }
+    return q;
+}
+
+// Pieces per block for pieces of at most `share` tiles.
+__device__ __forceinline__ int cut_of(const Request &q, int share)
+{
+    if (q.rows <= FEW) return q.tiles <= kFewWhole ? 1 : div_up(q.tiles, share > kFewSplit ? share : kFewSplit);
+    return q.tiles > 0 ? div_up(q.tiles, share > kMinSplit ? share : kMinSplit) : 1;
+}
+
+// Order of the pieces: the tiles of the last row of a block (all of a request's rows for a single block) over the cut.  Pieces of a
+// request whose key is at least x: those of its last blocks.
+__device__ __forceinline__ int pieces_from(const ChunkArgs &a, const Request &q, int cut, int x)
+{
+    if (x <= 0) return q.blocks * cut;
+    if (q.blocks == 0) return 0;
+    // tokens up to the end of block k: (k + 1) * ROWS / G;  rows seen there, and no more than the window
+    const int64_t need = (int64_t)x * cut * TK - (TK - 1);  // rows
+    if (a.window > 0 && need > a.window + ROWS) return 0;
+    const int64_t tokens = need - (q.kv - q.n);
+    if (tokens <= 0) return q.blocks * cut;
+    if (tokens > q.n + ROWS) return 0;
+    const int k = (int)((tokens * a.group + ROWS - 1) / ROWS) - 1;
+    return k < q.blocks ? (q.blocks - (k > 0 ? k : 0)) * cut : 0;
+}
+
+// Inclusive sums over the lanes of a wave.
+template <typename T> __device__ __forceinline__ T scan_lanes(T x)
+{
+    auto add = [&](auto ctrl, auto row_mask) __attribute__((always_inline)) {
+        const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(row_mask)::value, 0xf, false);
+        x += __builtin_bit_cast(T, y);
+    };
+    using all = std::integral_constant<int, 0xf>;
+    add(std::integral_constant<int, 0x111>{}, all{});  // from 1, 2, 4 and 8 lanes below in the row of 16
+    add(std::integral_constant<int, 0x112>{}, all{});
+    add(std::integral_constant<int, 0x114>{}, all{});
+    add(std::integral_constant<int, 0x118>{}, all{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // the last lane of the row before, to rows 1 and 3
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // lane 31, to rows 2 and 3
+    return x;
+}
+template <typename T> __device__ __forceinline__ T last_lane(T x)
+{
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+struct Piece {
+    Request q;
+    int32_t b, block, split, cut, slot, entry;  // slot, entry: of this block
+    bool valid;
+};
+
+// The share of tiles above which a block is cut.  sum(f): the sum of f over all requests.
+// While there are fewer blocks than compute units, the smallest share whose pieces take one unit each; else a unit's share, as
+// long as the partial rows have room.
+template <typename Sum> __device__ __forceinline__ int choose_share(const ChunkArgs &a, Sum sum)
+{
+    const int blocks = sum([](const Request &q) { return q.blocks; });
+    const float work = sum([](const Request &q) { return q.work; });
+    int share = (int)(work / (float)a.units) + 1;
+    while (share < (1 << 26)) {
+        const int pieces = sum([&](const Request &q) { return q.blocks * cut_of(q, share); });
+        const int slots = sum([&](const Request &q) { const int c = cut_of(q, share); return c > 1 ? q.blocks * c : 0; });
+        if ((blocks > a.units || pieces <= a.units) && slots <= a.slots) break;
+        share += share / 8 + 1;
+    }
+    return share;
+}
+
+// Piece i of those of a KV head, up to 64 requests, a lane each (every wave for itself).
+__device__ __forceinline__ Piece find_piece(const ChunkArgs &a, int i, int lane)
+{
+    const Request q = load_request(a, lane);
+    const int share = choose_share(a, [&](auto f) { return last_lane(scan_lanes(f(q))); });
+    const int cut = cut_of(q, share);
+    const int slots = cut > 1 ? q.blocks * cut : 0, entries = cut > 1 ? q.blocks : 0;
+    const int slot = scan_lanes(slots) - slots, entry_end = scan_lanes(entries);
+    Piece p{};
+    if (blockIdx.x == 0 && threadIdx.x == 63) *a.n_entries = entry_end;  // for the merge
+    if (i >= last_lane(scan_lanes(q.blocks * cut))) return p;
+    // the largest key x of which more than i pieces have it or more
+    int top = q.tiles / cut + 2;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        const int y = __shfl_xor(top, off, kWave);
+        top = y > top ? y : top;
+    }
+    int lo = 0, hi = top + 1;
+    while (last_lane(scan_lanes(pieces_from(a, q, cut, hi))) > 0) hi *= 2;  // (a block that is not full counts as one)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (last_lane(scan_lanes(pieces_from(a, q, cut, mid))) > i) lo = mid;
+        else hi = mid;
+    }
+    const int above = pieces_from(a, q, cut, hi), same = pieces_from(a, q, cut, lo) - above;
+    const int rest = i - last_lane(scan_lanes(above));
+    const int upto = scan_lanes(same);
+    const uint64_t holds = __ballot(upto > rest);
+    const int b = holds ? __builtin_ctzll(holds) : 63;
+    auto of = [&](int v) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, b); };
+    p.b = b;
+    p.q = Request{of(q.first), of(q.n), of(q.kv), of(q.rows), of(q.blocks), of(q.tiles), 0.f};
+    p.cut = of(cut);
+    const int at = of(above) + rest - of(upto - same);  // among the request's pieces, last block first
+    const int from_end = at / p.cut;
+    p.block = p.q.blocks - 1 - from_end;
+    p.split = at - from_end * p.cut;
+    p.slot = of(slot) + from_end * p.cut;
+    p.entry = of(entry_end - entries) + from_end;
+    p.valid = holds != 0 && p.block >= 0;
+    return p;
+}
+
+// More requests: a kernel of one workgroup sorts them by their longest piece and writes down where the pieces of each begin.
+struct Listed {
+    int32_t begin;  // pieces of the requests before it in this order; the last entry: all of them
+    int32_t b, cut, slot, entry;
+};
+constexpr int LIST_THREADS = 1024, LIST_PER = LS_MAX_STEP_BATCH / LIST_THREADS;
+
+__global__ void __launch_bounds__(LIST_THREADS)
+chunk_list_kernel(ChunkArgs a)
+{
+    __shared__ float part_f[LIST_THREADS / kWave];
+    __shared__ int32_t part_i[LIST_THREADS / kWave], bucket[64], bucket_at[64];
+    __shared__ int32_t order[LS_MAX_STEP_BATCH];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Request q[LIST_PER];
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j) q[j] = load_request(a, tid + j * LIST_THREADS);
+    auto sum_threads = [&](auto x) {
+        auto *part = [&] { if constexpr (std::is_same_v<decltype(x), float>) return part_f; else return part_i; }();
+        x = scan_lanes(x);
+        if (lane == 63) part[wave] = x;
+        __syncthreads();
+        decltype(x) all = 0;
+#pragma unroll
+        for (int w = 0; w < LIST_THREADS / kWave; ++w) all += part[w];
+        __syncthreads();
+        return all;
+    };
+    const int share = choose_share(a, [&](auto f) {
+        auto x = f(q[0]);
+#pragma unroll
+        for (int j = 1; j < LIST_PER; ++j) x += f(q[j]);
+        return sum_threads(x);
+    });
+    // sort by the longest piece, by its bits: bucket 63 - 2 * log2 - next bit
+    if (tid < 64) bucket[tid] = 0;
+    __syncthreads();
+    int in[LIST_PER], place[LIST_PER];
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j) {
+        const uint32_t key = (uint32_t)(q[j].tiles / cut_of(q[j], share)) + 1;
+        const int top = 31 - __builtin_clz(key);
+        in[j] = 63 - (2 * top + (top > 0 ? (key >> (top - 1)) & 1 : 0));
+        if (tid + j * LIST_THREADS < a.batch) place[j] = atomicAdd(&bucket[in[j]], 1);
+    }
+    __syncthreads();
+    if (tid < 64) bucket_at[tid] = scan_lanes(bucket[tid]) - bucket[tid];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j)
+        if (tid + j * LIST_THREADS < a.batch) order[bucket_at[in[j]] + place[j]] = tid + j * LIST_THREADS;
+    __syncthreads();
+    // LIST_PER requests in a row per thread, in that order: sums of pieces, partial blocks and cut blocks before each
+    Request r[LIST_PER];
+    int cut[LIST_PER], pieces = 0, slots = 0, entries = 0;
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j) {
+        const int at = tid * LIST_PER + j;
+        r[j] = load_request(a, at < a.batch ? order[at] : a.batch);
+        cut[j] = cut_of(r[j], share);
+        pieces += r[j].blocks * cut[j];
+        slots += cut[j] > 1 ? r[j].blocks * cut[j] : 0;
+        entries += cut[j] > 1 ? r[j].blocks : 0;
+    }
+    auto before = [&](int x) {  // sum over the threads before this one
+        const int upto = scan_lanes(x);
+        if (lane == 63) part_i[wave] = upto;
+        __syncthreads();
+        int sum = upto - x;
+#pragma unroll
+        for (int w = 0; w < LIST_THREADS / kWave; ++w) sum += w < wave ? part_i[w] : 0;
+        __syncthreads();
+        return sum;
+    };
+    int piece = before(pieces), slot = before(slots), entry = before(entries);
+    Listed *list = (Listed *)a.list;
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j) {
+        const int at = tid * LIST_PER + j;
+        if (at >= a.batch) continue;
+        list[at] = Listed{piece, order[at], cut[j], slot, entry};
+        piece += r[j].blocks * cut[j];
+        slot += cut[j] > 1 ? r[j].blocks * cut[j] : 0;
+        entry += cut[j] > 1 ? r[j].blocks : 0;
+        if (at == a.batch - 1) {
+            list[a.batch] = Listed{piece, 0, 1, 0, 0};
+            *a.n_entries = entry;
+        }
+    }
+}
+
+// Piece i by the list: the last request that begins at or before it, 64 candidates at a time.
+__device__ __forceinline__ Piece find_listed(const ChunkArgs &a, int i, int lane)
+{
+    const Listed *list = (const Listed *)a.list;
+    Piece p{};
+    int lo = 0, n = a.batch + 1;  // the one looked for is among lo .. lo + n - 1
+    while (n > 1) {
+        const int step = div_up(n, kWave);
+        const int at = lo + lane * step;
+        const bool below = lane * step < n && list[at].begin <= i;
+        const int last = 63 - __builtin_clzll(__ballot(below) | 1);
+        lo += last * step;
+        n = n - last * step < step ? n - last * step : step;
+    }
+    if (lo >= a.batch) return p;
+    const Listed e = list[lo];
+    p.b = __builtin_amdgcn_readfirstlane(e.b);
+    p.q = load_request(a, p.b);
+    p.cut = __builtin_amdgcn_readfirstlane(e.cut);
+    const int at = i - __builtin_amdgcn_readfirstlane(e.begin);
+    const int from_end = at / p.cut;
+    p.block = p.q.blocks - 1 - from_end;
+    p.split = at - from_end * p.cut;
+    p.slot = __builtin_amdgcn_readfirstlane(e.slot) + from_end * p.cut;
+    p.entry = __builtin_amdgcn_readfirstlane(e.entry) + from_end;
+    p.valid = p.block >= 0;
+    return p;
+}
+
+// ---- what both forms share ----------------------------------------------------------------------
+
+// Result of 32 query rows in the accumulator layout: lane l has row l % 32.
+template <int D> struct RowState {
+    floatx16 o[D / 32];
+    float m, l;  // l: the numerators of this lane's half of the keys until they are joined
+};
+
+// What a lane's query row is, and sees.
+struct QueryRow {
+    bool ok;
+    int32_t token, head;    // token of the packed rows
+    int32_t lo, place;      // rows seen: lo .. place
+};
+
+__device__ __forceinline__ QueryRow query_row(const ChunkArgs &a, const Request &q, int g, int r)
+{
+    QueryRow x;
+    x.ok = r < q.rows;
+    r = x.ok ? r : q.rows - 1;  // rows past the end repeat the last
+    const int i = (int)a.by_group.div((uint32_t)r);
+    x.token = q.first + i;
+    x.head = g * a.group + r - i * a.group;
+    x.place = q.kv - q.n + i;
+    x.lo = a.window > 0 && x.place - a.window + 1 > 0 ? x.place - a.window + 1 : 0;
+    return x;
+}
+
+// Partial block `slot` of KV head g: [row][D] fp32 numerator sums, and (m, l) of every row.
+template <int D> __device__ __forceinline__ float *part_rows(const ChunkArgs &a, int slot, int g)
+{
+    return a.parts + ((int64_t)slot * a.n_kv_heads + g) * a.part_rows * D;
+}
+__device__ __forceinline__ float2 *part_state(const ChunkArgs &a, int slot, int g)
+{
+    return a.part_ml + ((int64_t)slot * a.n_kv_heads + g) * a.part_rows;
+}
+
+// Blocks that are cut, for the merge.
+struct Entry {
+    int32_t first, row0, rows;  // first token of the request, first row of the block, its rows
+    int32_t cut, slot;
+};
+__device__ __forceinline__ void write_entry(const ChunkArgs &a, const Piece &p, int g)
+{
+    const int row0 = p.block * ROWS;
+    ((Entry *)a.entries)[p.entry * a.n_kv_heads + g] = Entry{p.q.first, row0, p.q.rows - row0 < ROWS ? p.q.rows - row0 : ROWS, p.cut, p.slot};
+}
+
+// ---- row blocks -------------------------------------------------------------------------------------
 
 template <int D, bool F16>
-__global__ void __launch_bounds__(64)
-chunk_attn_kernel(ChunkArgs a)
+__device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece, int g, uint8_t *smem)
 {
-    constexpr int KSTEPS = D / 16, MT = D / 32, CH = D / 8, ROWB = D * 2, TILEB = TK * ROWB;
-    typedef __attribute__((address_space(3))) const uint4 *lds_u4;
-    typedef __attribute__((address_space(3))) shortx4 *lds_s4;
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * TILEB];
-    const int lane = threadIdx.x, li = lane & 31, lh = lane >> 5;
-    const int g = blockIdx.x % a.n_kv_heads;
-    int block = blockIdx.x / a.n_kv_heads;
+    constexpr int KSTEPS = D / 16, MT = D / 32, CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
+    constexpr int RPL = 64 / CH;          // rows one copy of 64 lanes covers
+    constexpr int TPT = TK / RPL;         // copies per tile and tensor
+    constexpr int LOADS = TPT / NL;       // of which each copying wave does so many: eight rows in a row, which share a page
+    constexpr int INFLIGHT = 2 * LOADS;   // copies per copying wave and request
+    constexpr uint32_t V_RING = KS * TILEB;
+    static_assert(LOADS * RPL == 8 && (PD + 1) * INFLIGHT + TPT <= 63, "copies of a wave");
+    const Request &q = piece.q;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int row0 = piece.block * ROWS, wave_row0 = row0 + wave * 32;
+    const bool has_rows = wave_row0 < q.rows;
+    const QueryRow x = query_row(a, q, g, wave_row0 + li);
 
-    // the request whose row block this is
-    int b = 0, first = 0, n = 0;
-    for (; b < a.batch; ++b) {
-        first = a.cu_new[b];
-        first = first < 0 ? 0 : (first > a.n_tokens ? a.n_tokens : first);
-        int end = a.cu_new[b + 1];
-        end = end < first ? first : (end > a.n_tokens ? a.n_tokens : end);
-        n = end - first;
-        const int rows = (n < a.max_new_len ? n : a.max_new_len) * a.group, blocks = (rows + 31) / 32;
-        if (block < blocks) break;
-        block -= blocks;
-    }
-    if (b == a.batch) return;
-    int kv = a.kv_lens[b];
-    kv = kv < 0 ? 0 : (kv > a.max_kv_len ? a.max_kv_len : kv);
-    const int rows = (n < a.max_new_len ? n : a.max_new_len) * a.group;
-    const int r = block * 32 + li;
-    const bool ok = r < rows;
-    const int token = first + (ok ? r : rows - 1) / a.group, head = g * a.group + (ok ? r : rows - 1) % a.group;
-    const int place = kv - n + (token - first);  // the row this query stands at
-    const int seen_lo = a.window > 0 && place - a.window + 1 > 0 ? place - a.window + 1 : 0;
-    // rows that some query of the block sees
-    const int lo = __builtin_amdgcn_readfirstlane(seen_lo);
-    int hi = kv - n + (block * 32 + 31 < rows ? block * 32 + 31 : rows - 1) / a.group + 1;
+    // tiles of this piece
+    const int2 span = block_tiles(a, q, piece.block);
+    int per = div_up(span.y, piece.cut);
+    per += piece.cut > 1 ? per & 1 : 0;  // tiles go in pairs
+    int t_lo = piece.split * per, t_hi = t_lo + per;
+    t_hi = span.x + (t_hi < span.y ? t_hi : span.y);
+    t_lo = span.x + (t_lo < span.y ? t_lo : span.y);
+    const int n_tiles = t_hi - t_lo;
+    const int kv = q.kv;
 
-    const uint8_t *q_ptr = a.q + token * a.q_s[0] + head * a.q_s[1];
-    bf16x8 q_reg[KSTEPS];
-#pragma unroll
-    for (int kk = 0; kk < KSTEPS; ++kk) q_reg[kk] = __builtin_bit_cast(bf16x8, *(const uint4 *)(q_ptr + kk * 32 + lh * 16));
-
-    floatx16 o[MT];
+    RowState<D> st;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[mt][e] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    const float c = a.scale_log2;
-    const int32_t *tab = a.block_table + (int64_t)b * a.bt_stride;
-    const int page_mask = (1 << a.page_shift) - 1;
-    const uint32_t base = lds_offset(smem);
-    const uint32_t k_off = base + li * ROWB + ((lh ^ (li & (CH - 1))) * 16);
-    const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
-    const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
-    const uint32_t v_off = base + TILEB + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
+        for (int e = 0; e < 16; ++e) st.o[mt][e] = 0.f;
+    st.m = -INFINITY;
+    st.l = 0.f;
 
-    for (int k0 = lo & ~(TK - 1); k0 < hi; k0 += TK) {
+    if (n_tiles > 0) {
+        // ---- copies -----------------------------------------------------------------------------
+        const uint32_t base = lds_offset(smem);
+        const uint8_t *kp = uniform_ptr(a.k_pages + g * a.kc_s[1]), *vp = uniform_ptr(a.v_pages + g * a.vc_s[1]);
+        const int32_t k_rb = (int32_t)a.kc_s[2], v_rb = (int32_t)a.vc_s[2];
+        const int page_mask = (1 << a.page_shift) - 1;
+        const int ld_row = lane / CH, ld_pos = lane % CH;
+        const bool loader = wave < NL;
+        const int my_row = (wave % NL) * 8;  // first of the rows of a tile that this wave copies
+        uint32_t k_voff[LOADS], v_voff[LOADS];
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int row = my_row + j * RPL + ld_row;
+            k_voff[j] = (uint32_t)((j * RPL + ld_row) * k_rb) + (ld_pos ^ (row & (CH - 1))) * 16;
+            v_voff[j] = (uint32_t)((j * RPL + ld_row) * v_rb) + (ld_pos ^ (vswz(row) & (CH - 1))) * 16;
+        }
+        // Page ids: page i of the request at word i % PAGES; the half that is behind is filled again while the other one is in use.
+        uint32_t *ids = (uint32_t *)(smem + 2 * NW * TILEB);
+        const int32_t *tab = a.block_table + (int64_t)piece.b * a.bt_stride;
+        const int last_page = (kv - 1) >> a.page_shift;
+        auto fill = [&](int page0, int n, int from, int step) __attribute__((always_inline)) {
+            for (int i = from; i < n; i += step) {
+                const int page = page0 + i < last_page ? page0 + i : last_page;
+                ids[(page0 + i) & (PAGES - 1)] = (uint32_t)tab[page];
+            }
+        };
+        int next_fill = ((t_lo * TK) >> a.page_shift) & ~(PAGES / 2 - 1);  // first page of the half in use
+        fill(next_fill, PAGES, tid, NW * 64);
+        uint32_t *const found = ids + PAGES;  // whether values were replaced by zeros
+        if (tid == 0) *found = 0;
         __syncthreads();
+
+        auto page_of = [&](int k0) __attribute__((always_inline)) {  // of this wave's rows of the tile at row k0
+            int row = k0 + my_row;
+            row = row < kv ? row : kv - 1;
+            return ids[(row >> a.page_shift) & (PAGES - 1)];
+        };
+        auto issue = [&](auto v_tag, int k0, uint32_t page, uint32_t dst) __attribute__((always_inline)) {
+            constexpr bool V = decltype(v_tag)::value;
+            const int64_t page_bytes = V ? a.vc_s[0] : a.kc_s[0];
+            const int32_t rb = V ? v_rb : k_rb;
+            const int last = kv - 1 - k0;  // last valid row of the tile; rows past it repeat it
+            const int row = my_row < last ? my_row : last;
+            const uint8_t *src = uniform_ptr((V ? vp : kp) + (int64_t)__builtin_amdgcn_readfirstlane(page) * page_bytes +
+                                             (int64_t)((k0 + row) & page_mask) * rb);
+            const uint32_t to = __builtin_amdgcn_readfirstlane(base + dst + my_row * ROWB);
+            if (last >= TK - 1) {
 #pragma unroll
-        for (int i = 0; i < TK * CH / 64; ++i) {
-            const int row = (i * 64 + lane) / CH, pos = lane % CH;
-            const int src = k0 + row < kv ? k0 + row : kv - 1;  // rows past the end repeat the last; their scores are masked
-            const int64_t page = tab[src >> a.page_shift];
-            const int in_page = src & page_mask;
-            const uint8_t *kr = a.k_pages + page * a.kc_s[0] + g * a.kc_s[1] + in_page * a.kc_s[2];
-            const uint8_t *vr = a.v_pages + page * a.vc_s[0] + g * a.vc_s[1] + in_page * a.vc_s[2];
-            *(uint4 *)(smem + row * ROWB + (pos ^ (row & (CH - 1))) * 16) = *(const uint4 *)(kr + pos * 16);
-            *(uint4 *)(smem + TILEB + row * ROWB + (pos ^ (vswz(row) & (CH - 1))) * 16) = *(const uint4 *)(vr + pos * 16);
+                for (int j = 0; j < LOADS; ++j) copy_to_lds(src, V ? v_voff[j] : k_voff[j], to + j * RPL * ROWB);
+            } else {
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) {
+                    const int r = my_row + j * RPL + ld_row;
+                    const int swz = (V ? vswz(r) : r) & (CH - 1);
+                    copy_to_lds(src, (uint32_t)(((r < last ? r : last) - row) * rb) + (ld_pos ^ swz) * 16, to + j * RPL * ROWB);
+                }
+            }
+        };
+        auto next_k = [&](uint32_t off) __attribute__((always_inline)) { return off + TILEB == KS * TILEB ? 0u : off + TILEB; };
+        auto next_v = [&](uint32_t off) __attribute__((always_inline)) { return off + TILEB == V_RING + VS * TILEB ? V_RING : off + TILEB; };
+        // Request r (r >= -(PD + 1)) is the K rows of tile r + PD + 1 and the V rows of tile r + PD, as far as they exist.
+        int rq_k = 0;            // tile of the next K request; the next V request is for the one before
+        uint32_t rq_koff = 0, rq_voff = V_RING, page_k = 0, page_v = 0;
+        auto request_k = [&]() __attribute__((always_inline)) {
+            const int k0 = (t_lo + rq_k) * TK;
+            if (rq_k < n_tiles) issue(std::false_type{}, k0, page_k, rq_koff);
+            ++rq_k;
+            rq_koff = next_k(rq_koff);
+            page_v = page_k;
+            page_k = page_of(k0 + TK);
+        };
+        auto request_v = [&](uint32_t page) __attribute__((always_inline)) {  // of tile rq_k - 2, after its successor's K request
+            if (rq_k - 2 < n_tiles) issue(std::true_type{}, (t_lo + rq_k - 2) * TK, page, rq_voff);
+            rq_voff = next_v(rq_voff);
+        };
+        auto request = [&]() __attribute__((always_inline)) {
+            const uint32_t page = page_v;  // of the K tile requested last
+            request_k();
+            request_v(page);
+        };
+        if (loader) {
+            page_k = page_of(t_lo * TK);
+            request_k();
         }
-        __syncthreads();
-        floatx16 s;
+        // Query rows: through LDS, in the stages that the first requests leave free, in the layout of a K tile.
+        const uint32_t q_at = wave < 2 ? (PD + 1 + wave) * TILEB : wave < 6 ? V_RING + (PD + wave - 2) * TILEB : (KS + VS + wave - 6) * TILEB;
+        if (has_rows) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < KSTEPS; ++kk)
-            s = mfma32<F16>(__builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)(k_off ^ (uint32_t)(kk << 5))), q_reg[kk], s);
-        float mx = -INFINITY;
-        uint32_t seen = 0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int key = k0 + 8 * (e >> 2) + 4 * lh + (e & 3);
-            const bool sees = key >= seen_lo && key <= place;
-            seen |= (uint32_t)sees << e;
-            s[e] = sees ? s[e] : -INFINITY;
-            mx = fmaxf(mx, s[e]);
+            for (int j = 0; j < TPT; ++j) {
+                const int r = j * RPL + ld_row;
+                const QueryRow y = query_row(a, q, g, wave_row0 + r);
+                copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ (r & (CH - 1))) * 16,
+                                __builtin_amdgcn_readfirstlane(base + q_at + j * RPL * ROWB));
+            }
         }
-        mx = half_max(mx);
-        const float m_new = fmaxf(m, mx);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * c);
-        m = m_new;
-        l *= alpha;
-        const float mc = m == -INFINITY ? 0.f : m * c;
-        uint32_t pp[8];
+        if (loader)
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -mc)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c, -mc));
-            l += p0 + p1;
-            pp[e >> 1] = pack16<F16>(p0, p1);
-        }
-        bf16x8 frag[KSTEPS];
+            for (int r = 0; r < PD; ++r) request();
+        if (loader && n_tiles > PD) wait_vmem<PD * INFLIGHT>();
+        else wait_vmem<0>();
+        __syncthreads();  // tile 0 and the query rows are in LDS
+
+        auto ring_barrier = [&]() __attribute__((always_inline)) { asm volatile("s_barrier" ::: "memory"); };
+        // Tiles that every row of the block sees whole: rows all_lo .. all_hi - 1.
+        const QueryRow top_row = query_row(a, q, g, row0), end_row = query_row(a, q, g, row0 + ROWS - 1);
+        const int all_hi = top_row.place + 1, all_lo = end_row.lo;
+        auto partly_seen = [&](int t) __attribute__((always_inline)) { return t * TK + TK > all_hi || t * TK < all_lo; };
+        // V tiles up to `landed` (of this piece) are there: values that are not finite leave those that some row does not see whole.
+        // (A tile's first fragments are read a half-step later, at the earliest.)
+        int cleaned = 0;
+        auto clean = [&](int landed) __attribute__((always_inline)) {
+            bool any = false;
+            for (int t = cleaned; t < landed; ++t) {
+                if (!partly_seen(t_lo + t)) continue;  // (the same in all waves)
+                any = true;
+                if (tid >= TILEB / 16) continue;
+                uint4 *at = (uint4 *)(smem + V_RING + (t % VS) * TILEB + tid * 16);
+                bf16x8 v[1] = {__builtin_bit_cast(bf16x8, *at)};
+                if (drop_not_finite<F16>(v)) {
+                    *at = __builtin_bit_cast(uint4, v[0]);
+                    *found = 1;
+                }
+            }
+            cleaned = landed;
+            if (any) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        };
+        if (n_tiles == 1) clean(1);
+        // Before half-step 1, which reads K rows of tile 1: request -PD has landed; request 0 follows.
+        auto advance0 = [&]() __attribute__((always_inline)) {
+            if (n_tiles > 1) {
+                if (n_tiles > PD) wait_vmem<(PD - 1) * INFLIGHT>();
+                else wait_vmem<0>();
+                ring_barrier();
+                if (loader) request();
+                clean(n_tiles > PD ? 1 : n_tiles);
+            }
+        };
+        // Before half-steps h and h + 1 (h odd), which read K rows up to tile h + 2: requests up to h + 1 - PD have landed; requests
+        // h and h + 1 follow, into stages last read in half-step h - 1 or earlier.
+        auto advance_pair = [&](int h) __attribute__((always_inline)) {
+            if (h + PD < n_tiles) wait_vmem<(PD - 2) * INFLIGHT>();
+            else wait_vmem<0>();
+            ring_barrier();
+            if (loader) {
+                request();
+                request();
+            } else if (wave == NW - 1) {
+                // pages behind tile h are not asked for again; those of the half that follows are, 128 tiles on at the earliest
+                const int page = ((t_lo + h) * TK) >> a.page_shift;
+                if (page >= next_fill + PAGES / 2) {
+                    fill(next_fill + PAGES, PAGES / 2, lane, 64);
+                    next_fill += PAGES / 2;
+                }
+            }
+            clean(h + PD < n_tiles ? h + 2 : n_tiles);
+        };
+
+        if (!has_rows) {  // only feeds the rings
+            advance0();
+            for (int h = 1; h + 1 < n_tiles; h += 2) advance_pair(h);
+        } else {
+            typedef __attribute__((address_space(3))) const uint4 *lds_u4;
+            typedef __attribute__((address_space(3))) shortx4 *lds_s4;
+            const float c = a.scale_log2;
+            const uint32_t k_off0 = base + li * ROWB + ((lh ^ (li & (CH - 1))) * 16);
+            const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
+            const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
+            const uint32_t v_off0 = base + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
+            auto read_k = [&](uint32_t k_base, int f) __attribute__((always_inline)) {
+                return __builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)(k_base ^ (uint32_t)(f << 5)));
+            };
+            auto read_v = [&](uint32_t v_base, int f) __attribute__((always_inline)) {  // f = 16-key half * MT + d tile
+                const uint32_t at = (v_base ^ (uint32_t)((f % MT) << 6)) + ((f / MT) * 16) * ROWB;
+                const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)at));
+                const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB)));
+                return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+            };
+            // Rows that every query of the wave sees: free_lo .. free_hi - 1.
+            const int free_hi = __builtin_amdgcn_readfirstlane(x.place) + 1;
+            const int free_lo = __builtin_amdgcn_readlane(x.lo, 31);
+            auto mask = [&](floatx16 &s, int key0) __attribute__((always_inline)) {
+                if (key0 + TK <= free_hi && key0 >= free_lo) return;  // wave-uniform
 #pragma unroll
-        for (int f = 0; f < KSTEPS; ++f) {
-            const uint32_t at = (v_off ^ (uint32_t)((f % MT) << 6)) + ((f / MT) * 16) * ROWB;
-            const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)at));
-            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB)));
-            frag[f] = __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
+                for (int e = 0; e < 16; ++e) {
+                    const int key = key0 + 8 * (e >> 2) + 4 * lh + (e & 3);
+                    s[e] = key >= x.lo && key <= x.place ? s[e] : -INFINITY;
+                }
+            };
+            auto numerators = [&](const floatx16 &s, uint32_t (&pp)[8]) __attribute__((always_inline)) {  // with the current m
+                const float mc = st.m == -INFINITY ? 0.f : st.m * c;
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -mc)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c, -mc));
+                    pp[e >> 1] = pack16<F16>(p0, p1);
+                    sum += p0 + p1;
+                }
+                return sum;
+            };
+            auto raise = [&](const floatx16 &s) __attribute__((always_inline)) {
+                float mx = s[0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+                mx = half_max(mx);
+                if (__any((mx - st.m) * c > kLazy)) {  // also true while m is -inf
+                    const float m_new = fmaxf(st.m, mx);
+                    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((st.m - m_new) * c);
+                    st.m = m_new;
+                    st.l *= alpha;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) st.o[mt][e] *= alpha;
+                }
+            };
+
+            bf16x8 q_reg[KSTEPS];
+            {
+                const uint32_t at = k_off0 + q_at;
+#pragma unroll
+                for (int kk = 0; kk < KSTEPS; ++kk) q_reg[kk] = read_k(at, kk);
+            }
+
+            // ---- pipeline -----------------------------------------------------------------------
+            // A step is one tile: a score product (KSTEPS matrix instructions), the softmax arithmetic of 16 scores a lane, and an output
+            // product (KSTEPS).  Half-step h issues the score product of step h and the output product of step h - 2, one matrix
+            // instruction at a time, and between them the softmax of step h - 1, in two register slots that alternate.  K and V
+            // fragments rotate through FS registers each, refilled right after the instruction that read them.  The scheduling
+            // barriers pin this order.
+            constexpr int FS = KSTEPS / 2, PPG = 8 / KSTEPS;
+            bf16x8 k_frag[FS], v_frag[FS];
+            floatx16 s_sl[2];
+            uint32_t p_sl[2][8];
+            float mc = 0.f;
+            using yes = std::true_type;
+            using no = std::false_type;
+            auto half_step = [&](auto x_tag, auto qk_tag, auto sm_tag, auto kn_tag, auto vn_tag, uint32_t k_cur, uint32_t k_next,
+                                 uint32_t v_cur, uint32_t v_next) __attribute__((always_inline)) {
+                constexpr int X = decltype(x_tag)::value, Y = 1 - X;
+                constexpr bool QK = decltype(qk_tag)::value, SM = decltype(sm_tag)::value;
+                constexpr bool KN = decltype(kn_tag)::value, VN = decltype(vn_tag)::value;
+                bf16x8 pb[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    pb[i] = __builtin_bit_cast(bf16x8, make_uint4(p_sl[X][4 * i], p_sl[X][4 * i + 1], p_sl[X][4 * i + 2], p_sl[X][4 * i + 3]));
+                const float neg_mc = -mc;
+                const uint32_t kc = k_cur + k_off0, kn = k_next + k_off0, vc = v_cur + v_off0, vn = v_next + v_off0;
+                float sum = 0.f;
+                floatx16 s_new;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s_new[e] = 0.f;
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < KSTEPS; ++i) {
+                    float pe[PPG][2];
+                    st.o[i % MT] = mfma32<F16>(v_frag[i % FS], pb[i / MT], st.o[i % MT]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (SM) {
+#pragma unroll
+                        for (int u = 0; u < PPG; ++u) {
+                            const int e = 2 * (i * PPG + u);
+                            pe[u][0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s_sl[Y][e], c, neg_mc));
+                            pe[u][1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s_sl[Y][e + 1], c, neg_mc));
+                        }
+                    }
+                    if (i < FS) v_frag[i % FS] = read_v(vc, i + FS);
+                    else if constexpr (VN) v_frag[i % FS] = read_v(vn, i - FS);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (QK) s_new = mfma32<F16>(k_frag[i % FS], q_reg[i], s_new);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (SM) {
+#pragma unroll
+                        for (int u = 0; u < PPG; ++u) {
+                            p_sl[Y][i * PPG + u] = pack16<F16>(pe[u][0], pe[u][1]);
+                            sum += pe[u][0] + pe[u][1];
+                            asm volatile("" : "+v"(p_sl[Y][i * PPG + u]), "+v"(sum));  // (they would be sunk below the loop)
+                        }
+                    }
+                    if (i < FS) {
+                        if constexpr (QK) k_frag[i % FS] = read_k(kc, i + FS);
+                    } else if constexpr (KN) {
+                        k_frag[i % FS] = read_k(kn, i - FS);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (QK) s_sl[X] = s_new;
+                if constexpr (SM) {
+                    if (__any(!(sum < kSumCap<F16>))) {  // also infinities and NaN, and rows that have seen nothing yet
+                        raise(s_sl[Y]);
+                        sum = numerators(s_sl[Y], p_sl[Y]);
+                        mc = st.m * c;
+                    }
+                    st.l += sum;
+                }
+            };
+            using X0 = std::integral_constant<int, 0>;
+            using X1 = std::integral_constant<int, 1>;
+
+            const int key_first = t_lo * TK;
+#pragma unroll
+            for (int f = 0; f < FS; ++f) v_frag[f] = k_frag[f] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p_sl[s][e] = 0;  // an output product of zeros adds nothing
+            // scores of step 0; their largest is the reference exponent
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s_sl[0][e] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < KSTEPS; ++kk) s_sl[0] = mfma32<F16>(read_k(k_off0, kk), q_reg[kk], s_sl[0]);
+            mask(s_sl[0], key_first);
+            {
+                float mx = s_sl[0][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s_sl[0][e]);
+                st.m = half_max(mx);
+            }
+            mc = st.m * c;
+            advance0();
+            if (n_tiles > 1) {
+#pragma unroll
+                for (int f = 0; f < FS; ++f) k_frag[f] = read_k(TILEB + k_off0, f);
+            }
+            // Step -1 does not exist: its numerators are zeros, the "V tile" they are multiplied with is the K tile in stage 0 of its
+            // ring, which may hold infinities, and what comes of it is thrown away.
+            uint32_t k_cur = TILEB, k_nxt = 2 * TILEB, v_cur = 0, v_nxt = V_RING;
+            int key_h = key_first + TK;
+            auto step_on = [&]() __attribute__((always_inline)) {
+                k_cur = k_nxt;
+                k_nxt = next_k(k_nxt);
+                v_cur = v_nxt;
+                v_nxt = next_v(v_nxt);
+                key_h += TK;
+            };
+            int h = 1;
+            auto first_output = [&]() __attribute__((always_inline)) {
+                if (h != 1) return;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) st.o[mt][e] = 0.f;
+            };
+            for (; h + 1 < n_tiles; h += 2) {
+                advance_pair(h);
+                half_step(X1{}, yes{}, yes{}, yes{}, yes{}, k_cur, k_nxt, v_cur, v_nxt);
+                first_output();
+                mask(s_sl[1], key_h);
+                step_on();
+                half_step(X0{}, yes{}, yes{}, yes{}, yes{}, k_cur, k_nxt, v_cur, v_nxt);
+                mask(s_sl[0], key_h);
+                step_on();
+            }
+            // h = n_tiles - 1 (one step left to score) or h = n_tiles (none: the step scored here is void)
+            const bool is_void = h >= n_tiles;
+            half_step(X1{}, yes{}, yes{}, no{}, yes{}, is_void ? 0u : k_cur, 0, v_cur, v_nxt);
+            first_output();
+            if (is_void) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s_sl[1][e] = -INFINITY;
+            } else {
+                mask(s_sl[1], key_h);
+            }
+            step_on();
+            if (is_void) v_nxt = 0;  // V of the void step: read, not used
+            half_step(X0{}, no{}, yes{}, no{}, yes{}, 0, 0, v_cur, v_nxt);  // output h - 1, softmax h
+            step_on();
+            if (!is_void) half_step(X1{}, no{}, no{}, no{}, no{}, 0, 0, v_cur, 0);  // output h
         }
-        // infinities and NaN among the values reach the rows that see them, and no others (0 * inf in the product)
-        const bool not_finite = __any(seen != 0xffffu) && drop_not_finite<F16>(frag);
+        __syncthreads();  // every wave is done reading tiles: the rings are free
+        if (has_rows && __builtin_amdgcn_readfirstlane(*found))
+            for (int t = t_lo; t < t_hi; ++t) {
+                if (!partly_seen(t)) continue;
+                for (int key = t * TK; key < t * TK + TK && key < kv; ++key)
+                    if (key >= x.lo && key <= x.place)
+                        add_not_finite<F16>(st.o, vp + (int64_t)tab[key >> a.page_shift] * a.vc_s[0] + (int64_t)(key & page_mask) * v_rb, lh);
+            }
+    }
+    if (!has_rows) return;
+
+    // ---- rows out ------------------------------------------------------------------------------
+    const float l = half_sum(st.l);
+    if (piece.cut > 1) {
+        if (piece.split == 0 && tid == 0) write_entry(a, piece, g);
+        const int r = wave * 32 + li;
+        if (!x.ok) return;
+        float *dst = part_rows<D>(a, piece.slot + piece.split, g) + (int64_t)r * D;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[mt][e] *= alpha;
-#pragma unroll
-        for (int f = 0; f < KSTEPS; ++f) {
-            const uint32_t *u = pp + 4 * (f / MT);
-            o[f % MT] = mfma32<F16>(frag[f], __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), o[f % MT]);
-        }
-        if (not_finite)
-            for (int key = k0; key < k0 + TK && key < kv; ++key)
-                if (key >= seen_lo && key <= place)
-                    add_not_finite<F16>(o, a.v_pages + (int64_t)tab[key >> a.page_shift] * a.vc_s[0] + g * a.vc_s[1] + (key & page_mask) * a.vc_s[2], lh);
+            for (int rg = 0; rg < 4; ++rg)
+                *(float4 *)(dst + mt * 32 + 8 * rg + 4 * lh) = make_float4(st.o[mt][4 * rg], st.o[mt][4 * rg + 1], st.o[mt][4 * rg + 2], st.o[mt][4 * rg + 3]);
+        if (lh == 0) part_state(a, piece.slot + piece.split, g)[r] = make_float2(st.m, l);
+        return;
     }
-    if (!ok) return;
-    l = half_sum(l);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint8_t *dst = a.out + token * a.o_s[0] + head * a.o_s[1];
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing; NaN stays NaN
+    // through LDS (each wave its own rows), so that they leave whole, 16 bytes a lane
+    uint8_t *mine = smem + wave * (32 * ROWB);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int rg = 0; rg < 4; ++rg)
-            *(uint2 *)(dst + (mt * 32 + rg * 8 + 4 * lh) * 2) = make_uint2(pack16<F16>(o[mt][4 * rg] * inv, o[mt][4 * rg + 1] * inv),
-                                                                         pack16<F16>(o[mt][4 * rg + 2] * inv, o[mt][4 * rg + 3] * inv));
-    if (lh == 0) a.lse[(int64_t)token * a.n_q_heads + head] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+            *(uint2 *)(mine + li * ROWB + ((4 * mt + rg) ^ (li & (CH - 1))) * 16 + lh * 8) =
+                make_uint2(pack16<F16>(st.o[mt][4 * rg] * inv, st.o[mt][4 * rg + 1] * inv),
+                           pack16<F16>(st.o[mt][4 * rg + 2] * inv, st.o[mt][4 * rg + 3] * inv));
+#pragma unroll
+    for (int j = 0; j < TPT; ++j) {
+        const int r = j * RPL + lane / CH, pos = lane % CH;
+        const uint4 v = *(const uint4 *)(mine + r * ROWB + ((pos ^ (r & (CH - 1))) * 16));
+        const QueryRow y = query_row(a, q, g, wave_row0 + r);
+        if (y.ok) *(uint4 *)(a.out + y.token * a.o_s[0] + y.head * a.o_s[1] + pos * 16) = v;
+    }
+    if (lh == 0 && x.ok) a.lse[(int64_t)x.token * a.n_q_heads + x.head] = l == 0.f ? -INFINITY : (st.m * a.scale_log2 + log2f(l)) * kLn2;
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------
+
+// A word that no kernel of the call writes, at a wave-uniform address: through the scalar cache, so that
+// waiting for it does not wait for the copies in flight.
+__device__ __forceinline__ int32_t scalar_load(const int32_t *p)
+{
+    return *(__attribute__((address_space(4))) const int32_t *)(uintptr_t)p;
+}
+
+template <int D, bool F16>
+__device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece, int g, uint8_t *smem)
+{
+    constexpr int KSTEPS = D / 16, MT = D / 32, CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
+    constexpr int RPL = 64 / CH, LOADS = TK / RPL;
+    typedef std::conditional_t<F16, half_t, uint16_t> T16;
+    typedef __attribute__((address_space(3))) const uint4 *lds_u4;
+    typedef __attribute__((address_space(3))) shortx4 *lds_s4;
+    const Request &q = piece.q;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const QueryRow x = query_row(a, q, g, li);
+    const int2 span = block_tiles(a, q, 0);
+    const int per = div_up(span.y, piece.cut);
+    int t_lo = piece.split * per, t_hi = t_lo + per;
+    t_hi = span.x + (t_hi < span.y ? t_hi : span.y);
+    t_lo = span.x + (t_lo < span.y ? t_lo : span.y);
+    const int n_tiles = t_hi - t_lo, kv = q.kv;
+    const bool busy = wave < n_tiles;
+
+    const uint32_t base = lds_offset(smem), stage = base + wave * 2 * TILEB;  // K; the V stage follows
+    const uint8_t *kp = uniform_ptr(a.k_pages + g * a.kc_s[1]), *vp = uniform_ptr(a.v_pages + g * a.vc_s[1]);
+    const int page_mask = (1 << a.page_shift) - 1;
+    const int32_t *tab = a.block_table + (int64_t)piece.b * a.bt_stride;
+    const int ld_row = lane / CH, ld_pos = lane % CH;
+    const uint32_t k_chunk = (uint32_t)(ld_pos ^ ld_row), v_chunk = (uint32_t)(ld_pos ^ (vswz(ld_row) & (CH - 1)));
+    // the pages of rows 0..15 and 16..31 of tile t
+    auto pages_of = [&](int t) __attribute__((always_inline)) {
+        int r0 = (t_lo + t) * TK, r1 = r0 + 16;
+        r0 = r0 < kv ? r0 : kv - 1;
+        r1 = r1 < kv ? r1 : kv - 1;
+        return make_int2(scalar_load(tab + (r0 >> a.page_shift)), scalar_load(tab + (r1 >> a.page_shift)));
+    };
+    auto request = [&](auto v_tag, int t, int2 pages) __attribute__((always_inline)) {
+        constexpr bool V = decltype(v_tag)::value;
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(stage + (V ? TILEB : 0));
+        const int first = (t_lo + t) * TK, last = kv - 1 - first;
+        const int64_t page_bytes = V ? a.vc_s[0] : a.kc_s[0];
+        const int32_t rb = (int32_t)(V ? a.vc_s[2] : a.kc_s[2]);
+        const int last_group = last & ~(RPL - 1);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            // RPL rows in a row, which share a page; rows past the end repeat the last one, by that row's own group
+            const int src0 = j * RPL < last_group ? j * RPL : last_group;
+            int src = src0 + ld_row;
+            src = src < last ? src : last;
+            const int64_t page = src0 < 16 ? pages.x : pages.y;
+            const uint32_t chunk = RPL >= CH || V ? (V ? v_chunk : k_chunk) * 16 : (k_chunk * 16) ^ (uint32_t)(((j * RPL) & (CH - 1)) * 16);
+            copy_to_lds((V ? vp : kp) + page * page_bytes + (int64_t)((first + src0) & page_mask) * rb, (uint32_t)((src - src0) * rb) + chunk,
+                        dst + j * RPL * ROWB);
+        }
+    };
+    RowState<D> st;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st.o[mt][e] = 0.f;
+    st.m = -INFINITY;
+    st.l = 0.f;
+    if (busy) {
+        int2 pages = pages_of(wave);
+        // query rows into the V stage, in the layout of a K tile, and on into registers
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int r = j * RPL + ld_row;
+            const QueryRow y = query_row(a, q, g, r);
+            copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ (r & (CH - 1))) * 16,
+                            __builtin_amdgcn_readfirstlane(stage + TILEB + j * RPL * ROWB));
+        }
+        request(std::false_type{}, wave, pages);
+        int2 pages_next = pages_of(wave + NW);
+        const uint32_t k_off0 = stage + li * ROWB + ((lh ^ (li & (CH - 1))) * 16);
+        const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
+        const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
+        const uint32_t v_off0 = stage + TILEB + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
+        auto read_tile = [&](uint32_t off, bf16x8 (&frag)[KSTEPS]) __attribute__((always_inline)) {
+            asm volatile("" : "+v"(off));  // the fragments' addresses are formed here, not kept over the loop
+#pragma unroll
+            for (int kk = 0; kk < KSTEPS; ++kk) frag[kk] = __builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)(off ^ (uint32_t)(kk << 5)));
+#pragma unroll
+            for (int kk = 0; kk < KSTEPS; ++kk) asm volatile("" : "+v"(frag[kk]));  // in registers: the stage is free
+        };
+        bf16x8 q_reg[KSTEPS];
+        wait_vmem<LOADS>();
+        read_tile(k_off0 + TILEB, q_reg);
+        request(std::true_type{}, wave, pages);
+        const float c = a.scale_log2;
+        const int all_hi = __builtin_amdgcn_readfirstlane(x.place) + 1, all_lo = __builtin_amdgcn_readlane(x.lo, 31);
+        for (int t = wave; t < n_tiles; t += NW) {
+            bf16x8 frag[KSTEPS];
+            uint32_t pp[8];
+            if (t == wave) {
+                wait_vmem<LOADS>();  // the K rows; the V rows are the copies behind them
+            } else {
+                wait_vmem<0>();
+                request(std::true_type{}, t, pages);
+            }
+            read_tile(k_off0, frag);
+            floatx16 s;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < KSTEPS; ++kk) s = mfma32<F16>(frag[kk], q_reg[kk], s);
+            const int key0 = (t_lo + t) * TK;
+            const bool part = key0 + TK > all_hi || key0 < all_lo;  // some row does not see all of the tile
+            if (part) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = key0 + 8 * (e >> 2) + 4 * lh + (e & 3);
+                    s[e] = key >= x.lo && key <= x.place ? s[e] : -INFINITY;
+                }
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+            mx = half_max(mx);
+            if (__any((mx - st.m) * c > kLazy)) {  // also while m is -inf
+                const float m_new = fmaxf(st.m, mx);
+                const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((st.m - m_new) * c);
+                st.m = m_new;
+                st.l *= alpha;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) st.o[mt][e] *= alpha;
+            }
+            const float mc = st.m == -INFINITY ? 0.f : st.m * c;
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -mc)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c, -mc));
+                sum += p0 + p1;
+                pp[e >> 1] = pack16<F16>(p0, p1);
+            }
+            st.l += sum;
+            wait_vmem<0>();  // the V rows of tile t
+            pages = pages_next;
+            if (t + NW < n_tiles) request(std::false_type{}, t + NW, pages);
+            pages_next = pages_of(t + 2 * NW);
+            {
+                uint32_t off = v_off0;
+                asm volatile("" : "+v"(off));
+#pragma unroll
+                for (int f = 0; f < KSTEPS; ++f) {
+                    const uint32_t at = (off ^ (uint32_t)((f % MT) << 6)) + ((f / MT) * 16) * ROWB;
+                    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)at));
+                    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB)));
+                    frag[f] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+                }
+#pragma unroll
+                for (int f = 0; f < KSTEPS; ++f) asm volatile("" : "+v"(frag[f]));
+            }
+            const bool found = part && drop_not_finite<F16>(frag);
+#pragma unroll
+            for (int f = 0; f < KSTEPS; ++f) {
+                const uint32_t *u = pp + 4 * (f / MT);
+                st.o[f % MT] = mfma32<F16>(frag[f], __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), st.o[f % MT]);
+            }
+            if (found)
+                for (int key = key0; key < key0 + TK && key < kv; ++key)
+                    if (key >= x.lo && key <= x.place)
+                        add_not_finite<F16>(st.o, vp + (int64_t)tab[key >> a.page_shift] * a.vc_s[0] + (int64_t)(key & page_mask) * a.vc_s[2], lh);
+        }
+    }
+
+    // ---- merge of the waves, in fp32, through the stages (each wave its own: nothing reads them any more)
+    constexpr int CPR = D / 4;                // 16-byte pieces (4 floats) per row
+    constexpr int TPR = NW * 64 / 32;         // threads per row
+    constexpr int PASSES = CPR / TPR;         // pieces per thread
+    float2 *ml = (float2 *)(smem + 2 * NW * TILEB);  // (m, l) [row][wave]
+    static_assert(NW * 32 * 8 <= PAGES * 4, "the states lie in the place of the page ids");
+    const int n_active = n_tiles < NW ? n_tiles : NW;
+    const int row = tid / TPR;                // the row this thread finishes
+    const float l_tot = half_sum(st.l);
+    if (lh == 0) ml[li * NW + wave] = make_float2(st.m, l_tot);
+    if (busy) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int rg = 0; rg < 4; ++rg)
+                *(float4 *)(smem + wave * 2 * TILEB + li * (D * 4) + ((8 * mt + 2 * rg + lh) ^ (li & (CPR - 1))) * 16) =
+                    make_float4(st.o[mt][4 * rg], st.o[mt][4 * rg + 1], st.o[mt][4 * rg + 2], st.o[mt][4 * rg + 3]);
+    }
+    __syncthreads();
+    if (piece.cut > 1 && piece.split == 0 && tid == 0) write_entry(a, piece, g);
+    if (row >= q.rows) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) top = fmaxf(top, ml[row * NW + k].x);
+    float o[PASSES][4], l_sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[u][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+        if (k >= n_active) continue;
+        const float2 s = ml[row * NW + k];
+        const float scale = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * a.scale_log2);  // (NaN stays NaN)
+        l_sum += scale * s.y;
+#pragma unroll
+        for (int u = 0; u < PASSES; ++u) {
+            const float4 v = *(const float4 *)(smem + k * 2 * TILEB + row * (D * 4) + (((tid % TPR + u * TPR) ^ (row & (CPR - 1))) * 16));
+            o[u][0] += scale * v.x;
+            o[u][1] += scale * v.y;
+            o[u][2] += scale * v.z;
+            o[u][3] += scale * v.w;
+        }
+    }
+    if (piece.cut > 1) {
+        float *dst = part_rows<D>(a, piece.slot + piece.split, g) + row * D;
+#pragma unroll
+        for (int u = 0; u < PASSES; ++u) *(float4 *)(dst + (tid % TPR + u * TPR) * 4) = make_float4(o[u][0], o[u][1], o[u][2], o[u][3]);
+        if (tid % TPR == 0) part_state(a, piece.slot + piece.split, g)[row] = make_float2(top, l_sum);
+        return;
+    }
+    const QueryRow y = query_row(a, q, g, row);
+    const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;  // a row that sees nothing; NaN stays NaN
+    T16 *dst = (T16 *)(a.out + y.token * a.o_s[0] + y.head * a.o_s[1]);
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u)
+        *(uint2 *)(dst + (tid % TPR + u * TPR) * 4) = make_uint2(pack16<F16>(o[u][0] * inv, o[u][1] * inv), pack16<F16>(o[u][2] * inv, o[u][3] * inv));
+    if (tid % TPR == 0) a.lse[(int64_t)y.token * a.n_q_heads + y.head] = l_sum == 0.f ? -INFINITY : (top * a.scale_log2 + log2f(l_sum)) * kLn2;
+}
+
+// BLOCKS: the call may have requests with more than FEW rows
+template <int D, bool F16, bool BLOCKS>
+__global__ void __launch_bounds__(NW * 64, 2)
+chunk_attn_kernel(ChunkArgs a)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    const int i = (int)a.by_kv_heads.div(blockIdx.x), g = (int)blockIdx.x - i * a.n_kv_heads;
+    const int lane = threadIdx.x & 63;
+    const Piece piece = a.list ? find_listed(a, i, lane) : find_piece(a, i, lane);
+    if (!piece.valid) return;
+    if (!BLOCKS || piece.q.rows <= FEW) few_rows<D, F16>(a, piece, g, smem);
+    else if constexpr (BLOCKS) row_block<D, F16>(a, piece, g, smem);
+}
+
+// Joins the partial rows of a block that was cut: sum of O 2^((m - top) c) over that of l.
+template <int D, bool F16>
+__global__ void __launch_bounds__(256)
+chunk_merge_kernel(ChunkArgs a)
+{
+    constexpr int TPR = D / 4, RPW = 256 / TPR;  // threads per row, rows per workgroup
+    const int e = (int)a.by_kv_heads.div(blockIdx.x), g = (int)blockIdx.x - e * a.n_kv_heads;
+    if (e >= *a.n_entries) return;
+    const Entry x = ((const Entry *)a.entries)[e * a.n_kv_heads + g];
+    const int r = blockIdx.y * RPW + threadIdx.x / TPR, col = threadIdx.x % TPR * 4;
+    if (r >= x.rows) return;
+    float top = -INFINITY;
+    for (int k = 0; k < x.cut; ++k) top = fmaxf(top, part_state(a, x.slot + k, g)[r].x);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < x.cut; ++k) {
+        const float2 s = part_state(a, x.slot + k, g)[r];
+        const float4 v = *(const float4 *)(part_rows<D>(a, x.slot + k, g) + (int64_t)r * D + col);
+        const float scale = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * a.scale_log2);  // (NaN stays NaN)
+        l += scale * s.y;
+        o.x += scale * v.x;
+        o.y += scale * v.y;
+        o.z += scale * v.z;
+        o.w += scale * v.w;
+    }
+    const int row = x.row0 + r, token = (int)a.by_group.div((uint32_t)row), head = g * a.group + row - token * a.group;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *(uint2 *)(a.out + (x.first + token) * a.o_s[0] + head * a.o_s[1] + col * 2) =
+        make_uint2(pack16<F16>(o.x * inv, o.y * inv), pack16<F16>(o.z * inv, o.w * inv));
+    if (col == 0) a.lse[(int64_t)(x.first + token) * a.n_q_heads + head] = l == 0.f ? -INFINITY : (top * a.scale_log2 + log2f(l)) * kLn2;
+}
+
+template <int D, bool F16, bool BLOCKS> hipError_t launch_form(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream)
+{
+    auto kernel = chunk_attn_kernel<D, F16, BLOCKS>;
+    static std::atomic<uint64_t> allowed{0};
+    if (const hipError_t e = allow_dynamic_lds((const void *)kernel, kLds<D>, allowed); e != hipSuccess) return e;
+    if (a.list) {
+        hipLaunchKernelGGL(chunk_list_kernel, dim3(1), dim3(LIST_THREADS), 0, stream, a);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(NW * 64), kLds<D>, stream, a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || !plan.may_cut) return e;
+    constexpr int RPW = 256 / (D / 4);
+    hipLaunchKernelGGL((chunk_merge_kernel<D, F16>), dim3((unsigned)(plan.slots / 2) * a.n_kv_heads, (plan.part_rows + RPW - 1) / RPW), dim3(256), 0,
+                       stream, a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_chunk_attn(const ChunkArgs &a, int dtype, int head_dim, hipStream_t stream)
+ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units)
 {
-    // row blocks: each request rounds up by less than one
-    const int64_t rows = (int64_t)a.n_tokens * a.group, most = (int64_t)a.max_new_len * a.group;
-    int64_t blocks = (rows + 31 * (int64_t)(a.batch < a.n_tokens ? a.batch : a.n_tokens)) / 32;
-    if (blocks > a.batch * ((most + 31) / 32)) blocks = a.batch * ((most + 31) / 32);
-    const dim3 grid((unsigned)(blocks * a.n_kv_heads));
-    auto kernel = head_dim == 128 ? (dtype == LS_F16 ? chunk_attn_kernel<128, true> : chunk_attn_kernel<128, false>)
-                                  : (dtype == LS_F16 ? chunk_attn_kernel<64, true> : chunk_attn_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, a);
-    return hipGetLastError();
+    ChunkPlan plan{};
+    const int64_t group = d.n_q_heads / d.n_kv_heads, most = d.max_new_len * group;
+    plan.blocks_possible = most > FEW;
+    plan.part_rows = plan.blocks_possible ? (int)(most < ROWS ? most : ROWS) : (int)most;
+    plan.units = compute_units / d.n_kv_heads;
+    if (plan.units < 2) plan.units = 2;
+    plan.slots = plan.units;
+    // blocks at most: those of the rows there are, and one more per request with any
+    const int64_t rows = (int64_t)d.n_tokens * group, requests = d.batch < d.n_tokens ? d.batch : d.n_tokens;
+    int64_t blocks = (rows + (ROWS - 1) * requests) / ROWS, by_request = requests * ((most + ROWS - 1) / ROWS);
+    if (blocks > by_request) blocks = by_request;
+    if (blocks > rows) blocks = rows;
+    plan.may_cut = (d.max_kv_len + TK - 1) / TK + 1 > (plan.blocks_possible ? kMinSplit : kFewWhole);
+    // pieces: one per unit while the blocks are no more than the units, else the blocks and what cutting adds
+    plan.pieces = !plan.may_cut ? blocks : blocks <= plan.units ? plan.units : blocks + plan.slots;
+    plan.listed = d.batch > kWave;
+    return plan;
 }
+
+hipError_t launch_chunk_attn(const ChunkArgs &a, const ChunkPlan &plan, int dtype, int head_dim, hipStream_t stream)
+{
+#define LS_CHUNK_CASE(DD, HH) (plan.blocks_possible ? launch_form<DD, HH, true>(a, plan, stream) : launch_form<DD, HH, false>(a, plan, stream))
+    if (head_dim == 128) return dtype == LS_F16 ? LS_CHUNK_CASE(128, true) : LS_CHUNK_CASE(128, false);
+    return dtype == LS_F16 ? LS_CHUNK_CASE(64, true) : LS_CHUNK_CASE(64, false);
+#undef LS_CHUNK_CASE
+}
+
+size_t chunk_list_bytes(int batch) { return ((size_t)batch + 1) * sizeof(Listed); }
+size_t chunk_entry_bytes() { return sizeof(Entry); }
 
 }  // namespace ls

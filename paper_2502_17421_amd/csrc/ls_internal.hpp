@@ -155,6 +155,22 @@ struct WholeCall {
     int32_t in_parts;             // rows leave as parts, also those of a single split
 };
 
+// Compute units of the current device.
+inline int compute_units()
+{
+    static int cached = 0;
+    if (cached) return cached;
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) == hipSuccess &&
+        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
+        cached = n;
+    else {
+        (void)hipGetLastError();
+        return 256;  // MI355X; not cached so a later call with a device present asks again
+    }
+    return cached;
+}
+
 // Lets `kernel` have `bytes` of dynamic LDS on the current device; asked once per kernel and device (`done`: a bit per device).
 // A refusal is reported and asked for again by the next call.
 inline hipError_t allow_dynamic_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done)

@@ -34,10 +34,31 @@ struct ChunkArgs {
     int32_t batch, n_tokens, max_new_len, max_kv_len, n_q_heads, n_kv_heads, group, page_shift, bt_stride, window;
     FastDiv by_group, by_kv_heads;
     float scale_log2;
+    // how the work is cut (ChunkPlan); in the workspace: blocks that are cut and their number, partial rows with their (m, l), and
+    // for more than 64 requests the order of the pieces
+    int32_t units, slots, part_rows;
+    int32_t *n_entries;
+    void *entries, *list;
+    float2 *part_ml;
+    float *parts;
 };
+
+// What the host knows of the pieces of a call, all per KV head.
+struct ChunkPlan {
+    int64_t pieces;        // workgroups launched
+    int32_t units;         // compute units
+    int32_t slots;         // partial blocks there is room for
+    int32_t part_rows;     // query rows of a partial block
+    bool may_cut;          // some block may be cut: the merge is launched
+    bool blocks_possible;  // some request may have more rows than the few that waves share
+    bool listed;           // more requests than a wave has lanes
+};
+ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units);
+size_t chunk_list_bytes(int batch);
+size_t chunk_entry_bytes();
 
 hipError_t launch_page_plan(const PagePlanArgs &a, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream);
-hipError_t launch_chunk_attn(const ChunkArgs &a, int dtype, int head_dim, hipStream_t stream);
+hipError_t launch_chunk_attn(const ChunkArgs &a, const ChunkPlan &plan, int dtype, int head_dim, hipStream_t stream);
 
 }  // namespace ls

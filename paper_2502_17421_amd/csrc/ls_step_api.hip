@@ -80,6 +80,11 @@ int validate(const ls_chunk_desc *d)
         d->page_size < 16 || !power_of_two(d->page_size) || (int64_t)d->n_tokens * d->n_q_heads > (1 << 27) ||
         d->max_kv_len > (1 << 30) || d->n_q_heads > 65536)
         return LS_ERR_UNSUPPORTED;
+    // the kernels' divisions are exact in this range, and a launch has fewer than 2^32 threads
+    const int64_t group = d->n_q_heads / d->n_kv_heads;
+    if ((int64_t)d->max_new_len * group * group >= (1ll << 32)) return LS_ERR_UNSUPPORTED;
+    const ChunkPlan plan = plan_chunk(*d, compute_units());
+    if (plan.pieces * d->n_kv_heads >= (1 << 23) || plan.pieces * d->n_kv_heads * d->n_kv_heads >= (1ll << 32)) return LS_ERR_UNSUPPORTED;
     int rc;
     if ((rc = check_strides(d->q_stride, 2, d->head_dim, 2, false))) return rc;
     if ((rc = check_strides(d->o_stride, 2, d->head_dim, 2, true))) return rc;
@@ -88,6 +93,23 @@ int validate(const ls_chunk_desc *d)
     if (d->kc_stride[2] < d->head_dim || d->vc_stride[2] < d->head_dim) return LS_ERR_STRIDE;
     if (d->kc_stride[2] > kMaxRowStride || d->vc_stride[2] > kMaxRowStride) return LS_ERR_UNSUPPORTED;
     return LS_OK;
+}
+
+struct ChunkWorkspace {
+    size_t entries, list, part_ml, parts, total;
+};
+
+ChunkWorkspace layout(const ls_chunk_desc &d, const ChunkPlan &plan)
+{
+    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    const size_t rows = plan.may_cut ? (size_t)plan.slots * d.n_kv_heads * plan.part_rows : 0;
+    ChunkWorkspace w;
+    w.entries = 256;  // after the number of blocks that are cut
+    w.list = up(w.entries + (size_t)(plan.slots / 2) * d.n_kv_heads * chunk_entry_bytes());
+    w.part_ml = up(w.list + (plan.listed ? chunk_list_bytes(d.batch) : 0));
+    w.parts = up(w.part_ml + rows * sizeof(float2));
+    w.total = up(w.parts + rows * d.head_dim * sizeof(float));
+    return w;
 }
 
 int rope(const ls_rope_desc *d, const void *q, const void *k, const void *v, const int32_t *positions, const float *cos_sin,
@@ -176,7 +198,7 @@ int ls_chunk_workspace_bytes(const ls_chunk_desc *desc, size_t *bytes_out)
     const int rc = validate(desc);
     if (rc) return rc;
     if (!bytes_out) return LS_ERR_NULL;
-    *bytes_out = 256;
+    *bytes_out = layout(*desc, plan_chunk(*desc, compute_units())).total;
     return LS_OK;
 }
 
@@ -189,9 +211,9 @@ int ls_chunk_attn_paged(const ls_chunk_desc *desc, const void *q, const void *k_
     if (!q || !block_table || !cu_new || !kv_lens || !out || !lse) return LS_ERR_NULL;
     if (desc->max_kv_len > 0 && (!k_pages || !v_pages)) return LS_ERR_NULL;
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return LS_ERR_STRIDE;
-    size_t need = 0;
-    ls_chunk_workspace_bytes(desc, &need);
-    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need) return LS_ERR_WORKSPACE;
+    const ChunkPlan plan = plan_chunk(*desc, compute_units());
+    const ChunkWorkspace w = layout(*desc, plan);
+    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < w.total) return LS_ERR_WORKSPACE;
     ChunkArgs a{};
     a.q = (const uint8_t *)q, a.k_pages = (const uint8_t *)k_pages, a.v_pages = (const uint8_t *)v_pages;
     a.block_table = block_table, a.cu_new = cu_new, a.kv_lens = kv_lens;
@@ -206,7 +228,14 @@ int ls_chunk_attn_paged(const ls_chunk_desc *desc, const void *q, const void *k_
     a.by_group = FastDiv::of(a.group), a.by_kv_heads = FastDiv::of(a.n_kv_heads);
     const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / std::sqrt((float)desc->head_dim);
     a.scale_log2 = scale * kLog2e;
-    return launch_chunk_attn(a, desc->dtype, desc->head_dim, (hipStream_t)stream) == hipSuccess ? LS_OK : LS_ERR_HIP;
+    a.units = plan.units, a.slots = plan.may_cut ? plan.slots : 0, a.part_rows = plan.part_rows;
+    char *base = (char *)workspace;
+    a.n_entries = (int32_t *)base;
+    a.entries = base + w.entries;
+    a.list = plan.listed ? base + w.list : nullptr;
+    a.part_ml = (float2 *)(base + w.part_ml);
+    a.parts = (float *)(base + w.parts);
+    return launch_chunk_attn(a, plan, desc->dtype, desc->head_dim, (hipStream_t)stream) == hipSuccess ? LS_OK : LS_ERR_HIP;
 }
 
 }  // extern "C"
