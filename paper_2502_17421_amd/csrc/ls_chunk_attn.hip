@@ -5,8 +5,8 @@
 // first, row r = token r / G, head r % G, so that what a row sees grows with r.
 //
 // Two forms of work, in one launch, because a step mixes them.  Keys go in tiles of 32:
-//   row blocks    up to 256 query rows of a request and KV head; eight waves of 32 rows share the tiles, which four of them copy
-//                 into rings in LDS.  Bound by the matrix cores: 512 flops per byte of a tile.
+//   row blocks    up to 256 query rows (128 at head_dim 64) of a request and KV head; waves of 32 rows share the tiles, which
+//                 they copy into rings in LDS.  Bound by the matrix cores: 512 flops per byte of a tile.
 //   few rows      requests with at most 32 rows per KV head (single tokens); the eight waves hold the same rows and take
 //                 every eighth tile each, without barriers, and are merged at the end.  Bound by HBM.
 // Both take about the same time per tile while the chip is full (1.0 and 0.75 us), so work is counted in tiles.
@@ -36,21 +36,21 @@ namespace ls {
 namespace {
 
 constexpr int TK = 32;            // keys per tile
-constexpr int NW = 8;             // waves per workgroup
-constexpr int NL = 4;             // of which copy the tiles of a row block
-constexpr int ROWS = NW * 32;     // query rows per row block
+template <int D> constexpr int kWaves = D == 128 ? 8 : 4;  // per workgroup; at head_dim 64 two workgroups share a compute unit
+template <int D> constexpr int kRows = 32 * kWaves<D>;  // query rows per row block
 constexpr int FEW = 32;           // rows per KV head up to which the waves split the keys
-constexpr int PD = 3;             // requests (a K and a V tile) in flight of a row block
-constexpr int KS = PD + 3, VS = PD + 4;  // stages of its rings
-constexpr int PAGES = 512;        // page ids of a row block in LDS, a ring of two halves
+constexpr int PD = 4;             // requests (a K and a V tile) in flight of a row block
+constexpr int RS = 8;             // stages of its K ring, and of its V ring
+static_assert(RS >= PD + 4, "V rows are requested PD tiles ahead and read until two steps after");
 constexpr int kMinSplit = 24;     // a row block's pieces have at least so many tiles
 constexpr int kFewWhole = 48, kFewSplit = 16;  // few rows: up to so many tiles in one piece; fewest of a piece
 constexpr float kLazy = 8.f;      // the reference exponent is raised when a score exceeds it by 2^8
 template <bool F16> constexpr float kSumCap = F16 ? 0x1p15f : 0x1p40f;  // largest sum of a step's numerators without raising it
 
 template <int D> constexpr int kTileBytes = TK * D * 2;
-template <int D> constexpr int kLds = 2 * NW * kTileBytes<D> + PAGES * 4 + 16;
-static_assert(KS + VS + 2 <= 2 * NW, "two stages beyond the rings, for the query rows of the last two waves");
+// the rings, a stage for the query rows that find no free one, page ids, a flag;  or two stages per wave, and (m, l) of the rows
+template <int D> constexpr int kLds = (2 * RS + 1) * kTileBytes<D> + kWaves<D> * 512 + 16;
+static_assert(2 * 8 <= 2 * RS && 8 * 32 * 8 <= kTileBytes<64>, "LDS of the few rows");
 
 // ---- which piece --------------------------------------------------------------------------------
 
@@ -71,7 +71,7 @@ struct Cut {
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 
 // First tile and tiles of block k.
-__device__ __forceinline__ int2 block_tiles(const ChunkArgs &a, const Request &q, int k)
+template <int ROWS> __device__ __forceinline__ int2 block_tiles(const ChunkArgs &a, const Request &q, int k)
 {
     const int top = (k + 1) * ROWS < q.rows ? (k + 1) * ROWS : q.rows;
     const int place0 = q.kv - q.n;
@@ -81,7 +81,7 @@ __device__ __forceinline__ int2 block_tiles(const ChunkArgs &a, const Request &q
     return hi > lo ? make_int2(lo / TK, (hi + TK - 1) / TK - lo / TK) : make_int2(0, 0);
 }
 
-__device__ __forceinline__ Request load_request(const ChunkArgs &a, int b)
+template <int ROWS> __device__ __forceinline__ Request load_request(const ChunkArgs &a, int b)
 {
     Request q{0, 0, 0, 0, 0, 0, 0.f};
     if (b >= a.batch) return q;
@@ -94,7 +94,7 @@ __device__ __forceinline__ Request load_request(const ChunkArgs &a, int b)
     q.rows = (q.n < a.max_new_len ? q.n : a.max_new_len) * a.group;
     q.blocks = div_up(q.rows, ROWS);
     if (q.blocks > 0) {
-        const int t0 = block_tiles(a, q, 0).y, t1 = block_tiles(a, q, q.blocks - 1).y;
+        const int t0 = block_tiles<ROWS>(a, q, 0).y, t1 = block_tiles<ROWS>(a, q, q.blocks - 1).y;
         q.tiles = t0 > t1 ? t0 : t1;
         q.work = 0.5f * (float)q.blocks * (float)(t0 + t1);
     }
@@ -110,7 +110,7 @@ __device__ __forceinline__ int cut_of(const Request &q, int share)
 
 // Order of the pieces: the tiles of the last row of a block (all of a request's rows for a single block) over the cut.  Pieces of a
 // request whose key is at least x: those of its last blocks.
-__device__ __forceinline__ int pieces_from(const ChunkArgs &a, const Request &q, int cut, int x)
+template <int ROWS> __device__ __forceinline__ int pieces_from(const ChunkArgs &a, const Request &q, int cut, int x)
 {
     if (x <= 0) return q.blocks * cut;
     if (q.blocks == 0) return 0;
@@ -169,9 +169,9 @@ template <typename Sum> __device__ __forceinline__ int choose_share(const ChunkA
 }
 
 // Piece i of those of a KV head, up to 64 requests, a lane each (every wave for itself).
-__device__ __forceinline__ Piece find_piece(const ChunkArgs &a, int i, int lane)
+template <int ROWS> __device__ __forceinline__ Piece find_piece(const ChunkArgs &a, int i, int lane)
 {
-    const Request q = load_request(a, lane);
+    const Request q = load_request<ROWS>(a, lane);
     const int share = choose_share(a, [&](auto f) { return last_lane(scan_lanes(f(q))); });
     const int cut = cut_of(q, share);
     const int slots = cut > 1 ? q.blocks * cut : 0, entries = cut > 1 ? q.blocks : 0;
@@ -187,13 +187,13 @@ __device__ __forceinline__ Piece find_piece(const ChunkArgs &a, int i, int lane)
         top = y > top ? y : top;
     }
     int lo = 0, hi = top + 1;
-    while (last_lane(scan_lanes(pieces_from(a, q, cut, hi))) > 0) hi *= 2;  // (a block that is not full counts as one)
+    while (last_lane(scan_lanes(pieces_from<ROWS>(a, q, cut, hi))) > 0) hi *= 2;  // (a block that is not full counts as one)
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (last_lane(scan_lanes(pieces_from(a, q, cut, mid))) > i) lo = mid;
+        if (last_lane(scan_lanes(pieces_from<ROWS>(a, q, cut, mid))) > i) lo = mid;
         else hi = mid;
     }
-    const int above = pieces_from(a, q, cut, hi), same = pieces_from(a, q, cut, lo) - above;
+    const int above = pieces_from<ROWS>(a, q, cut, hi), same = pieces_from<ROWS>(a, q, cut, lo) - above;
     const int rest = i - last_lane(scan_lanes(above));
     const int upto = scan_lanes(same);
     const uint64_t holds = __ballot(upto > rest);
@@ -219,6 +219,7 @@ struct Listed {
 };
 constexpr int LIST_THREADS = 1024, LIST_PER = LS_MAX_STEP_BATCH / LIST_THREADS;
 
+template <int ROWS>
 __global__ void __launch_bounds__(LIST_THREADS)
 chunk_list_kernel(ChunkArgs a)
 {
@@ -228,7 +229,7 @@ chunk_list_kernel(ChunkArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Request q[LIST_PER];
 #pragma unroll
-    for (int j = 0; j < LIST_PER; ++j) q[j] = load_request(a, tid + j * LIST_THREADS);
+    for (int j = 0; j < LIST_PER; ++j) q[j] = load_request<ROWS>(a, tid + j * LIST_THREADS);
     auto sum_threads = [&](auto x) {
         auto *part = [&] { if constexpr (std::is_same_v<decltype(x), float>) return part_f; else return part_i; }();
         x = scan_lanes(x);
@@ -270,7 +271,7 @@ chunk_list_kernel(ChunkArgs a)
 #pragma unroll
     for (int j = 0; j < LIST_PER; ++j) {
         const int at = tid * LIST_PER + j;
-        r[j] = load_request(a, at < a.batch ? order[at] : a.batch);
+        r[j] = load_request<ROWS>(a, at < a.batch ? order[at] : a.batch);
         cut[j] = cut_of(r[j], share);
         pieces += r[j].blocks * cut[j];
         slots += cut[j] > 1 ? r[j].blocks * cut[j] : 0;
@@ -304,7 +305,7 @@ chunk_list_kernel(ChunkArgs a)
 }
 
 // Piece i by the list: the last request that begins at or before it, 64 candidates at a time.
-__device__ __forceinline__ Piece find_listed(const ChunkArgs &a, int i, int lane)
+template <int ROWS> __device__ __forceinline__ Piece find_listed(const ChunkArgs &a, int i, int lane)
 {
     const Listed *list = (const Listed *)a.list;
     Piece p{};
@@ -320,7 +321,7 @@ __device__ __forceinline__ Piece find_listed(const ChunkArgs &a, int i, int lane
     if (lo >= a.batch) return p;
     const Listed e = list[lo];
     p.b = __builtin_amdgcn_readfirstlane(e.b);
-    p.q = load_request(a, p.b);
+    p.q = load_request<ROWS>(a, p.b);
     p.cut = __builtin_amdgcn_readfirstlane(e.cut);
     const int at = i - __builtin_amdgcn_readfirstlane(e.begin);
     const int from_end = at / p.cut;
@@ -375,7 +376,7 @@ struct Entry {
     int32_t first, row0, rows;  // first token of the request, first row of the block, its rows
     int32_t cut, slot;
 };
-__device__ __forceinline__ void write_entry(const ChunkArgs &a, const Piece &p, int g)
+template <int ROWS> __device__ __forceinline__ void write_entry(const ChunkArgs &a, const Piece &p, int g)
 {
     const int row0 = p.block * ROWS;
     ((Entry *)a.entries)[p.entry * a.n_kv_heads + g] = Entry{p.q.first, row0, p.q.rows - row0 < ROWS ? p.q.rows - row0 : ROWS, p.cut, p.slot};
@@ -383,24 +384,34 @@ __device__ __forceinline__ void write_entry(const ChunkArgs &a, const Piece &p, 
 
 // ---- row blocks -------------------------------------------------------------------------------------
 
+// A copy of 64 lanes whose LDS and global addresses are AT bytes further than lds_base and the lane's own.
+template <int AT> __device__ __forceinline__ void copy_tile_rows(const uint8_t *base, uint32_t voff, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" : : "s"(lds_base), "v"(voff), "s"(base), "n"(AT) : "memory");
+}
+
+// What bounds it: two waves share a SIMD, and each issues an instruction in five cycles or more, so 16 matrix instructions of 32 cycles
+// leave a wave some 200 slots.  The arithmetic of a tile takes 110 of them; hence rings of 8 stages, whose addresses wrap by a
+// mask, half of the waves for K and half for V, addresses of 64 tiles worked out at a time, a tile per lane, and one
+// comparison per mask.  (With 85 scalar instructions per tile and wave instead of 20 the matrix cores were busy half of the time.)
 template <int D, bool F16>
 __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece, int g, uint8_t *smem)
 {
+    constexpr int NW = kWaves<D>, ROWS = kRows<D>;
     constexpr int KSTEPS = D / 16, MT = D / 32, CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
     constexpr int RPL = 64 / CH;          // rows one copy of 64 lanes covers
     constexpr int TPT = TK / RPL;         // copies per tile and tensor
-    constexpr int LOADS = TPT / NL;       // of which each copying wave does so many: eight rows in a row, which share a page
-    constexpr int INFLIGHT = 2 * LOADS;   // copies per copying wave and request
-    constexpr uint32_t V_RING = KS * TILEB;
-    static_assert(LOADS * RPL == 8 && (PD + 1) * INFLIGHT + TPT <= 63, "copies of a wave");
+    constexpr int LOADS = TPT / (NW / 2); // of which a wave does so many: 8 or 16 rows in a row, which share a page
+    constexpr int MINE = LOADS * RPL;     // these rows
+    constexpr uint32_t RING = RS * TILEB; // bytes of a ring: K, then V
+    static_assert(LOADS == 2 && MINE <= 16 && (PD + 1) * LOADS + TPT + 1 <= 63, "copies of a wave");
     const Request &q = piece.q;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int row0 = piece.block * ROWS, wave_row0 = row0 + wave * 32;
     const bool has_rows = wave_row0 < q.rows;
-    const QueryRow x = query_row(a, q, g, wave_row0 + li);
 
     // tiles of this piece
-    const int2 span = block_tiles(a, q, piece.block);
+    const int2 span = block_tiles<ROWS>(a, q, piece.block);
     int per = div_up(span.y, piece.cut);
     per += piece.cut > 1 ? per & 1 : 0;  // tiles go in pairs
     int t_lo = piece.split * per, t_hi = t_lo + per;
@@ -419,91 +430,75 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
 
     if (n_tiles > 0) {
         // ---- copies -----------------------------------------------------------------------------
+        // The first half of the waves copies K rows, the other half V rows: MINE rows of each tile.
         const uint32_t base = lds_offset(smem);
-        const uint8_t *kp = uniform_ptr(a.k_pages + g * a.kc_s[1]), *vp = uniform_ptr(a.v_pages + g * a.vc_s[1]);
-        const int32_t k_rb = (int32_t)a.kc_s[2], v_rb = (int32_t)a.vc_s[2];
+        const bool is_v = wave >= NW / 2;
+        const int64_t *stride = is_v ? a.vc_s : a.kc_s;
+        const uint8_t *pool = uniform_ptr((is_v ? a.v_pages : a.k_pages) + g * stride[1]);
+        const int32_t rb = (int32_t)stride[2];
         const int page_mask = (1 << a.page_shift) - 1;
         const int ld_row = lane / CH, ld_pos = lane % CH;
-        const bool loader = wave < NL;
-        const int my_row = (wave % NL) * 8;  // first of the rows of a tile that this wave copies
-        uint32_t k_voff[LOADS], v_voff[LOADS];
+        const int my_row = wave % (NW / 2) * MINE;
+        auto chunk_at = [&](int row) __attribute__((always_inline)) { return (uint32_t)(ld_pos ^ ((is_v ? vswz(row) : row) & (CH - 1))) * 16; };
+        // Lane's offset for copy j from the first of those rows, less what the instruction adds (rows are at least ROWB apart).
+        uint32_t voff[LOADS];
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int row = my_row + j * RPL + ld_row;
-            k_voff[j] = (uint32_t)((j * RPL + ld_row) * k_rb) + (ld_pos ^ (row & (CH - 1))) * 16;
-            v_voff[j] = (uint32_t)((j * RPL + ld_row) * v_rb) + (ld_pos ^ (vswz(row) & (CH - 1))) * 16;
-        }
-        // Page ids: page i of the request at word i % PAGES; the half that is behind is filled again while the other one is in use.
-        uint32_t *ids = (uint32_t *)(smem + 2 * NW * TILEB);
+        for (int j = 0; j < LOADS; ++j) voff[j] = (uint32_t)((j * RPL + ld_row) * rb) + chunk_at(my_row + j * RPL + ld_row) - j * RPL * ROWB;
+        // Where this wave's rows of 64 tiles are, a tile per lane, as byte offsets into the pool; rows past the end repeat the last
+        // one, tiles past the last repeat it.  The page ids of the 64 tiles after those are on their way to LDS.
         const int32_t *tab = a.block_table + (int64_t)piece.b * a.bt_stride;
-        const int last_page = (kv - 1) >> a.page_shift;
-        auto fill = [&](int page0, int n, int from, int step) __attribute__((always_inline)) {
-            for (int i = from; i < n; i += step) {
-                const int page = page0 + i < last_page ? page0 + i : last_page;
-                ids[(page0 + i) & (PAGES - 1)] = (uint32_t)tab[page];
-            }
+        uint32_t *const ids = (uint32_t *)(smem + (2 * RS + 1) * TILEB) + wave * 128;
+        uint32_t *const found = (uint32_t *)(smem + (2 * RS + 1) * TILEB) + NW * 128;  // whether values were replaced by zeros
+        auto tile_row = [&](int tile) __attribute__((always_inline)) {
+            const int row = (t_lo + (tile < n_tiles ? tile : n_tiles - 1)) * TK + my_row;
+            return row < kv ? row : kv - 1;
         };
-        int next_fill = ((t_lo * TK) >> a.page_shift) & ~(PAGES / 2 - 1);  // first page of the half in use
-        fill(next_fill, PAGES, tid, NW * 64);
-        uint32_t *const found = ids + PAGES;  // whether values were replaced by zeros
+        uint64_t offs = 0;
+        auto place = [&](int first, uint32_t page) __attribute__((always_inline)) {
+            offs = (uint64_t)page * (uint64_t)stride[0] + (uint64_t)((int64_t)(tile_row(first + lane) & page_mask) * rb);
+        };
+        auto fetch_ids = [&](int first) __attribute__((always_inline)) {
+            const int32_t *src = tab + (tile_row(first + lane) >> a.page_shift);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                         : : "s"(__builtin_amdgcn_readfirstlane(lds_offset(ids + (first & 64)))), "v"(src) : "memory");
+        };
+        place(0, (uint32_t)tab[tile_row(lane) >> a.page_shift]);
         if (tid == 0) *found = 0;
-        __syncthreads();
+        if (n_tiles + PD + 2 > 64) fetch_ids(64);
 
-        auto page_of = [&](int k0) __attribute__((always_inline)) {  // of this wave's rows of the tile at row k0
-            int row = k0 + my_row;
-            row = row < kv ? row : kv - 1;
-            return ids[(row >> a.page_shift) & (PAGES - 1)];
-        };
-        auto issue = [&](auto v_tag, int k0, uint32_t page, uint32_t dst) __attribute__((always_inline)) {
-            constexpr bool V = decltype(v_tag)::value;
-            const int64_t page_bytes = V ? a.vc_s[0] : a.kc_s[0];
-            const int32_t rb = V ? v_rb : k_rb;
-            const int last = kv - 1 - k0;  // last valid row of the tile; rows past it repeat it
-            const int row = my_row < last ? my_row : last;
-            const uint8_t *src = uniform_ptr((V ? vp : kp) + (int64_t)__builtin_amdgcn_readfirstlane(page) * page_bytes +
-                                             (int64_t)((k0 + row) & page_mask) * rb);
-            const uint32_t to = __builtin_amdgcn_readfirstlane(base + dst + my_row * ROWB);
-            if (last >= TK - 1) {
-#pragma unroll
-                for (int j = 0; j < LOADS; ++j) copy_to_lds(src, V ? v_voff[j] : k_voff[j], to + j * RPL * ROWB);
+        // Request r (r >= -(PD + 1)) is the K rows of tile r + PD + 1 and the V rows of tile r + PD.
+        int rq = 0;  // tile of this wave's next request
+        uint32_t rq_off = 0;  // its place in the ring
+        const uint32_t rq_base = base + (is_v ? RING : 0) + my_row * ROWB;
+        const int tail = kv < t_hi * TK ? n_tiles - 1 : 1 << 30;  // first tile that is not whole
+        auto request = [&]() __attribute__((always_inline)) {
+            const int i = rq & 63;
+            if (i == 0 && rq > 0) {
+                place(rq, ids[(rq & 64) + lane]);
+                fetch_ids(rq + 64);
+            }
+            const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)offs, i) |
+                                 (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(offs >> 32), i) << 32;
+            const uint8_t *src = pool + off;
+            const uint32_t to = rq_base + rq_off;
+            if (rq < tail) {
+                copy_tile_rows<0>(src, voff[0], to);
+                copy_tile_rows<RPL * ROWB>(src, voff[1], to);
             } else {
+                const int last = kv - 1 - (t_hi - 1) * TK, first = my_row < last ? my_row : last;  // src is that row
 #pragma unroll
                 for (int j = 0; j < LOADS; ++j) {
                     const int r = my_row + j * RPL + ld_row;
-                    const int swz = (V ? vswz(r) : r) & (CH - 1);
-                    copy_to_lds(src, (uint32_t)(((r < last ? r : last) - row) * rb) + (ld_pos ^ swz) * 16, to + j * RPL * ROWB);
+                    copy_to_lds(src, (uint32_t)(((r < last ? r : last) - first) * rb) + chunk_at(r), to + j * RPL * ROWB);
                 }
             }
+            ++rq;
+            rq_off = (rq_off + TILEB) & (RING - 1);
         };
-        auto next_k = [&](uint32_t off) __attribute__((always_inline)) { return off + TILEB == KS * TILEB ? 0u : off + TILEB; };
-        auto next_v = [&](uint32_t off) __attribute__((always_inline)) { return off + TILEB == V_RING + VS * TILEB ? V_RING : off + TILEB; };
-        // Request r (r >= -(PD + 1)) is the K rows of tile r + PD + 1 and the V rows of tile r + PD, as far as they exist.
-        int rq_k = 0;            // tile of the next K request; the next V request is for the one before
-        uint32_t rq_koff = 0, rq_voff = V_RING, page_k = 0, page_v = 0;
-        auto request_k = [&]() __attribute__((always_inline)) {
-            const int k0 = (t_lo + rq_k) * TK;
-            if (rq_k < n_tiles) issue(std::false_type{}, k0, page_k, rq_koff);
-            ++rq_k;
-            rq_koff = next_k(rq_koff);
-            page_v = page_k;
-            page_k = page_of(k0 + TK);
-        };
-        auto request_v = [&](uint32_t page) __attribute__((always_inline)) {  // of tile rq_k - 2, after its successor's K request
-            if (rq_k - 2 < n_tiles) issue(std::true_type{}, (t_lo + rq_k - 2) * TK, page, rq_voff);
-            rq_voff = next_v(rq_voff);
-        };
-        auto request = [&]() __attribute__((always_inline)) {
-            const uint32_t page = page_v;  // of the K tile requested last
-            request_k();
-            request_v(page);
-        };
-        if (loader) {
-            page_k = page_of(t_lo * TK);
-            request_k();
-        }
-        // Query rows: through LDS, in the stages that the first requests leave free, in the layout of a K tile.
-        const uint32_t q_at = wave < 2 ? (PD + 1 + wave) * TILEB : wave < 6 ? V_RING + (PD + wave - 2) * TILEB : (KS + VS + wave - 6) * TILEB;
-        if (has_rows) {
+        if (!is_v) request();
+        // Query rows: through LDS, in stages that the first requests leave free, in the layout of a K tile.
+        const uint32_t q_at = (uint32_t)(wave < RS - PD - 1 ? PD + 1 + wave : wave < RS - PD - 1 + RS - PD ? RS + PD + wave - (RS - PD - 1) : 2 * RS) * TILEB;
+        if (has_rows)
 #pragma unroll
             for (int j = 0; j < TPT; ++j) {
                 const int r = j * RPL + ld_row;
@@ -511,80 +506,77 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
                 copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ (r & (CH - 1))) * 16,
                                 __builtin_amdgcn_readfirstlane(base + q_at + j * RPL * ROWB));
             }
-        }
-        if (loader)
 #pragma unroll
-            for (int r = 0; r < PD; ++r) request();
-        if (loader && n_tiles > PD) wait_vmem<PD * INFLIGHT>();
-        else wait_vmem<0>();
+        for (int r = 0; r < PD; ++r) request();
+        wait_vmem<PD * LOADS>();
         __syncthreads();  // tile 0 and the query rows are in LDS
 
         auto ring_barrier = [&]() __attribute__((always_inline)) { asm volatile("s_barrier" ::: "memory"); };
-        // Tiles that every row of the block sees whole: rows all_lo .. all_hi - 1.
-        const QueryRow top_row = query_row(a, q, g, row0), end_row = query_row(a, q, g, row0 + ROWS - 1);
-        const int all_hi = top_row.place + 1, all_lo = end_row.lo;
-        auto partly_seen = [&](int t) __attribute__((always_inline)) { return t * TK + TK > all_hi || t * TK < all_lo; };
-        // V tiles up to `landed` (of this piece) are there: values that are not finite leave those that some row does not see whole.
+        // Tiles (of this piece) that all rows between two see whole: the first of them, and how many.
+        auto seen_whole = [&](int first_row, int last_row) __attribute__((always_inline)) {
+            const QueryRow top = query_row(a, q, g, first_row), end = query_row(a, q, g, last_row);
+            const int from = div_up(end.lo, TK) - t_lo, to = (top.place + 1 > 0 ? top.place + 1 : 0) / TK - t_lo;
+            return make_int2(__builtin_amdgcn_readfirstlane(from), __builtin_amdgcn_readfirstlane(to > from ? to - from : 0));
+        };
+        auto inside = [&](int t, int2 range) __attribute__((always_inline)) { return (uint32_t)(t - range.x) < (uint32_t)range.y; };
+        const int2 block_whole = seen_whole(row0, row0 + ROWS - 1);
+        // V tiles h and h + 1 are there: values that are not finite leave tiles that some row of the block does not see whole.
         // (A tile's first fragments are read a half-step later, at the earliest.)
-        int cleaned = 0;
-        auto clean = [&](int landed) __attribute__((always_inline)) {
-            bool any = false;
-            for (int t = cleaned; t < landed; ++t) {
-                if (!partly_seen(t_lo + t)) continue;  // (the same in all waves)
-                any = true;
-                if (tid >= TILEB / 16) continue;
-                uint4 *at = (uint4 *)(smem + V_RING + (t % VS) * TILEB + tid * 16);
-                bf16x8 v[1] = {__builtin_bit_cast(bf16x8, *at)};
-                if (drop_not_finite<F16>(v)) {
-                    *at = __builtin_bit_cast(uint4, v[0]);
-                    *found = 1;
+        auto clean = [&](int from, int to) __attribute__((always_inline)) {
+            to = to < n_tiles ? to : n_tiles;
+            if (from >= to || (inside(from, block_whole) && inside(to - 1, block_whole))) return;
+            for (int t = from; t < to; ++t) {
+                if (inside(t, block_whole)) continue;  // (the same in all waves)
+                for (int i = tid; i < TILEB / 16; i += NW * 64) {
+                    uint4 *at = (uint4 *)(smem + RING + ((t * TILEB) & (RING - 1)) + i * 16);
+                    bf16x8 v[1] = {__builtin_bit_cast(bf16x8, *at)};
+                    if (drop_not_finite<F16>(v)) {
+                        *at = __builtin_bit_cast(uint4, v[0]);
+                        *found = 1;
+                    }
                 }
             }
-            cleaned = landed;
-            if (any) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         };
-        if (n_tiles == 1) clean(1);
         // Before half-step 1, which reads K rows of tile 1: request -PD has landed; request 0 follows.
         auto advance0 = [&]() __attribute__((always_inline)) {
-            if (n_tiles > 1) {
-                if (n_tiles > PD) wait_vmem<(PD - 1) * INFLIGHT>();
-                else wait_vmem<0>();
-                ring_barrier();
-                if (loader) request();
-                clean(n_tiles > PD ? 1 : n_tiles);
-            }
-        };
-        // Before half-steps h and h + 1 (h odd), which read K rows up to tile h + 2: requests up to h + 1 - PD have landed; requests
-        // h and h + 1 follow, into stages last read in half-step h - 1 or earlier.
-        auto advance_pair = [&](int h) __attribute__((always_inline)) {
-            if (h + PD < n_tiles) wait_vmem<(PD - 2) * INFLIGHT>();
-            else wait_vmem<0>();
+            wait_vmem<(PD - 1) * LOADS>();
             ring_barrier();
-            if (loader) {
-                request();
-                request();
-            } else if (wave == NW - 1) {
-                // pages behind tile h are not asked for again; those of the half that follows are, 128 tiles on at the earliest
-                const int page = ((t_lo + h) * TK) >> a.page_shift;
-                if (page >= next_fill + PAGES / 2) {
-                    fill(next_fill + PAGES, PAGES / 2, lane, 64);
-                    next_fill += PAGES / 2;
-                }
-            }
-            clean(h + PD < n_tiles ? h + 2 : n_tiles);
+            request();
+            clean(0, 1);
+        };
+        // Before half-steps h and h + 1 (h odd), which read K rows up to tile h + 2: requests up to h + 1 - PD have landed.  Requests
+        // h and h + 1 follow in these half-steps, into stages last read in half-step h - 1 or earlier.
+        auto advance_pair = [&](int h) __attribute__((always_inline)) {
+            wait_vmem<(PD - 2) * LOADS>();
+            ring_barrier();
+            if (!(inside(h, block_whole) && inside(h + 1, block_whole))) clean(h, h + 2);
+        };
+        // After the pairs: the V rows of the last tile have landed, request n_tiles - 1 - PD of n_tiles - 2 at least.
+        auto advance_last = [&](int h) __attribute__((always_inline)) {
+            wait_vmem<(PD - 1) * LOADS>();
+            ring_barrier();
+            clean(h, n_tiles);
         };
 
         if (!has_rows) {  // only feeds the rings
             advance0();
-            for (int h = 1; h + 1 < n_tiles; h += 2) advance_pair(h);
+            int h = 1;
+            for (; h + 1 < n_tiles; h += 2) {
+                advance_pair(h);
+                request();
+                request();
+            }
+            advance_last(h);
         } else {
             typedef __attribute__((address_space(3))) const uint4 *lds_u4;
             typedef __attribute__((address_space(3))) shortx4 *lds_s4;
             const float c = a.scale_log2;
+            const QueryRow x = query_row(a, q, g, wave_row0 + li);
             const uint32_t k_off0 = base + li * ROWB + ((lh ^ (li & (CH - 1))) * 16);
             const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
             const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
-            const uint32_t v_off0 = base + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
+            const uint32_t v_off0 = base + RING + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
             auto read_k = [&](uint32_t k_base, int f) __attribute__((always_inline)) {
                 return __builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)(k_base ^ (uint32_t)(f << 5)));
             };
@@ -594,14 +586,12 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
                 const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB)));
                 return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
             };
-            // Rows that every query of the wave sees: free_lo .. free_hi - 1.
-            const int free_hi = __builtin_amdgcn_readfirstlane(x.place) + 1;
-            const int free_lo = __builtin_amdgcn_readlane(x.lo, 31);
-            auto mask = [&](floatx16 &s, int key0) __attribute__((always_inline)) {
-                if (key0 + TK <= free_hi && key0 >= free_lo) return;  // wave-uniform
+            const int2 wave_whole = seen_whole(wave_row0, wave_row0 + 31);
+            auto mask = [&](floatx16 &s, int t) __attribute__((always_inline)) {
+                if (inside(t, wave_whole)) return;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = key0 + 8 * (e >> 2) + 4 * lh + (e & 3);
+                    const int key = (t_lo + t) * TK + 8 * (e >> 2) + 4 * lh + (e & 3);
                     s[e] = key >= x.lo && key <= x.place ? s[e] : -INFINITY;
                 }
             };
@@ -634,35 +624,31 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             };
 
             bf16x8 q_reg[KSTEPS];
-            {
-                const uint32_t at = k_off0 + q_at;
 #pragma unroll
-                for (int kk = 0; kk < KSTEPS; ++kk) q_reg[kk] = read_k(at, kk);
-            }
+            for (int kk = 0; kk < KSTEPS; ++kk) q_reg[kk] = read_k(k_off0 + q_at, kk);
 
             // ---- pipeline -----------------------------------------------------------------------
-            // A step is one tile: a score product (KSTEPS matrix instructions), the softmax arithmetic of 16 scores a lane, and an output
-            // product (KSTEPS).  Half-step h issues the score product of step h and the output product of step h - 2, one matrix
-            // instruction at a time, and between them the softmax of step h - 1, in two register slots that alternate.  K and V
-            // fragments rotate through FS registers each, refilled right after the instruction that read them.  The scheduling
+            // A step is one tile: KSTEPS matrix instructions for the scores, the softmax arithmetic of 16 scores a lane, and KSTEPS for
+            // the output.  Half-step h issues the score product of step h and the output product of step h - 2, and between them
+            // the softmax of step h - 1, in two register slots that alternate, and this wave's copies of a request.  K and V
+            // fragments rotate through FS registers each, refilled right after the instructions that read them.  The scheduling
             // barriers pin this order.
             constexpr int FS = KSTEPS / 2, PPG = 8 / KSTEPS;
             bf16x8 k_frag[FS], v_frag[FS];
             floatx16 s_sl[2];
             uint32_t p_sl[2][8];
-            float mc = 0.f;
+            float neg_mc = 0.f;
             using yes = std::true_type;
             using no = std::false_type;
-            auto half_step = [&](auto x_tag, auto qk_tag, auto sm_tag, auto kn_tag, auto vn_tag, uint32_t k_cur, uint32_t k_next,
+            auto half_step = [&](auto x_tag, auto qk_tag, auto sm_tag, auto kn_tag, auto vn_tag, auto rq_tag, uint32_t k_cur, uint32_t k_next,
                                  uint32_t v_cur, uint32_t v_next) __attribute__((always_inline)) {
                 constexpr int X = decltype(x_tag)::value, Y = 1 - X;
                 constexpr bool QK = decltype(qk_tag)::value, SM = decltype(sm_tag)::value;
-                constexpr bool KN = decltype(kn_tag)::value, VN = decltype(vn_tag)::value;
+                constexpr bool KN = decltype(kn_tag)::value, VN = decltype(vn_tag)::value, RQ = decltype(rq_tag)::value;
                 bf16x8 pb[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     pb[i] = __builtin_bit_cast(bf16x8, make_uint4(p_sl[X][4 * i], p_sl[X][4 * i + 1], p_sl[X][4 * i + 2], p_sl[X][4 * i + 3]));
-                const float neg_mc = -mc;
                 const uint32_t kc = k_cur + k_off0, kn = k_next + k_off0, vc = v_cur + v_off0, vn = v_next + v_off0;
                 float sum = 0.f;
                 floatx16 s_new;
@@ -701,13 +687,16 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
                         k_frag[i % FS] = read_k(kn, i - FS);
                     }
                     __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (RQ)
+                        if (i == 0) request();
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 if constexpr (QK) s_sl[X] = s_new;
                 if constexpr (SM) {
                     if (__any(!(sum < kSumCap<F16>))) {  // also infinities and NaN, and rows that have seen nothing yet
                         raise(s_sl[Y]);
                         sum = numerators(s_sl[Y], p_sl[Y]);
-                        mc = st.m * c;
+                        neg_mc = -(st.m * c);
                     }
                     st.l += sum;
                 }
@@ -715,43 +704,31 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             using X0 = std::integral_constant<int, 0>;
             using X1 = std::integral_constant<int, 1>;
 
-            const int key_first = t_lo * TK;
 #pragma unroll
             for (int f = 0; f < FS; ++f) v_frag[f] = k_frag[f] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p_sl[s][e] = 0;  // an output product of zeros adds nothing
+            for (int e = 0; e < 8; ++e) p_sl[0][e] = p_sl[1][e] = 0;  // an output product of zeros adds nothing
             // scores of step 0; their largest is the reference exponent
 #pragma unroll
             for (int e = 0; e < 16; ++e) s_sl[0][e] = 0.f;
 #pragma unroll
             for (int kk = 0; kk < KSTEPS; ++kk) s_sl[0] = mfma32<F16>(read_k(k_off0, kk), q_reg[kk], s_sl[0]);
-            mask(s_sl[0], key_first);
+            mask(s_sl[0], 0);
             {
                 float mx = s_sl[0][0];
 #pragma unroll
                 for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s_sl[0][e]);
                 st.m = half_max(mx);
+                neg_mc = -(st.m * c);
             }
-            mc = st.m * c;
             advance0();
-            if (n_tiles > 1) {
 #pragma unroll
-                for (int f = 0; f < FS; ++f) k_frag[f] = read_k(TILEB + k_off0, f);
-            }
-            // Step -1 does not exist: its numerators are zeros, the "V tile" they are multiplied with is the K tile in stage 0 of its
-            // ring, which may hold infinities, and what comes of it is thrown away.
-            uint32_t k_cur = TILEB, k_nxt = 2 * TILEB, v_cur = 0, v_nxt = V_RING;
-            int key_h = key_first + TK;
-            auto step_on = [&]() __attribute__((always_inline)) {
-                k_cur = k_nxt;
-                k_nxt = next_k(k_nxt);
-                v_cur = v_nxt;
-                v_nxt = next_v(v_nxt);
-                key_h += TK;
-            };
+            for (int f = 0; f < FS; ++f) k_frag[f] = read_k(TILEB + k_off0, f);
+            // Step -1 does not exist: its numerators are zeros, the V stage they are multiplied with is any, and what comes of it is
+            // thrown away.
+            uint32_t k_cur = TILEB, v_cur = 0;  // K tile h, V tile h - 2
             int h = 1;
+            auto next = [&](uint32_t off) __attribute__((always_inline)) { return (off + TILEB) & (RING - 1); };
             auto first_output = [&]() __attribute__((always_inline)) {
                 if (h != 1) return;
 #pragma unroll
@@ -759,47 +736,54 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
 #pragma unroll
                     for (int e = 0; e < 16; ++e) st.o[mt][e] = 0.f;
             };
+            v_cur = RING - TILEB;
             for (; h + 1 < n_tiles; h += 2) {
                 advance_pair(h);
-                half_step(X1{}, yes{}, yes{}, yes{}, yes{}, k_cur, k_nxt, v_cur, v_nxt);
+                const uint32_t k1 = next(k_cur), k2 = next(k1), v1 = next(v_cur), v2 = next(v1);
+                half_step(X1{}, yes{}, yes{}, yes{}, yes{}, yes{}, k_cur, k1, v_cur, v1);
                 first_output();
-                mask(s_sl[1], key_h);
-                step_on();
-                half_step(X0{}, yes{}, yes{}, yes{}, yes{}, k_cur, k_nxt, v_cur, v_nxt);
-                mask(s_sl[0], key_h);
-                step_on();
+                mask(s_sl[1], h);
+                half_step(X0{}, yes{}, yes{}, yes{}, yes{}, yes{}, k1, k2, v1, v2);
+                mask(s_sl[0], h + 1);
+                k_cur = k2;
+                v_cur = v2;
             }
+            advance_last(h);
             // h = n_tiles - 1 (one step left to score) or h = n_tiles (none: the step scored here is void)
             const bool is_void = h >= n_tiles;
-            half_step(X1{}, yes{}, yes{}, no{}, yes{}, is_void ? 0u : k_cur, 0, v_cur, v_nxt);
+            const uint32_t v1 = next(v_cur), v2 = next(v1);
+            half_step(X1{}, yes{}, yes{}, no{}, yes{}, no{}, k_cur, 0, v_cur, v1);
             first_output();
             if (is_void) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s_sl[1][e] = -INFINITY;
             } else {
-                mask(s_sl[1], key_h);
+                mask(s_sl[1], h);
             }
-            step_on();
-            if (is_void) v_nxt = 0;  // V of the void step: read, not used
-            half_step(X0{}, no{}, yes{}, no{}, yes{}, 0, 0, v_cur, v_nxt);  // output h - 1, softmax h
-            step_on();
-            if (!is_void) half_step(X1{}, no{}, no{}, no{}, no{}, 0, 0, v_cur, 0);  // output h
+            half_step(X0{}, no{}, yes{}, no{}, yes{}, no{}, 0, 0, v1, v2);  // output h - 1, softmax h
+            if (!is_void) half_step(X1{}, no{}, no{}, no{}, no{}, no{}, 0, 0, v2, 0);  // output h
         }
+        wait_vmem<0>();   // requests past the last tile
         __syncthreads();  // every wave is done reading tiles: the rings are free
-        if (has_rows && __builtin_amdgcn_readfirstlane(*found))
+        if (has_rows && __builtin_amdgcn_readfirstlane(*found)) {
+            const QueryRow x = query_row(a, q, g, wave_row0 + li);
             for (int t = t_lo; t < t_hi; ++t) {
-                if (!partly_seen(t)) continue;
+                if (inside(t - t_lo, block_whole)) continue;
                 for (int key = t * TK; key < t * TK + TK && key < kv; ++key)
                     if (key >= x.lo && key <= x.place)
-                        add_not_finite<F16>(st.o, vp + (int64_t)tab[key >> a.page_shift] * a.vc_s[0] + (int64_t)(key & page_mask) * v_rb, lh);
+                        add_not_finite<F16>(st.o, a.v_pages + (int64_t)tab[key >> a.page_shift] * a.vc_s[0] + g * a.vc_s[1] + (key & page_mask) * a.vc_s[2], lh);
             }
+        }
     }
     if (!has_rows) return;
 
     // ---- rows out ------------------------------------------------------------------------------
+    int out_row = wave_row0 + li;
+    asm volatile("" : "+v"(out_row));  // (worked out again: kept, the row's place would take registers over the loop)
+    const QueryRow x = query_row(a, q, g, out_row);
     const float l = half_sum(st.l);
     if (piece.cut > 1) {
-        if (piece.split == 0 && tid == 0) write_entry(a, piece, g);
+        if (piece.split == 0 && tid == 0) write_entry<ROWS>(a, piece, g);
         const int r = wave * 32 + li;
         if (!x.ok) return;
         float *dst = part_rows<D>(a, piece.slot + piece.split, g) + (int64_t)r * D;
@@ -813,7 +797,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing; NaN stays NaN
     // through LDS (each wave its own rows), so that they leave whole, 16 bytes a lane
-    uint8_t *mine = smem + wave * (32 * ROWB);
+    uint8_t *mine = smem + wave * TILEB;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -843,6 +827,7 @@ __device__ __forceinline__ int32_t scalar_load(const int32_t *p)
 template <int D, bool F16>
 __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece, int g, uint8_t *smem)
 {
+    constexpr int NW = kWaves<D>, ROWS = kRows<D>;
     constexpr int KSTEPS = D / 16, MT = D / 32, CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
     constexpr int RPL = 64 / CH, LOADS = TK / RPL;
     typedef std::conditional_t<F16, half_t, uint16_t> T16;
@@ -851,7 +836,7 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
     const Request &q = piece.q;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const QueryRow x = query_row(a, q, g, li);
-    const int2 span = block_tiles(a, q, 0);
+    const int2 span = block_tiles<ROWS>(a, q, 0);
     const int per = div_up(span.y, piece.cut);
     int t_lo = piece.split * per, t_hi = t_lo + per;
     t_hi = span.x + (t_hi < span.y ? t_hi : span.y);
@@ -1009,7 +994,6 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
     constexpr int TPR = NW * 64 / 32;         // threads per row
     constexpr int PASSES = CPR / TPR;         // pieces per thread
     float2 *ml = (float2 *)(smem + 2 * NW * TILEB);  // (m, l) [row][wave]
-    static_assert(NW * 32 * 8 <= PAGES * 4, "the states lie in the place of the page ids");
     const int n_active = n_tiles < NW ? n_tiles : NW;
     const int row = tid / TPR;                // the row this thread finishes
     const float l_tot = half_sum(st.l);
@@ -1023,7 +1007,7 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
                     make_float4(st.o[mt][4 * rg], st.o[mt][4 * rg + 1], st.o[mt][4 * rg + 2], st.o[mt][4 * rg + 3]);
     }
     __syncthreads();
-    if (piece.cut > 1 && piece.split == 0 && tid == 0) write_entry(a, piece, g);
+    if (piece.cut > 1 && piece.split == 0 && tid == 0) write_entry<ROWS>(a, piece, g);
     if (row >= q.rows) return;
     float top = -INFINITY;
 #pragma unroll
@@ -1066,13 +1050,13 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
 
 // BLOCKS: the call may have requests with more than FEW rows
 template <int D, bool F16, bool BLOCKS>
-__global__ void __launch_bounds__(NW * 64, 2)
+__global__ void __launch_bounds__(kWaves<D> * 64, 2)
 chunk_attn_kernel(ChunkArgs a)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int i = (int)a.by_kv_heads.div(blockIdx.x), g = (int)blockIdx.x - i * a.n_kv_heads;
     const int lane = threadIdx.x & 63;
-    const Piece piece = a.list ? find_listed(a, i, lane) : find_piece(a, i, lane);
+    const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>>(a, i, lane);
     if (!piece.valid) return;
     if (!BLOCKS || piece.q.rows <= FEW) few_rows<D, F16>(a, piece, g, smem);
     else if constexpr (BLOCKS) row_block<D, F16>(a, piece, g, smem);
@@ -1117,10 +1101,10 @@ template <int D, bool F16, bool BLOCKS> hipError_t launch_form(const ChunkArgs &
     static std::atomic<uint64_t> allowed{0};
     if (const hipError_t e = allow_dynamic_lds((const void *)kernel, kLds<D>, allowed); e != hipSuccess) return e;
     if (a.list) {
-        hipLaunchKernelGGL(chunk_list_kernel, dim3(1), dim3(LIST_THREADS), 0, stream, a);
+        hipLaunchKernelGGL(chunk_list_kernel<kRows<D>>, dim3(1), dim3(LIST_THREADS), 0, stream, a);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(NW * 64), kLds<D>, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(kWaves<D> * 64), kLds<D>, stream, a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || !plan.may_cut) return e;
     constexpr int RPW = 256 / (D / 4);
     hipLaunchKernelGGL((chunk_merge_kernel<D, F16>), dim3((unsigned)(plan.slots / 2) * a.n_kv_heads, (plan.part_rows + RPW - 1) / RPW), dim3(256), 0,
@@ -1134,6 +1118,7 @@ ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units)
 {
     ChunkPlan plan{};
     const int64_t group = d.n_q_heads / d.n_kv_heads, most = d.max_new_len * group;
+    const int ROWS = d.head_dim == 128 ? kRows<128> : kRows<64>;
     plan.blocks_possible = most > FEW;
     plan.part_rows = plan.blocks_possible ? (int)(most < ROWS ? most : ROWS) : (int)most;
     plan.units = compute_units / d.n_kv_heads;
