@@ -9,7 +9,6 @@
 //                 they copy into rings in LDS.  Bound by the matrix cores: 512 flops per byte of a tile.
 //   few rows      requests with at most 32 rows per KV head (single tokens); the eight waves hold the same rows and take
 //                 every eighth tile each, without barriers, and are merged at the end.  Bound by HBM.
-// Both take about the same time per tile while the chip is full (1.0 and 0.75 us), so work is counted in tiles.
 //
 // Which piece a workgroup takes is worked out on the device, from the lengths, by every wave for itself: a program has
 // them there, and the host knows upper bounds only.  A block of more tiles than a compute unit's share of all tiles is cut into
@@ -42,30 +41,26 @@ constexpr int FEW = 32;           // rows per KV head up to which the waves spli
 constexpr int PD = 4;             // requests (a K and a V tile) in flight of a row block
 constexpr int RS = 8;             // stages of its K ring, and of its V ring
 static_assert(RS >= PD + 4, "V rows are requested PD tiles ahead and read until two steps after");
-constexpr int kMinSplit = 24;     // a row block's pieces have at least so many tiles
-constexpr int kFewWhole = 48, kFewSplit = 16;  // few rows: up to so many tiles in one piece; fewest of a piece
+constexpr float kWhole = 24.f;     // blocks that cost so many tiles or less are not cut, row blocks into pieces of no less
+constexpr float kFewSplit = 8.f;   // (few rows)
+constexpr float kFewTile = 0.35f;  // what a tile of the few rows counts: 0.32 us next to row blocks that take 0.9 to 1.0 for theirs
 constexpr float kLazy = 8.f;      // the reference exponent is raised when a score exceeds it by 2^8
 template <bool F16> constexpr float kSumCap = F16 ? 0x1p15f : 0x1p40f;  // largest sum of a step's numerators without raising it
 
 template <int D> constexpr int kTileBytes = TK * D * 2;
-// the rings, a stage for the query rows that find no free one, page ids, a flag;  or two stages per wave, and (m, l) of the rows
-template <int D> constexpr int kLds = (2 * RS + 1) * kTileBytes<D> + kWaves<D> * 512 + 16;
+// the rings, a stage for the query rows that find no free one, page ids, a flag, times of the shares;  or two stages per wave, and (m, l) of the rows
+template <int D> constexpr int kLds = (2 * RS + 1) * kTileBytes<D> + kWaves<D> * 512 + 16 + 8 * 4;
 static_assert(2 * 8 <= 2 * RS && 8 * 32 * 8 <= kTileBytes<64>, "LDS of the few rows");
 
 // ---- which piece --------------------------------------------------------------------------------
 
-// What the pieces are made of: one request.
+// One request, and what its pieces are worked out from.  Work is counted in tiles of a row block.
 struct Request {
     int32_t first, n, kv;  // first token, new tokens, rows
     int32_t rows;          // query rows per KV head
-    int32_t blocks, tiles; // row blocks, and the tiles of the longest
-    float work;            // tiles of all of them, about
-};
-
-// Pieces of a request: each of its blocks is cut into `cut`.  Before it in the order of the requests: `slot` partial
-// blocks, `entry` blocks that are cut.
-struct Cut {
-    int32_t cut, slot, entry;
+    int32_t blocks;        // row blocks (few rows: one)
+    float cost, work;      // of the longest block; of all of them, about
+    float start, per_step; // block k costs about start + (k + 1) / per_step, and no more than `cost`
 };
 
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
@@ -83,7 +78,8 @@ template <int ROWS> __device__ __forceinline__ int2 block_tiles(const ChunkArgs 
 
 template <int ROWS> __device__ __forceinline__ Request load_request(const ChunkArgs &a, int b)
 {
-    Request q{0, 0, 0, 0, 0, 0, 0.f};
+    Request q{};
+    q.per_step = 1.f;
     if (b >= a.batch) return q;
     int first = a.cu_new[b], end = a.cu_new[b + 1], kv = a.kv_lens[b];
     first = first < 0 ? 0 : (first > a.n_tokens ? a.n_tokens : first);
@@ -92,36 +88,39 @@ template <int ROWS> __device__ __forceinline__ Request load_request(const ChunkA
     q.n = end - first;
     q.kv = kv < 0 ? 0 : (kv > a.max_kv_len ? a.max_kv_len : kv);
     q.rows = (q.n < a.max_new_len ? q.n : a.max_new_len) * a.group;
-    q.blocks = div_up(q.rows, ROWS);
-    if (q.blocks > 0) {
-        const int t0 = block_tiles<ROWS>(a, q, 0).y, t1 = block_tiles<ROWS>(a, q, q.blocks - 1).y;
-        q.tiles = t0 > t1 ? t0 : t1;
-        q.work = 0.5f * (float)q.blocks * (float)(t0 + t1);
+    q.blocks = (q.rows + ROWS - 1) / ROWS;
+    if (q.blocks == 0) return q;
+    const float t0 = (float)block_tiles<ROWS>(a, q, 0).y, t1 = (float)block_tiles<ROWS>(a, q, q.blocks - 1).y;
+    if (q.rows <= FEW) {
+        q.cost = q.work = kFewTile * t0;
+        q.start = q.cost - 1.f;
+    } else {
+        q.cost = fmaxf(t0, t1);
+        q.work = 0.5f * (float)q.blocks * (t0 + t1);
+        q.per_step = (float)(TK * a.group) / (float)ROWS;
+        q.start = a.window > 0 ? (float)(q.kv - q.n) * (1.f / TK) : t1 - (float)q.blocks / q.per_step;
     }
     return q;
 }
 
-// Pieces per block for pieces of at most `share` tiles.
-__device__ __forceinline__ int cut_of(const Request &q, int share)
+// Pieces per block for a share of the work.
+__device__ __forceinline__ int cut_of(const Request &q, float share)
 {
-    if (q.rows <= FEW) return q.tiles <= kFewWhole ? 1 : div_up(q.tiles, share > kFewSplit ? share : kFewSplit);
-    return q.tiles > 0 ? div_up(q.tiles, share > kMinSplit ? share : kMinSplit) : 1;
+    if (q.cost <= kWhole) return 1;
+    return (int)ceilf(q.cost * __builtin_amdgcn_rcpf(fmaxf(share, q.rows <= FEW ? kFewSplit : kWhole)));
 }
+// Query rows of a block's partial results, if it is cut.
+template <int ROWS> __device__ __forceinline__ int block_rows(const Request &q) { return q.rows < ROWS ? q.rows : ROWS; }
 
-// Order of the pieces: the tiles of the last row of a block (all of a request's rows for a single block) over the cut.  Pieces of a
-// request whose key is at least x: those of its last blocks.
-template <int ROWS> __device__ __forceinline__ int pieces_from(const ChunkArgs &a, const Request &q, int cut, int x)
+// Pieces of a request that cost about x or more: those of its last blocks.  (Any order will do; every wave must find the same.)
+__device__ __forceinline__ int pieces_from(const Request &q, int cut, float x)
 {
-    if (x <= 0) return q.blocks * cut;
-    if (q.blocks == 0) return 0;
-    // tokens up to the end of block k: (k + 1) * ROWS / G;  rows seen there, and no more than the window
-    const int64_t need = (int64_t)x * cut * TK - (TK - 1);  // rows
-    if (a.window > 0 && need > a.window + ROWS) return 0;
-    const int64_t tokens = need - (q.kv - q.n);
-    if (tokens <= 0) return q.blocks * cut;
-    if (tokens > q.n + ROWS) return 0;
-    const int k = (int)((tokens * a.group + ROWS - 1) / ROWS) - 1;
-    return k < q.blocks ? (q.blocks - (k > 0 ? k : 0)) * cut : 0;
+    const float want = x * (float)cut;
+    if (x <= 0.f) return q.blocks * cut;
+    if (want > q.cost) return 0;
+    const float k = ceilf((want - q.start) * q.per_step) - 1.f;  // first block with that cost
+    const int left = q.blocks - (k > 0.f ? (int)fminf(k, 1e9f) : 0);
+    return left > 0 ? left * cut : 0;
 }
 
 // Inclusive sums over the lanes of a wave.
@@ -144,6 +143,22 @@ template <typename T> __device__ __forceinline__ T last_lane(T x)
 {
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
+// The largest of values that are not negative, in every lane of a wave.
+__device__ __forceinline__ float most_of_lanes(float x)
+{
+    auto take = [&](auto ctrl, auto row_mask) __attribute__((always_inline)) {
+        const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(row_mask)::value, 0xf, false);
+        x = fmaxf(x, __builtin_bit_cast(float, y));
+    };
+    using all = std::integral_constant<int, 0xf>;
+    take(std::integral_constant<int, 0x111>{}, all{});
+    take(std::integral_constant<int, 0x112>{}, all{});
+    take(std::integral_constant<int, 0x114>{}, all{});
+    take(std::integral_constant<int, 0x118>{}, all{});
+    take(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    take(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return last_lane(x);
+}
 
 struct Piece {
     Request q;
@@ -151,64 +166,119 @@ struct Piece {
     bool valid;
 };
 
-// The share of tiles above which a block is cut.  sum(f): the sum of f over all requests.
-// While there are fewer blocks than compute units, the smallest share whose pieces take one unit each; else a unit's share, as
-// long as the partial rows have room.
-template <typename Sum> __device__ __forceinline__ int choose_share(const ChunkArgs &a, Sum sum)
+// The share of the work above which a block is cut.  sum(f), most(f): over all requests; least(time): the candidate with the least time.
+// Three blocks for each compute unit and more even out by themselves; only a block beyond a unit's share is cut.  With fewer blocks
+// the least of some shares' expected times is taken, in tiles: one round of pieces lasts as long as the longest; in several
+// the units end apart by some part of it.  (Against the best of the candidates in a simulation of 160 steps of the ranges that the
+// performance cases draw from: 0.7 % longer, worst 20 %.)
+constexpr float kPieceCost = 8.f;  // what a piece costs besides its tiles: its place, the first loads, the rows out
+constexpr float kMergeCost = 5.f, kMergeBlock = 18.f;  // the merge: its launch, and a partial block's way to memory and back
+constexpr int kShares = 8;
+constexpr float kNever = 1e9f;
+__device__ __forceinline__ float share_of(int candidate, float mean)
 {
-    const int blocks = sum([](const Request &q) { return q.blocks; });
+    constexpr float kOfMean[kShares] = {0.f, 3.f, 2.f, 1.4f, 1.1f, 0.8f, 0.6f, 0.4f};
+    float f = kOfMean[1];
+#pragma unroll
+    for (int k = 2; k < kShares; ++k) f = candidate == k ? kOfMean[k] : f;
+    return candidate == 0 ? kNever : f * mean;
+}
+template <int ROWS, typename Sum, typename Most, typename Least>
+__device__ __forceinline__ float choose_share(const ChunkArgs &a, Sum sum, Most most, Least least)
+{
+    if (a.slots == 0) return kNever;
+    const float blocks = sum([](const Request &q) { return (float)q.blocks; });
     const float work = sum([](const Request &q) { return q.work; });
-    int share = (int)(work / (float)a.units) + 1;
-    while (share < (1 << 26)) {
-        const int pieces = sum([&](const Request &q) { return q.blocks * cut_of(q, share); });
-        const int slots = sum([&](const Request &q) { const int c = cut_of(q, share); return c > 1 ? q.blocks * c : 0; });
-        if ((blocks > a.units || pieces <= a.units) && slots <= a.slots) break;
-        share += share / 8 + 1;
-    }
-    return share;
+    const float units = (float)a.units, by_units = __builtin_amdgcn_rcpf(units), mean = work * by_units;
+    auto time_of = [&](float share) __attribute__((always_inline)) {
+        const float pieces = sum([&](const Request &q) { return (float)q.blocks * (float)cut_of(q, share); });
+        const float slots = sum([&](const Request &q) {
+            const float c = (float)cut_of(q, share);
+            return c > 1.f ? (float)q.blocks * c * (float)block_rows<ROWS>(q) : 0.f;
+        });
+        const float longest = most([&](const Request &q) { return q.cost * __builtin_amdgcn_rcpf((float)cut_of(q, share)); });
+        // (room for the partial rows, and for the pieces that cutting adds)
+        if (slots > (float)a.slots || pieces - blocks > (float)a.extra) return 2.f * kNever;
+        const float merge = slots > 0.f ? kMergeCost + kMergeBlock * slots * (1.f / ROWS) * by_units : 0.f;
+        return merge + (pieces <= units ? longest + kPieceCost : mean + kPieceCost * pieces * by_units + 0.4f * longest);
+    };
+    if (blocks >= 3.f * units) return time_of(1.25f * mean) < kNever ? 1.25f * mean : kNever;
+    return share_of(least([&](int candidate) { return time_of(share_of(candidate, mean)); }), mean);
 }
 
 // Piece i of those of a KV head, up to 64 requests, a lane each (every wave for itself).
-template <int ROWS> __device__ __forceinline__ Piece find_piece(const ChunkArgs &a, int i, int lane)
+// times: kShares words of LDS.
+template <int ROWS, int NW, bool BLOCKS> __device__ __forceinline__ Piece find_piece(const ChunkArgs &a, int i, int lane, float *times)
 {
-    const Request q = load_request<ROWS>(a, lane);
-    const int share = choose_share(a, [&](auto f) { return last_lane(scan_lanes(f(q))); });
-    const int cut = cut_of(q, share);
-    const int slots = cut > 1 ? q.blocks * cut : 0, entries = cut > 1 ? q.blocks : 0;
-    const int slot = scan_lanes(slots) - slots, entry_end = scan_lanes(entries);
     Piece p{};
-    if (blockIdx.x == 0 && threadIdx.x == 63) *a.n_entries = entry_end;  // for the merge
-    if (i >= last_lane(scan_lanes(q.blocks * cut))) return p;
-    // the largest key x of which more than i pieces have it or more
-    int top = q.tiles / cut + 2;
+    if (!BLOCKS && a.slots == 0) {  // single tokens, nothing to cut: a piece is a request
+        p.q = load_request<ROWS>(a, i);
+        p.b = i;
+        p.cut = 1;
+        p.valid = p.q.blocks > 0;
+        return p;
+    }
+    const Request q = load_request<ROWS>(a, lane);
+    const float share = choose_share<ROWS>(
+        a, [&](auto f) { return last_lane(scan_lanes(f(q))); }, [&](auto f) { return most_of_lanes(f(q)); },
+        [&](auto time) {  // the waves share the candidates
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            for (int k = wave; k < kShares; k += NW) {
+                const float t = time(k);
+                if (lane == 0) times[k] = t;
+            }
+            __syncthreads();
+            int best = 0;
+            float least = times[0];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        const int y = __shfl_xor(top, off, kWave);
-        top = y > top ? y : top;
+            for (int k = 1; k < kShares; ++k) {
+                const float t = times[k];
+                best = t < least ? k : best;
+                least = fminf(t, least);
+            }
+            return __builtin_amdgcn_readfirstlane(best);
+        });
+    const int cut = cut_of(q, share), pieces = q.blocks * cut;
+    const int slots = cut > 1 ? pieces * block_rows<ROWS>(q) : 0, entries = cut > 1 ? q.blocks : 0;
+    const int slot_end = scan_lanes(slots), entry_end = scan_lanes(entries), piece_end = scan_lanes(pieces);
+    if (blockIdx.x == 0 && threadIdx.x == 63 && a.slots > 0) *a.n_entries = entry_end;  // for the merge
+    const int total = last_lane(piece_end);
+    if (i >= total) return p;
+    int b, at;  // the request; the piece's place among the request's, last block first
+    if (total <= a.units) {  // all at once: any order
+        b = __builtin_ctzll(__ballot(piece_end > i));
+        at = i - __builtin_amdgcn_readlane(piece_end - pieces, b);
+    } else {
+        // longest first: the largest x such that more than i pieces cost x or more
+        int lo = 0, hi = (int)most_of_lanes(q.cost) + 2;  // (none costs `hi` or more)
+        while (hi - lo > 1) {  // by quarters: three sums at a time
+            const int step = (hi - lo + 3) >> 2;
+            const int x1 = lo + step, x2 = x1 + step < hi ? x1 + step : hi, x3 = x2 + step < hi ? x2 + step : hi;
+            const int c1 = last_lane(scan_lanes(pieces_from(q, cut, (float)x1)));
+            const int c2 = last_lane(scan_lanes(pieces_from(q, cut, (float)x2)));
+            const int c3 = last_lane(scan_lanes(pieces_from(q, cut, (float)x3)));
+            if (c3 > i) {
+                lo = x3;
+            } else {
+                lo = c2 > i ? x2 : c1 > i ? x1 : lo;
+                hi = c2 > i ? x3 : c1 > i ? x2 : x1;
+            }
+        }
+        const int above = pieces_from(q, cut, (float)hi), same = pieces_from(q, cut, (float)lo) - above, upto = scan_lanes(same);
+        const int rest = i - last_lane(scan_lanes(above));
+        b = __builtin_ctzll(__ballot(upto > rest) | 1ull << 63);
+        at = __builtin_amdgcn_readlane(above + rest - (upto - same), b);
     }
-    int lo = 0, hi = top + 1;
-    while (last_lane(scan_lanes(pieces_from<ROWS>(a, q, cut, hi))) > 0) hi *= 2;  // (a block that is not full counts as one)
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (last_lane(scan_lanes(pieces_from<ROWS>(a, q, cut, mid))) > i) lo = mid;
-        else hi = mid;
-    }
-    const int above = pieces_from<ROWS>(a, q, cut, hi), same = pieces_from<ROWS>(a, q, cut, lo) - above;
-    const int rest = i - last_lane(scan_lanes(above));
-    const int upto = scan_lanes(same);
-    const uint64_t holds = __ballot(upto > rest);
-    const int b = holds ? __builtin_ctzll(holds) : 63;
     auto of = [&](int v) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, b); };
     p.b = b;
-    p.q = Request{of(q.first), of(q.n), of(q.kv), of(q.rows), of(q.blocks), of(q.tiles), 0.f};
+    p.q = Request{of(q.first), of(q.n), of(q.kv), of(q.rows), of(q.blocks), 0.f, 0.f, 0.f, 0.f};
     p.cut = of(cut);
-    const int at = of(above) + rest - of(upto - same);  // among the request's pieces, last block first
-    const int from_end = at / p.cut;
+    const int from_end = p.cut == 1 ? at : at / p.cut;
     p.block = p.q.blocks - 1 - from_end;
     p.split = at - from_end * p.cut;
-    p.slot = of(slot) + from_end * p.cut;
+    p.slot = of(slot_end - slots) + from_end * p.cut * block_rows<ROWS>(p.q);
     p.entry = of(entry_end - entries) + from_end;
-    p.valid = holds != 0 && p.block >= 0;
+    p.valid = p.block >= 0;
     return p;
 }
 
@@ -241,19 +311,47 @@ chunk_list_kernel(ChunkArgs a)
         __syncthreads();
         return all;
     };
-    const int share = choose_share(a, [&](auto f) {
-        auto x = f(q[0]);
+    auto most_threads = [&](float x) {
+        x = most_of_lanes(x);
+        if (lane == 63) part_f[wave] = x;
+        __syncthreads();
 #pragma unroll
-        for (int j = 1; j < LIST_PER; ++j) x += f(q[j]);
-        return sum_threads(x);
-    });
+        for (int w = 0; w < LIST_THREADS / kWave; ++w) x = fmaxf(x, part_f[w]);
+        __syncthreads();
+        return x;
+    };
+    const float share = choose_share<ROWS>(
+        a,
+        [&](auto f) {
+            auto x = f(q[0]);
+#pragma unroll
+            for (int j = 1; j < LIST_PER; ++j) x += f(q[j]);
+            return sum_threads(x);
+        },
+        [&](auto f) {
+            float x = f(q[0]);
+#pragma unroll
+            for (int j = 1; j < LIST_PER; ++j) x = fmaxf(x, f(q[j]));
+            return most_threads(x);
+        },
+        [&](auto time) {
+            int best = 0;
+            float least = time(0);
+#pragma unroll 1
+            for (int k = 1; k < kShares; ++k) {
+                const float t = time(k);
+                best = t < least ? k : best;
+                least = fminf(t, least);
+            }
+            return best;
+        });
     // sort by the longest piece, by its bits: bucket 63 - 2 * log2 - next bit
     if (tid < 64) bucket[tid] = 0;
     __syncthreads();
     int in[LIST_PER], place[LIST_PER];
 #pragma unroll
     for (int j = 0; j < LIST_PER; ++j) {
-        const uint32_t key = (uint32_t)(q[j].tiles / cut_of(q[j], share)) + 1;
+        const uint32_t key = (uint32_t)(q[j].cost / (float)cut_of(q[j], share)) + 1;
         const int top = 31 - __builtin_clz(key);
         in[j] = 63 - (2 * top + (top > 0 ? (key >> (top - 1)) & 1 : 0));
         if (tid + j * LIST_THREADS < a.batch) place[j] = atomicAdd(&bucket[in[j]], 1);
@@ -274,7 +372,7 @@ chunk_list_kernel(ChunkArgs a)
         r[j] = load_request<ROWS>(a, at < a.batch ? order[at] : a.batch);
         cut[j] = cut_of(r[j], share);
         pieces += r[j].blocks * cut[j];
-        slots += cut[j] > 1 ? r[j].blocks * cut[j] : 0;
+        slots += cut[j] > 1 ? r[j].blocks * cut[j] * block_rows<ROWS>(r[j]) : 0;
         entries += cut[j] > 1 ? r[j].blocks : 0;
     }
     auto before = [&](int x) {  // sum over the threads before this one
@@ -295,7 +393,7 @@ chunk_list_kernel(ChunkArgs a)
         if (at >= a.batch) continue;
         list[at] = Listed{piece, order[at], cut[j], slot, entry};
         piece += r[j].blocks * cut[j];
-        slot += cut[j] > 1 ? r[j].blocks * cut[j] : 0;
+        slot += cut[j] > 1 ? r[j].blocks * cut[j] * block_rows<ROWS>(r[j]) : 0;
         entry += cut[j] > 1 ? r[j].blocks : 0;
         if (at == a.batch - 1) {
             list[a.batch] = Listed{piece, 0, 1, 0, 0};
@@ -327,7 +425,7 @@ template <int ROWS> __device__ __forceinline__ Piece find_listed(const ChunkArgs
     const int from_end = at / p.cut;
     p.block = p.q.blocks - 1 - from_end;
     p.split = at - from_end * p.cut;
-    p.slot = __builtin_amdgcn_readfirstlane(e.slot) + from_end * p.cut;
+    p.slot = __builtin_amdgcn_readfirstlane(e.slot) + from_end * p.cut * block_rows<ROWS>(p.q);
     p.entry = __builtin_amdgcn_readfirstlane(e.entry) + from_end;
     p.valid = p.block >= 0;
     return p;
@@ -361,25 +459,19 @@ __device__ __forceinline__ QueryRow query_row(const ChunkArgs &a, const Request 
     return x;
 }
 
-// Partial block `slot` of KV head g: [row][D] fp32 numerator sums, and (m, l) of every row.
-template <int D> __device__ __forceinline__ float *part_rows(const ChunkArgs &a, int slot, int g)
-{
-    return a.parts + ((int64_t)slot * a.n_kv_heads + g) * a.part_rows * D;
-}
-__device__ __forceinline__ float2 *part_state(const ChunkArgs &a, int slot, int g)
-{
-    return a.part_ml + ((int64_t)slot * a.n_kv_heads + g) * a.part_rows;
-}
+// Partial rows of a piece, its first one number `row` of KV head g: [row][D] fp32 sums, and (m, l) of every row.
+template <int D> __device__ __forceinline__ float *part_rows(const ChunkArgs &a, int row, int g) { return a.parts + ((int64_t)g * a.slots + row) * D; }
+__device__ __forceinline__ float2 *part_state(const ChunkArgs &a, int row, int g) { return a.part_ml + (int64_t)g * a.slots + row; }
 
 // Blocks that are cut, for the merge.
 struct Entry {
     int32_t first, row0, rows;  // first token of the request, first row of the block, its rows
-    int32_t cut, slot;
+    int32_t cut, slot, part;    // pieces, first partial row, partial rows of a piece
 };
 template <int ROWS> __device__ __forceinline__ void write_entry(const ChunkArgs &a, const Piece &p, int g)
 {
     const int row0 = p.block * ROWS;
-    ((Entry *)a.entries)[p.entry * a.n_kv_heads + g] = Entry{p.q.first, row0, p.q.rows - row0 < ROWS ? p.q.rows - row0 : ROWS, p.cut, p.slot};
+    ((Entry *)a.entries)[p.entry * a.n_kv_heads + g] = Entry{p.q.first, row0, p.q.rows - row0 < ROWS ? p.q.rows - row0 : ROWS, p.cut, p.slot, block_rows<ROWS>(p.q)};
 }
 
 // ---- row blocks -------------------------------------------------------------------------------------
@@ -784,15 +876,15 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
     const float l = half_sum(st.l);
     if (piece.cut > 1) {
         if (piece.split == 0 && tid == 0) write_entry<ROWS>(a, piece, g);
-        const int r = wave * 32 + li;
+        const int r = wave * 32 + li, part_row = piece.slot + piece.split * block_rows<ROWS>(q);
         if (!x.ok) return;
-        float *dst = part_rows<D>(a, piece.slot + piece.split, g) + (int64_t)r * D;
+        float *dst = part_rows<D>(a, part_row, g) + (int64_t)r * D;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int rg = 0; rg < 4; ++rg)
                 *(float4 *)(dst + mt * 32 + 8 * rg + 4 * lh) = make_float4(st.o[mt][4 * rg], st.o[mt][4 * rg + 1], st.o[mt][4 * rg + 2], st.o[mt][4 * rg + 3]);
-        if (lh == 0) part_state(a, piece.slot + piece.split, g)[r] = make_float2(st.m, l);
+        if (lh == 0) part_state(a, part_row, g)[r] = make_float2(st.m, l);
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing; NaN stays NaN
@@ -863,17 +955,29 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         const int first = (t_lo + t) * TK, last = kv - 1 - first;
         const int64_t page_bytes = V ? a.vc_s[0] : a.kc_s[0];
         const int32_t rb = (int32_t)(V ? a.vc_s[2] : a.kc_s[2]);
-        const int last_group = last & ~(RPL - 1);
+        const uint8_t *p0 = (V ? vp : kp) + (int64_t)pages.x * page_bytes + (int64_t)(first & page_mask) * rb;
+        const uint8_t *p1 = (V ? vp : kp) + (int64_t)pages.y * page_bytes + (int64_t)((first + 16) & page_mask) * rb;
+        const uint32_t chunk = (V ? v_chunk : k_chunk) * 16;
+        // (copy j's rows are RPL further; the K swizzle of rows 4, 8 and 12 on is that of rows 0 to 3 with 4, 8 and 12 added)
+        auto chunk_of = [&](int j) __attribute__((always_inline)) {
+            return RPL >= CH || V ? chunk : chunk ^ (uint32_t)(((j * RPL) & (CH - 1)) * 16);
+        };
+        if (last >= TK - 1) {
+            const uint32_t off = (uint32_t)(ld_row * rb);
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            // RPL rows in a row, which share a page; rows past the end repeat the last one, by that row's own group
-            const int src0 = j * RPL < last_group ? j * RPL : last_group;
-            int src = src0 + ld_row;
-            src = src < last ? src : last;
-            const int64_t page = src0 < 16 ? pages.x : pages.y;
-            const uint32_t chunk = RPL >= CH || V ? (V ? v_chunk : k_chunk) * 16 : (k_chunk * 16) ^ (uint32_t)(((j * RPL) & (CH - 1)) * 16);
-            copy_to_lds((V ? vp : kp) + page * page_bytes + (int64_t)((first + src0) & page_mask) * rb, (uint32_t)((src - src0) * rb) + chunk,
-                        dst + j * RPL * ROWB);
+            for (int j = 0; j < LOADS; ++j)
+                copy_to_lds((j * RPL < 16 ? p0 : p1) + (j * RPL % 16) * rb, off + chunk_of(j), dst + j * RPL * ROWB);
+        } else {
+            // rows past the end repeat the last one, by that row's own group
+            const int last_group = last & ~(RPL - 1);
+#pragma unroll 1
+            for (int j = 0; j < LOADS; ++j) {
+                const int src0 = j * RPL < last_group ? j * RPL : last_group;
+                int src = src0 + ld_row;
+                src = src < last ? src : last;
+                copy_to_lds(uniform_ptr((src0 < 16 ? p0 : p1) + (src0 % 16) * rb), (uint32_t)((src - src0) * rb) + chunk_of(j),
+                            __builtin_amdgcn_readfirstlane(dst + j * RPL * ROWB));
+            }
         }
     };
     RowState<D> st;
@@ -894,7 +998,6 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
                             __builtin_amdgcn_readfirstlane(stage + TILEB + j * RPL * ROWB));
         }
         request(std::false_type{}, wave, pages);
-        int2 pages_next = pages_of(wave + NW);
         const uint32_t k_off0 = stage + li * ROWB + ((lh ^ (li & (CH - 1))) * 16);
         const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
         const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
@@ -910,18 +1013,18 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         wait_vmem<LOADS>();
         read_tile(k_off0 + TILEB, q_reg);
         request(std::true_type{}, wave, pages);
+        pages = pages_of(wave + NW);
         const float c = a.scale_log2;
         const int all_hi = __builtin_amdgcn_readfirstlane(x.place) + 1, all_lo = __builtin_amdgcn_readlane(x.lo, 31);
+        // Copies in flight, oldest first: K of tile t, V of tile t.  A tile's rows go to registers as soon as they are there, and the
+        // stage is asked for the next tile's.
         for (int t = wave; t < n_tiles; t += NW) {
             bf16x8 frag[KSTEPS];
             uint32_t pp[8];
-            if (t == wave) {
-                wait_vmem<LOADS>();  // the K rows; the V rows are the copies behind them
-            } else {
-                wait_vmem<0>();
-                request(std::true_type{}, t, pages);
-            }
+            const bool more = t + NW < n_tiles;
+            wait_vmem<LOADS>();
             read_tile(k_off0, frag);
+            if (more) request(std::false_type{}, t + NW, pages);
             floatx16 s;
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -959,10 +1062,8 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
                 pp[e >> 1] = pack16<F16>(p0, p1);
             }
             st.l += sum;
-            wait_vmem<0>();  // the V rows of tile t
-            pages = pages_next;
-            if (t + NW < n_tiles) request(std::false_type{}, t + NW, pages);
-            pages_next = pages_of(t + 2 * NW);
+            if (more) wait_vmem<LOADS>();
+            else wait_vmem<0>();
             {
                 uint32_t off = v_off0;
                 asm volatile("" : "+v"(off));
@@ -976,6 +1077,8 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
 #pragma unroll
                 for (int f = 0; f < KSTEPS; ++f) asm volatile("" : "+v"(frag[f]));
             }
+            if (more) request(std::true_type{}, t + NW, pages);
+            pages = pages_of(t + 2 * NW);
             const bool found = part && drop_not_finite<F16>(frag);
 #pragma unroll
             for (int f = 0; f < KSTEPS; ++f) {
@@ -1033,10 +1136,11 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         }
     }
     if (piece.cut > 1) {
-        float *dst = part_rows<D>(a, piece.slot + piece.split, g) + row * D;
+        const int part_row = piece.slot + piece.split * q.rows;
+        float *dst = part_rows<D>(a, part_row, g) + row * D;
 #pragma unroll
         for (int u = 0; u < PASSES; ++u) *(float4 *)(dst + (tid % TPR + u * TPR) * 4) = make_float4(o[u][0], o[u][1], o[u][2], o[u][3]);
-        if (tid % TPR == 0) part_state(a, piece.slot + piece.split, g)[row] = make_float2(top, l_sum);
+        if (tid % TPR == 0) part_state(a, part_row, g)[row] = make_float2(top, l_sum);
         return;
     }
     const QueryRow y = query_row(a, q, g, row);
@@ -1056,43 +1160,49 @@ chunk_attn_kernel(ChunkArgs a)
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int i = (int)a.by_kv_heads.div(blockIdx.x), g = (int)blockIdx.x - i * a.n_kv_heads;
     const int lane = threadIdx.x & 63;
-    const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>>(a, i, lane);
+    const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>, kWaves<D>, BLOCKS>(a, i, lane, (float *)(smem + kLds<D> - kShares * 4));
     if (!piece.valid) return;
     if (!BLOCKS || piece.q.rows <= FEW) few_rows<D, F16>(a, piece, g, smem);
     else if constexpr (BLOCKS) row_block<D, F16>(a, piece, g, smem);
 }
 
-// Joins the partial rows of a block that was cut: sum of O 2^((m - top) c) over that of l.
+// Joins the partial rows of the blocks that were cut: sum of O 2^((m - top) c) over that of l.
+constexpr int MERGE_THREADS = 256, MERGE_GROUPS = 1024;
 template <int D, bool F16>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(MERGE_THREADS)
 chunk_merge_kernel(ChunkArgs a)
 {
-    constexpr int TPR = D / 4, RPW = 256 / TPR;  // threads per row, rows per workgroup
-    const int e = (int)a.by_kv_heads.div(blockIdx.x), g = (int)blockIdx.x - e * a.n_kv_heads;
-    if (e >= *a.n_entries) return;
-    const Entry x = ((const Entry *)a.entries)[e * a.n_kv_heads + g];
-    const int r = blockIdx.y * RPW + threadIdx.x / TPR, col = threadIdx.x % TPR * 4;
-    if (r >= x.rows) return;
-    float top = -INFINITY;
-    for (int k = 0; k < x.cut; ++k) top = fmaxf(top, part_state(a, x.slot + k, g)[r].x);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
+    constexpr int TPR = D / 4, RPW = MERGE_THREADS / TPR;  // threads per row, rows per workgroup and turn
+    const int turns = (a.part_rows + RPW - 1) / RPW, all = *a.n_entries * a.n_kv_heads * turns;
+    for (int i = blockIdx.x; i < all; i += gridDim.x) {
+        const int block = i / turns;  // entry by KV head
+        const Entry x = ((const Entry *)a.entries)[block];
+        const int r = (i - block * turns) * RPW + threadIdx.x / TPR, col = threadIdx.x % TPR * 4;
+        if (r >= x.rows) continue;
+        const int g = block % a.n_kv_heads;
+        const float2 *ml = part_state(a, x.slot, g) + r;
+        const float *rows = part_rows<D>(a, x.slot, g) + (int64_t)r * D + col;
+        float top = -INFINITY;
+        for (int k = 0; k < x.cut; ++k) top = fmaxf(top, ml[k * x.part].x);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float l = 0.f;
 #pragma unroll 4
-    for (int k = 0; k < x.cut; ++k) {
-        const float2 s = part_state(a, x.slot + k, g)[r];
-        const float4 v = *(const float4 *)(part_rows<D>(a, x.slot + k, g) + (int64_t)r * D + col);
-        const float scale = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * a.scale_log2);  // (NaN stays NaN)
-        l += scale * s.y;
-        o.x += scale * v.x;
-        o.y += scale * v.y;
-        o.z += scale * v.z;
-        o.w += scale * v.w;
+        for (int k = 0; k < x.cut; ++k) {
+            const float2 s = ml[k * x.part];
+            const float4 v = *(const float4 *)(rows + (int64_t)k * x.part * D);
+            const float scale = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * a.scale_log2);  // (NaN stays NaN)
+            l += scale * s.y;
+            o.x += scale * v.x;
+            o.y += scale * v.y;
+            o.z += scale * v.z;
+            o.w += scale * v.w;
+        }
+        const int row = x.row0 + r, token = (int)a.by_group.div((uint32_t)row), head = g * a.group + row - token * a.group;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        *(uint2 *)(a.out + (x.first + token) * a.o_s[0] + head * a.o_s[1] + col * 2) =
+            make_uint2(pack16<F16>(o.x * inv, o.y * inv), pack16<F16>(o.z * inv, o.w * inv));
+        if (col == 0) a.lse[(int64_t)(x.first + token) * a.n_q_heads + head] = l == 0.f ? -INFINITY : (top * a.scale_log2 + log2f(l)) * kLn2;
     }
-    const int row = x.row0 + r, token = (int)a.by_group.div((uint32_t)row), head = g * a.group + row - token * a.group;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    *(uint2 *)(a.out + (x.first + token) * a.o_s[0] + head * a.o_s[1] + col * 2) =
-        make_uint2(pack16<F16>(o.x * inv, o.y * inv), pack16<F16>(o.z * inv, o.w * inv));
-    if (col == 0) a.lse[(int64_t)(x.first + token) * a.n_q_heads + head] = l == 0.f ? -INFINITY : (top * a.scale_log2 + log2f(l)) * kLn2;
 }
 
 template <int D, bool F16, bool BLOCKS> hipError_t launch_form(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream)
@@ -1105,10 +1215,8 @@ template <int D, bool F16, bool BLOCKS> hipError_t launch_form(const ChunkArgs &
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(kWaves<D> * 64), kLds<D>, stream, a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || !plan.may_cut) return e;
-    constexpr int RPW = 256 / (D / 4);
-    hipLaunchKernelGGL((chunk_merge_kernel<D, F16>), dim3((unsigned)(plan.slots / 2) * a.n_kv_heads, (plan.part_rows + RPW - 1) / RPW), dim3(256), 0,
-                       stream, a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || plan.slots == 0) return e;
+    hipLaunchKernelGGL((chunk_merge_kernel<D, F16>), dim3(MERGE_GROUPS), dim3(MERGE_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -1118,21 +1226,28 @@ ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units)
 {
     ChunkPlan plan{};
     const int64_t group = d.n_q_heads / d.n_kv_heads, most = d.max_new_len * group;
-    const int ROWS = d.head_dim == 128 ? kRows<128> : kRows<64>;
+    const int64_t per_block = d.head_dim == 128 ? kRows<128> : kRows<64>;
     plan.blocks_possible = most > FEW;
-    plan.part_rows = plan.blocks_possible ? (int)(most < ROWS ? most : ROWS) : (int)most;
-    plan.units = compute_units / d.n_kv_heads;
+    // (at head_dim 64 two workgroups share a compute unit)
+    plan.units = (d.head_dim == 128 ? 1 : 2) * compute_units / d.n_kv_heads;
     if (plan.units < 2) plan.units = 2;
-    plan.slots = plan.units;
     // blocks at most: those of the rows there are, and one more per request with any
     const int64_t rows = (int64_t)d.n_tokens * group, requests = d.batch < d.n_tokens ? d.batch : d.n_tokens;
-    int64_t blocks = (rows + (ROWS - 1) * requests) / ROWS, by_request = requests * ((most + ROWS - 1) / ROWS);
+    int64_t blocks = (rows + (per_block - 1) * requests) / per_block, by_request = requests * ((most + per_block - 1) / per_block);
     if (blocks > by_request) blocks = by_request;
     if (blocks > rows) blocks = rows;
-    plan.may_cut = (d.max_kv_len + TK - 1) / TK + 1 > (plan.blocks_possible ? kMinSplit : kFewWhole);
-    // pieces: one per unit while the blocks are no more than the units, else the blocks and what cutting adds
-    plan.pieces = !plan.may_cut ? blocks : blocks <= plan.units ? plan.units : blocks + plan.slots;
-    plan.listed = d.batch > kWave;
+    // tiles of a block at most: the rows it sees, and a part of one at either end
+    int64_t seen = d.max_kv_len;
+    if (d.window > 0 && seen > d.window + (per_block + group - 1) / group) seen = d.window + (per_block + group - 1) / group;
+    const int64_t tiles = (seen + TK - 1) / TK + 1;
+    const bool may_cut = (float)tiles * (plan.blocks_possible ? 1.f : kFewTile) > kWhole;
+    // room for the pieces that cutting adds, and for partial rows
+    plan.part_rows = (int)(most < per_block ? most : per_block);
+    plan.extra = may_cut ? (plan.blocks_possible ? 2 : 4) * plan.units : 0;
+    plan.slots = plan.extra * plan.part_rows;
+    const bool one_each = !plan.blocks_possible && !may_cut;  // a piece is a request
+    plan.pieces = one_each ? d.batch : blocks + plan.extra;
+    plan.listed = d.batch > kWave && !one_each;
     return plan;
 }
 

@@ -16,6 +16,7 @@ namespace {
 
 constexpr int NT = 256;   // threads per workgroup
 constexpr int BATCH = 4;  // heads whose loads are in flight together
+constexpr int kFewTokens = 1024;
 
 // 16-byte pieces of 8 elements
 template <typename T> constexpr int kPieces = sizeof(T) * 8 / 16;
@@ -72,9 +73,33 @@ rope_kernel(RopeArgs a)
     const int t = blockIdx.x * TOKENS + threadIdx.x / (UNITS * SLOTS);
     if (t >= a.n_tokens) return;
 
-    // this unit's cosines and sines
     const bool rotates = unit * 8 < a.pairs;
-    float cs[8], sn[8];
+    // byte offsets of the unit's two pieces of 8 elements
+    const int at0 = (int)sizeof(T) * (rotates && !INTERLEAVED ? 8 * unit : 16 * unit);
+    const int at1 = (int)sizeof(T) * (rotates && !INTERLEAVED ? 8 * unit + a.pairs : 16 * unit + 8);
+    const int n_k = a.k ? a.n_kv_heads : 0, n_v = a.v ? a.n_kv_heads : 0;
+    const int last_k = a.n_q_heads + n_k, n_heads = last_k + n_v;  // queries, then keys, then values
+
+    uint4 raw[BATCH][2][PIECES];
+    auto load = [&](int h0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int h = h0 + i * SLOTS;
+            if (h >= n_heads) continue;
+            const uint8_t *src = h < a.n_q_heads ? a.q + t * a.q_s[0] + h * a.q_s[1]
+                                 : h < last_k    ? a.k + t * a.k_s[0] + (h - a.n_q_heads) * a.k_s[1]
+                                                 : a.v + t * a.v_s[0] + (h - last_k) * a.v_s[1];
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) {
+                raw[i][0][j] = *(const uint4 *)(src + at0 + 16 * j);
+                raw[i][1][j] = *(const uint4 *)(src + at1 + 16 * j);
+            }
+        }
+    };
+    load(head0);  // on their way while the token's position and its row of the table are read, one after the other
+
+    int32_t slot = a.slots ? a.slots[t] : 0;
+    float cs[8], sn[8];  // this unit's cosines and sines
     if (rotates) {
         const int i0 = unit * 8;
         int axis = 0;
@@ -102,49 +127,21 @@ rope_kernel(RopeArgs a)
             }
         }
     }
-    // byte offsets of the unit's two pieces of 8 elements
-    const int at0 = (int)sizeof(T) * (rotates && !INTERLEAVED ? 8 * unit : 16 * unit);
-    const int at1 = (int)sizeof(T) * (rotates && !INTERLEAVED ? 8 * unit + a.pairs : 16 * unit + 8);
-
-    int32_t slot = a.slots ? a.slots[t] : 0;
     const bool stored = !a.slots || (uint32_t)slot < (uint32_t)a.n_slots;
     const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
     const int64_t k_dst = a.slots ? page * a.ko_s[0] + row * a.ko_s[2] : t * a.ko_s[0];
     const int64_t v_dst = page * a.vo_s[0] + row * a.vo_s[2];
-    const int n_k = a.k ? a.n_kv_heads : 0, n_v = a.v ? a.n_kv_heads : 0;
-    const int last_k = a.n_q_heads + n_k, n_heads = last_k + n_v;  // queries, then keys, then values
 
     for (int h0 = head0; h0 < n_heads; h0 += BATCH * SLOTS) {
-        uint4 raw[BATCH][2][PIECES];
-        uint8_t *dst[BATCH];
-        bool turn[BATCH];
+        if (h0 != head0) load(h0);
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const int h = h0 + i * SLOTS;
-            dst[i] = nullptr;
-            if (h >= n_heads) continue;
-            const uint8_t *src;
-            if (h < a.n_q_heads) {
-                src = a.q + t * a.q_s[0] + h * a.q_s[1];
-                dst[i] = a.q_out + t * a.qo_s[0] + h * a.qo_s[1];
-            } else if (h < last_k) {
-                src = a.k + t * a.k_s[0] + (h - a.n_q_heads) * a.k_s[1];
-                dst[i] = stored ? a.k_out + k_dst + (h - a.n_q_heads) * a.ko_s[1] : nullptr;
-            } else {
-                src = a.v + t * a.v_s[0] + (h - last_k) * a.v_s[1];
-                dst[i] = stored ? a.v_out + v_dst + (h - last_k) * a.vo_s[1] : nullptr;
-            }
-            turn[i] = rotates && h < last_k;
-#pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-                raw[i][0][j] = *(const uint4 *)(src + at0 + 16 * j);
-                raw[i][1][j] = *(const uint4 *)(src + at1 + 16 * j);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            if (!dst[i]) continue;
-            if (turn[i]) {
+            if (h >= n_heads || (h >= a.n_q_heads && !stored)) continue;
+            uint8_t *dst = h < a.n_q_heads ? a.q_out + t * a.qo_s[0] + h * a.qo_s[1]
+                           : h < last_k    ? a.k_out + k_dst + (h - a.n_q_heads) * a.ko_s[1]
+                                           : a.v_out + v_dst + (h - last_k) * a.vo_s[1];
+            if (rotates && h < last_k) {
                 float x[2][8], y[2][8];
                 unpack<T>(raw[i][0], x[0]);
                 unpack<T>(raw[i][1], x[1]);
@@ -161,8 +158,8 @@ rope_kernel(RopeArgs a)
             }
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) {
-                *(uint4 *)(dst[i] + at0 + 16 * j) = raw[i][0][j];
-                *(uint4 *)(dst[i] + at1 + 16 * j) = raw[i][1][j];
+                *(uint4 *)(dst + at0 + 16 * j) = raw[i][0][j];
+                *(uint4 *)(dst + at1 + 16 * j) = raw[i][1][j];
             }
         }
     }
@@ -179,6 +176,8 @@ template <typename T, int D, int SLOTS> hipError_t launch_form(const RopeArgs &a
 
 template <typename T> hipError_t launch_type(const RopeArgs &a, int head_dim, hipStream_t stream)
 {
+    // few tokens: a workgroup each, all heads in one turn
+    if (a.n_tokens <= kFewTokens) return head_dim == 128 ? launch_form<T, 128, 32>(a, stream) : launch_form<T, 64, 64>(a, stream);
     return head_dim == 128 ? launch_form<T, 128, 8>(a, stream) : launch_form<T, 64, 16>(a, stream);
 }
 

@@ -36,7 +36,7 @@ struct ChunkArgs {
     float scale_log2;
     // how the work is cut (ChunkPlan); in the workspace: blocks that are cut and their number, partial rows with their (m, l), and
     // for more than 64 requests the order of the pieces
-    int32_t units, slots, part_rows;
+    int32_t units, extra, slots, part_rows;
     int32_t *n_entries;
     void *entries, *list;
     float2 *part_ml;
@@ -46,12 +46,12 @@ struct ChunkArgs {
 // What the host knows of the pieces of a call, all per KV head.
 struct ChunkPlan {
     int64_t pieces;        // workgroups launched
-    int32_t units;         // compute units
-    int32_t slots;         // partial blocks there is room for
-    int32_t part_rows;     // query rows of a partial block
-    bool may_cut;          // some block may be cut: the merge is launched
+    int32_t units;         // workgroups that run at a time
+    int32_t extra;         // pieces that cutting blocks may add; 0: none is cut, no merge
+    int32_t slots;         // partial rows there is room for
+    int32_t part_rows;     // query rows of a block at most
     bool blocks_possible;  // some request may have more rows than the few that waves share
-    bool listed;           // more requests than a wave has lanes
+    bool listed;           // more requests than a wave has lanes: their pieces are listed first
 };
 ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units);
 size_t chunk_list_bytes(int batch);

@@ -102,10 +102,10 @@ struct ChunkWorkspace {
 ChunkWorkspace layout(const ls_chunk_desc &d, const ChunkPlan &plan)
 {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-    const size_t rows = plan.may_cut ? (size_t)plan.slots * d.n_kv_heads * plan.part_rows : 0;
+    const size_t rows = (size_t)plan.slots * d.n_kv_heads;
     ChunkWorkspace w;
     w.entries = 256;  // after the number of blocks that are cut
-    w.list = up(w.entries + (size_t)(plan.slots / 2) * d.n_kv_heads * chunk_entry_bytes());
+    w.list = up(w.entries + (size_t)plan.extra * d.n_kv_heads * chunk_entry_bytes());
     w.part_ml = up(w.list + (plan.listed ? chunk_list_bytes(d.batch) : 0));
     w.parts = up(w.part_ml + rows * sizeof(float2));
     w.total = up(w.parts + rows * d.head_dim * sizeof(float));
@@ -228,7 +228,7 @@ int ls_chunk_attn_paged(const ls_chunk_desc *desc, const void *q, const void *k_
     a.by_group = FastDiv::of(a.group), a.by_kv_heads = FastDiv::of(a.n_kv_heads);
     const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / std::sqrt((float)desc->head_dim);
     a.scale_log2 = scale * kLog2e;
-    a.units = plan.units, a.slots = plan.may_cut ? plan.slots : 0, a.part_rows = plan.part_rows;
+    a.units = plan.units, a.extra = plan.extra, a.slots = plan.slots, a.part_rows = plan.part_rows;
     char *base = (char *)workspace;
     a.n_entries = (int32_t *)base;
     a.entries = base + w.entries;
