@@ -102,26 +102,34 @@ rope_kernel(RopeArgs a)
     float cs[8], sn[8];  // this unit's cosines and sines
     if (rotates) {
         const int i0 = unit * 8;
-        int axis = 0;
-        while (axis + 1 < a.n_axes && i0 >= a.axis_end[axis]) ++axis;
-        auto row_of = [&](int x) {
-            int p = a.positions[x * a.positions_stride + t];
-            p = p < 0 ? 0 : (p < a.n_positions ? p : a.n_positions - 1);
-            return a.cos_sin + (int64_t)p * (2 * a.pairs);
+        int32_t place[LS_MAX_AXES];
+#pragma unroll
+        for (int x = 0; x < LS_MAX_AXES; ++x) {
+            const int p = x < a.n_axes ? a.positions[x * a.positions_stride + t] : 0;
+            place[x] = p < 0 ? 0 : (p < a.n_positions ? p : a.n_positions - 1);
+        }
+        // the position by which pair i goes
+        auto place_of = [&](int i) __attribute__((always_inline)) {
+            int p = place[0];
+#pragma unroll
+            for (int x = 1; x < LS_MAX_AXES; ++x) p = x < a.n_axes && i >= a.axis_end[x - 1] ? place[x] : p;
+            return p;
         };
-        if (i0 + 8 <= a.axis_end[axis]) {
-            const float *row = row_of(axis) + i0;
+        bool whole = true;  // no axis ends inside the unit
+#pragma unroll
+        for (int x = 0; x + 1 < LS_MAX_AXES; ++x) whole &= x + 1 >= a.n_axes || a.axis_end[x] <= i0 || a.axis_end[x] >= i0 + 8;
+        if (whole) {
+            const float *row = a.cos_sin + (int64_t)place_of(i0) * (2 * a.pairs) + i0;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float4 c = *(const float4 *)(row + 4 * i), s = *(const float4 *)(row + a.pairs + 4 * i);
                 cs[4 * i] = c.x, cs[4 * i + 1] = c.y, cs[4 * i + 2] = c.z, cs[4 * i + 3] = c.w;
                 sn[4 * i] = s.x, sn[4 * i + 1] = s.y, sn[4 * i + 2] = s.z, sn[4 * i + 3] = s.w;
             }
-        } else {  // an axis ends inside the unit
+        } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                while (axis + 1 < a.n_axes && i0 + i >= a.axis_end[axis]) ++axis;
-                const float *row = row_of(axis) + i0 + i;
+                const float *row = a.cos_sin + (int64_t)place_of(i0 + i) * (2 * a.pairs) + i0 + i;
                 cs[i] = row[0];
                 sn[i] = row[a.pairs];
             }

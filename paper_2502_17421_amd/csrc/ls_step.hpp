@@ -1,6 +1,8 @@
 // What the host side and the kernels of a serving step share (page plan, rotary positions, attention of new tokens).
 #pragma once
 
+#include <type_traits>
+
 #include "ls_internal.hpp"
 
 namespace ls {
@@ -57,6 +59,26 @@ ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units);
 size_t chunk_list_bytes(int batch);
 size_t chunk_entry_bytes();
 
+// Inclusive sums over the lanes of a wave.
+template <typename T> __device__ __forceinline__ T scan_lanes(T x)
+{
+    auto add = [&](auto ctrl, auto row_mask) __attribute__((always_inline)) {
+        const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(row_mask)::value, 0xf, false);
+        x += __builtin_bit_cast(T, y);
+    };
+    using all = std::integral_constant<int, 0xf>;
+    add(std::integral_constant<int, 0x111>{}, all{});  // from 1, 2, 4 and 8 lanes below in the row of 16
+    add(std::integral_constant<int, 0x112>{}, all{});
+    add(std::integral_constant<int, 0x114>{}, all{});
+    add(std::integral_constant<int, 0x118>{}, all{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // the last lane of the row before, to rows 1 and 3
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // lane 31, to rows 2 and 3
+    return x;
+}
+template <typename T> __device__ __forceinline__ T last_lane(T x)
+{
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
 hipError_t launch_page_plan(const PagePlanArgs &a, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_chunk_attn(const ChunkArgs &a, const ChunkPlan &plan, int dtype, int head_dim, hipStream_t stream);
