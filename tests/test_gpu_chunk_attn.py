@@ -258,3 +258,32 @@ def test_pool_beyond_4_gb():
     want = chunk_attention(st.q.double(), [st.k_rows[0].double()], [st.v_rows[0].double()], [n], [kv], 0, d ** -0.5, "bf16")
     compare(out.cpu().double(), want[0], want[2], "out")
     compare(lse.cpu().double(), want[1], want[3], "lse")
+
+
+LISTED = [  # more requests than a workgroup's lanes: ended ones among them, blocks cut, single tokens
+    ([1, 0, 3, 1] * 30, [(97 * i) % 700 + 3 for i in range(120)], 0),
+    ([2] * 64 + [0] * 7 + [150, 1, 400], [5 + 11 * i for i in range(64)] + [9] * 7 + [3000, 2500, 400], 0),
+    ([70] * 66, [70 + 5 * i for i in range(66)], 100),
+    ([0] * 90 + [1, 33], [40] * 90 + [6000, 2000], 0),
+]
+
+
+@pytest.mark.parametrize("news,lens,window", LISTED)
+@pytest.mark.parametrize("heads,dtype", [("gqa", "bf16"), ("small", "f16")])
+def test_more_requests_than_lanes(heads, dtype, news, lens, window):
+    Step(dtype, HEADS[heads], news, lens, seed=18).check(window=window, times=2)
+
+
+@pytest.mark.parametrize("batch", [65, 300])
+def test_more_requests_than_tokens(batch):
+    """Most requests of a table idle: a request is a piece whether it has tokens or not."""
+    news, lens = [0] * batch, [3 * i % 90 for i in range(batch)]
+    news[7], news[batch - 1], lens[7], lens[batch - 1] = 1, 2, 40, 77
+    Step("bf16", HEADS["gqa"], news, lens, seed=19).check()
+
+
+def test_the_largest_batch():
+    news = [1 if i % 3 else 0 for i in range(ls.LS_MAX_STEP_BATCH)]
+    Step("f16", (2, 1, 64), news, [1 + i % 37 for i in range(len(news))], seed=20).check()
+    news[5] = 90
+    Step("f16", (2, 1, 64), news, [90 + i % 37 for i in range(len(news))], seed=21).check()

@@ -122,3 +122,40 @@ def test_sizes_and_alignment():
         ls.ls_page_plan(ls.make_page_desc(table, n_tokens, 16, st.n_pages), kv, new, held, table, free, dev([st.n_free]), *small, slots, positions)
         assert slots.cpu().tolist() == want["slots"].tolist() and positions.cpu().tolist() == want["positions"].tolist()
         assert buf[:, 0].tolist() == [-99, -99] and (buf[:, 1 + n_tokens:] == -99).all()
+
+
+@pytest.mark.parametrize("n_tokens", [65535, 65536, 65537, 200003])
+def test_many_tokens(n_tokens):
+    """Around the number of tokens from which a thread takes four."""
+    rng = np.random.default_rng(5)
+    kv = rng.integers(0, 900, 90)
+    new = rng.integers(0, 1500, 90)
+    new[[3, 40]] = 0
+    kv[3] = 0
+    held = -(-kv // 16) + rng.integers(0, 3, 90)
+    check(State(rng, held, 400, 9000, 16), kv, new, held, n_tokens)
+
+
+def test_on_another_stream():
+    """The stream given, and torch's current one: the call waits for what that stream holds and for nothing else."""
+    rng = np.random.default_rng(6)
+    kv, new, held = np.array([20, 0, 7], np.int32), np.array([30, 5, 0], np.int32), np.array([3, 0, 2], np.int32)
+    st = State(rng, held, 8, 20, 16)
+    want = page_plan(kv, new, held, st.table, st.free, st.n_free, 16, 40)
+    for explicit in (False, True):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            late = torch.zeros(3, dtype=torch.int32, device="cuda")
+            torch.cuda._sleep(2000000)
+            late.copy_(dev(new))  # the lengths arrive on the side stream
+            table, free, out = dev(st.table), dev(st.free), [torch.empty(n, dtype=torch.int32, device="cuda") for n in (3, 1, 4, 3, 40, 40, 3)]
+            args = (dev(kv), late, dev(held), table, free, dev([st.n_free]), *out)
+            desc = ls.make_page_desc(table, 40, 16, st.n_pages)
+            if not explicit:
+                ls.ls_page_plan(desc, *args)
+        if explicit:
+            ls.ls_page_plan(desc, *args, stream=side)
+        side.synchronize()
+        np.testing.assert_array_equal(out[4].cpu().numpy(), want["slots"])
+        np.testing.assert_array_equal(table.cpu().numpy(), want["table"])

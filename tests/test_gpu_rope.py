@@ -147,3 +147,57 @@ def test_pool_beyond_4_gb():
     rows = torch.cat([pages[0][-2], pages[0][-1]], dim=1)[:, -20:].transpose(0, 1)
     close(rows, *expected(k, pos.cpu().numpy(), table(50, 64), [64], False, "bf16"), "k")
     assert torch.equal(torch.cat([pages[1][-2], pages[1][-1]], dim=1)[:, -20:].transpose(0, 1), v)
+
+
+@pytest.mark.parametrize("t", [1024, 1025, 1331])
+@pytest.mark.parametrize("dtype,heads,d,rotary,sections,interleaved", [
+    ("bf16", (32, 8), 128, 128, [64], False), ("f32", (3, 1), 128, 64, [9, 23], True), ("f16", (16, 4), 64, 64, [32], False),
+    ("bf16", (5, 5), 64, 48, [8, 8, 8], True)])
+def test_many_tokens(t, dtype, heads, d, rotary, sections, interleaved):
+    """Around the number of tokens from which few threads share a token."""
+    rng = np.random.default_rng(t)
+    cos_sin = table(2000, rotary // 2)
+    positions = rng.integers(0, 2000, (len(sections), t)).astype(np.int32)
+    q, k, v = inputs(rng, t, heads, d, dtype)
+    n_pages, page_size = t // 16 + 3, 16
+    k_pages = torch.full((n_pages, heads[1], page_size, d), 7.0, dtype=q.dtype, device="cuda")
+    v_pages, q_out = k_pages.clone(), torch.empty_like(q)
+    slots = rng.permutation(n_pages * page_size)[:t].astype(np.int32)
+    slots[t // 2] = -1
+    pos, cs, sl = torch.from_numpy(positions).cuda(), torch.from_numpy(cos_sin).cuda(), torch.from_numpy(slots).cuda()
+    desc = ls.make_rope_desc(q, k, v, q_out, None, k_pages, v_pages, pos, cs, sections, interleaved)
+    ls.ls_rope_store_paged(desc, q, k, v, pos, cs, sl, q_out, k_pages, v_pages)
+    want, bound = expected(q, positions, cos_sin, sections, interleaved, dtype)
+    close(q_out, want, bound, "q")
+    rows = lambda x: x.transpose(1, 2).reshape(n_pages * page_size, heads[1], d)  # noqa: E731
+    real = slots >= 0
+    want, bound = expected(k, positions, cos_sin, sections, interleaved, dtype)
+    close(rows(k_pages)[slots[real]], want[real], bound[real], "k")
+    at = torch.from_numpy(slots[real].astype(np.int64)).cuda()
+    assert torch.equal(rows(v_pages)[at], v[torch.from_numpy(real).cuda()])
+    other = torch.ones(n_pages * page_size, dtype=torch.bool, device="cuda")
+    other[at] = False
+    assert (rows(k_pages)[other] == 7).all() and (rows(v_pages)[other] == 7).all()
+
+
+def test_on_another_stream():
+    rng = np.random.default_rng(8)
+    positions, cos_sin = rng.integers(0, 50, (1, 9)).astype(np.int32), table(50, 64)
+    q, k, _ = inputs(rng, 9, (4, 2), 128, "bf16")
+    pos, cs = torch.from_numpy(positions).cuda(), torch.from_numpy(cos_sin).cuda()
+    want, bound = expected(q, positions, cos_sin, [64], False, "bf16")
+    for explicit in (False, True):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            late = torch.zeros_like(q)
+            torch.cuda._sleep(2000000)
+            late.copy_(q)  # the queries arrive on the side stream
+            k_out, desc = torch.empty_like(k), None
+            desc = ls.make_rope_desc(late, k, None, late, k_out, None, None, pos, cs)
+            if not explicit:
+                ls.ls_rope(desc, late, k, pos, cs, late, k_out)
+        if explicit:
+            ls.ls_rope(desc, late, k, pos, cs, late, k_out, stream=side)
+        side.synchronize()
+        close(late, want, bound, "q")
