@@ -649,11 +649,21 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
             const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
             const uint32_t v_off0 = base + RING + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
-            auto read_k = [&](uint32_t k_base, int f) __attribute__((always_inline)) {
-                return __builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)(k_base ^ (uint32_t)(f << 5)));
+            // A fragment's place in stage 0, kept: the stages of the main loop are constants and go into the instructions' offsets.
+            uint32_t k_at[KSTEPS], v_at[MT];
+#pragma unroll
+            for (int f = 0; f < KSTEPS; ++f) k_at[f] = k_off0 ^ (uint32_t)(f << 5);
+#pragma unroll
+            for (int f = 0; f < MT; ++f) v_at[f] = v_off0 ^ (uint32_t)(f << 6);
+#pragma unroll
+            for (int f = 0; f < KSTEPS; ++f) asm volatile("" : "+v"(k_at[f]));  // (they would be worked out again in the loop)
+#pragma unroll
+            for (int f = 0; f < MT; ++f) asm volatile("" : "+v"(v_at[f]));
+            auto read_k = [&](uint32_t stage, int f) __attribute__((always_inline)) {
+                return __builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)(k_at[f] + stage));
             };
-            auto read_v = [&](uint32_t v_base, int f) __attribute__((always_inline)) {  // f = 16-key half * MT + d tile
-                const uint32_t at = (v_base ^ (uint32_t)((f % MT) << 6)) + ((f / MT) * 16) * ROWB;
+            auto read_v = [&](uint32_t stage, int f) __attribute__((always_inline)) {  // f = 16-key half * MT + d tile
+                const uint32_t at = v_at[f % MT] + (stage + (f / MT) * 16 * ROWB);
                 const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)at));
                 const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB)));
                 return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
@@ -697,7 +707,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
 
             bf16x8 q_reg[KSTEPS];
 #pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) q_reg[kk] = read_k(k_off0 + q_at, kk);
+            for (int kk = 0; kk < KSTEPS; ++kk) q_reg[kk] = read_k(q_at, kk);
 
             // ---- pipeline -----------------------------------------------------------------------
             // A step is one tile: KSTEPS matrix instructions for the scores, the softmax arithmetic of 16 scores a lane, and KSTEPS for
@@ -712,8 +722,8 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             float neg_mc = 0.f;
             using yes = std::true_type;
             using no = std::false_type;
-            auto half_step = [&](auto x_tag, auto qk_tag, auto sm_tag, auto kn_tag, auto vn_tag, auto rq_tag, uint32_t k_cur, uint32_t k_next,
-                                 uint32_t v_cur, uint32_t v_next) __attribute__((always_inline)) {
+            auto half_step = [&](auto x_tag, auto qk_tag, auto sm_tag, auto kn_tag, auto vn_tag, auto rq_tag, auto k_cur, auto k_next, auto v_cur,
+                                 auto v_next) __attribute__((always_inline)) {
                 constexpr int X = decltype(x_tag)::value, Y = 1 - X;
                 constexpr bool QK = decltype(qk_tag)::value, SM = decltype(sm_tag)::value;
                 constexpr bool KN = decltype(kn_tag)::value, VN = decltype(vn_tag)::value, RQ = decltype(rq_tag)::value;
@@ -721,7 +731,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     pb[i] = __builtin_bit_cast(bf16x8, make_uint4(p_sl[X][4 * i], p_sl[X][4 * i + 1], p_sl[X][4 * i + 2], p_sl[X][4 * i + 3]));
-                const uint32_t kc = k_cur + k_off0, kn = k_next + k_off0, vc = v_cur + v_off0, vn = v_next + v_off0;
+                const uint32_t kc = k_cur, kn = k_next, vc = v_cur, vn = v_next;
                 float sum = 0.f;
                 floatx16 s_new;
 #pragma unroll
@@ -784,7 +794,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
 #pragma unroll
             for (int e = 0; e < 16; ++e) s_sl[0][e] = 0.f;
 #pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) s_sl[0] = mfma32<F16>(read_k(k_off0, kk), q_reg[kk], s_sl[0]);
+            for (int kk = 0; kk < KSTEPS; ++kk) s_sl[0] = mfma32<F16>(read_k(0, kk), q_reg[kk], s_sl[0]);
             mask(s_sl[0], 0);
             {
                 float mx = s_sl[0][0];
@@ -795,12 +805,10 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             }
             advance0();
 #pragma unroll
-            for (int f = 0; f < FS; ++f) k_frag[f] = read_k(TILEB + k_off0, f);
+            for (int f = 0; f < FS; ++f) k_frag[f] = read_k(TILEB, f);
             // Step -1 does not exist: its numerators are zeros, the V stage they are multiplied with is any, and what comes of it is
             // thrown away.
-            uint32_t k_cur = TILEB, v_cur = 0;  // K tile h, V tile h - 2
             int h = 1;
-            auto next = [&](uint32_t off) __attribute__((always_inline)) { return (off + TILEB) & (RING - 1); };
             auto first_output = [&]() __attribute__((always_inline)) {
                 if (h != 1) return;
 #pragma unroll
@@ -808,23 +816,35 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
 #pragma unroll
                     for (int e = 0; e < 16; ++e) st.o[mt][e] = 0.f;
             };
-            v_cur = RING - TILEB;
-            for (; h + 1 < n_tiles; h += 2) {
+            auto stage = [&](int tile) __attribute__((always_inline)) { return (uint32_t)(tile * TILEB) & (RING - 1); };
+            // Half-steps h and h + 1: K tiles h to h + 2, V tiles h - 2 to h.
+            auto pair = [&](auto k0, auto k1, auto k2, auto v0, auto v1) __attribute__((always_inline)) {
                 advance_pair(h);
-                const uint32_t k1 = next(k_cur), k2 = next(k1), v1 = next(v_cur), v2 = next(v1);
-                half_step(X1{}, yes{}, yes{}, yes{}, yes{}, yes{}, k_cur, k1, v_cur, v1);
+                half_step(X1{}, yes{}, yes{}, yes{}, yes{}, yes{}, k0, k1, v0, v1);
                 first_output();
                 mask(s_sl[1], h);
-                half_step(X0{}, yes{}, yes{}, yes{}, yes{}, yes{}, k1, k2, v1, v2);
+                half_step(X0{}, yes{}, yes{}, yes{}, yes{}, yes{}, k1, k2, v1, k0);
                 mask(s_sl[0], h + 1);
-                k_cur = k2;
-                v_cur = v2;
+                h += 2;
+            };
+            auto pair_at = [&](auto first) __attribute__((always_inline)) {  // h = first + a multiple of RS
+                constexpr uint32_t T = decltype(first)::value;
+                pair(std::integral_constant<uint32_t, T % RS * TILEB>{}, std::integral_constant<uint32_t, (T + 1) % RS * TILEB>{},
+                     std::integral_constant<uint32_t, (T + 2) % RS * TILEB>{}, std::integral_constant<uint32_t, (T + RS - 2) % RS * TILEB>{},
+                     std::integral_constant<uint32_t, (T + RS - 1) % RS * TILEB>{});
+            };
+            while (h + RS - 1 < n_tiles) {
+                pair_at(std::integral_constant<uint32_t, 1>{});
+                pair_at(std::integral_constant<uint32_t, 3>{});
+                pair_at(std::integral_constant<uint32_t, 5>{});
+                pair_at(std::integral_constant<uint32_t, 7>{});
             }
+            while (h + 1 < n_tiles) pair(stage(h), stage(h + 1), stage(h + 2), stage(h - 2), stage(h - 1));
             advance_last(h);
             // h = n_tiles - 1 (one step left to score) or h = n_tiles (none: the step scored here is void)
             const bool is_void = h >= n_tiles;
-            const uint32_t v1 = next(v_cur), v2 = next(v1);
-            half_step(X1{}, yes{}, yes{}, no{}, yes{}, no{}, k_cur, 0, v_cur, v1);
+            const uint32_t v1 = stage(h - 1), v2 = stage(h);
+            half_step(X1{}, yes{}, yes{}, no{}, yes{}, no{}, stage(h), 0u, stage(h - 2), v1);
             first_output();
             if (is_void) {
 #pragma unroll
@@ -832,8 +852,8 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             } else {
                 mask(s_sl[1], h);
             }
-            half_step(X0{}, no{}, yes{}, no{}, yes{}, no{}, 0, 0, v1, v2);  // output h - 1, softmax h
-            if (!is_void) half_step(X1{}, no{}, no{}, no{}, no{}, no{}, 0, 0, v2, 0);  // output h
+            half_step(X0{}, no{}, yes{}, no{}, yes{}, no{}, 0u, 0u, v1, v2);  // output h - 1, softmax h
+            if (!is_void) half_step(X1{}, no{}, no{}, no{}, no{}, no{}, 0u, 0u, v2, 0u);  // output h
         }
         wait_vmem<0>();   // requests past the last tile
         __syncthreads();  // every wave is done reading tiles: the rings are free
