@@ -103,11 +103,15 @@ template <int ROWS> __device__ __forceinline__ Request load_request(const ChunkA
     return q;
 }
 
-// Pieces per block for a share of the work.
-__device__ __forceinline__ int cut_of(const Request &q, float share)
+// Above which cost a block is cut.
+struct Shares {
+    float rows, few;
+};
+// Pieces per block.
+__device__ __forceinline__ int cut_of(const Request &q, const Shares &share)
 {
     if (q.cost <= kWhole) return 1;
-    return (int)ceilf(q.cost * __builtin_amdgcn_rcpf(fmaxf(share, q.rows <= FEW ? kFewSplit : kWhole)));
+    return (int)ceilf(q.cost * __builtin_amdgcn_rcpf(q.rows <= FEW ? fmaxf(share.few, kFewSplit) : fmaxf(share.rows, kWhole)));
 }
 // Query rows of a block's partial results, if it is cut.
 template <int ROWS> __device__ __forceinline__ int block_rows(const Request &q) { return q.rows < ROWS ? q.rows : ROWS; }
@@ -146,44 +150,58 @@ struct Piece {
     bool valid;
 };
 
-// The share of the work above which a block is cut.  sum(f), most(f): over all requests; least(time): the candidate with the least time.
+// The shares of the work above which blocks are cut.  sum(f), most(f): over all requests; least(time): the candidate with the least time.
 // Three blocks for each compute unit and more even out by themselves; only a block beyond a unit's share is cut.  With fewer blocks
-// the least of some shares' expected times is taken, in tiles: one round of pieces lasts as long as the longest; in several
-// the units end apart by some part of it.  (Against the best of the candidates in a simulation of 160 steps of the ranges that the
-// performance cases draw from: 0.7 % longer, worst 20 %.)
+// the least of some candidates' expected times is taken, in tiles: one round of pieces lasts as long as the longest; in several
+// the units end apart by some part of it, which the few rows' pieces, dealt last and cut small, fill up.  (Against the best of 90
+// pairs of shares in a simulation of 300 steps of the ranges that the performance cases draw from: 0.1 % longer, worst 23 %.
+// Without the pairs that cut the few rows alone a step of two pieces of prompts and 18 single tokens took 15 % longer there.)
 constexpr float kPieceCost = 8.f;  // what a piece costs besides its tiles: its place, the first loads, the rows out
 constexpr float kMergeCost = 5.f, kMergeBlock = 18.f;  // the merge: its launch, and a partial block's way to memory and back
+constexpr float kUneven = 0.3f;
 constexpr int kShares = 8;
 constexpr float kNever = 1e9f;
-__device__ __forceinline__ float share_of(int candidate, float mean)
+__device__ __forceinline__ Shares shares_of(int candidate, float mean)
 {
-    constexpr float kOfMean[kShares] = {0.f, 3.f, 2.f, 1.4f, 1.1f, 0.8f, 0.6f, 0.4f};
-    float f = kOfMean[1];
+    constexpr float kRows[kShares] = {kNever, 2.f, 1.4f, 1.1f, 0.7f, 0.4f, kNever, 1.2f};
+    constexpr float kFew[kShares] = {kNever, 2.f, 1.4f, 1.1f, 0.7f, 0.4f, 0.2f, 0.2f};
+    float rows = kRows[0], few = kFew[0];
 #pragma unroll
-    for (int k = 2; k < kShares; ++k) f = candidate == k ? kOfMean[k] : f;
-    return candidate == 0 ? kNever : f * mean;
+    for (int k = 1; k < kShares; ++k) {
+        rows = candidate == k ? kRows[k] : rows;
+        few = candidate == k ? kFew[k] : few;
+    }
+    return {rows == kNever ? rows : rows * mean, few == kNever ? few : few * mean};
 }
 template <int ROWS, typename Sum, typename Most, typename Least>
-__device__ __forceinline__ float choose_share(const ChunkArgs &a, Sum sum, Most most, Least least)
+__device__ __forceinline__ Shares choose_shares(const ChunkArgs &a, Sum sum, Most most, Least least)
 {
-    if (a.slots == 0) return kNever;
+    if (a.slots == 0) return {kNever, kNever};
     const float blocks = sum([](const Request &q) { return (float)q.blocks; });
     const float work = sum([](const Request &q) { return q.work; });
+    const float few_work = sum([](const Request &q) { return q.rows <= FEW ? q.work : 0.f; });
     const float units = (float)a.units, by_units = __builtin_amdgcn_rcpf(units), mean = work * by_units;
-    auto time_of = [&](float share) __attribute__((always_inline)) {
+    auto time_of = [&](const Shares &share) __attribute__((always_inline)) {
         const float pieces = sum([&](const Request &q) { return (float)q.blocks * (float)cut_of(q, share); });
         const float slots = sum([&](const Request &q) {
             const float c = (float)cut_of(q, share);
             return c > 1.f ? (float)q.blocks * c * (float)block_rows<ROWS>(q) : 0.f;
         });
-        const float longest = most([&](const Request &q) { return q.cost * __builtin_amdgcn_rcpf((float)cut_of(q, share)); });
+        auto longest = [&](bool few) __attribute__((always_inline)) {
+            return most([&](const Request &q) { return (q.rows <= FEW) == few ? q.cost * __builtin_amdgcn_rcpf((float)cut_of(q, share)) : 0.f; });
+        };
+        const float rows = longest(false), few = longest(true), longer = fmaxf(rows, few) + kPieceCost;
         // (room for the partial rows, and for the pieces that cutting adds)
         if (slots > (float)a.slots || pieces - blocks > (float)a.extra) return 2.f * kNever;
         const float merge = slots > 0.f ? kMergeCost + kMergeBlock * slots * (1.f / ROWS) * by_units : 0.f;
-        return merge + (pieces <= units ? longest + kPieceCost : mean + kPieceCost * pieces * by_units + 0.4f * longest);
+        if (pieces <= units) return merge + longer;
+        return merge + fmaxf(longer, mean + kPieceCost * pieces * by_units + fmaxf(kUneven * rows - few_work * by_units, kUneven * few));
     };
-    if (blocks >= 3.f * units) return time_of(1.25f * mean) < kNever ? 1.25f * mean : kNever;
-    return share_of(least([&](int candidate) { return time_of(share_of(candidate, mean)); }), mean);
+    if (blocks >= 3.f * units) {
+        const Shares share{1.25f * mean, 1.25f * mean};
+        return time_of(share) < kNever ? share : Shares{kNever, kNever};
+    }
+    return shares_of(least([&](int candidate) { return time_of(shares_of(candidate, mean)); }), mean);
 }
 
 // Piece i of those of a KV head, up to 64 requests, a lane each (every wave for itself).
@@ -199,7 +217,7 @@ template <int ROWS, int NW, bool BLOCKS> __device__ __forceinline__ Piece find_p
         return p;
     }
     const Request q = load_request<ROWS>(a, lane);
-    const float share = choose_share<ROWS>(
+    const Shares share = choose_shares<ROWS>(
         a, [&](auto f) { return last_lane(scan_lanes(f(q))); }, [&](auto f) { return most_of_lanes(f(q)); },
         [&](auto time) {  // the waves share the candidates
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -300,7 +318,7 @@ chunk_list_kernel(ChunkArgs a)
         __syncthreads();
         return x;
     };
-    const float share = choose_share<ROWS>(
+    const Shares share = choose_shares<ROWS>(
         a,
         [&](auto f) {
             auto x = f(q[0]);
@@ -473,10 +491,10 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
     constexpr int KSTEPS = D / 16, MT = D / 32, CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
     constexpr int RPL = 64 / CH;          // rows one copy of 64 lanes covers
     constexpr int TPT = TK / RPL;         // copies per tile and tensor
-    constexpr int LOADS = TPT / (NW / 2); // of which a wave does so many: 8 or 16 rows in a row, which share a page
-    constexpr int MINE = LOADS * RPL;     // these rows
+    // A wave copies 16 rows in a row of a tile, which share a page: of every tile (head_dim 64), or of every other one.
+    constexpr int MINE = 16, LOADS = MINE / RPL, STEP = NW / 2 * MINE / TK;
     constexpr uint32_t RING = RS * TILEB; // bytes of a ring: K, then V
-    static_assert(LOADS == 2 && MINE <= 16 && (PD + 1) * LOADS + TPT + 1 <= 63, "copies of a wave");
+    static_assert(STEP <= 2 && PD == 4 && (PD + 1) * LOADS + TPT + 1 <= 63, "copies of a wave");
     const Request &q = piece.q;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int row0 = piece.block * ROWS, wave_row0 = row0 + wave * 32;
@@ -502,7 +520,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
 
     if (n_tiles > 0) {
         // ---- copies -----------------------------------------------------------------------------
-        // The first half of the waves copies K rows, the other half V rows: MINE rows of each tile.
+        // The first half of the waves copies K rows, the other half V rows.
         const uint32_t base = lds_offset(smem);
         const bool is_v = wave >= NW / 2;
         const int64_t *stride = is_v ? a.vc_s : a.kc_s;
@@ -510,7 +528,9 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
         const int32_t rb = (int32_t)stride[2];
         const int page_mask = (1 << a.page_shift) - 1;
         const int ld_row = lane / CH, ld_pos = lane % CH;
-        const int my_row = wave % (NW / 2) * MINE;
+        const int my_row = wave % (TK / MINE) * MINE;
+        // Every other one: of K waves 0 and 1 tiles 0, 2, 4 ..., of V waves 4 and 5 tiles 1, 3, 5 ...
+        const int first_tile = STEP == 1 ? 0 : (wave / (TK / MINE) & 1) ^ (int)is_v;
         auto chunk_at = [&](int row) __attribute__((always_inline)) { return (uint32_t)(ld_pos ^ ((is_v ? vswz(row) : row) & (CH - 1))) * 16; };
         // Lane's offset for copy j from the first of those rows, less what the instruction adds (rows are at least ROWB apart).
         uint32_t voff[LOADS];
@@ -538,16 +558,17 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
         if (tid == 0) *found = 0;
         if (n_tiles + PD + 2 > 64) fetch_ids(64);
 
-        // Request r (r >= -(PD + 1)) is the K rows of tile r + PD + 1 and the V rows of tile r + PD.
-        int rq = 0;  // tile of this wave's next request
-        uint32_t rq_off = 0;  // its place in the ring
+        // One tile after the other: request r (r >= -(PD + 1)) is the K rows of tile r + PD + 1 and the V rows of tile r + PD; every
+        // other one: request r (r >= -3) is those of K tiles 2 r + 6 and 2 r + 7, of V tiles 2 r + 5 and 2 r + 6.
+        int rq = first_tile;  // tile of this wave's next request
+        uint32_t rq_off = (uint32_t)first_tile * TILEB;  // its place in the ring
         const uint32_t rq_base = base + (is_v ? RING : 0) + my_row * ROWB;
         const int tail = kv < t_hi * TK ? n_tiles - 1 : 1 << 30;  // first tile that is not whole
         auto request = [&]() __attribute__((always_inline)) {
             const int i = rq & 63;
-            if (i == 0 && rq > 0) {
-                place(rq, ids[(rq & 64) + lane]);
-                fetch_ids(rq + 64);
+            if (i < STEP && rq >= 64) {
+                place(rq - i, ids[(rq & 64) + lane]);
+                fetch_ids(rq - i + 64);
             }
             const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)offs, i) |
                                  (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(offs >> 32), i) << 32;
@@ -556,6 +577,10 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             if (rq < tail) {
                 copy_tile_rows<0>(src, voff[0], to);
                 copy_tile_rows<RPL * ROWB>(src, voff[1], to);
+                if constexpr (LOADS == 4) {
+                    copy_tile_rows<2 * RPL * ROWB>(src, voff[2], to);
+                    copy_tile_rows<3 * RPL * ROWB>(src, voff[3], to);
+                }
             } else {
                 const int last = kv - 1 - (t_hi - 1) * TK, first = my_row < last ? my_row : last;  // src is that row
 #pragma unroll
@@ -564,8 +589,8 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
                     copy_to_lds(src, (uint32_t)(((r < last ? r : last) - first) * rb) + chunk_at(r), to + j * RPL * ROWB);
                 }
             }
-            ++rq;
-            rq_off = (rq_off + TILEB) & (RING - 1);
+            rq += STEP;
+            rq_off = (rq_off + STEP * TILEB) & (RING - 1);
         };
         if (!is_v) request();
         // Query rows: through LDS, in stages that the first requests leave free, in the layout of a K tile.
@@ -578,10 +603,16 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
                 copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ (r & (CH - 1))) * 16,
                                 __builtin_amdgcn_readfirstlane(base + q_at + j * RPL * ROWB));
             }
+        if constexpr (STEP == 1) {
 #pragma unroll
-        for (int r = 0; r < PD; ++r) request();
-        wait_vmem<PD * LOADS>();
-        __syncthreads();  // tile 0 and the query rows are in LDS
+            for (int r = 0; r < PD; ++r) request();
+            wait_vmem<PD * LOADS>();
+        } else {
+            if (is_v && first_tile == 0) request();
+            request();
+            wait_vmem<LOADS>();  // also K tile 1 and V tile 0
+        }
+        __syncthreads();  // K tile 0 and the query rows are in LDS
 
         auto ring_barrier = [&]() __attribute__((always_inline)) { asm volatile("s_barrier" ::: "memory"); };
         // Tiles (of this piece) that all rows between two see whole: the first of them, and how many.
@@ -610,23 +641,25 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         };
-        // Before half-step 1, which reads K rows of tile 1: request -PD has landed; request 0 follows.
+        // Before half-step 1, which reads K rows of tile 1: request -PD has landed; request 0 (-1) follows, over query rows.
         auto advance0 = [&]() __attribute__((always_inline)) {
-            wait_vmem<(PD - 1) * LOADS>();
+            if constexpr (STEP == 1) wait_vmem<(PD - 1) * LOADS>();
             ring_barrier();
             request();
             clean(0, 1);
         };
-        // Before half-steps h and h + 1 (h odd), which read K rows up to tile h + 2: requests up to h + 1 - PD have landed.  Requests
-        // h and h + 1 follow in these half-steps, into stages last read in half-step h - 1 or earlier.
+        // Before half-steps h and h + 1 (h odd), which read K rows up to tile h + 2, V rows up to tile h: requests up to h + 1 - PD
+        // ((h - 5) / 2) have landed.  Requests h and h + 1 ((h - 1) / 2) follow in these half-steps, into stages last read in
+        // half-step h - 1 or earlier: K tiles up to h + 6, V tiles up to h + 5.
         auto advance_pair = [&](int h) __attribute__((always_inline)) {
-            wait_vmem<(PD - 2) * LOADS>();
+            wait_vmem<(STEP == 1 ? PD - 2 : 1) * LOADS>();
             ring_barrier();
             if (!(inside(h, block_whole) && inside(h + 1, block_whole))) clean(h, h + 2);
         };
-        // After the pairs: the V rows of the last tile have landed, request n_tiles - 1 - PD of n_tiles - 2 at least.
+        // After the pairs: the V rows of the last tile have landed, request n_tiles - 1 - PD of n_tiles - 2 at least ((h - 5) / 2 of
+        // (h - 3) / 2).
         auto advance_last = [&](int h) __attribute__((always_inline)) {
-            wait_vmem<(PD - 1) * LOADS>();
+            wait_vmem<(STEP == 1 ? PD - 1 : 1) * LOADS>();
             ring_barrier();
             clean(h, n_tiles);
         };
@@ -637,7 +670,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             for (; h + 1 < n_tiles; h += 2) {
                 advance_pair(h);
                 request();
-                request();
+                if constexpr (STEP == 1) request();
             }
             advance_last(h);
         } else {
@@ -823,7 +856,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
                 half_step(X1{}, yes{}, yes{}, yes{}, yes{}, yes{}, k0, k1, v0, v1);
                 first_output();
                 mask(s_sl[1], h);
-                half_step(X0{}, yes{}, yes{}, yes{}, yes{}, yes{}, k1, k2, v1, k0);
+                half_step(X0{}, yes{}, yes{}, yes{}, yes{}, std::bool_constant<STEP == 1>{}, k1, k2, v1, k0);
                 mask(s_sl[0], h + 1);
                 h += 2;
             };
