@@ -110,8 +110,10 @@ struct Shares {
 // Pieces per block.
 __device__ __forceinline__ int cut_of(const Request &q, const Shares &share)
 {
-    if (q.cost <= kWhole) return 1;
-    return (int)ceilf(q.cost * __builtin_amdgcn_rcpf(q.rows <= FEW ? fmaxf(share.few, kFewSplit) : fmaxf(share.rows, kWhole)));
+    // (no branches here and in what follows: every workgroup goes through this before its first load)
+    const float few = __builtin_amdgcn_rcpf(fmaxf(share.few, kFewSplit)), rows = __builtin_amdgcn_rcpf(fmaxf(share.rows, kWhole));
+    const int cut = (int)ceilf(q.cost * (q.rows <= FEW ? few : rows));
+    return q.cost <= kWhole ? 1 : cut;
 }
 // Query rows of a block's partial results, if it is cut.
 template <int ROWS> __device__ __forceinline__ int block_rows(const Request &q) { return q.rows < ROWS ? q.rows : ROWS; }
@@ -119,20 +121,20 @@ template <int ROWS> __device__ __forceinline__ int block_rows(const Request &q) 
 // Pieces of a request that cost about x or more: those of its last blocks.  (Any order will do; every wave must find the same.)
 __device__ __forceinline__ int pieces_from(const Request &q, int cut, float x)
 {
-    const float want = x * (float)cut;
-    if (x <= 0.f) return q.blocks * cut;
-    if (want > q.cost) return 0;
-    const float k = ceilf((want - q.start) * q.per_step) - 1.f;  // first block with that cost
-    const int left = q.blocks - (k > 0.f ? (int)fminf(k, 1e9f) : 0);
-    return left > 0 ? left * cut : 0;
+    const float want = x * (float)cut, k = ceilf((want - q.start) * q.per_step) - 1.f;  // first block with that cost
+    int below = (int)__builtin_amdgcn_fmed3f(k, 0.f, (float)q.blocks);
+    below = want > q.cost ? q.blocks : below;
+    below = x > 0.f ? below : 0;
+    return (q.blocks - below) * cut;
 }
 
-// The largest of values that are not negative, in every lane of a wave.
-__device__ __forceinline__ float most_of_lanes(float x)
+// The largest of values that are not negative (so ordered like their bits), in every lane of a wave.
+__device__ __forceinline__ float most_of_lanes(float value)
 {
+    int x = __builtin_bit_cast(int, value);
     auto take = [&](auto ctrl, auto row_mask) __attribute__((always_inline)) {
-        const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(row_mask)::value, 0xf, false);
-        x = fmaxf(x, __builtin_bit_cast(float, y));
+        const int y = __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(row_mask)::value, 0xf, false);
+        x = x > y ? x : y;
     };
     using all = std::integral_constant<int, 0xf>;
     take(std::integral_constant<int, 0x111>{}, all{});
@@ -141,7 +143,14 @@ __device__ __forceinline__ float most_of_lanes(float x)
     take(std::integral_constant<int, 0x118>{}, all{});
     take(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
     take(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
-    return last_lane(x);
+    return __builtin_bit_cast(float, last_lane(x));
+}
+
+// Sums over the lanes of a wave, in every lane.
+template <typename T, int N> __device__ __forceinline__ void sum_lanes(T (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = last_lane(scan_lanes(x[i]));
 }
 
 struct Piece {
@@ -150,7 +159,7 @@ struct Piece {
     bool valid;
 };
 
-// The shares of the work above which blocks are cut.  sum(f), most(f): over all requests; least(time): the candidate with the least time.
+// The shares of the work above which blocks are cut.  sums(x, f): x[] as f adds them up for every request; most(f): over all requests; least(time): the candidate with the least time.
 // Three blocks for each compute unit and more even out by themselves; only a block beyond a unit's share is cut.  With fewer blocks
 // the least of some candidates' expected times is taken, in tiles: one round of pieces lasts as long as the longest; in several
 // the units end apart by some part of it, which the few rows' pieces, dealt last and cut small, fill up.  (Against the best of 90
@@ -173,29 +182,35 @@ __device__ __forceinline__ Shares shares_of(int candidate, float mean)
     }
     return {rows == kNever ? rows : rows * mean, few == kNever ? few : few * mean};
 }
-template <int ROWS, typename Sum, typename Most, typename Least>
-__device__ __forceinline__ Shares choose_shares(const ChunkArgs &a, Sum sum, Most most, Least least)
+template <int ROWS, typename Sums, typename Most, typename Least>
+__device__ __forceinline__ Shares choose_shares(const ChunkArgs &a, Sums sums, Most most, Least least)
 {
     if (a.slots == 0) return {kNever, kNever};
-    const float blocks = sum([](const Request &q) { return (float)q.blocks; });
-    const float work = sum([](const Request &q) { return q.work; });
-    const float few_work = sum([](const Request &q) { return q.rows <= FEW ? q.work : 0.f; });
-    const float units = (float)a.units, by_units = __builtin_amdgcn_rcpf(units), mean = work * by_units;
+    float of_all[3] = {0.f, 0.f, 0.f};  // blocks, work, work of the few rows
+    sums(of_all, [](const Request &q, float (&x)[3]) {
+        x[0] += (float)q.blocks;
+        x[1] += q.work;
+        x[2] += q.rows <= FEW ? q.work : 0.f;
+    });
+    const float blocks = of_all[0], units = (float)a.units, by_units = __builtin_amdgcn_rcpf(units), mean = of_all[1] * by_units;
+    const float few_work = of_all[2];
     auto time_of = [&](const Shares &share) __attribute__((always_inline)) {
-        const float pieces = sum([&](const Request &q) { return (float)q.blocks * (float)cut_of(q, share); });
-        const float slots = sum([&](const Request &q) {
+        float cuts[2] = {0.f, 0.f};  // pieces, partial rows
+        sums(cuts, [&](const Request &q, float (&x)[2]) {
             const float c = (float)cut_of(q, share);
-            return c > 1.f ? (float)q.blocks * c * (float)block_rows<ROWS>(q) : 0.f;
+            x[0] += (float)q.blocks * c;
+            x[1] += c > 1.f ? (float)q.blocks * c * (float)block_rows<ROWS>(q) : 0.f;
         });
+        const float pieces = cuts[0], slots = cuts[1];
         auto longest = [&](bool few) __attribute__((always_inline)) {
             return most([&](const Request &q) { return (q.rows <= FEW) == few ? q.cost * __builtin_amdgcn_rcpf((float)cut_of(q, share)) : 0.f; });
         };
         const float rows = longest(false), few = longest(true), longer = fmaxf(rows, few) + kPieceCost;
-        // (room for the partial rows, and for the pieces that cutting adds)
-        if (slots > (float)a.slots || pieces - blocks > (float)a.extra) return 2.f * kNever;
         const float merge = slots > 0.f ? kMergeCost + kMergeBlock * slots * (1.f / ROWS) * by_units : 0.f;
-        if (pieces <= units) return merge + longer;
-        return merge + fmaxf(longer, mean + kPieceCost * pieces * by_units + fmaxf(kUneven * rows - few_work * by_units, kUneven * few));
+        const float several = fmaxf(longer, mean + kPieceCost * pieces * by_units + fmaxf(kUneven * rows - few_work * by_units, kUneven * few));
+        const float time = merge + (pieces <= units ? longer : several);
+        // (room for the partial rows, and for the pieces that cutting adds)
+        return slots > (float)a.slots || pieces - blocks > (float)a.extra ? 2.f * kNever : time;
     };
     if (blocks >= 3.f * units) {
         const Shares share{1.25f * mean, 1.25f * mean};
@@ -218,7 +233,12 @@ template <int ROWS, int NW, bool BLOCKS> __device__ __forceinline__ Piece find_p
     }
     const Request q = load_request<ROWS>(a, lane);
     const Shares share = choose_shares<ROWS>(
-        a, [&](auto f) { return last_lane(scan_lanes(f(q))); }, [&](auto f) { return most_of_lanes(f(q)); },
+        a,
+        [&](auto &x, auto f) {
+            f(q, x);
+            sum_lanes(x);
+        },
+        [&](auto f) { return most_of_lanes(f(q)); },
         [&](auto time) {  // the waves share the candidates
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
             for (int k = wave; k < kShares; k += NW) {
@@ -247,23 +267,21 @@ template <int ROWS, int NW, bool BLOCKS> __device__ __forceinline__ Piece find_p
         b = __builtin_ctzll(__ballot(piece_end > i));
         at = i - __builtin_amdgcn_readlane(piece_end - pieces, b);
     } else {
-        // longest first: the largest x such that more than i pieces cost x or more
-        int lo = 0, hi = (int)most_of_lanes(q.cost) + 2;  // (none costs `hi` or more)
+        // longest first, by sixteenths of the longest: the largest x such that more than i pieces cost x sixteenths or more
+        const float unit = most_of_lanes(q.cost * __builtin_amdgcn_rcpf((float)cut)) * (1.f / 16.f) + 0x1p-10f;
+        int lo = 0, hi = 17;  // (none costs 17 or more)
         while (hi - lo > 1) {  // by quarters: three sums at a time
             const int step = (hi - lo + 3) >> 2;
             const int x1 = lo + step, x2 = x1 + step < hi ? x1 + step : hi, x3 = x2 + step < hi ? x2 + step : hi;
-            const int c1 = last_lane(scan_lanes(pieces_from(q, cut, (float)x1)));
-            const int c2 = last_lane(scan_lanes(pieces_from(q, cut, (float)x2)));
-            const int c3 = last_lane(scan_lanes(pieces_from(q, cut, (float)x3)));
-            if (c3 > i) {
-                lo = x3;
-            } else {
-                lo = c2 > i ? x2 : c1 > i ? x1 : lo;
-                hi = c2 > i ? x3 : c1 > i ? x2 : x1;
-            }
+            int c[3] = {pieces_from(q, cut, (float)x1 * unit), pieces_from(q, cut, (float)x2 * unit), pieces_from(q, cut, (float)x3 * unit)};
+            sum_lanes(c);
+            lo = c[2] > i ? x3 : c[1] > i ? x2 : c[0] > i ? x1 : lo;
+            hi = c[2] > i ? hi : c[1] > i ? x3 : c[0] > i ? x2 : x1;
         }
-        const int above = pieces_from(q, cut, (float)hi), same = pieces_from(q, cut, (float)lo) - above, upto = scan_lanes(same);
-        const int rest = i - last_lane(scan_lanes(above));
+        const int above = pieces_from(q, cut, (float)hi * unit), same = pieces_from(q, cut, (float)lo * unit) - above, upto = scan_lanes(same);
+        int all_above[1] = {above};
+        sum_lanes(all_above);
+        const int rest = i - all_above[0];
         b = __builtin_ctzll(__ballot(upto > rest) | 1ull << 63);
         at = __builtin_amdgcn_readlane(above + rest - (upto - same), b);
     }
@@ -320,11 +338,11 @@ chunk_list_kernel(ChunkArgs a)
     };
     const Shares share = choose_shares<ROWS>(
         a,
-        [&](auto f) {
-            auto x = f(q[0]);
+        [&](auto &x, auto f) {
 #pragma unroll
-            for (int j = 1; j < LIST_PER; ++j) x += f(q[j]);
-            return sum_threads(x);
+            for (int j = 0; j < LIST_PER; ++j) f(q[j], x);
+#pragma unroll
+            for (float &part : x) part = sum_threads(part);
         },
         [&](auto f) {
             float x = f(q[0]);
@@ -456,6 +474,35 @@ __device__ __forceinline__ QueryRow query_row(const ChunkArgs &a, const Request 
     x.lo = a.window > 0 && x.place - a.window + 1 > 0 ? x.place - a.window + 1 : 0;
     return x;
 }
+
+// Byte offsets of query rows r, r + step, r + 2 step ... in q or out, by additions.  Past the last row it stays where it is.
+struct RowWalk {
+    int64_t at, jump, wrap;  // jump: step rows further; wrap: from a group's end to the next token's first
+    int32_t head, heads, r, step, rows, group;
+    __device__ __forceinline__ RowWalk(const ChunkArgs &a, const Request &q, int g, int first, int row_step, const int64_t (&stride)[2])
+    {
+        const QueryRow x = query_row(a, q, g, first);
+        at = x.token * stride[0] + x.head * stride[1];
+        group = a.group;
+        head = x.head - g * group;
+        const int tokens = (int)a.by_group.div((uint32_t)row_step);
+        heads = row_step - tokens * group;
+        jump = tokens * stride[0] + heads * stride[1];
+        wrap = stride[0] - group * stride[1];
+        r = first;
+        step = row_step;
+        rows = q.rows;
+    }
+    __device__ __forceinline__ void next()
+    {
+        r += step;
+        head += heads;
+        const bool over = head >= group;
+        head -= over ? group : 0;
+        const int64_t by = jump + (over ? wrap : 0);
+        at += r < rows ? by : 0;
+    }
+};
 
 // Partial rows of a piece, its first one number `row` of KV head g: [row][D] fp32 sums, and (m, l) of every row.
 template <int D> __device__ __forceinline__ float *part_rows(const ChunkArgs &a, int row, int g) { return a.parts + ((int64_t)g * a.slots + row) * D; }
@@ -595,14 +642,15 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
         if (!is_v) request();
         // Query rows: through LDS, in stages that the first requests leave free, in the layout of a K tile.
         const uint32_t q_at = (uint32_t)(wave < RS - PD - 1 ? PD + 1 + wave : wave < RS - PD - 1 + RS - PD ? RS + PD + wave - (RS - PD - 1) : 2 * RS) * TILEB;
-        if (has_rows)
+        if (has_rows) {
+            RowWalk y(a, q, g, wave_row0 + ld_row, RPL, a.q_s);
 #pragma unroll
             for (int j = 0; j < TPT; ++j) {
-                const int r = j * RPL + ld_row;
-                const QueryRow y = query_row(a, q, g, wave_row0 + r);
-                copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ (r & (CH - 1))) * 16,
+                copy_row_to_lds(a.q + y.at + (ld_pos ^ ((j * RPL + ld_row) & (CH - 1))) * 16,
                                 __builtin_amdgcn_readfirstlane(base + q_at + j * RPL * ROWB));
+                y.next();
             }
+        }
         if constexpr (STEP == 1) {
 #pragma unroll
             for (int r = 0; r < PD; ++r) request();
@@ -930,12 +978,13 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             *(uint2 *)(mine + li * ROWB + ((4 * mt + rg) ^ (li & (CH - 1))) * 16 + lh * 8) =
                 make_uint2(pack16<F16>(st.o[mt][4 * rg] * inv, st.o[mt][4 * rg + 1] * inv),
                            pack16<F16>(st.o[mt][4 * rg + 2] * inv, st.o[mt][4 * rg + 3] * inv));
+    RowWalk y(a, q, g, wave_row0 + lane / CH, RPL, a.o_s);
 #pragma unroll
     for (int j = 0; j < TPT; ++j) {
         const int r = j * RPL + lane / CH, pos = lane % CH;
         const uint4 v = *(const uint4 *)(mine + r * ROWB + ((pos ^ (r & (CH - 1))) * 16));
-        const QueryRow y = query_row(a, q, g, wave_row0 + r);
-        if (y.ok) *(uint4 *)(a.out + y.token * a.o_s[0] + y.head * a.o_s[1] + pos * 16) = v;
+        if (y.r < q.rows) *(uint4 *)(a.out + y.at + pos * 16) = v;
+        y.next();
     }
     if (lh == 0 && x.ok) a.lse[(int64_t)x.token * a.n_q_heads + x.head] = l == 0.f ? -INFINITY : (st.m * a.scale_log2 + log2f(l)) * kLn2;
 }
