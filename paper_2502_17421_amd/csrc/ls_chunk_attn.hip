@@ -52,6 +52,12 @@ template <int D> constexpr int kTileBytes = TK * D * 2;
 template <int D> constexpr int kLds = (2 * RS + 1) * kTileBytes<D> + kWaves<D> * 512 + 16 + 8 * 4;
 static_assert(2 * 8 <= 2 * RS && 8 * 32 * 8 <= kTileBytes<64>, "LDS of the few rows");
 
+// Row r of a tile keeps its 16-byte chunk c at place c ^ swizzle(r).  Rows of 256 bytes (head_dim 128) all begin at the same bank,
+// rows of 128 at one of two, so that there pairs of rows go together.  (With the swizzles for 256 bytes half of the LDS cycles at
+// head_dim 64 were conflicts.)
+template <int D> __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? vswz(row) : (row & 2) << 1; }
+
 // ---- which piece --------------------------------------------------------------------------------
 
 // One request, and what its pieces are worked out from.  Work is counted in tiles of a row block.
@@ -578,7 +584,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
         const int my_row = wave % (TK / MINE) * MINE;
         // Every other one: of K waves 0 and 1 tiles 0, 2, 4 ..., of V waves 4 and 5 tiles 1, 3, 5 ...
         const int first_tile = STEP == 1 ? 0 : (wave / (TK / MINE) & 1) ^ (int)is_v;
-        auto chunk_at = [&](int row) __attribute__((always_inline)) { return (uint32_t)(ld_pos ^ ((is_v ? vswz(row) : row) & (CH - 1))) * 16; };
+        auto chunk_at = [&](int row) __attribute__((always_inline)) { return (uint32_t)(ld_pos ^ (is_v ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16; };
         // Lane's offset for copy j from the first of those rows, less what the instruction adds (rows are at least ROWB apart).
         uint32_t voff[LOADS];
 #pragma unroll
@@ -646,7 +652,7 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             RowWalk y(a, q, g, wave_row0 + ld_row, RPL, a.q_s);
 #pragma unroll
             for (int j = 0; j < TPT; ++j) {
-                copy_row_to_lds(a.q + y.at + (ld_pos ^ ((j * RPL + ld_row) & (CH - 1))) * 16,
+                copy_row_to_lds(a.q + y.at + (ld_pos ^ k_swizzle<D>(j * RPL + ld_row)) * 16,
                                 __builtin_amdgcn_readfirstlane(base + q_at + j * RPL * ROWB));
                 y.next();
             }
@@ -726,10 +732,10 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
             typedef __attribute__((address_space(3))) shortx4 *lds_s4;
             const float c = a.scale_log2;
             const QueryRow x = query_row(a, q, g, wave_row0 + li);
-            const uint32_t k_off0 = base + li * ROWB + ((lh ^ (li & (CH - 1))) * 16);
+            const uint32_t k_off0 = base + li * ROWB + ((lh ^ k_swizzle<D>(li)) * 16);
             const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
             const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
-            const uint32_t v_off0 = base + RING + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
+            const uint32_t v_off0 = base + RING + tr_row * ROWB + ((tr_dchunk ^ v_swizzle<D>(tr_row)) * 16) + (tr_s & 1) * 8;
             // A fragment's place in stage 0, kept: the stages of the main loop are constants and go into the instructions' offsets.
             uint32_t k_at[KSTEPS], v_at[MT];
 #pragma unroll
@@ -975,14 +981,14 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int rg = 0; rg < 4; ++rg)
-            *(uint2 *)(mine + li * ROWB + ((4 * mt + rg) ^ (li & (CH - 1))) * 16 + lh * 8) =
+            *(uint2 *)(mine + li * ROWB + ((4 * mt + rg) ^ k_swizzle<D>(li)) * 16 + lh * 8) =
                 make_uint2(pack16<F16>(st.o[mt][4 * rg] * inv, st.o[mt][4 * rg + 1] * inv),
                            pack16<F16>(st.o[mt][4 * rg + 2] * inv, st.o[mt][4 * rg + 3] * inv));
     RowWalk y(a, q, g, wave_row0 + lane / CH, RPL, a.o_s);
 #pragma unroll
     for (int j = 0; j < TPT; ++j) {
         const int r = j * RPL + lane / CH, pos = lane % CH;
-        const uint4 v = *(const uint4 *)(mine + r * ROWB + ((pos ^ (r & (CH - 1))) * 16));
+        const uint4 v = *(const uint4 *)(mine + r * ROWB + ((pos ^ k_swizzle<D>(r)) * 16));
         if (y.r < q.rows) *(uint4 *)(a.out + y.at + pos * 16) = v;
         y.next();
     }
@@ -1023,7 +1029,7 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
     const int page_mask = (1 << a.page_shift) - 1;
     const int32_t *tab = a.block_table + (int64_t)piece.b * a.bt_stride;
     const int ld_row = lane / CH, ld_pos = lane % CH;
-    const uint32_t k_chunk = (uint32_t)(ld_pos ^ ld_row), v_chunk = (uint32_t)(ld_pos ^ (vswz(ld_row) & (CH - 1)));
+    const uint32_t k_chunk = (uint32_t)(ld_pos ^ k_swizzle<D>(ld_row)), v_chunk = (uint32_t)(ld_pos ^ v_swizzle<D>(ld_row));
     // the pages of rows 0..15 and 16..31 of tile t
     auto pages_of = [&](int t) __attribute__((always_inline)) {
         int r0 = (t_lo + t) * TK, r1 = r0 + 16;
@@ -1040,10 +1046,8 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         const uint8_t *p0 = (V ? vp : kp) + (int64_t)pages.x * page_bytes + (int64_t)(first & page_mask) * rb;
         const uint8_t *p1 = (V ? vp : kp) + (int64_t)pages.y * page_bytes + (int64_t)((first + 16) & page_mask) * rb;
         const uint32_t chunk = (V ? v_chunk : k_chunk) * 16;
-        // (copy j's rows are RPL further; the K swizzle of rows 4, 8 and 12 on is that of rows 0 to 3 with 4, 8 and 12 added)
-        auto chunk_of = [&](int j) __attribute__((always_inline)) {
-            return RPL >= CH || V ? chunk : chunk ^ (uint32_t)(((j * RPL) & (CH - 1)) * 16);
-        };
+        // (copy j's rows are RPL further, a power of two above theirs: the swizzle of the sum is that of both)
+        auto chunk_of = [&](int j) __attribute__((always_inline)) { return V ? chunk : chunk ^ (uint32_t)(k_swizzle<D>(j * RPL) * 16); };
         if (last >= TK - 1) {
             const uint32_t off = (uint32_t)(ld_row * rb);
 #pragma unroll
@@ -1076,14 +1080,14 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         for (int j = 0; j < LOADS; ++j) {
             const int r = j * RPL + ld_row;
             const QueryRow y = query_row(a, q, g, r);
-            copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ (r & (CH - 1))) * 16,
+            copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ k_swizzle<D>(r)) * 16,
                             __builtin_amdgcn_readfirstlane(stage + TILEB + j * RPL * ROWB));
         }
         request(std::false_type{}, wave, pages);
-        const uint32_t k_off0 = stage + li * ROWB + ((lh ^ (li & (CH - 1))) * 16);
+        const uint32_t k_off0 = stage + li * ROWB + ((lh ^ k_swizzle<D>(li)) * 16);
         const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
         const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
-        const uint32_t v_off0 = stage + TILEB + tr_row * ROWB + ((tr_dchunk ^ (vswz(tr_row) & (CH - 1))) * 16) + (tr_s & 1) * 8;
+        const uint32_t v_off0 = stage + TILEB + tr_row * ROWB + ((tr_dchunk ^ v_swizzle<D>(tr_row)) * 16) + (tr_s & 1) * 8;
         auto read_tile = [&](uint32_t off, bf16x8 (&frag)[KSTEPS]) __attribute__((always_inline)) {
             asm volatile("" : "+v"(off));  // the fragments' addresses are formed here, not kept over the loop
 #pragma unroll
