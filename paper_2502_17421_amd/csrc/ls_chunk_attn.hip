@@ -30,7 +30,7 @@
 //   four first prompts of 611 to 4003 tokens    240 us, 0.95 PFLOP/s
 //   24 single tokens, 1 to 30 thousand rows     265 us, 5.7 TB/s
 //   18 single tokens and two pieces of prompts, up to 9 thousand rows, 40 query heads   184 us
-//   window of 512, 16 and 4 heads of 64, f16    38 us;  four single tokens, up to 1.5 thousand rows    14 us
+//   window of 512, 16 and 4 heads of 64, f16    36 us;  four single tokens, up to 1.5 thousand rows    14 us
 // Long row blocks are held by the power limit (with zeros for inputs the first takes 0.63 ms; 1.5 to 1.95 GHz), head_dim 64 by the vector
 // ALUs (16 exponentials a lane and tile at a quarter of their rate), long few rows by HBM, short calls by latency.
 #include <type_traits>
@@ -678,14 +678,15 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
         __syncthreads();  // K tile 0 and the query rows are in LDS
 
         auto ring_barrier = [&]() __attribute__((always_inline)) { asm volatile("s_barrier" ::: "memory"); };
-        // Tiles (of this piece) that all rows between two see whole: the first of them, and how many.
+        // Tiles (of this piece) that all rows between two see whole: the first of them, and how many; and the first one past whose
+        // end some row does not see.
         auto seen_whole = [&](int first_row, int last_row) __attribute__((always_inline)) {
             const QueryRow top = query_row(a, q, g, first_row), end = query_row(a, q, g, last_row);
             const int from = div_up(end.lo, TK) - t_lo, to = (top.place + 1 > 0 ? top.place + 1 : 0) / TK - t_lo;
-            return make_int2(__builtin_amdgcn_readfirstlane(from), __builtin_amdgcn_readfirstlane(to > from ? to - from : 0));
+            return int3{__builtin_amdgcn_readfirstlane(from), __builtin_amdgcn_readfirstlane(to > from ? to - from : 0), __builtin_amdgcn_readfirstlane(to)};
         };
-        auto inside = [&](int t, int2 range) __attribute__((always_inline)) { return (uint32_t)(t - range.x) < (uint32_t)range.y; };
-        const int2 block_whole = seen_whole(row0, row0 + ROWS - 1);
+        auto inside = [&](int t, int3 range) __attribute__((always_inline)) { return (uint32_t)(t - range.x) < (uint32_t)range.y; };
+        const int3 block_whole = seen_whole(row0, row0 + ROWS - 1);
         // V tiles h and h + 1 are there: values that are not finite leave tiles that some row of the block does not see whole.
         // (A tile's first fragments are read a half-step later, at the earliest.)
         auto clean = [&](int from, int to) __attribute__((always_inline)) {
@@ -764,14 +765,16 @@ __device__ __forceinline__ void row_block(const ChunkArgs &a, const Piece &piece
                 const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB)));
                 return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
             };
-            const int2 wave_whole = seen_whole(wave_row0, wave_row0 + 31);
+            const int3 wave_whole = seen_whole(wave_row0, wave_row0 + 31);
             auto mask = [&](floatx16 &s, int t) __attribute__((always_inline)) {
                 if (inside(t, wave_whole)) return;
+                const int key0 = (t_lo + t) * TK + 4 * lh;  // (one comparison a score at either edge)
+                if (t >= wave_whole.z)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = (t_lo + t) * TK + 8 * (e >> 2) + 4 * lh + (e & 3);
-                    s[e] = key >= x.lo && key <= x.place ? s[e] : -INFINITY;
-                }
+                    for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= x.place - key0 ? s[e] : -INFINITY;
+                if (t < wave_whole.x)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) >= x.lo - key0 ? s[e] : -INFINITY;
             };
             auto numerators = [&](const floatx16 &s, uint32_t (&pp)[8]) __attribute__((always_inline)) {  // with the current m
                 const float mc = st.m == -INFINITY ? 0.f : st.m * c;
