@@ -1195,24 +1195,34 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
     constexpr int TPR = NW * 64 / 32;         // threads per row
     constexpr int PASSES = CPR / TPR;         // pieces per thread
     float2 *ml = (float2 *)(smem + 2 * NW * TILEB);  // (m, l) [row][wave]
-    const int n_active = n_tiles < NW ? n_tiles : NW;
     const int row = tid / TPR;                // the row this thread finishes
     const float l_tot = half_sum(st.l);
     if (lh == 0) ml[li * NW + wave] = make_float2(st.m, l_tot);
-    if (busy) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt)  // (waves without a tile: zeros, so that what follows has no branches and its reads go out together)
 #pragma unroll
-            for (int rg = 0; rg < 4; ++rg)
-                *(float4 *)(smem + wave * 2 * TILEB + li * (D * 4) + ((8 * mt + 2 * rg + lh) ^ (li & (CPR - 1))) * 16) =
-                    make_float4(st.o[mt][4 * rg], st.o[mt][4 * rg + 1], st.o[mt][4 * rg + 2], st.o[mt][4 * rg + 3]);
-    }
+        for (int rg = 0; rg < 4; ++rg)
+            *(float4 *)(smem + wave * 2 * TILEB + li * (D * 4) + ((8 * mt + 2 * rg + lh) ^ (li & (CPR - 1))) * 16) =
+                make_float4(st.o[mt][4 * rg], st.o[mt][4 * rg + 1], st.o[mt][4 * rg + 2], st.o[mt][4 * rg + 3]);
     __syncthreads();
     if (piece.cut > 1 && piece.split == 0 && tid == 0) write_entry<ROWS>(a, piece, g);
     if (row >= q.rows) return;
+    float2 states[NW];
+#pragma unroll
+    for (int k = 0; k < NW; k += 2) {
+        const float4 two = *(const float4 *)(ml + row * NW + k);
+        states[k] = make_float2(two.x, two.y);
+        states[k + 1] = make_float2(two.z, two.w);
+    }
+    float4 parts[NW][PASSES];
+#pragma unroll
+    for (int k = 0; k < NW; ++k)
+#pragma unroll
+        for (int u = 0; u < PASSES; ++u)
+            parts[k][u] = *(const float4 *)(smem + k * 2 * TILEB + row * (D * 4) + (((tid % TPR + u * TPR) ^ (row & (CPR - 1))) * 16));
     float top = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < NW; ++k) top = fmaxf(top, ml[row * NW + k].x);
+    for (int k = 0; k < NW; ++k) top = fmaxf(top, states[k].x);
     float o[PASSES][4], l_sum = 0.f;
 #pragma unroll
     for (int u = 0; u < PASSES; ++u)
@@ -1220,13 +1230,12 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         for (int i = 0; i < 4; ++i) o[u][i] = 0.f;
 #pragma unroll
     for (int k = 0; k < NW; ++k) {
-        if (k >= n_active) continue;
-        const float2 s = ml[row * NW + k];
+        const float2 s = states[k];
         const float scale = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * a.scale_log2);  // (NaN stays NaN)
         l_sum += scale * s.y;
 #pragma unroll
         for (int u = 0; u < PASSES; ++u) {
-            const float4 v = *(const float4 *)(smem + k * 2 * TILEB + row * (D * 4) + (((tid % TPR + u * TPR) ^ (row & (CPR - 1))) * 16));
+            const float4 v = parts[k][u];
             o[u][0] += scale * v.x;
             o[u][1] += scale * v.y;
             o[u][2] += scale * v.z;
