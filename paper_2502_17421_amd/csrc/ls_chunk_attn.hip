@@ -227,6 +227,7 @@ __device__ __forceinline__ Shares choose_shares(const ChunkArgs &a, Sums sums, M
         return slots > (float)a.slots || pieces - blocks > (float)a.extra ? 2.f * kNever : time;
     };
     if (blocks >= 3.f * units) {
+        if (most([](const Request &q) { return q.cost; }) <= 1.25f * mean) return {kNever, kNever};
         const Shares share{1.25f * mean, 1.25f * mean};
         return time_of(share) < kNever ? share : Shares{kNever, kNever};
     }
@@ -272,7 +273,12 @@ template <int ROWS, int NW, bool BLOCKS> __device__ __forceinline__ Piece find_p
         });
     const int cut = cut_of(q, share), pieces = q.blocks * cut;
     const int slots = cut > 1 ? pieces * block_rows<ROWS>(q) : 0, entries = cut > 1 ? q.blocks : 0;
-    const int slot_end = scan_lanes(slots), entry_end = scan_lanes(entries), piece_end = scan_lanes(pieces);
+    const int piece_end = scan_lanes(pieces);
+    int slot_end = 0, entry_end = 0;
+    if (share.rows != kNever || share.few != kNever) {
+        slot_end = scan_lanes(slots);
+        entry_end = scan_lanes(entries);
+    }
     if (blockIdx.x == 0 && threadIdx.x == 63 && a.slots > 0) *a.n_entries = entry_end;  // for the merge
     const int total = last_lane(piece_end);
     if (i >= total) return p;
