@@ -17,7 +17,10 @@
 // apart at least where there are 8 heads, so an XCD sees one head and its L2 holds the tiles that its workgroups share.
 //
 // Products (operand layouts: ls_mfma.hpp).  S^T = K Q^T, so a lane holds 16 scores of ONE query row, and the numerators go
-// from the accumulators to the operand of O^T = V^T P^T by a pack to 16 bits, which the row sum does not take part in.
+// from the accumulators to the operand of O^T = V^T P^T by a pack to 16 bits, which the row sum does not take part in.  Row blocks
+// round the numerators once, to nearest: on average as much as the result's own rounding (error 1.4 times that of a result rounded
+// once), and a second product would take half as long again where the matrix cores bind.  The few rows wait for memory: they
+// take what the rounding left along as a second operand, and err no more than the result's rounding.
 //
 // Softmax state of a row: reference exponent m (raw scores) and l, the sum of exp2((s - m) c), c = scale * log2(e).  Any m
 // gives the same result, so the row blocks only raise it when a step's sum leaves the range of the operand type.
@@ -1124,7 +1127,7 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         // stage is asked for the next tile's.
         for (int t = wave; t < n_tiles; t += NW) {
             bf16x8 frag[KSTEPS];
-            uint32_t pp[8];
+            uint32_t pp[2][8];
             const bool more = t + NW < n_tiles;
             wait_vmem<LOADS>();
             read_tile(k_off0, frag);
@@ -1163,7 +1166,8 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
             for (int e = 0; e < 16; e += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -mc)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c, -mc));
                 sum += p0 + p1;
-                pp[e >> 1] = pack16<F16>(p0, p1);
+                pp[0][e >> 1] = pack16<F16>(p0, p1);
+                pp[1][e >> 1] = pack16<F16>(p0 - low16<F16>(pp[0][e >> 1]), p1 - high16<F16>(pp[0][e >> 1]));
             }
             st.l += sum;
             if (more) wait_vmem<LOADS>();
@@ -1185,10 +1189,12 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
             pages = pages_of(t + 2 * NW);
             const bool found = part && drop_not_finite<F16>(frag);
 #pragma unroll
-            for (int f = 0; f < KSTEPS; ++f) {
-                const uint32_t *u = pp + 4 * (f / MT);
-                st.o[f % MT] = mfma32<F16>(frag[f], __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), st.o[f % MT]);
-            }
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int f = 0; f < KSTEPS; ++f) {
+                    const uint32_t *u = pp[part] + 4 * (f / MT);
+                    st.o[f % MT] = mfma32<F16>(frag[f], __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), st.o[f % MT]);
+                }
             if (found)
                 for (int key = key0; key < key0 + TK && key < kv; ++key)
                     if (key >= x.lo && key <= x.place)
