@@ -33,7 +33,7 @@
 //   four first prompts of 611 to 4003 tokens    240 us, 0.95 PFLOP/s
 //   24 single tokens, 1 to 30 thousand rows     265 us, 5.7 TB/s
 //   18 single tokens and two pieces of prompts, up to 9 thousand rows, 40 query heads   184 us
-//   window of 512, 16 and 4 heads of 64, f16    36 us;  four single tokens, up to 1.5 thousand rows    14 us
+//   window of 512, 16 and 4 heads of 64, f16    36 us;  four single tokens, up to 1.5 thousand rows    13 us
 // Long row blocks are held by the power limit (with zeros for inputs the first takes 0.63 ms; 1.5 to 1.95 GHz), head_dim 64 by the vector
 // ALUs (16 exponentials a lane and tile at a quarter of their rate), long few rows by HBM, short calls by latency.
 #include <type_traits>
@@ -1025,17 +1025,80 @@ __device__ __forceinline__ int32_t scalar_load(const int32_t *p)
     return *(__attribute__((address_space(4))) const int32_t *)(uintptr_t)p;
 }
 
-template <int D, bool F16>
+// Shapes of the products: R = 16 or 32 query rows.  A lane holds scores of row lane % R, keys (256 / R) (e / 4) + 4 (lane / R) + e % 4; the
+// operands of the output product take the keys in this order.
+template <int R> struct FewShape {
+    static constexpr int KD = 512 / R;              // depth of a matrix instruction
+    static constexpr int SCORES = R / 2;            // per lane and tile
+    static constexpr int ACC = R * R / 64;          // per accumulator
+    typedef float Acc __attribute__((ext_vector_type(ACC)));
+};
+template <int R, bool F16>
+__device__ __forceinline__ typename FewShape<R>::Acc few_product(bf16x8 x, bf16x8 y, typename FewShape<R>::Acc z)
+{
+    typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+    if constexpr (R == 32) return mfma32<F16>(x, y, z);
+    else if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, x), __builtin_bit_cast(halfx8, y), z, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0);
+}
+// Largest and sum over the 64 / R lanes that share a row.
+template <int R> __device__ __forceinline__ float row_max(float x)
+{
+    x = half_max(x);
+    if constexpr (R == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return x;
+}
+template <int R> __device__ __forceinline__ float row_sum(float x)
+{
+    x = half_sum(x);
+    if constexpr (R == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return x;
+}
+// Where chunks of a V row go (see v_swizzle): with 16 rows a transposing read takes 32 bytes of eight rows, not 64 of four.
+template <int D, int R> __device__ __forceinline__ int few_v_swizzle(int row)
+{
+    if constexpr (R == 32) return v_swizzle<D>(row);
+    else return D == 128 ? (row & 7) << 1 : row & 6;
+}
+
+template <bool F16, int DT>
+__device__ __forceinline__ void few_add_not_finite(typename FewShape<16>::Acc (&o)[DT], const uint8_t *v_row, int lg)
+{
+    constexpr uint32_t kInf = F16 ? 0x7c00u : 0x7f80u;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        const uint2 x = *(const uint2 *)(v_row + dt * 32 + lg * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair = i < 2 ? x.x : x.y;
+            const bool bad = ((i & 1 ? pair >> 16 : pair) & 0x7fffu) >= kInf;
+            o[dt][i] += bad ? (i & 1 ? high16<F16>(pair) : low16<F16>(pair)) : 0.f;
+        }
+    }
+}
+
+// R: query rows there is room for.  Up to 16 (single tokens of up to 16 heads a KV head) take half the instructions of 32 (four
+// single tokens, 32 and 8 heads, f16: 11.8 us from warm caches, by 32 rows 14.3).
+template <int D, bool F16, int R>
 __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece, int g, uint8_t *smem)
 {
     constexpr int NW = kWaves<D>, ROWS = kRows<D>;
-    constexpr int KSTEPS = D / 16, MT = D / 32, CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
+    constexpr int CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
     constexpr int RPL = 64 / CH, LOADS = TK / RPL;
+    typedef FewShape<R> S;
+    constexpr int FRAGS = D / 16;                              // of a tile, K or V
+    constexpr int KS = D / S::KD, DT = D / R;                  // steps of a score product, accumulators of the output
     typedef std::conditional_t<F16, half_t, uint16_t> T16;
     typedef __attribute__((address_space(3))) const uint4 *lds_u4;
     typedef __attribute__((address_space(3))) shortx4 *lds_s4;
     const Request &q = piece.q;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane % R, lg = lane / R;
     const QueryRow x = query_row(a, q, g, li);
     const int2 span = block_tiles<ROWS>(a, q, 0);
     const int per = div_up(span.y, piece.cut);
@@ -1050,7 +1113,7 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
     const int page_mask = (1 << a.page_shift) - 1;
     const int32_t *tab = a.block_table + (int64_t)piece.b * a.bt_stride;
     const int ld_row = lane / CH, ld_pos = lane % CH;
-    const uint32_t k_chunk = (uint32_t)(ld_pos ^ k_swizzle<D>(ld_row)), v_chunk = (uint32_t)(ld_pos ^ v_swizzle<D>(ld_row));
+    const uint32_t k_chunk = (uint32_t)(ld_pos ^ k_swizzle<D>(ld_row)), v_chunk = (uint32_t)(ld_pos ^ few_v_swizzle<D, R>(ld_row));
     // the pages of rows 0..15 and 16..31 of tile t
     auto pages_of = [&](int t) __attribute__((always_inline)) {
         int r0 = (t_lo + t) * TK, r1 = r0 + 16;
@@ -1068,7 +1131,9 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
         const uint8_t *p1 = (V ? vp : kp) + (int64_t)pages.y * page_bytes + (int64_t)((first + 16) & page_mask) * rb;
         const uint32_t chunk = (V ? v_chunk : k_chunk) * 16;
         // (copy j's rows are RPL further, a power of two above theirs: the swizzle of the sum is that of both)
-        auto chunk_of = [&](int j) __attribute__((always_inline)) { return V ? chunk : chunk ^ (uint32_t)(k_swizzle<D>(j * RPL) * 16); };
+        auto chunk_of = [&](int j) __attribute__((always_inline)) {
+            return chunk ^ (uint32_t)((V ? few_v_swizzle<D, R>(j * RPL) : k_swizzle<D>(j * RPL)) * 16);
+        };
         if (last >= TK - 1) {
             const uint32_t off = (uint32_t)(ld_row * rb);
 #pragma unroll
@@ -1087,83 +1152,95 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
             }
         }
     };
-    RowState<D> st;
+    struct {
+        typename S::Acc o[DT];
+        float m, l;  // l: the numerators of this lane's keys until they are joined
+    } st;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) st.o[mt][e] = 0.f;
+        for (int e = 0; e < S::ACC; ++e) st.o[dt][e] = 0.f;
     st.m = -INFINITY;
     st.l = 0.f;
     if (busy) {
         int2 pages = pages_of(wave);
         // query rows into the V stage, in the layout of a K tile, and on into registers
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
+        for (int j = 0; j < R / RPL; ++j) {
             const int r = j * RPL + ld_row;
             const QueryRow y = query_row(a, q, g, r);
             copy_row_to_lds(a.q + y.token * a.q_s[0] + y.head * a.q_s[1] + (ld_pos ^ k_swizzle<D>(r)) * 16,
                             __builtin_amdgcn_readfirstlane(stage + TILEB + j * RPL * ROWB));
         }
         request(std::false_type{}, wave, pages);
-        const uint32_t k_off0 = stage + li * ROWB + ((lh ^ k_swizzle<D>(li)) * 16);
-        const int tr_s = lane & 15, tr_row = 4 * lh + (tr_s >> 2);
-        const int tr_dchunk = 2 * ((lane >> 4) & 1) + ((tr_s & 3) >> 1);
-        const uint32_t v_off0 = stage + TILEB + tr_row * ROWB + ((tr_dchunk ^ v_swizzle<D>(tr_row)) * 16) + (tr_s & 1) * 8;
-        auto read_tile = [&](uint32_t off, bf16x8 (&frag)[KSTEPS]) __attribute__((always_inline)) {
+        const uint32_t k_off0 = stage + li * ROWB + ((lg ^ k_swizzle<D>(li)) * 16);
+        const int tr_s = lane & 15, tr_row = 4 * lg + (tr_s >> 2);
+        const int tr_dchunk = (R == 32 ? 2 * ((lane >> 4) & 1) : 0) + ((tr_s & 3) >> 1);
+        const uint32_t v_off0 = stage + TILEB + tr_row * ROWB + ((tr_dchunk ^ few_v_swizzle<D, R>(tr_row)) * 16) + (tr_s & 1) * 8;
+        // K rows to registers, fragment KS * (16 or 32 rows) + step; query rows the same way
+        auto read_rows = [&](uint32_t off, auto &frag) __attribute__((always_inline)) {
+            constexpr int N = sizeof(frag) / sizeof(frag[0]);
             asm volatile("" : "+v"(off));  // the fragments' addresses are formed here, not kept over the loop
 #pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) frag[kk] = __builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)(off ^ (uint32_t)(kk << 5)));
+            for (int f = 0; f < N; ++f)
+                frag[f] = __builtin_bit_cast(bf16x8, *(lds_u4)(uintptr_t)((off ^ (uint32_t)(f % KS * (S::KD * 2))) + f / KS * R * ROWB));
 #pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) asm volatile("" : "+v"(frag[kk]));  // in registers: the stage is free
+            for (int f = 0; f < N; ++f) asm volatile("" : "+v"(frag[f]));  // in registers: the stage is free
         };
-        bf16x8 q_reg[KSTEPS];
+        bf16x8 q_reg[KS];
         wait_vmem<LOADS>();
-        read_tile(k_off0 + TILEB, q_reg);
+        read_rows(k_off0 + TILEB, q_reg);
         request(std::true_type{}, wave, pages);
         pages = pages_of(wave + NW);
         const float c = a.scale_log2;
-        const int all_hi = __builtin_amdgcn_readfirstlane(x.place) + 1, all_lo = __builtin_amdgcn_readlane(x.lo, 31);
+        const int all_hi = __builtin_amdgcn_readfirstlane(x.place) + 1, all_lo = __builtin_amdgcn_readlane(x.lo, R - 1);
         // Copies in flight, oldest first: K of tile t, V of tile t.  A tile's rows go to registers as soon as they are there, and the
         // stage is asked for the next tile's.
         for (int t = wave; t < n_tiles; t += NW) {
-            bf16x8 frag[KSTEPS];
-            uint32_t pp[2][8];
+            bf16x8 frag[FRAGS];
+            uint32_t pp[2][S::SCORES / 2];
             const bool more = t + NW < n_tiles;
             wait_vmem<LOADS>();
-            read_tile(k_off0, frag);
+            read_rows(k_off0, frag);
             if (more) request(std::false_type{}, t + NW, pages);
-            floatx16 s;
+            typename S::Acc scores[TK / R];
+            float s[S::SCORES];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+            for (int f = 0; f < FRAGS; ++f) {
+                if (f % KS == 0)
 #pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) s = mfma32<F16>(frag[kk], q_reg[kk], s);
+                    for (int e = 0; e < S::ACC; ++e) scores[f / KS][e] = 0.f;
+                scores[f / KS] = few_product<R, F16>(frag[f], q_reg[f % KS], scores[f / KS]);
+            }
+#pragma unroll
+            for (int e = 0; e < S::SCORES; ++e) s[e] = scores[e / S::ACC][e % S::ACC];
             const int key0 = (t_lo + t) * TK;
             const bool part = key0 + TK > all_hi || key0 < all_lo;  // some row does not see all of the tile
             if (part) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = key0 + 8 * (e >> 2) + 4 * lh + (e & 3);
+                for (int e = 0; e < S::SCORES; ++e) {
+                    const int key = key0 + 256 / R * (e >> 2) + 4 * lg + (e & 3);
                     s[e] = key >= x.lo && key <= x.place ? s[e] : -INFINITY;
                 }
             }
             float mx = s[0];
 #pragma unroll
-            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-            mx = half_max(mx);
+            for (int e = 1; e < S::SCORES; ++e) mx = fmaxf(mx, s[e]);
+            mx = row_max<R>(mx);
             if (__any((mx - st.m) * c > kLazy)) {  // also while m is -inf
                 const float m_new = fmaxf(st.m, mx);
                 const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((st.m - m_new) * c);
                 st.m = m_new;
                 st.l *= alpha;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) st.o[mt][e] *= alpha;
+                    for (int e = 0; e < S::ACC; ++e) st.o[dt][e] *= alpha;
             }
             const float mc = st.m == -INFINITY ? 0.f : st.m * c;
             float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
+            for (int e = 0; e < S::SCORES; e += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -mc)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c, -mc));
                 sum += p0 + p1;
                 pp[0][e >> 1] = pack16<F16>(p0, p1);
@@ -1176,14 +1253,14 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
                 uint32_t off = v_off0;
                 asm volatile("" : "+v"(off));
 #pragma unroll
-                for (int f = 0; f < KSTEPS; ++f) {
-                    const uint32_t at = (off ^ (uint32_t)((f % MT) << 6)) + ((f / MT) * 16) * ROWB;
+                for (int f = 0; f < FRAGS; ++f) {
+                    const uint32_t at = (off ^ (uint32_t)(f % DT * (R * 2))) + f / DT * 16 * ROWB;
                     const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)at));
-                    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB)));
+                    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 256 / R * ROWB)));
                     frag[f] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
                 }
 #pragma unroll
-                for (int f = 0; f < KSTEPS; ++f) asm volatile("" : "+v"(frag[f]));
+                for (int f = 0; f < FRAGS; ++f) asm volatile("" : "+v"(frag[f]));
             }
             if (more) request(std::true_type{}, t + NW, pages);
             pages = pages_of(t + 2 * NW);
@@ -1191,31 +1268,34 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
 #pragma unroll
             for (int part = 0; part < 2; ++part)
 #pragma unroll
-                for (int f = 0; f < KSTEPS; ++f) {
-                    const uint32_t *u = pp[part] + 4 * (f / MT);
-                    st.o[f % MT] = mfma32<F16>(frag[f], __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), st.o[f % MT]);
+                for (int f = 0; f < FRAGS; ++f) {
+                    const uint32_t *u = pp[part] + 4 * (f / DT);
+                    st.o[f % DT] = few_product<R, F16>(frag[f], __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), st.o[f % DT]);
                 }
             if (found)
                 for (int key = key0; key < key0 + TK && key < kv; ++key)
-                    if (key >= x.lo && key <= x.place)
-                        add_not_finite<F16>(st.o, vp + (int64_t)tab[key >> a.page_shift] * a.vc_s[0] + (int64_t)(key & page_mask) * a.vc_s[2], lh);
+                    if (key >= x.lo && key <= x.place) {
+                        const uint8_t *v_row = vp + (int64_t)tab[key >> a.page_shift] * a.vc_s[0] + (int64_t)(key & page_mask) * a.vc_s[2];
+                        if constexpr (R == 32) add_not_finite<F16>(st.o, v_row, lg);
+                        else few_add_not_finite<F16>(st.o, v_row, lg);
+                    }
         }
     }
 
     // ---- merge of the waves, in fp32, through the stages (each wave its own: nothing reads them any more)
     constexpr int CPR = D / 4;                // 16-byte pieces (4 floats) per row
-    constexpr int TPR = NW * 64 / 32;         // threads per row
+    constexpr int TPR = NW * 64 / R;          // threads per row
     constexpr int PASSES = CPR / TPR;         // pieces per thread
     float2 *ml = (float2 *)(smem + 2 * NW * TILEB);  // (m, l) [row][wave]
     const int row = tid / TPR;                // the row this thread finishes
-    const float l_tot = half_sum(st.l);
-    if (lh == 0) ml[li * NW + wave] = make_float2(st.m, l_tot);
+    const float l_tot = row_sum<R>(st.l);
+    if (lg == 0) ml[li * NW + wave] = make_float2(st.m, l_tot);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)  // (waves without a tile: zeros, so that what follows has no branches and its reads go out together)
+    for (int dt = 0; dt < DT; ++dt)  // (waves without a tile: zeros, so that what follows has no branches and its reads go out together)
 #pragma unroll
-        for (int rg = 0; rg < 4; ++rg)
-            *(float4 *)(smem + wave * 2 * TILEB + li * (D * 4) + ((8 * mt + 2 * rg + lh) ^ (li & (CPR - 1))) * 16) =
-                make_float4(st.o[mt][4 * rg], st.o[mt][4 * rg + 1], st.o[mt][4 * rg + 2], st.o[mt][4 * rg + 3]);
+        for (int e = 0; e < S::ACC; e += 4)
+            *(float4 *)(smem + wave * 2 * TILEB + li * (D * 4) + ((R / 4 * dt + e / 4 * (64 / R) + lg) ^ (li & (CPR - 1))) * 16) =
+                make_float4(st.o[dt][e], st.o[dt][e + 1], st.o[dt][e + 2], st.o[dt][e + 3]);
     __syncthreads();
     if (piece.cut > 1 && piece.split == 0 && tid == 0) write_entry<ROWS>(a, piece, g);
     if (row >= q.rows) return;
@@ -1281,7 +1361,10 @@ chunk_attn_kernel(ChunkArgs a)
     const int lane = threadIdx.x & 63;
     const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>, kWaves<D>, BLOCKS>(a, i, lane, (float *)(smem + kLds<D> - kShares * 4));
     if (!piece.valid) return;
-    if (!BLOCKS || piece.q.rows <= FEW) few_rows<D, F16>(a, piece, g, smem);
+    if (!BLOCKS || piece.q.rows <= FEW) {
+        if (piece.q.rows <= 16) few_rows<D, F16, 16>(a, piece, g, smem);
+        else few_rows<D, F16, 32>(a, piece, g, smem);
+    }
     else if constexpr (BLOCKS) row_block<D, F16>(a, piece, g, smem);
 }
 

@@ -287,3 +287,37 @@ def test_the_largest_batch():
     Step("f16", (2, 1, 64), news, [1 + i % 37 for i in range(len(news))], seed=20).check()
     news[5] = 90
     Step("f16", (2, 1, 64), news, [90 + i % 37 for i in range(len(news))], seed=21).check()
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16")])
+@pytest.mark.parametrize("n", [15, 16, 17, 31, 32, 33])
+def test_around_the_rows_of_a_product(n, d, dtype):
+    """16 and 32 rows per KV head are where the kernels change."""
+    Step(dtype, (2, 2, d), [n, 1, n], [n, 90, 500 + n], seed=22).check()
+    Step(dtype, (2, 2, d), [n], [300 + n], page_size=64, seed=23).check(window=33)
+
+
+@pytest.mark.parametrize("heads,dtype", [("gqa", "bf16"), ("small", "f16")])
+@pytest.mark.parametrize("n", [4, 7])
+@pytest.mark.parametrize("window", [0, 2])
+def test_unseen_values_and_keys_have_no_part_in_few_rows(heads, dtype, n, window):
+    st, bad = (Step(dtype, HEADS[heads], [n, 1], [150, 70], seed=24) for _ in range(2))
+    clean = st.run(window)
+    at = 150 - 3  # the row of token n - 3
+    bad.v_rows[0][:, at, 3] = float("-inf")
+    bad.v_rows[0][:, at, 61] = float("nan")
+    bad.k_rows[0][:, at + 1, 1] = float("nan")
+    bad.v_rows[0][:, 150 - n - 4] = float("inf")  # before every window of two
+    out, lse = bad.run(window)
+    before, only_v, after = slice(0, n - 3), n - 3, slice(n - 2, n)
+    others = [i for i in range(out.shape[2]) if i not in (3, 61)]
+    if window:
+        assert torch.equal(out[before], clean[0][before]) and torch.equal(lse[before], clean[1][before])
+        assert torch.isneginf(out[only_v][:, 3]).all() and torch.equal(out[only_v][:, others], clean[0][only_v][:, others])
+        assert torch.isnan(out[after]).all() and torch.isnan(lse[after]).all()
+    else:  # all see the infinite row, the last two a key of NaN as well
+        assert torch.isposinf(out[before]).all() and torch.equal(lse[before], clean[1][before])
+        assert torch.isnan(out[only_v][:, [3, 61]]).all() and torch.isposinf(out[only_v][:, others]).all()
+        assert torch.isnan(out[after]).all()
+    assert torch.isnan(out[only_v][:, 61]).all() and torch.equal(lse[only_v], clean[1][only_v])
+    assert torch.equal(out[n], clean[0][n]) and torch.equal(lse[n], clean[1][n])
