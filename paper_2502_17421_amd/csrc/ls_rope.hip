@@ -7,7 +7,7 @@
 // once and stay in registers, queries, keys and values pass through once, 16 bytes a lane.  A rotated unit is two pieces of 8
 // elements rotary_dim/2 apart, or 16 neighbouring elements (interleaved).
 //
-// Bound by HBM for prompts (8192 tokens of 56 heads of 128, bf16: 51 us, 4.7 TB/s read and written), by latency for a few
+// Bound by HBM for prompts (8192 tokens of 56 heads of 128, bf16: 48 us, 5.0 TB/s read and written), by latency for a few
 // tokens (24 tokens: 4 us).
 #include "ls_step.hpp"
 
@@ -17,7 +17,7 @@ namespace {
 
 constexpr int NT = 256;   // threads per workgroup
 constexpr int BATCH = 2;  // heads whose loads are in flight together
-constexpr int kFewTokens = 1024;
+constexpr int kFewTokens = 2048;
 
 // 16-byte pieces of 8 elements
 template <typename T> constexpr int kPieces = sizeof(T) * 8 / 16;
@@ -185,10 +185,11 @@ template <typename T, int D, int SLOTS> hipError_t launch_form(const RopeArgs &a
 
 template <typename T> hipError_t launch_type(const RopeArgs &a, int head_dim, hipStream_t stream)
 {
-    // Few tokens: a workgroup each, all heads in one turn (a rope of 24 tokens: 4 us).  Many: 32 threads a token that go through its
-    // heads, so that a cosine read serves many heads (8192 tokens of 40 + 8 + 8 heads: 16 threads 67 us, 32 51, 64 54).
-    if (a.n_tokens <= kFewTokens) return head_dim == 128 ? launch_form<T, 128, 32>(a, stream) : launch_form<T, 64, 64>(a, stream);
-    return head_dim == 128 ? launch_form<T, 128, 4>(a, stream) : launch_form<T, 64, 8>(a, stream);
+    // head_dim 128: a token's heads go through one workgroup, so that its reads and writes are in one place (8000 tokens of 32 + 8 + 8
+    // heads: 16 threads a token 60 us, 32 48, 64 46, 128 43, 256 42).  head_dim 64, 16 + 4 + 4 heads: 32 slots up to 2048 tokens
+    // (2000: 5.6 us, by 8 slots 6.9), beyond by 8, which leave no thread idle (8000: 11.8 us, by 32 slots 13.7).
+    if (head_dim == 128) return launch_form<T, 128, 32>(a, stream);
+    return a.n_tokens <= kFewTokens ? launch_form<T, 64, 32>(a, stream) : launch_form<T, 64, 8>(a, stream);
 }
 
 }  // namespace

@@ -201,3 +201,10 @@ def test_on_another_stream():
             ls.ls_rope(desc, late, k, pos, cs, late, k_out, stream=side)
         side.synchronize()
         close(late, want, bound, "q")
+
+
+@pytest.mark.parametrize("t", [2048, 2049, 2600])
+@pytest.mark.parametrize("dtype,heads,rotary,sections,interleaved", [
+    ("f16", (16, 4), 64, [32], False), ("bf16", (5, 5), 48, [8, 8, 8], True), ("f32", (33, 3), 32, [16], False)])
+def test_many_tokens_of_64(t, dtype, heads, rotary, sections, interleaved):
+    test_many_tokens(t, dtype, heads, 64, rotary, sections, interleaved)
