@@ -1368,42 +1368,97 @@ chunk_attn_kernel(ChunkArgs a)
     else if constexpr (BLOCKS) row_block<D, F16>(a, piece, g, smem);
 }
 
-// Joins the partial rows of the blocks that were cut: sum of O 2^((m - top) c) over that of l.
+// Joins the partial rows of the blocks that were cut: sum of O 2^((m - top) c) over that of l.  D / 4 threads pass a row's pieces, with
+// the loads of BATCH of them in flight; the many pieces of a few rows are dealt to all groups of the workgroup, which then join theirs
+// in LDS.  Bound by round trips to memory: entry, pieces, and out.
 constexpr int MERGE_THREADS = 256, MERGE_GROUPS = 1024;
+template <int D> __device__ __forceinline__ int merge_turns(int part_rows)  // of a block and KV head
+{
+    constexpr int GROUPS = MERGE_THREADS / (D / 4);
+    const int by_rows = (part_rows + GROUPS - 1) / GROUPS, few = part_rows < FEW ? part_rows : FEW;
+    return by_rows > few ? by_rows : few;
+}
 template <int D, bool F16>
 __global__ void __launch_bounds__(MERGE_THREADS)
 chunk_merge_kernel(ChunkArgs a)
 {
-    constexpr int TPR = D / 4, RPW = MERGE_THREADS / TPR;  // threads per row, rows per workgroup and turn
-    const int turns = (a.part_rows + RPW - 1) / RPW, all = *a.n_entries * a.n_kv_heads * turns;
+    constexpr int TPR = D / 4, GROUPS = MERGE_THREADS / TPR, BATCH = 8;
+    __shared__ float4 sums[MERGE_THREADS];
+    __shared__ float2 states[GROUPS];
+    const int turns = merge_turns<D>(a.part_rows), all = *a.n_entries * a.n_kv_heads * turns;
+    const int group = threadIdx.x / TPR, col = threadIdx.x % TPR * 4;
     for (int i = blockIdx.x; i < all; i += gridDim.x) {
-        const int block = i / turns;  // entry by KV head
+        const int block = i / turns, turn = i - block * turns;  // entry by KV head
         const Entry x = ((const Entry *)a.entries)[block];
-        const int r = (i - block * turns) * RPW + threadIdx.x / TPR, col = threadIdx.x % TPR * 4;
-        if (r >= x.rows) continue;
+        const bool few = x.rows <= FEW;  // a row a turn; else a group takes one
+        const int r = few ? turn : turn * GROUPS + group;
+        if (few ? turn >= x.rows : turn * GROUPS >= x.rows) continue;
         const int g = block % a.n_kv_heads;
-        const float2 *ml = part_state(a, x.slot, g) + r;
-        const float *rows = part_rows<D>(a, x.slot, g) + (int64_t)r * D + col;
-        float top = -INFINITY;
-        for (int k = 0; k < x.cut; ++k) top = fmaxf(top, ml[k * x.part].x);
+        float m = -INFINITY, l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        float l = 0.f;
-#pragma unroll 4
-        for (int k = 0; k < x.cut; ++k) {
-            const float2 s = ml[k * x.part];
-            const float4 v = *(const float4 *)(rows + (int64_t)k * x.part * D);
-            const float scale = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * a.scale_log2);  // (NaN stays NaN)
-            l += scale * s.y;
-            o.x += scale * v.x;
-            o.y += scale * v.y;
-            o.z += scale * v.z;
-            o.w += scale * v.w;
+        if (r < x.rows) {
+            const float2 *ml = part_state(a, x.slot, g) + r;
+            const float *rows = part_rows<D>(a, x.slot, g) + (int64_t)r * D + col;
+            for (int k0 = few ? group : 0; k0 < x.cut; k0 += few ? GROUPS * BATCH : BATCH) {
+                float2 s[BATCH];
+                float4 v[BATCH];
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    const int k = k0 + (few ? GROUPS : 1) * j;
+                    const int at = k < x.cut ? k : k0;
+                    s[j] = ml[at * x.part];
+                    v[j] = *(const float4 *)(rows + (int64_t)at * x.part * D);
+                    if (k >= x.cut) s[j].y = 0.f;
+                }
+                float top = m;
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) top = fmaxf(top, s[j].x);
+                const float old = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);  // (NaN stays NaN)
+                m = top;
+                l *= old;
+                o.x *= old, o.y *= old, o.z *= old, o.w *= old;
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    const float scale = s[j].y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s[j].x - top) * a.scale_log2);
+                    const bool none = k0 + (few ? GROUPS : 1) * j >= x.cut;
+                    l += scale * s[j].y;
+                    o.x += none ? 0.f : scale * v[j].x;
+                    o.y += none ? 0.f : scale * v[j].y;
+                    o.z += none ? 0.f : scale * v[j].z;
+                    o.w += none ? 0.f : scale * v[j].w;
+                }
+            }
         }
+        if (few) {  // (the same for the whole workgroup)
+            __syncthreads();  // the turn before is done with the sums
+            sums[threadIdx.x] = o;
+            if (col == 0) states[group] = make_float2(m, l);
+            __syncthreads();
+            if (group != 0) continue;
+            float top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, states[k].x);
+            m = top;
+            l = 0.f;
+            o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < GROUPS; ++k) {
+                const float2 s = states[k];
+                const float4 v = sums[k * TPR + threadIdx.x];
+                const float scale = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * a.scale_log2);
+                l += scale * s.y;
+                o.x += scale * v.x;
+                o.y += scale * v.y;
+                o.z += scale * v.z;
+                o.w += scale * v.w;
+            }
+        }
+        if (r >= x.rows) continue;
         const int row = x.row0 + r, token = (int)a.by_group.div((uint32_t)row), head = g * a.group + row - token * a.group;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         *(uint2 *)(a.out + (x.first + token) * a.o_s[0] + head * a.o_s[1] + col * 2) =
             make_uint2(pack16<F16>(o.x * inv, o.y * inv), pack16<F16>(o.z * inv, o.w * inv));
-        if (col == 0) a.lse[(int64_t)(x.first + token) * a.n_q_heads + head] = l == 0.f ? -INFINITY : (top * a.scale_log2 + log2f(l)) * kLn2;
+        if (col == 0) a.lse[(int64_t)(x.first + token) * a.n_q_heads + head] = l == 0.f ? -INFINITY : (m * a.scale_log2 + log2f(l)) * kLn2;
     }
 }
 
