@@ -59,9 +59,12 @@ constexpr float kLazy = 8.f;      // the reference exponent is raised when a sco
 template <bool F16> constexpr float kSumCap = F16 ? 0x1p15f : 0x1p40f;  // largest sum of a step's numerators without raising it
 
 template <int D> constexpr int kTileBytes = TK * D * 2;
-// the rings, a stage for the query rows that find no free one, page ids, a flag, times of the shares;  or two stages per wave, and (m, l) of the rows
-template <int D> constexpr int kLds = (2 * RS + 1) * kTileBytes<D> + kWaves<D> * 512 + 16 + 8 * 4;
-static_assert(2 * 8 <= 2 * RS && 8 * 32 * 8 <= kTileBytes<64>, "LDS of the few rows");
+// Few rows: two stages per wave, and (m, l) of the rows; at head_dim 64 four workgroups then share a compute unit.
+template <int D> constexpr int kLdsFew = 2 * kWaves<D> * kTileBytes<D> + kWaves<D> * FEW * 8;
+// Row blocks: the rings, a stage for the query rows that find no free one, page ids, a flag.  At the end of either the times of the shares.
+constexpr int kShares = 8;
+template <int D, bool BLOCKS> constexpr int kLds = (BLOCKS ? (2 * RS + 1) * kTileBytes<D> + kWaves<D> * 512 + 16 : kLdsFew<D>) + kShares * 4;
+static_assert(kLdsFew<128> < kLds<128, true> && kLdsFew<64> < kLds<64, true>, "LDS of the few rows");
 
 // Row r of a tile keeps its 16-byte chunk c at place c ^ swizzle(r).  Rows of 256 bytes (head_dim 128) all begin at the same bank,
 // rows of 128 at one of two, so that there pairs of rows go together.  (With the swizzles for 256 bytes half of the LDS cycles at
@@ -179,13 +182,12 @@ struct Piece {
 // The shares of the work above which blocks are cut.  sums(x, f): x[] as f adds them up for every request; most(f): over all requests; least(time): the candidate with the least time.
 // Three blocks for each compute unit and more even out by themselves; only a block beyond a unit's share is cut.  With fewer blocks
 // the least of some candidates' expected times is taken, in tiles: one round of pieces lasts as long as the longest; in several
-// the units end apart by some part of it, which the few rows' pieces, dealt last and cut small, fill up.  (Against the best of 90
-// pairs of shares in a simulation of 300 steps of the ranges that the performance cases draw from: 0.1 % longer, worst 23 %.
+// the units end apart by some part of it, which the few rows' pieces, dealt last and cut small, fill up.  (Against the best of 100
+// pairs of shares in a simulation of 300 steps of the ranges that the performance cases draw from: 0.2 % longer, worst 23 %.
 // Without the pairs that cut the few rows alone a step of two pieces of prompts and 18 single tokens took 15 % longer there.)
 constexpr float kPieceCost = 8.f;  // what a piece costs besides its tiles: its place, the first loads, the rows out
 constexpr float kMergeCost = 5.f, kMergeBlock = 18.f;  // the merge: its launch, and a partial block's way to memory and back
 constexpr float kUneven = 0.3f;
-constexpr int kShares = 8;
 constexpr float kNever = 1e9f;
 __device__ __forceinline__ Shares shares_of(int candidate, float mean)
 {
@@ -1359,7 +1361,7 @@ chunk_attn_kernel(ChunkArgs a)
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int i = (int)a.by_kv_heads.div(blockIdx.x), g = (int)blockIdx.x - i * a.n_kv_heads;
     const int lane = threadIdx.x & 63;
-    const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>, kWaves<D>, BLOCKS>(a, i, lane, (float *)(smem + kLds<D> - kShares * 4));
+    const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>, kWaves<D>, BLOCKS>(a, i, lane, (float *)(smem + kLds<D, BLOCKS> - kShares * 4));
     if (!piece.valid) return;
     if (!BLOCKS || piece.q.rows <= FEW) {
         if (piece.q.rows <= 16) few_rows<D, F16, 16>(a, piece, g, smem);
@@ -1466,12 +1468,12 @@ template <int D, bool F16, bool BLOCKS> hipError_t launch_form(const ChunkArgs &
 {
     auto kernel = chunk_attn_kernel<D, F16, BLOCKS>;
     static std::atomic<uint64_t> allowed{0};
-    if (const hipError_t e = allow_dynamic_lds((const void *)kernel, kLds<D>, allowed); e != hipSuccess) return e;
+    if (const hipError_t e = allow_dynamic_lds((const void *)kernel, kLds<D, BLOCKS>, allowed); e != hipSuccess) return e;
     if (a.list) {
         hipLaunchKernelGGL(chunk_list_kernel<kRows<D>>, dim3(1), dim3(LIST_THREADS), 0, stream, a);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(kWaves<D> * 64), kLds<D>, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(kWaves<D> * 64), (kLds<D, BLOCKS>), stream, a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || plan.slots == 0) return e;
     hipLaunchKernelGGL((chunk_merge_kernel<D, F16>), dim3(MERGE_GROUPS), dim3(MERGE_THREADS), 0, stream, a);
     return hipGetLastError();
@@ -1485,7 +1487,8 @@ ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units)
     const int64_t group = d.n_q_heads / d.n_kv_heads, most = d.max_new_len * group;
     const int64_t per_block = d.head_dim == 128 ? kRows<128> : kRows<64>;
     plan.blocks_possible = most > FEW;
-    // (at head_dim 64 two workgroups share a compute unit)
+    // At head_dim 64 two workgroups share a compute unit, of few rows alone four; counted as two they are cut less fine (one token after
+    // 30 thousand rows, 4 KV heads: 14.4 us, counted as four 19.3; 24 of 1 to 30 thousand: 77 and 76).
     plan.units = (d.head_dim == 128 ? 1 : 2) * compute_units / d.n_kv_heads;
     if (plan.units < 2) plan.units = 2;
     // blocks at most: those of the rows there are, and one more per request with any
