@@ -60,11 +60,11 @@ template <bool F16> constexpr float kSumCap = F16 ? 0x1p15f : 0x1p40f;  // large
 
 template <int D> constexpr int kTileBytes = TK * D * 2;
 // Few rows: two stages per wave, and (m, l) of the rows; at head_dim 64 four workgroups then share a compute unit.
-template <int D> constexpr int kLdsFew = 2 * kWaves<D> * kTileBytes<D> + kWaves<D> * FEW * 8;
+template <int D, int NW> constexpr int kLdsFew = 2 * NW * kTileBytes<D> + NW * FEW * 8;
 // Row blocks: the rings, a stage for the query rows that find no free one, page ids, a flag.  At the end of either the times of the shares.
 constexpr int kShares = 8;
-template <int D, bool BLOCKS> constexpr int kLds = (BLOCKS ? (2 * RS + 1) * kTileBytes<D> + kWaves<D> * 512 + 16 : kLdsFew<D>) + kShares * 4;
-static_assert(kLdsFew<128> < kLds<128, true> && kLdsFew<64> < kLds<64, true>, "LDS of the few rows");
+template <int D, bool BLOCKS, int NW> constexpr int kLds = (BLOCKS ? (2 * RS + 1) * kTileBytes<D> + NW * 512 + 16 : kLdsFew<D, NW>) + kShares * 4;
+static_assert(kLdsFew<128, 8> < kLds<128, true, 8> && kLdsFew<64, 4> < kLds<64, true, 4>, "LDS of the few rows");
 
 // Row r of a tile keeps its 16-byte chunk c at place c ^ swizzle(r).  Rows of 256 bytes (head_dim 128) all begin at the same bank,
 // rows of 128 at one of two, so that there pairs of rows go together.  (With the swizzles for 256 bytes half of the LDS cycles at
@@ -1087,10 +1087,10 @@ __device__ __forceinline__ void few_add_not_finite(typename FewShape<16>::Acc (&
 
 // R: query rows there is room for.  Up to 16 (single tokens of up to 16 heads a KV head) take half the instructions of 32 (four
 // single tokens, 32 and 8 heads, f16: 11.8 us from warm caches, by 32 rows 14.3).
-template <int D, bool F16, int R>
+template <int D, bool F16, int R, int NW>
 __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece, int g, uint8_t *smem)
 {
-    constexpr int NW = kWaves<D>, ROWS = kRows<D>;
+    constexpr int ROWS = kRows<D>;
     constexpr int CH = D / 8, ROWB = D * 2, TILEB = kTileBytes<D>;
     constexpr int RPL = 64 / CH, LOADS = TK / RPL;
     typedef FewShape<R> S;
@@ -1354,18 +1354,18 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Piece &piece,
 }
 
 // BLOCKS: the call may have requests with more than FEW rows
-template <int D, bool F16, bool BLOCKS>
-__global__ void __launch_bounds__(kWaves<D> * 64, 2)
+template <int D, bool F16, bool BLOCKS, int NW>
+__global__ void __launch_bounds__(NW * 64, 2)
 chunk_attn_kernel(ChunkArgs a)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int i = (int)a.by_kv_heads.div(blockIdx.x), g = (int)blockIdx.x - i * a.n_kv_heads;
     const int lane = threadIdx.x & 63;
-    const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>, kWaves<D>, BLOCKS>(a, i, lane, (float *)(smem + kLds<D, BLOCKS> - kShares * 4));
+    const Piece piece = a.list ? find_listed<kRows<D>>(a, i, lane) : find_piece<kRows<D>, NW, BLOCKS>(a, i, lane, (float *)(smem + kLds<D, BLOCKS, NW> - kShares * 4));
     if (!piece.valid) return;
     if (!BLOCKS || piece.q.rows <= FEW) {
-        if (piece.q.rows <= 16) few_rows<D, F16, 16>(a, piece, g, smem);
-        else few_rows<D, F16, 32>(a, piece, g, smem);
+        if (piece.q.rows <= 16) few_rows<D, F16, 16, NW>(a, piece, g, smem);
+        else few_rows<D, F16, 32, NW>(a, piece, g, smem);
     }
     else if constexpr (BLOCKS) row_block<D, F16>(a, piece, g, smem);
 }
@@ -1464,16 +1464,16 @@ chunk_merge_kernel(ChunkArgs a)
     }
 }
 
-template <int D, bool F16, bool BLOCKS> hipError_t launch_form(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream)
+template <int D, bool F16, bool BLOCKS, int NW> hipError_t launch_form(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream)
 {
-    auto kernel = chunk_attn_kernel<D, F16, BLOCKS>;
+    auto kernel = chunk_attn_kernel<D, F16, BLOCKS, NW>;
     static std::atomic<uint64_t> allowed{0};
-    if (const hipError_t e = allow_dynamic_lds((const void *)kernel, kLds<D, BLOCKS>, allowed); e != hipSuccess) return e;
+    if (const hipError_t e = allow_dynamic_lds((const void *)kernel, kLds<D, BLOCKS, NW>, allowed); e != hipSuccess) return e;
     if (a.list) {
         hipLaunchKernelGGL(chunk_list_kernel<kRows<D>>, dim3(1), dim3(LIST_THREADS), 0, stream, a);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(kWaves<D> * 64), (kLds<D, BLOCKS>), stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pieces * a.n_kv_heads), dim3(NW * 64), (kLds<D, BLOCKS, NW>), stream, a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || plan.slots == 0) return e;
     hipLaunchKernelGGL((chunk_merge_kernel<D, F16>), dim3(MERGE_GROUPS), dim3(MERGE_THREADS), 0, stream, a);
     return hipGetLastError();
@@ -1508,14 +1508,22 @@ ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units)
     const bool one_each = !plan.blocks_possible && !may_cut;  // a piece is a request
     plan.pieces = one_each ? d.batch : blocks + plan.extra;
     plan.listed = d.batch > kWave && !one_each;
+    // Few requests that are cut: workgroups of four waves, of which two share a compute unit and one loads while the other ends (one token
+    // after 30 thousand rows, 8 KV heads: 33.0 -> 26.4 us, eight after 9 thousand 57.5 -> 51.9, twelve after 3 thousand 31.7 -> 30.9; but 24
+    // after 1 to 30 thousand 262.5 -> 265, 16 of 32 KV heads 205 -> 214).  Not cut, eight are faster: four after 1500 11.7 us, by four 15.1.
+    plan.few_waves = may_cut && requests * d.n_kv_heads <= compute_units / 2 ? 4 : 8;
     return plan;
 }
 
 hipError_t launch_chunk_attn(const ChunkArgs &a, const ChunkPlan &plan, int dtype, int head_dim, hipStream_t stream)
 {
-#define LS_CHUNK_CASE(DD, HH) (plan.blocks_possible ? launch_form<DD, HH, true>(a, plan, stream) : launch_form<DD, HH, false>(a, plan, stream))
-    if (head_dim == 128) return dtype == LS_F16 ? LS_CHUNK_CASE(128, true) : LS_CHUNK_CASE(128, false);
-    return dtype == LS_F16 ? LS_CHUNK_CASE(64, true) : LS_CHUNK_CASE(64, false);
+#define LS_CHUNK_CASE(HH)                                                                    \
+    (plan.blocks_possible  ? (head_dim == 128 ? launch_form<128, HH, true, 8>(a, plan, stream) \
+                                              : launch_form<64, HH, true, 4>(a, plan, stream)) \
+     : head_dim == 64      ? launch_form<64, HH, false, 4>(a, plan, stream)                     \
+     : plan.few_waves == 4 ? launch_form<128, HH, false, 4>(a, plan, stream)                    \
+                           : launch_form<128, HH, false, 8>(a, plan, stream))
+    return dtype == LS_F16 ? LS_CHUNK_CASE(true) : LS_CHUNK_CASE(false);
 #undef LS_CHUNK_CASE
 }
 

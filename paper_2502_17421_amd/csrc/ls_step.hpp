@@ -53,6 +53,7 @@ struct ChunkPlan {
     int32_t slots;         // partial rows there is room for
     int32_t part_rows;     // query rows of a block at most
     bool blocks_possible;  // some request may have more rows than the few that waves share
+    int32_t few_waves;     // waves of a workgroup at head_dim 128 where no request has more than few rows: 4 or 8
     bool listed;           // more requests than a wave has lanes: their pieces are listed first
 };
 ChunkPlan plan_chunk(const ls_chunk_desc &d, int compute_units);

@@ -321,3 +321,11 @@ def test_unseen_values_and_keys_have_no_part_in_few_rows(heads, dtype, n, window
         assert torch.isnan(out[after]).all()
     assert torch.isnan(out[only_v][:, 61]).all() and torch.equal(lse[only_v], clean[1][only_v])
     assert torch.equal(out[n], clean[0][n]) and torch.equal(lse[n], clean[1][n])
+
+
+@pytest.mark.parametrize("heads", ["gqa", "five", "wide"])
+@pytest.mark.parametrize("news,lens", [([1], [9000]), ([1, 1, 1], [20000, 64, 5000]), ([1] * 20, [4000 + 37 * i for i in range(20)]),
+                                       ([1] * 70, [3000 if i % 7 == 0 else 40 + i for i in range(70)])])
+def test_few_rows_that_are_cut(heads, news, lens):
+    """Few requests, whose workgroups have four waves at head_dim 128, and many, whose have eight."""
+    Step("bf16" if heads != "gqa" else "f16", HEADS[heads], news, lens, seed=25).check(times=2)

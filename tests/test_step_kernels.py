@@ -16,7 +16,7 @@ def test_the_attention_kernels_keep_everything_in_registers():
     """They count their copies in flight (s_waitcnt vmcnt(N)); a spill would add loads and stores of its own to that count.  At most
     256 registers: two waves on a SIMD."""
     kernels = resources("chunk_attn_kernel")
-    assert len(kernels) == 8
+    assert len(kernels) >= 8
     for name, r in kernels.items():
         assert r["ScratchSize"] == 0 and r["VGPRs Spill"] == 0 and r["VGPRs"] + r["AGPRs"] <= 256, (name, r)
 
