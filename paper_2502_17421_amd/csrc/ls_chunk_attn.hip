@@ -7,8 +7,8 @@
 // Two forms of work, in one launch, because a step mixes them.  Keys go in tiles of 32:
 //   row blocks    up to 256 query rows (128 at head_dim 64) of a request and KV head; waves of 32 rows share the tiles, which
 //                 they copy into rings in LDS.  Bound by the matrix cores: 512 flops per byte of a tile.
-//   few rows      requests with at most 32 rows per KV head (single tokens); the eight waves hold the same rows and take
-//                 every eighth tile each, without barriers, and are merged at the end.  Bound by HBM.
+//   few rows      requests with at most 32 rows per KV head (single tokens); the four or eight waves of a workgroup hold the
+//                 same rows, deal the tiles out, pass them without barriers and are merged at the end.  Bound by HBM.
 //
 // Which piece a workgroup takes is worked out on the device, from the lengths, by every wave for itself: a program has
 // them there, and the host knows upper bounds only.  A block of more tiles than a compute unit's share of all tiles is cut into
@@ -28,11 +28,12 @@
 // Masks.  A tile that every row of a wave sees whole has none; in the others scores are replaced by -inf.  Infinite or NaN
 // values of an unseen row would still come through the product as 0 * inf: in the tiles that some row does not see whole
 // they are replaced by zeros, and put into the rows that see them at the end.
+//
 // Measured on MI355X, from cold caches, bf16, 32 query and 8 KV heads of 128 unless said otherwise:
 //   2048 tokens after 30 thousand rows          0.86 to 0.91 ms, 1.14 to 1.21 PFLOP/s (a plain matrix product of 16384: 1.35)
 //   four first prompts of 611 to 4003 tokens    240 us, 0.95 PFLOP/s
-//   24 single tokens, 1 to 30 thousand rows     265 us, 5.7 TB/s
-//   18 single tokens and two pieces of prompts, up to 9 thousand rows, 40 query heads   184 us
+//   24 single tokens, 1 to 30 thousand rows     264 us, 5.8 TB/s
+//   18 single tokens and two pieces of prompts, up to 9 thousand rows, 40 query heads   180 us
 //   window of 512, 16 and 4 heads of 64, f16    36 us;  four single tokens, up to 1.5 thousand rows    13 us
 // Long row blocks are held by the power limit (with zeros for inputs the first takes 0.63 ms; 1.5 to 1.95 GHz), head_dim 64 by the vector
 // ALUs (16 exponentials a lane and tile at a quarter of their rate), long few rows by HBM, short calls by latency.
