@@ -108,12 +108,17 @@ class PagedCache:
                                      ws)
 
     def commit(self, k_trees, v_trees, accept_path, accept_len):
-        """k_trees, v_trees: a tensor per layer.  The accepted rows go into the pages and count as cached."""
+        """k_trees, v_trees: a tensor per layer.  The accepted rows go into the pages and count as cached, as far as the pages reach that
+        the plan before gave the request: a request it refused commits nothing, a path beyond its pages ends with them.  err is then
+        1 (or what it was) for requests of which not all rows were committed."""
+        room = self.pages_held * self.page_size - self.kv_lens
+        fits = torch.where(self.err == 0, torch.minimum(accept_len, room), 0)
         for layer, (k_tree, v_tree) in enumerate(zip(k_trees, v_trees)):
             kp, vp = self.k_pages[layer], self.v_pages[layer]
             desc = ls.make_desc(k_tree, kp, vp, k_tree, v_tree, None, self.block_table.shape[1] * self.page_size)
-            ls.ls_kv_commit_paged(desc, k_tree, v_tree, accept_path, accept_len, self.kv_lens, kp, vp, self.block_table, self.page_size,
+            ls.ls_kv_commit_paged(desc, k_tree, v_tree, accept_path, fits, self.kv_lens, kp, vp, self.block_table, self.page_size,
                                   self._next_lens)
+        self.err.copy_(torch.maximum(self.err, self._next_lens - self.kv_lens < accept_len))
         self.kv_lens.copy_(self._next_lens)
 
 

@@ -1,0 +1,102 @@
+"""The state of paged_step.PagedCache on the CPU: plain stand-ins for the device calls, which write what those write."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_17421_amd import binding as ls
+from paper_2502_17421_amd import paged_step
+from step_reference import page_plan
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def plain_plan(desc, kv_lens, new_lens, pages_held, table, free, free_count, new_held, new_free_count, cu_new, total_lens, slots, positions,
+               err, stream=None, check=True):
+    want = page_plan(kv_lens.numpy(), new_lens.numpy(), pages_held.numpy(), table.numpy(), free.numpy(), int(free_count[0]), desc.page_size,
+                     desc.n_tokens)
+    outs = {"table": table, "free": free, "new_held": new_held, "cu": cu_new, "total": total_lens, "err": err}
+    if desc.n_tokens:
+        outs.update(slots=slots, positions=positions.view(-1))
+    for key, x in outs.items():
+        x.copy_(torch.from_numpy(want[key]))
+    new_free_count[0] = want["free_count"]
+    return 0
+
+
+def plain_commit(desc, k_tree, v_tree, accept_path, accept_len, prefix_lens, k_pages, v_pages, table, page_size, new_prefix_lens,
+                 err_flag=None, stream=None, check=True):
+    for b in range(k_tree.shape[0]):
+        n, had = max(0, int(accept_len[b])), int(prefix_lens[b])
+        n = min(n, table.shape[1] * page_size - had)
+        for j in range(n):
+            page, row, node = int(table[b, (had + j) // page_size]), (had + j) % page_size, int(accept_path[b, j])
+            k_pages[page, :, row], v_pages[page, :, row] = k_tree[b, :, node], v_tree[b, :, node]
+        new_prefix_lens[b] = had + n
+    return 0
+
+
+@pytest.fixture
+def plain_calls(monkeypatch):
+    monkeypatch.setattr(ls, "ls_page_plan", plain_plan)
+    monkeypatch.setattr(ls, "ls_kv_commit_paged", plain_commit)
+
+
+def filled_cache(lens, n_pages, page_size=16):
+    """Requests of these lengths, every row of the pool with values of its own."""
+    cache = paged_step.PagedCache(len(lens), 2, 2, 64, n_pages, page_size, 128, torch.float32, device="cpu")
+    for x in (cache.k_pages, cache.v_pages):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(1)))
+    cache.plan(ints(lens))
+    cache.keep_new()
+    assert cache.kv_lens.tolist() == lens
+    return cache
+
+
+def request_rows(cache, b, n):
+    pages = cache.block_table[b, :-(-n // cache.page_size)].long()
+    return [x[:, pages].transpose(1, 2).flatten(2, 3)[:, :, :n].clone() for x in (cache.k_pages, cache.v_pages)]
+
+
+def trees(batch, nodes):
+    gen = torch.Generator().manual_seed(2)
+    return [[torch.randn((batch, 2, nodes, 64), generator=gen) for _ in range(2)] for _ in range(2)]
+
+
+def test_a_refused_request_commits_nothing(plain_calls):
+    """Four pages: request 0 has room in its page, request 1 takes the last free one, none is left for request 2."""
+    cache = filled_cache([5, 16, 16], 4)
+    cache.plan(ints([4, 4, 4]))
+    assert cache.err.tolist() == [0, 0, 1] and cache.pages_held.tolist() == [1, 2, 1]
+    before = [request_rows(cache, b, n) for b, n in enumerate([5, 16, 16])]
+    path = ints([[0, 2, 3, 5, 0, 0]] * 3)
+    k_trees, v_trees = trees(3, 6)
+    cache.commit(k_trees, v_trees, path, ints([3, 2, 4]))
+    assert cache.kv_lens.tolist() == [8, 18, 16] and cache.err.tolist() == [0, 0, 1]
+    for b, (had, n) in enumerate(((5, 3), (16, 2), (16, 0))):
+        nodes = path[b, :n].long()
+        for was, now, tree in zip(before[b], request_rows(cache, b, had + n), (k_trees, v_trees)):
+            want = torch.cat([was, torch.stack([x[b][:, nodes] for x in tree])], 2)
+            assert torch.equal(now, want), b
+    cache.plan(ints([0, 0, 0]))  # the refused request is as it was: nothing is wrong with it
+    assert cache.err.tolist() == [0, 0, 0] and cache.kv_lens.tolist() == [8, 18, 16]
+
+
+def test_a_path_longer_than_planned_stays_in_its_pages(plain_calls):
+    """Rows for which no page was planned are not written; the request is flagged."""
+    cache = filled_cache([14, 30], 8)
+    cache.plan(ints([1, 1]))
+    assert cache.pages_held.tolist() == [1, 2]
+    free = cache.free_pages[:cache.free_count.item()].long()
+    before = [x[:, free].clone() for x in (cache.k_pages, cache.v_pages)]
+    path = ints([[0, 1, 2, 3, 4, 5]] * 2)
+    k_trees, v_trees = trees(2, 6)
+    cache.commit(k_trees, v_trees, path, ints([5, 2]))
+    assert cache.kv_lens.tolist() == [16, 32] and cache.err.tolist() == [1, 0]
+    for was, now in zip(before, (cache.k_pages, cache.v_pages)):
+        assert torch.equal(was, now[:, free])
+    for b in range(2):
+        rows = request_rows(cache, b, [16, 32][b])
+        for now, tree in zip(rows, (k_trees, v_trees)):
+            assert torch.equal(now[:, :, -2:], torch.stack([x[b][:, :2] for x in tree]))
