@@ -41,13 +41,15 @@ class PagedCache:
         self._next_held, self._next_free = ints(batch), ints(1)
         self._next_lens = ints(batch)
         self.slots = self.positions = None
-        self._workspaces = {}
+        self._buffers = {}
 
-    def _workspace(self, name, size):
-        ws = self._workspaces.get(name)
-        if ws is None or ws.numel() < size:
-            ws = self._workspaces[name] = torch.empty(size, dtype=torch.uint8, device=self.k_pages.device)
-        return ws
+    def _buffer(self, name, size, dtype=torch.uint8):
+        """`size` elements or more.  A recorded step goes on using the buffers it was recorded with, so one that a larger step outgrows is
+        kept (each is twice the one before, at least: together less than four times what the largest step takes)."""
+        kept = self._buffers.setdefault(name, [])
+        if not kept or kept[-1].numel() < size:
+            kept.append(torch.empty(max([size] + [2 * x.numel() for x in kept]), dtype=dtype, device=self.k_pages.device))
+        return kept[-1]
 
     # ---- the requests' lengths
 
@@ -58,9 +60,9 @@ class PagedCache:
     def plan(self, new_lens, n_tokens=0):
         """Pages for new_lens (int32 [batch], device) more rows of each request; with n_tokens, the packed tokens' slots and
         positions as well.  err says which requests were refused (they keep what they have)."""
-        if n_tokens and (self.slots is None or self.slots.shape[0] != n_tokens):
-            self.slots = torch.empty(n_tokens, dtype=torch.int32, device=new_lens.device)
-            self.positions = torch.empty((1, n_tokens), dtype=torch.int32, device=new_lens.device)
+        if n_tokens:
+            self.slots = self._buffer("slots", n_tokens, torch.int32)[:n_tokens]
+            self.positions = self._buffer("positions", n_tokens, torch.int32)[:n_tokens].view(1, n_tokens)
         ls.ls_page_plan(ls.make_page_desc(self.block_table, n_tokens, self.page_size, self.n_pages), self.kv_lens, new_lens,
                         self.pages_held, self.block_table, self.free_pages, self.free_count, self._next_held, self._next_free,
                         self.cu_new, self.total_lens, self.slots if n_tokens else None, self.positions if n_tokens else None,
@@ -86,7 +88,7 @@ class PagedCache:
         """max_new, max_kv: bounds, known to the host, of a request's new tokens and of its rows."""
         kp, vp = self.k_pages[layer], self.v_pages[layer]
         desc = ls.make_chunk_desc(q, kp, vp, self.block_table, out, max_new, max_kv, window)
-        ws = self._workspace("chunk", ls.ls_chunk_workspace_bytes(desc))
+        ws = self._buffer("chunk", ls.ls_chunk_workspace_bytes(desc))
         ls.ls_chunk_attn_paged(desc, q, kp, vp, self.block_table, self.cu_new, self.total_lens, out, lse, ws)
 
     # ---- speculation trees: q [batch, heads, nodes, head_dim], k and v [batch, kv heads, nodes, head_dim]
@@ -103,7 +105,7 @@ class PagedCache:
     def verify(self, layer, q, k_tree, v_tree, parents, out, lse, max_kv):
         kp, vp = self.k_pages[layer], self.v_pages[layer]
         desc = ls.make_desc(q, kp, vp, k_tree, v_tree, out, max_kv)
-        ws = self._workspace("tree", ls.ls_workspace_bytes(desc))
+        ws = self._buffer("tree", ls.ls_workspace_bytes(desc))
         ls.ls_hybrid_tree_attn_paged(desc, q, kp, vp, self.block_table, self.page_size, self.kv_lens, k_tree, v_tree, parents, out, lse,
                                      ws)
 

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2502_17421_amd import binding as ls
+from paper_2502_17421_amd import paged_step
 from test_gpu_paged_step import Run, ints
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +64,69 @@ def test_a_path_longer_than_planned():
         for b, had in enumerate((14, 30, 3, 0)):
             for now, was, tree in zip(run.cached(layer, b, lens[b]), run.rows[layer][b], trees):
                 assert torch.equal(now, torch.cat([was, tree[layer][b].cpu()[:, :lens[b] - had]], 1))
+
+
+def test_steps_of_other_sizes_between_replays():
+    """A recorded decoding step next to eager prompts, which need longer slots and a larger workspace, and other tensors that take up
+    what memory is free: after each replay state, rows and outputs are those of a side that records nothing, bit for bit."""
+    hq, hkv, d, dt = 8, 2, 128, torch.bfloat16
+    table = paged_step.rotary_table(8192, d)
+    gen = torch.Generator().manual_seed(5)
+
+    class Side:
+        def __init__(self):
+            self.cache = paged_step.PagedCache(3, 1, hkv, d, 1200, 16, 8192, dt)
+            self.sizes = {}
+
+        def step(self, t, max_new, max_kv):
+            c, (news, q, k, v, turned, out, lse) = self.cache, self.sizes[t]
+            c.plan(news, t)
+            c.write(0, q, k, v, table, turned)
+            c.attend(0, turned, out, lse, max_new, max_kv)
+            c.keep_new()
+
+        def fill(self, t, news, q, k, v):
+            if t not in self.sizes:
+                new = lambda x: torch.empty_like(x, device="cuda")  # noqa: E731
+                self.sizes[t] = (ints(news), new(q), new(k), new(v), new(q), new(q), torch.empty((t, hq), device="cuda"))
+            for x, value in zip(self.sizes[t], (torch.tensor(news, dtype=torch.int32), q, k, v)):
+                x.copy_(value)
+
+    sides = plain, recorded = Side(), Side()
+
+    def fill(t, news):
+        q, k, v = (torch.randn((t, h, d), generator=gen).to(dt) for h in (hq, hkv, hkv))
+        for side in sides:
+            side.fill(t, news, q, k, v)
+
+    def agree(t, what):
+        torch.cuda.synchronize()
+        for a, b in ((plain.sizes[t][5], recorded.sizes[t][5]), (plain.cache.k_pages, recorded.cache.k_pages),
+                     (plain.cache.v_pages, recorded.cache.v_pages)):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16)), what
+        assert torch.equal(plain.sizes[t][6].view(torch.int32), recorded.sizes[t][6].view(torch.int32)), what
+        for name in ("kv_lens", "pages_held", "free_count", "block_table", "free_pages", "cu_new", "err"):
+            assert torch.equal(getattr(plain.cache, name), getattr(recorded.cache, name)), (what, name)
+
+    for turn in range(2):
+        fill(3, [1, 1, 1])
+        for side in sides:
+            side.step(3, 1, 8192)
+        agree(3, turn)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded.step(3, 1, 8192)
+    others = []
+    for turn, (t, news, max_kv) in enumerate(((90, [60, 0, 30], 100), (2000, [3, 1997, 0], 6000), (40, [1, 38, 1], 7000), (5000, [2, 1998, 3000], 8192))):
+        fill(3, [1, 1, 1])
+        plain.step(3, 1, 8192)
+        graph.replay()
+        agree(3, ("replay", turn))
+        fill(t, news)
+        for side in sides:
+            side.step(t, max(news), max_kv)
+        agree(t, ("eager", turn))
+        others += [torch.full((n,), 0x7f, dtype=torch.uint8, device="cuda") for n in (512, 1024, 8192, 1 << 16, 1 << 20, 1 << 22) for _ in range(4)]
+        torch.cuda.synchronize()
+    for x in others:
+        assert (x == 0x7f).all(), "somebody else's memory"

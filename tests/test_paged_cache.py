@@ -1,5 +1,7 @@
 """The state of paged_step.PagedCache on the CPU: plain stand-ins for the device calls, which write what those write."""
-import numpy as np
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -100,3 +102,54 @@ def test_a_path_longer_than_planned_stays_in_its_pages(plain_calls):
         rows = request_rows(cache, b, [16, 32][b])
         for now, tree in zip(rows, (k_trees, v_trees)):
             assert torch.equal(now[:, :, -2:], torch.stack([x[b][:, :2] for x in tree]))
+
+
+class TestBuffersOfARecordedStep:
+    """A recorded step goes on using the addresses it was recorded with: what they point at has to stay the cache's."""
+
+    @pytest.fixture(autouse=True)
+    def seen_calls(self, plain_calls, monkeypatch):
+        self.used = []  # weak references to the storage of every buffer that a call was given
+
+        def plan(*args, **kwargs):
+            self.used += [weakref.ref(x.untyped_storage()) for x in args[11:13] if x is not None]
+            return plain_plan(*args, **kwargs)
+
+        def attend(desc, q, k, v, table, cu, lens, out, lse, workspace, stream=None, check=True):
+            assert workspace.numel() >= ls.ls_chunk_workspace_bytes(desc)
+            self.used.append(weakref.ref(workspace.untyped_storage()))
+            return 0
+
+        monkeypatch.setattr(ls, "ls_page_plan", plan)
+        monkeypatch.setattr(ls, "ls_chunk_attn_paged", attend)
+
+    def step(self, cache, news, max_kv):
+        t = sum(news)
+        cache.plan(ints(news), t)
+        slots = cache.slots
+        assert slots.shape == (t,) and cache.positions.shape == (1, t) and (slots >= 0).all()
+        q = torch.zeros((t, 8, 64), dtype=torch.bfloat16)
+        cache.attend(0, q, torch.empty_like(q), torch.empty((t, 8)), max(news), max_kv)
+        return slots
+
+    def test_they_stay(self):
+        cache = paged_step.PagedCache(2, 1, 2, 64, 4000, 16, 30000, torch.bfloat16, device="cpu")
+        self.step(cache, [1, 1], 40)
+        first = [ref() for ref in self.used]
+        assert len(first) == 3 and all(x is not None for x in first)
+        addresses = [x.data_ptr() for x in first]
+        del first
+        for news, max_kv in (([700, 30], 1000), ([3, 1], 30000), ([1, 1], 40), ([2000, 2000], 4000), ([1, 0], 40)):
+            self.step(cache, news, max_kv)
+            cache.plan(ints([4, 4]))
+        gc.collect()
+        assert [ref() is not None for ref in self.used] == [True] * len(self.used)
+        assert [ref().data_ptr() for ref in self.used[:3]] == addresses
+
+    def test_they_do_not_add_up(self):
+        """What is kept is less than four times what the largest step needs, however many sizes there were."""
+        cache = paged_step.PagedCache(1, 1, 2, 64, 4000, 16, 30000, torch.bfloat16, device="cpu")
+        for n in range(1, 3000, 7):
+            cache.plan(ints([n]), n)
+        storages = {ref().data_ptr(): ref().nbytes() for ref in self.used}
+        assert sum(storages.values()) < 4 * (2 * 4 * 3000)
