@@ -60,13 +60,15 @@ class PagedCache:
     def plan(self, new_lens, n_tokens=0):
         """Pages for new_lens (int32 [batch], device) more rows of each request; with n_tokens, the packed tokens' slots and
         positions as well.  err says which requests were refused (they keep what they have)."""
+        if new_lens.shape != self.kv_lens.shape or new_lens.dtype != torch.int32:
+            raise ValueError(f"new_lens: int32 [{self.batch}]")
+        self.slots = self.positions = None
         if n_tokens:
             self.slots = self._buffer("slots", n_tokens, torch.int32)[:n_tokens]
             self.positions = self._buffer("positions", n_tokens, torch.int32)[:n_tokens].view(1, n_tokens)
         ls.ls_page_plan(ls.make_page_desc(self.block_table, n_tokens, self.page_size, self.n_pages), self.kv_lens, new_lens,
                         self.pages_held, self.block_table, self.free_pages, self.free_count, self._next_held, self._next_free,
-                        self.cu_new, self.total_lens, self.slots if n_tokens else None, self.positions if n_tokens else None,
-                        self.err)
+                        self.cu_new, self.total_lens, self.slots, self.positions, self.err)
         # copied back, not exchanged: a recorded step finds its state in the same place at every replay
         self.pages_held.copy_(self._next_held)
         self.free_count.copy_(self._next_free)
@@ -81,11 +83,20 @@ class PagedCache:
         """positions: [axes, n_tokens] where they are not the rows' own (several axes, say)."""
         positions = self.positions if positions is None else positions
         kp, vp = self.k_pages[layer], self.v_pages[layer]
+        n = q.shape[0]
+        if self.slots is None or n > self.slots.shape[0] or n > positions.shape[1]:
+            raise ValueError("more tokens than were planned")
+        if q_out.shape != q.shape or not k.shape == v.shape == (n, kp.shape[1], kp.shape[3]):
+            raise ValueError("q_out: the shape of q; k and v: [tokens, kv heads, head_dim] for the same tokens")
+        if not q.dtype == k.dtype == v.dtype == q_out.dtype == kp.dtype:
+            raise ValueError("q, k, v and q_out: the type of the pages")
         desc = ls.make_rope_desc(q, k, v, q_out, None, kp, vp, positions, cos_sin, sections, interleaved)
         ls.ls_rope_store_paged(desc, q, k, v, positions, cos_sin, self.slots, q_out, kp, vp)
 
     def attend(self, layer, q, out, lse, max_new, max_kv, window=0):
         """max_new, max_kv: bounds, known to the host, of a request's new tokens and of its rows."""
+        if out.shape != q.shape or lse.shape != q.shape[:2] or not lse.is_contiguous():
+            raise ValueError("out: the shape of q; lse: [tokens, heads], contiguous")
         kp, vp = self.k_pages[layer], self.v_pages[layer]
         desc = ls.make_chunk_desc(q, kp, vp, self.block_table, out, max_new, max_kv, window)
         ws = self._buffer("chunk", ls.ls_chunk_workspace_bytes(desc))

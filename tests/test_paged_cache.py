@@ -153,3 +153,56 @@ class TestBuffersOfARecordedStep:
             cache.plan(ints([n]), n)
         storages = {ref().data_ptr(): ref().nbytes() for ref in self.used}
         assert sum(storages.values()) < 4 * (2 * 4 * 3000)
+
+
+class TestSizesThatDoNotFit:
+    """Tensors that hold fewer tokens than a call would read or write are refused before it is made."""
+
+    @pytest.fixture(autouse=True)
+    def calls(self, plain_calls, monkeypatch):
+        self.made = []
+        for name in ("ls_rope_store_paged", "ls_chunk_attn_paged"):
+            monkeypatch.setattr(ls, name, lambda *args, name=name, **kwargs: self.made.append(name))
+
+    def arguments(self, t, **sizes):
+        x = lambda name, *rest: torch.zeros((sizes.get(name, t), *rest))  # noqa: E731
+        return {"q": x("q", 4, 64), "k": x("k", 2, 64), "v": x("v", 2, 64), "cos_sin": torch.zeros((128, 64)), "q_out": x("q_out", 4, 64)}
+
+    def test_write(self):
+        cache = filled_cache([5, 9], 20)
+        cache.plan(ints([4, 2]), 8)  # two entries to spare
+        cache.write(0, **self.arguments(8))
+        cache.write(0, **self.arguments(6))
+        cache.write(0, **self.arguments(8), positions=torch.zeros((3, 8), dtype=torch.int32), sections=[8, 12, 12])
+        assert self.made == ["ls_rope_store_paged"] * 3
+        for sizes in ({"q": 9, "k": 9, "v": 9, "q_out": 9}, {"k": 7}, {"v": 7}, {"q_out": 7}, {"q": 7}):
+            with pytest.raises(ValueError):
+                cache.write(0, **self.arguments(8, **sizes))
+        with pytest.raises(ValueError):
+            cache.write(0, **self.arguments(8), positions=torch.zeros((3, 7), dtype=torch.int32), sections=[8, 12, 12])
+        for name, bad in (("k", torch.zeros((8, 3, 64))), ("v", torch.zeros((8, 2, 128))), ("q_out", torch.zeros((8, 2, 64))),
+                          ("k", torch.zeros((8, 2, 64), dtype=torch.bfloat16)), ("q", torch.zeros((8, 4, 64), dtype=torch.float64))):
+            with pytest.raises(ValueError):
+                cache.write(0, **{**self.arguments(8), name: bad})
+        cache.plan(ints([4, 4]))  # pages only: there are no slots
+        with pytest.raises(ValueError):
+            cache.write(0, **self.arguments(8))
+        assert self.made == ["ls_rope_store_paged"] * 3
+
+    def test_attend(self):
+        cache = filled_cache([5, 9], 20)
+        cache.plan(ints([4, 2]), 6)
+        q, lse = torch.zeros((6, 4, 64), dtype=torch.bfloat16), torch.zeros((6, 4))
+        cache.k_pages, cache.v_pages = cache.k_pages.bfloat16(), cache.v_pages.bfloat16()
+        cache.attend(0, q, torch.empty_like(q), lse, 4, 20)
+        for out, bad_lse in ((torch.empty_like(q)[:5], lse), (torch.empty_like(q), lse[:5]), (torch.empty_like(q), torch.zeros((4, 6)).T),
+                             (torch.empty_like(q)[:, :3], lse)):
+            with pytest.raises(ValueError):
+                cache.attend(0, q, out, bad_lse, 4, 20)
+        assert self.made == ["ls_chunk_attn_paged"]
+
+    def test_plan(self):
+        cache = filled_cache([5, 9], 20)
+        for new_lens in (ints([1]), ints([1, 1]).long(), ints([1, 1, 1])):
+            with pytest.raises(ValueError):
+                cache.plan(new_lens, 4)
