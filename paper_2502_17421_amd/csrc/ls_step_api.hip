@@ -224,7 +224,9 @@ int ls_chunk_attn_paged(const ls_chunk_desc *desc, const void *q, const void *k_
     bytes_of(desc->vc_stride, 2, a.vc_s);
     a.batch = desc->batch, a.n_tokens = desc->n_tokens, a.max_new_len = desc->max_new_len, a.max_kv_len = desc->max_kv_len;
     a.n_q_heads = desc->n_q_heads, a.n_kv_heads = desc->n_kv_heads, a.group = desc->n_q_heads / desc->n_kv_heads;
-    a.page_shift = log2_of(desc->page_size), a.bt_stride = desc->bt_stride, a.window = desc->window;
+    a.page_shift = log2_of(desc->page_size), a.bt_stride = desc->bt_stride;
+    // a window that no request outgrows is none; what is left is at most 2^30, and so place - window fits 32 bits for rows before the first
+    a.window = desc->window < desc->max_kv_len ? desc->window : 0;
     a.by_group = FastDiv::of(a.group), a.by_kv_heads = FastDiv::of(a.n_kv_heads);
     const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / std::sqrt((float)desc->head_dim);
     a.scale_log2 = scale * kLog2e;
