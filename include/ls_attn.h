@@ -451,8 +451,8 @@ typedef struct {
  *   positions       DEVICE int32[n_tokens], out: kv_lens[b] + index among the new ones; 0 past the last token
  *   err_flag        DEVICE int32[batch] or NULL, out: 0; 1 no page left; 2 lengths or pages_held
  *                   negative or beyond the table, pages that do not cover kv_lens, or tokens beyond
- *                   n_tokens.  A request with 1 or 2 keeps its pages; its tokens keep their place
- *                   in cu_new (a negative new_lens counts as 0).
+ *                   n_tokens (requests without new ones have none).  A request with 1 or 2 keeps its
+ *                   pages; its tokens keep their place in cu_new (a negative new_lens counts as 0).
  * bt_stride <= 2^18, bt_stride * page_size <= 2^31 - 1, n_tokens <= 2^30.
  * Outputs must not alias inputs (other workgroups still read those), block_table and free_pages
  * apart.  The same inputs give the same outputs, also when the call is repeated.  Page ids outside

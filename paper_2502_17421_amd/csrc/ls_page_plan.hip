@@ -104,7 +104,7 @@ page_plan_kernel(PagePlanArgs a)
         const int32_t n = cu[b];
         cu[b] = (int32_t)(at < INT32_MAX ? at : INT32_MAX);
         at += n;
-        if (!all_fit && at > a.n_tokens) {
+        if (!all_fit && n > 0 && at > a.n_tokens) {  // (a request without tokens has none that does not fit)
             state[b] = 2;
             taken[b] = given[b] = 0;
         }
