@@ -194,11 +194,25 @@ template <typename T> hipError_t launch_type(const RopeArgs &a, int head_dim, hi
 
 }  // namespace
 
-hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream)
+hipError_t launch_rope(const RopeArgs &all, int dtype, int head_dim, hipStream_t stream)
 {
-    if (dtype == LS_BF16) return launch_type<uint16_t>(a, head_dim, stream);
-    if (dtype == LS_F16) return launch_type<half_t>(a, head_dim, stream);
-    return launch_type<float>(a, head_dim, stream);
+    constexpr int32_t kMostTokens = 1 << 23;  // of a launch, which has fewer than 2^32 threads: up to 256 a token
+    for (int64_t done = 0; done < all.n_tokens; done += kMostTokens) {
+        RopeArgs a = all;
+        a.n_tokens = all.n_tokens - done < kMostTokens ? (int32_t)(all.n_tokens - done) : kMostTokens;
+        a.q += done * a.q_s[0];
+        a.q_out += done * a.qo_s[0];
+        a.positions += done;
+        if (a.k) a.k += done * a.k_s[0];
+        if (a.v) a.v += done * a.v_s[0];
+        if (a.slots) a.slots += done;
+        else if (a.k) a.k_out += done * a.ko_s[0];
+        const hipError_t e = dtype == LS_BF16  ? launch_type<uint16_t>(a, head_dim, stream)
+                             : dtype == LS_F16 ? launch_type<half_t>(a, head_dim, stream)
+                                               : launch_type<float>(a, head_dim, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace ls
