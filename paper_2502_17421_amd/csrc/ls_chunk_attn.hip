@@ -18,9 +18,12 @@
 //
 // Products (operand layouts: ls_mfma.hpp).  S^T = K Q^T, so a lane holds 16 scores of ONE query row, and the numerators go
 // from the accumulators to the operand of O^T = V^T P^T by a pack to 16 bits, which the row sum does not take part in.  Row blocks
-// round the numerators once, to nearest: on average as much as the result's own rounding (error 1.4 times that of a result rounded
-// once), and a second product would take half as long again where the matrix cores bind.  The few rows wait for memory: they
-// take what the rounding left along as a second operand, and err no more than the result's rounding.
+// round the numerators once, to nearest: on average as much as the result's own rounding (error 1.3 to 1.4 times that of a result
+// rounded once).  What that leaves as a second operand would end this (error 1.00 times), for half again as many matrix instructions and,
+// for every two scores, two subtractions and a pack on the vector ALUs, which bind at head_dim 64: there 2048 tokens after 30 thousand
+// rows took 427 us in place of 321, a window of 512 49 in place of 40, 19 prompts of 300 to 700 tokens 34 in place of 30.  At
+// head_dim 128, where the matrix cores bind, there are no registers for it (248 of 256 are taken; it spills).  The few rows wait for
+// memory: they take the second operand, and err no more than the result's rounding.
 //
 // Softmax state of a row: reference exponent m (raw scores) and l, the sum of exp2((s - m) c), c = scale * log2(e).  Any m
 // gives the same result, so the row blocks only raise it when a step's sum leaves the range of the operand type.
@@ -31,10 +34,12 @@
 //
 // Measured on MI355X, from cold caches, bf16, 32 query and 8 KV heads of 128 unless said otherwise:
 //   2048 tokens after 30 thousand rows          0.86 to 0.91 ms, 1.14 to 1.21 PFLOP/s (a plain matrix product of 16384: 1.35)
-//   four first prompts of 611 to 4003 tokens    240 us, 0.95 PFLOP/s
+//   four first prompts of 611 to 4003 tokens    237 us, 0.95 PFLOP/s
 //   24 single tokens, 1 to 30 thousand rows     264 us, 5.8 TB/s
 //   18 single tokens and two pieces of prompts, up to 9 thousand rows, 40 query heads   180 us
-//   window of 512, 16 and 4 heads of 64, f16    36 us;  four single tokens, up to 1.5 thousand rows    13 us
+//   window of 512, 16 and 4 heads of 64, f16    38 us;  four single tokens, up to 1.5 thousand rows    13 us
+//   16 and 4 heads of 64: 2048 tokens after 30 thousand rows 328 us, 0.79 PFLOP/s; four first prompts of 611 to 4003 tokens 86 to 90
+//   128 single tokens, 500 to 4000 rows         212 us, 5.6 TB/s (of which the list of the pieces 8); 100 to 900 rows, not cut    54
 // Long row blocks are held by the power limit (with zeros for inputs the first takes 0.63 ms; 1.5 to 1.95 GHz), head_dim 64 by the vector
 // ALUs (16 exponentials a lane and tile at a quarter of their rate), long few rows by HBM, short calls by latency.
 #include <type_traits>

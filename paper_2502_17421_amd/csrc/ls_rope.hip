@@ -186,8 +186,15 @@ template <typename T, int D, int SLOTS> hipError_t launch_form(const RopeArgs &a
 template <typename T> hipError_t launch_type(const RopeArgs &a, int head_dim, hipStream_t stream)
 {
     // head_dim 128: a token's heads go through one workgroup, so that its reads and writes are in one place (8000 tokens of 32 + 8 + 8
-    // heads: 16 threads a token 60 us, 32 48, 64 46, 128 43, 256 42).  head_dim 64, 16 + 4 + 4 heads: 32 slots up to 2048 tokens
-    // (2000: 5.6 us, by 8 slots 6.9), beyond by 8, which leave no thread idle (8000: 11.8 us, by 32 slots 13.7).
+    // heads: 16 threads a token 60 us, 32 48, 64 46, 128 43, 256 42).  head_dim 64: 32 slots up to 2048 tokens, beyond by 8, of which
+    // none is idle where heads come in eights.  us by 32 and by 8 slots, bf16, all of a head turned:
+    //   tokens               1500          2000          3000          4000          8000
+    //   16 + 4 + 4 heads   4.7   5.7     5.6   6.9     7.5   8.2     9.3   8.8    13.6  11.9
+    //   8 + 8 + 8          4.7   5.3     5.4   6.2     7.0   7.7     8.9   8.2    13.0  11.3
+    //   32 + 8 + 8         7.0  10.2     8.3  10.6    10.4  11.9    12.6  12.9    25.5  25.0
+    //   4 + 1 + 1          3.6   3.4     3.6   3.5     4.3   3.8     5.4   4.0     9.3   6.1
+    // (16 + 4 + 4 with three axes, neighbouring pairs, half a head: 6.9 and 7.3 at 2000, 9.4 and 8.9 at 3000.)  Where the two cross
+    // goes by the heads, from below 1500 to past 4500 tokens; just past 2048 the 8 slots cost 2.3 us more at most.
     if (head_dim == 128) return launch_form<T, 128, 32>(a, stream);
     return a.n_tokens <= kFewTokens ? launch_form<T, 64, 32>(a, stream) : launch_form<T, 64, 8>(a, stream);
 }

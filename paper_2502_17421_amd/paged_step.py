@@ -1,5 +1,6 @@
 """A serving program's state around the entry points of a paged cache: which request holds which pages, and the calls of a
-step in their order.  Argument marshalling and buffers only; all arithmetic runs in the HIP kernels.
+step in their order.  The operators run in the HIP kernels; what is left to torch is the bookkeeping of [batch] integers between them: the
+pages held and the free ones taken over after a plan, the lengths after a step, which rows of an accepted path have room.
 
 A step of new tokens (prompts, pieces of prompts, single tokens, any mixture of them):
 
@@ -16,7 +17,8 @@ A verification round over a speculation tree:
     cache.commit(layers, ...)                                       # ls_kv_commit_paged; surplus pages go back with the next plan
 
 Everything runs on torch's current stream and nothing waits for the GPU: lengths, tables and the number of free pages stay on
-the device, so a step can be recorded into a graph and replayed.  `python -m paper_2502_17421_amd.paged_step` runs three requests through both.
+the device, so a step can be recorded into a graph and replayed, other steps in between.
+`python -m paper_2502_17421_amd.paged_step` runs three requests through both.
 """
 from __future__ import annotations
 
