@@ -512,8 +512,8 @@ int ls_rope_store_paged(const ls_rope_desc *desc, const void *q, const void *k, 
 typedef struct {
     int32_t batch;           /* 1 .. LS_MAX_STEP_BATCH */
     int32_t n_tokens;        /* rows of q and out */
-    int32_t max_new_len;     /* host-known upper bounds of a request's new tokens and of its rows; the closer */
-    int32_t max_kv_len;      /*   they are the better the kernels and the cut are chosen */
+    int32_t max_new_len;     /* host-known upper bounds of a request's new tokens (at most n_tokens) and of its */
+    int32_t max_kv_len;      /*   rows; the closer they are the better the kernels and the cut are chosen */
     int32_t n_q_heads, n_kv_heads;
     int32_t head_dim;        /* 64 or 128 */
     int32_t dtype;           /* LS_BF16 or LS_F16 */
