@@ -550,6 +550,142 @@ int ls_chunk_attn_paged(const ls_chunk_desc *desc, const void *q, const void *k_
                         const int32_t *block_table, const int32_t *cu_new, const int32_t *kv_lens,
                         void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- sampled decoding: drafted trees against the target's distribution -------------------- */
+
+#define LS_MAX_VOCAB (1 << 19)
+
+typedef struct {
+    int32_t batch;             /* 1 .. 65535 */
+    int32_t n_tree;            /* 1 .. LS_MAX_TREE */
+    int32_t vocab;             /* 1 .. LS_MAX_VOCAB */
+    int32_t target_dtype;      /* ls_dtype of the target's logits */
+    int32_t draft_dtype;       /* ls_dtype of the draft's logits (any where there are none) */
+    int32_t with_replacement;  /* 0: the children of a node are different tokens, drawn one after the other without those before;
+                                  else independent draws, in which a token may come twice */
+    int64_t target_stride[2], draft_stride[2];  /* elements, (sequence, node); rows need no alignment but their elements' */
+} ls_sample_desc;
+
+/* Bytes of DEVICE workspace that ls_tree_accept_sampled needs (256-byte aligned). */
+int ls_sample_workspace_bytes(const ls_sample_desc *desc, size_t *bytes_out);
+
+/*
+ * Acceptance of the speculation tree at a temperature (Section 3.3: all candidate sequences are verified in one pass
+ * without altering the final result; Fig. 3 evaluates at T = 1): the tokens that it lets through are distributed as if the target had sampled
+ * them one by one.  Node 0 holds the last token already sampled and is always accepted.  At a node that the path has
+ * reached let p be the target's distribution after it, softmax(target_logits / temperature), and q the one its children were drawn
+ * from, softmax(draft_logits / draft_temperature).  The children are tried in the order of their indices: child i of
+ * token x is accepted if accept_uniforms[i] < p(x) / q(x), and the path goes on from it; if not, p becomes the normalised
+ * positive part of p - q and, without replacement, q loses x and is normalised again.  If no child is accepted (a leaf has none) the path ends,
+ * and the next token is drawn from p: the first one at which the cumulated probability passes sample_uniforms times their sum.
+ * Tokens that were chosen and not drawn (the likeliest ones of a beam) have q(x) = 1: accepted if accept_uniforms[i] < p(x), else p loses x.
+ * All arithmetic on probabilities is in 64 bits; a
+ * token whose weight is below 2^-1000 of the likeliest one's has none.  Only the rows of nodes that the path reaches are read, of a last node that is a leaf the target's alone.
+ *   parents, draft_tokens  DEVICE int32[batch, n_tree], as for ls_tree_accept_greedy; a child whose token is outside
+ *                     [0, vocab) is passed over
+ *   target_logits     DEVICE target_dtype [batch, n_tree, vocab].  -inf and NaN have no probability (the result of a filter, say); +inf counts
+ *                     as the largest finite number.
+ *   draft_logits      DEVICE draft_dtype [batch, n_tree, vocab], or NULL: all tokens were chosen.  Rows of leaves may be anything.
+ *   temperature       DEVICE float[batch]; 0: greedy, as ls_tree_accept_greedy with the likeliest tokens, the lowest of equal ones
+ *   draft_temperature DEVICE float[batch] or NULL: as temperature; 0: that sequence's tokens were chosen
+ *   accept_uniforms   DEVICE float[batch, n_tree] in [0, 1); node 0's is not used
+ *   sample_uniforms   DEVICE float[batch] in [0, 1)
+ *   accept_path, accept_len, next_token  out, as for ls_tree_accept_greedy
+ *   logprobs          DEVICE float[batch, n_tree] or NULL, out: entry j is the log probability under softmax(target_logits / temperature)
+ *                     (temperature 0: softmax(target_logits)) of the j-th new token, j < accept_len: the accepted nodes' after node 0, then next_token's;
+ *                     0 behind them
+ *   err_flag          DEVICE int32[batch] or NULL, out: the sum of 1: a parents entry was invalid (its node counts as a root);
+ *                     2: a temperature is negative, infinite or NaN (taken as 0); 4: nothing was left to draw from (logits without any
+ *                     probability, or drafted tokens that were not drawn from the distribution given): next_token is -1, its logprob -inf
+ *   workspace         DEVICE, >= ls_sample_workspace_bytes(); contents are scratch, nothing in it has to start at zero
+ * Outputs must not overlap inputs.
+ */
+int ls_tree_accept_sampled(const ls_sample_desc *desc, const int32_t *parents, const int32_t *draft_tokens,
+                           const void *target_logits, const void *draft_logits, const float *temperature,
+                           const float *draft_temperature, const float *accept_uniforms, const float *sample_uniforms,
+                           int32_t *accept_path, int32_t *accept_len, int32_t *next_token, float *logprobs, int32_t *err_flag,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- several continuations of a prompt: requests that share pages -------------------------- */
+
+/*
+ * Requests share pages by holding the same page in their block tables; the tables are all there is to it, no counts are kept.
+ * ls_page_fork lets a request go on from another one's rows: full pages are shared, and a page that is filled in part is
+ * held by one request alone, so that ls_page_plan, which appends rows to it, needs to know nothing of sharing.
+ * A request that shares pages must not shrink below its full pages by ls_page_plan (which would put pages on the stack that others hold): it ends, or goes back
+ * to fewer rows, by ls_page_fork.
+ */
+#define LS_MAX_POOL_PAGES (1 << 24)
+
+/* Bytes of DEVICE workspace of the two (256-byte aligned).  desc->n_tokens is not used. */
+int ls_page_fork_workspace_bytes(const ls_page_desc *desc, size_t *bytes_out);
+int ls_page_compact_workspace_bytes(const ls_page_desc *desc, size_t *bytes_out);
+
+/*
+ * New block tables in which request b goes on from the first keep_lens[b] rows of request sources[b] as it was before the call: a
+ * prompt that becomes several samples, the beams of a search dealt anew, requests that go back to earlier rows
+ * (sources[b] = b) or end (sources[b] = -1, none).  It holds ceil(keep / page_size) pages; pages reserved beyond are given back.
+ *
+ *   The keep / page_size full ones are its source's.  A last one filled in part (keep % page_size rows) stays with the lowest-numbered request that goes on
+ *   in it, unless some request holds it as a full page; every other one gets a page of its own, and copies[] says what to copy into it
+ *   (ls_page_copy).  Pages that no request holds any more go on top of the stack of free pages in the order
+ *   in which the requests held them before (request after request, entries ascending, a page at its first place); the pages for copies then come from the top, request
+ *   after request.  A request whose page is no longer there (the first one that does not fit, and every later
+ *   one that needs a page) is left with its full pages: new_kv_lens says how many rows these are.
+ *
+ *   sources          DEVICE int32[batch]: -1 or a request
+ *   keep_lens        DEVICE int32[batch], or NULL: all rows of the source, kv_lens[sources[b]]
+ *   kv_lens, pages_held, block_table, free_pages, free_count  as for ls_page_plan; block_table is only read
+ *   new_block_table  DEVICE int32[batch, bt_stride], out: the entries of pages held, nothing else
+ *   new_kv_lens, new_pages_held  DEVICE int32[batch], out    new_free_count  DEVICE int32[1], out
+ *   copies           DEVICE int32[batch, 4], 16-byte aligned, out: page copied from, page copied to, rows, request; n_copies[0] of them, in order of the requests
+ *   n_copies         DEVICE int32[1], out
+ *   err_flag         DEVICE int32[batch] or NULL, out: 0; 1 no page left; 2 sources[b] is no request, or keep_lens[b], kv_lens[b] or
+ *                    pages_held[b] is negative, beyond the table, or more than the pages hold.  A request with 2 keeps the pages it held,
+ *                    all of them, as full pages.
+ * Page ids outside the pool are taken over as they are, and neither given back nor copied.  A page must not be held twice
+ * by one request, nor lie on the stack while it is held.
+ * n_pages <= LS_MAX_POOL_PAGES; other limits as for ls_page_plan.  Outputs must not alias inputs, free_pages apart (its entries from free_count[0] on are written).
+ * The same inputs give the same outputs, also when the call is repeated.
+ */
+int ls_page_fork(const ls_page_desc *desc, const int32_t *sources, const int32_t *keep_lens, const int32_t *kv_lens,
+                 const int32_t *pages_held, const int32_t *block_table, int32_t *free_pages, const int32_t *free_count,
+                 int32_t *new_block_table, int32_t *new_kv_lens, int32_t *new_pages_held, int32_t *new_free_count,
+                 int32_t *copies, int32_t *n_copies, int32_t *err_flag, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The n pages in use (those that some request holds) to the front of the pool, so that the rest of it can be given up or used as one piece: pages
+ * below n stay, each one from n on, in ascending order, moves to the next page below n that is free.
+ *   new_block_table  DEVICE int32[batch, bt_stride], out: the entries of pages held, with the new page ids
+ *   free_pages       DEVICE int32[n_pages], out: n_pages - 1 down to n, the stack from its bottom up (pages that were neither held nor on the stack come back
+ *                    with it); the entries above are left as they are
+ *   new_free_count   DEVICE int32[1], out: n_pages - n
+ *   copies           DEVICE int32[n_pages / 2 + 1, 4], 16-byte aligned, out: page copied from, page copied to, page_size, -1; n_copies[0] of them.  Until ls_page_copy has run
+ *                    for every pool of the table, the rows are where the old table says.
+ * Page ids outside the pool are taken over as they are.  Limits and aliasing as for ls_page_fork; pages_held is clamped into [0, bt_stride].
+ */
+int ls_page_compact(const ls_page_desc *desc, const int32_t *pages_held, const int32_t *block_table, int32_t *new_block_table,
+                    int32_t *free_pages, int32_t *new_free_count, int32_t *copies, int32_t *n_copies,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+typedef struct {
+    int32_t n_layers, n_pages, n_kv_heads, page_size;
+    int32_t row_bytes;     /* of one head of one row: a multiple of 16, up to 65536 */
+    int32_t max_copies;    /* entries of copies, at least n_copies[0]; the closer it is the better the grid */
+    int64_t k_stride[4], v_stride[4];  /* BYTES, (layer, page, head, row in the page): multiples of 16 */
+} ls_copy_desc;
+
+/*
+ * Rows of pages to other pages of the same pool, K and V of all layers: rows 0 .. copies[i][2] - 1 of page copies[i][0] go to
+ * page copies[i][1], bit for bit, for i < n_copies[0].  What ls_page_fork and ls_page_compact ask for; any page_size.
+ *   copies    DEVICE int32[max_copies, 4], 16-byte aligned, read; entries with a page outside the pool, with the same page twice or without rows do nothing, rows
+ *             are clamped to page_size
+ *   n_copies  DEVICE int32[1], clamped into [0, max_copies]
+ *   k_pages   DEVICE, rows written in place      v_pages  DEVICE, alike, or NULL: one pool alone
+ * No page may be copied to twice, nor be copied from and to.
+ */
+int ls_page_copy(const ls_copy_desc *desc, const int32_t *copies, const int32_t *n_copies, void *k_pages, void *v_pages,
+                 void *stream);
+
 #ifdef __cplusplus
 }
 #endif

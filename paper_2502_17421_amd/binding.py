@@ -69,6 +69,20 @@ class ls_chunk_desc(ctypes.Structure):
         ("softmax_scale", _f32), ("q_stride", _i64 * 2), ("o_stride", _i64 * 2), ("kc_stride", _i64 * 3), ("vc_stride", _i64 * 3)]
 
 
+LS_MAX_VOCAB = 1 << 19
+LS_MAX_POOL_PAGES = 1 << 24
+
+
+class ls_sample_desc(ctypes.Structure):
+    _fields_ = [(name, _i32) for name in ("batch", "n_tree", "vocab", "target_dtype", "draft_dtype", "with_replacement")] + [
+        ("target_stride", _i64 * 2), ("draft_stride", _i64 * 2)]
+
+
+class ls_copy_desc(ctypes.Structure):
+    _fields_ = [(name, _i32) for name in ("n_layers", "n_pages", "n_kv_heads", "page_size", "row_bytes", "max_copies")] + [
+        ("k_stride", _i64 * 4), ("v_stride", _i64 * 4)]
+
+
 class LsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -119,15 +133,23 @@ def lib() -> ctypes.CDLL:
     L.ls_rope_store_paged.argtypes = [ctypes.POINTER(ls_rope_desc)] + [_vp] * 10
     L.ls_chunk_workspace_bytes.argtypes = [ctypes.POINTER(ls_chunk_desc), ctypes.POINTER(_sz)]
     L.ls_chunk_attn_paged.argtypes = [ctypes.POINTER(ls_chunk_desc)] + [_vp] * 9 + [_sz, _vp]
+    L.ls_sample_workspace_bytes.argtypes = [ctypes.POINTER(ls_sample_desc), ctypes.POINTER(_sz)]
+    L.ls_tree_accept_sampled.argtypes = [ctypes.POINTER(ls_sample_desc)] + [_vp] * 14 + [_sz, _vp]
+    for name in ("ls_page_fork_workspace_bytes", "ls_page_compact_workspace_bytes"):
+        getattr(L, name).argtypes = [ctypes.POINTER(ls_page_desc), ctypes.POINTER(_sz)]
+    L.ls_page_fork.argtypes = [ctypes.POINTER(ls_page_desc)] + [_vp] * 15 + [_sz, _vp]
+    L.ls_page_compact.argtypes = [ctypes.POINTER(ls_page_desc)] + [_vp] * 8 + [_sz, _vp]
+    L.ls_page_copy.argtypes = [ctypes.POINTER(ls_copy_desc)] + [_vp] * 5
     for name in ("ls_validate_desc", "ls_validate_parents_host", "ls_prefix_num_splits", "ls_prefix_split_len",
                  "ls_workspace_bytes", "ls_workspace_error", "ls_hybrid_tree_attn", "ls_hybrid_tree_attn_single",
                  "ls_hybrid_tree_attn_static",
                  "ls_cache_attn", "ls_build_tree_mask",
                  "ls_prefix_attn_splitkv", "ls_tree_attn_masked", "ls_lse_merge", "ls_tree_accept_greedy",
                  "ls_kv_commit", "ls_hybrid_tree_attn_paged", "ls_cache_attn_paged",
-                 "ls_kv_commit_paged", "ls_chunk_workspace_bytes", *_STEP_CALLS):
+                 "ls_kv_commit_paged", "ls_chunk_workspace_bytes", "ls_sample_workspace_bytes", "ls_page_fork_workspace_bytes",
+                 "ls_page_compact_workspace_bytes", *_STEP_CALLS, *_SAMPLING_CALLS):
         getattr(L, name).restype = ctypes.c_int
-    L.call = _device_calls(L, addresses=False, names=_DEVICE_CALLS + _STEP_CALLS)  # the functions below take tensors
+    L.call = _device_calls(L, addresses=False, names=_DEVICE_CALLS + _STEP_CALLS + _SAMPLING_CALLS)  # the functions below take tensors
     _lib = L
     return L
 
@@ -137,6 +159,7 @@ _DEVICE_CALLS = ("ls_hybrid_tree_attn", "ls_hybrid_tree_attn_single", "ls_hybrid
                  "ls_cache_attn_paged", "ls_build_tree_mask", "ls_prefix_attn_splitkv", "ls_tree_attn_masked",
                  "ls_lse_merge", "ls_tree_accept_greedy", "ls_kv_commit", "ls_kv_commit_paged")
 _STEP_CALLS = ("ls_page_plan", "ls_rope", "ls_rope_store_paged", "ls_chunk_attn_paged")  # a step of new tokens into a paged cache
+_SAMPLING_CALLS = ("ls_tree_accept_sampled", "ls_page_fork", "ls_page_compact", "ls_page_copy")  # sampled decoding
 
 
 def _call_module(L):
@@ -533,4 +556,95 @@ def ls_chunk_attn_paged(desc, q, k_pages, v_pages, block_table, cu_new, kv_lens,
                                         _bytes(workspace), _stream(stream))
     if check:
         _check(st, "ls_chunk_attn_paged")
+    return int(st)
+
+
+# ------------------------------------------------ sampled decoding, several continuations of a prompt ----
+
+def make_sample_desc(target_logits, draft_logits=None, with_replacement=False) -> ls_sample_desc:
+    """target_logits, draft_logits: [batch, n_tree, vocab], the last axis contiguous; draft_logits None: all tokens were chosen."""
+    d = ls_sample_desc()
+    d.batch, d.n_tree, d.vocab = target_logits.shape
+    assert draft_logits is None or draft_logits.shape == target_logits.shape
+    draft = draft_logits if draft_logits is not None else target_logits
+    d.target_dtype, d.draft_dtype, d.with_replacement = _dtype_code(target_logits), _dtype_code(draft), int(bool(with_replacement))
+    for field, ten in ((d.target_stride, target_logits), (d.draft_stride, draft)):
+        assert ten.stride(2) == 1 or ten.shape[2] == 1, "the vocabulary's axis must be contiguous"
+        field[0], field[1] = ten.stride(0), ten.stride(1)
+    return d
+
+
+def _workspace_bytes(name: str, desc) -> int:
+    n = _sz(0)
+    _check(getattr(lib(), name)(ctypes.byref(desc), ctypes.byref(n)), name)
+    return int(n.value)
+
+
+def ls_sample_workspace_bytes(desc: ls_sample_desc) -> int:
+    return _workspace_bytes("ls_sample_workspace_bytes", desc)
+
+
+def ls_tree_accept_sampled(desc, parents, draft_tokens, target_logits, draft_logits, temperature, draft_temperature, accept_uniforms,
+                           sample_uniforms, accept_path, accept_len, next_token, logprobs, err_flag, workspace, stream=None,
+                           check: bool = True) -> int:
+    """Device int32: parents, draft_tokens, accept_path [batch, n_tree], accept_len, next_token, err_flag [batch].  Device float32:
+    temperature, draft_temperature, sample_uniforms [batch], accept_uniforms, logprobs [batch, n_tree].  draft_logits, draft_temperature,
+    logprobs and err_flag may be None."""
+    st = lib().call.ls_tree_accept_sampled(desc, parents, draft_tokens, target_logits, draft_logits, temperature, draft_temperature,
+                                           accept_uniforms, sample_uniforms, accept_path, accept_len, next_token, logprobs, err_flag,
+                                           workspace, _bytes(workspace), _stream(stream))
+    if check:
+        _check(st, "ls_tree_accept_sampled")
+    return int(st)
+
+
+def ls_page_fork_workspace_bytes(desc: ls_page_desc) -> int:
+    return _workspace_bytes("ls_page_fork_workspace_bytes", desc)
+
+
+def ls_page_fork(desc, sources, keep_lens, kv_lens, pages_held, block_table, free_pages, free_count, new_block_table, new_kv_lens,
+                 new_pages_held, new_free_count, copies, n_copies, err_flag, workspace, stream=None, check: bool = True) -> int:
+    """All tensors device int32: [batch], block_table / new_block_table [batch, bt_stride], free_pages [n_pages], copies [batch, 4],
+    free_count / new_free_count / n_copies [1].  keep_lens and err_flag may be None."""
+    st = lib().call.ls_page_fork(desc, sources, keep_lens, kv_lens, pages_held, block_table, free_pages, free_count, new_block_table,
+                                 new_kv_lens, new_pages_held, new_free_count, copies, n_copies, err_flag, workspace, _bytes(workspace),
+                                 _stream(stream))
+    if check:
+        _check(st, "ls_page_fork")
+    return int(st)
+
+
+def ls_page_compact_workspace_bytes(desc: ls_page_desc) -> int:
+    return _workspace_bytes("ls_page_compact_workspace_bytes", desc)
+
+
+def ls_page_compact(desc, pages_held, block_table, new_block_table, free_pages, new_free_count, copies, n_copies, workspace, stream=None,
+                    check: bool = True) -> int:
+    """All tensors device int32: pages_held [batch], block_table / new_block_table [batch, bt_stride], free_pages [n_pages],
+    copies [n_pages // 2 + 1, 4], new_free_count / n_copies [1]."""
+    st = lib().call.ls_page_compact(desc, pages_held, block_table, new_block_table, free_pages, new_free_count, copies, n_copies,
+                                    workspace, _bytes(workspace), _stream(stream))
+    if check:
+        _check(st, "ls_page_compact")
+    return int(st)
+
+
+def make_copy_desc(k_pages, v_pages, max_copies: int) -> ls_copy_desc:
+    """k_pages, v_pages (or None): [layers, n_pages, n_kv_heads, page_size, head_dim] (any strides but the last)."""
+    d = ls_copy_desc()
+    d.n_layers, d.n_pages, d.n_kv_heads, d.page_size = k_pages.shape[:4]
+    d.row_bytes, d.max_copies = k_pages.shape[4] * k_pages.element_size(), int(max_copies)
+    assert v_pages is None or (v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype)
+    for field, ten in ((d.k_stride, k_pages), (d.v_stride, v_pages if v_pages is not None else k_pages)):
+        _put_strides(field, ten)
+        for i in range(4):
+            field[i] *= ten.element_size()
+    return d
+
+
+def ls_page_copy(desc, copies, n_copies, k_pages, v_pages, stream=None, check: bool = True) -> int:
+    """copies: device int32 [max_copies, 4]; n_copies: device int32 [1]."""
+    st = lib().call.ls_page_copy(desc, copies, n_copies, k_pages, v_pages, _stream(stream))
+    if check:
+        _check(st, "ls_page_copy")
     return int(st)

@@ -1,0 +1,59 @@
+// What the host side and the kernels of sampled decoding share: acceptance of drafted trees by rejection, forks and
+// compaction of block tables, page copies.
+#pragma once
+
+#include "ls_internal.hpp"
+
+namespace ls {
+
+// Strides in elements, (sequence, node).
+struct SampleArgs {
+    const int32_t *parents, *draft_tokens;
+    const void *target, *draft;  // draft == nullptr: all tokens were chosen
+    const float *temperature, *draft_temperature, *accept_uniforms, *sample_uniforms;
+    int32_t *path, *len, *next, *err_flag;
+    float *logprobs;
+    int64_t t_stride[2], d_stride[2];
+    int32_t batch, n_tree, vocab, with_replacement;
+    int32_t slices;  // pieces of the vocabulary
+};
+constexpr int kSampleThreads = 512;
+constexpr int kSampleSlice = kSampleThreads * 16;  // entries of a piece
+constexpr int kSampleSlices = 64;                  // at most
+static_assert(kSampleSlice * kSampleSlices == LS_MAX_VOCAB, "every vocabulary fits");
+hipError_t launch_tree_sample(const SampleArgs &a, int target_dtype, int draft_dtype, hipStream_t stream);
+
+// holder[page]: what the new tables hold it for: kNobody, kFull (some request, as a full page), or the lowest request that goes on in it.
+// first[page]: the lowest request that held it.  given: the pages that request b gives back, from b * bt_stride on, and their number.
+constexpr int32_t kNobody = INT32_MAX, kFull = -1;
+struct ForkArgs {
+    const int32_t *sources, *keep_lens, *kv_lens, *pages_held, *block_table, *free_count;
+    int32_t *free_pages, *new_block_table, *new_kv_lens, *new_pages_held, *new_free_count, *n_copies, *err_flag;
+    int4 *copies;
+    int32_t *holder, *first, *given, *n_given, *wants;
+    int32_t batch, page_shift, n_pages, bt_stride;
+};
+hipError_t launch_page_fork(const ForkArgs &a, hipStream_t stream);
+
+// used: a bit per page; before[word]: pages in use before the 64 of a word; head: their number, and those of them below it.
+struct CompactArgs {
+    const int32_t *pages_held, *block_table;
+    int32_t *new_block_table, *free_pages, *new_free_count, *n_copies;
+    int4 *copies;
+    uint64_t *used;
+    int32_t *before, *head;
+    int32_t batch, page_size, n_pages, bt_stride;
+};
+hipError_t launch_page_compact(const CompactArgs &a, hipStream_t stream);
+
+// Strides in bytes, (layer, page, head, row).
+struct PageCopyArgs {
+    const int4 *copies;
+    const int32_t *n_copies;
+    uint8_t *k, *v;
+    int64_t k_s[4], v_s[4];
+    int32_t n_layers, n_pages, n_kv_heads, page_size, row_bytes, max_copies;
+};
+hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream);
+
+}  // namespace ls

@@ -33,6 +33,8 @@ bool convert(PyObject *obj, const ls_desc *&value, bool) { return descriptor(obj
 bool convert(PyObject *obj, const ls_page_desc *&value, bool) { return descriptor(obj, value, "expected an ls_page_desc"); }
 bool convert(PyObject *obj, const ls_rope_desc *&value, bool) { return descriptor(obj, value, "expected an ls_rope_desc"); }
 bool convert(PyObject *obj, const ls_chunk_desc *&value, bool) { return descriptor(obj, value, "expected an ls_chunk_desc"); }
+bool convert(PyObject *obj, const ls_sample_desc *&value, bool) { return descriptor(obj, value, "expected an ls_sample_desc"); }
+bool convert(PyObject *obj, const ls_copy_desc *&value, bool) { return descriptor(obj, value, "expected an ls_copy_desc"); }
 
 bool integer(PyObject *obj, unsigned long long &value)  // wraps around like a C conversion
 {
@@ -111,7 +113,8 @@ const Entry kEntries[] = {
     LS_ENTRY(ls_cache_attn), LS_ENTRY(ls_cache_attn_paged), LS_ENTRY(ls_build_tree_mask), LS_ENTRY(ls_prefix_attn_splitkv),
     LS_ENTRY(ls_tree_attn_masked), LS_ENTRY(ls_lse_merge), LS_ENTRY(ls_tree_accept_greedy), LS_ENTRY(ls_kv_commit),
     LS_ENTRY(ls_kv_commit_paged), LS_ENTRY(ls_page_plan), LS_ENTRY(ls_rope), LS_ENTRY(ls_rope_store_paged),
-    LS_ENTRY(ls_chunk_attn_paged),
+    LS_ENTRY(ls_chunk_attn_paged), LS_ENTRY(ls_tree_accept_sampled), LS_ENTRY(ls_page_fork), LS_ENTRY(ls_page_compact),
+    LS_ENTRY(ls_page_copy),
 };
 
 struct Caller {
