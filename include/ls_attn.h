@@ -220,7 +220,7 @@ int ls_hybrid_tree_attn_static(const ls_desc *desc, const void *q,
  *     block) triples run in two launches, the second one with the tree attention and the merge;
  *     f32 problems run as in ls_hybrid_tree_attn.
  *   - ls_set_single_launch_polls(n) sets the number of polls (about half a microsecond
- *     apart) for later calls of this process: 0 makes every launch the nobody-waits form,
+ *     apart) for later calls of this process, also of ls_tree_accept_sampled: 0 makes every launch the nobody-waits form,
  *     a negative n restores the default (about 20 ms); n above 2^24 is LS_ERR_SHAPE.  A wait
  *     that runs out costs time, never correctness.
  *   - On MI355X this form was slower than the two launches of ls_hybrid_tree_attn on every
@@ -579,7 +579,9 @@ int ls_sample_workspace_bytes(const ls_sample_desc *desc, size_t *bytes_out);
  * and the next token is drawn from p: the first one at which the cumulated probability passes sample_uniforms times their sum.
  * Tokens that were chosen and not drawn (the likeliest ones of a beam) have q(x) = 1: accepted if accept_uniforms[i] < p(x), else p loses x.
  * All arithmetic on probabilities is in 64 bits; a
- * token whose weight is below 2^-1000 of the likeliest one's has none.  Only the rows of nodes that the path reaches are read, of a last node that is a leaf the target's alone.
+ * token whose weight is below 2^-1074 of the likeliest one's has none.  Only the rows of nodes that the path reaches are read, of a last node that is a leaf the target's alone.
+ * A sequence's vocabulary is dealt to several workgroups, which wait for each other's sums, a bounded number of polls
+ * (ls_set_single_launch_polls); one that waits longer walks its tree alone.  The results have the same bits either way.
  *   parents, draft_tokens  DEVICE int32[batch, n_tree], as for ls_tree_accept_greedy; a child whose token is outside
  *                     [0, vocab) is passed over
  *   target_logits     DEVICE target_dtype [batch, n_tree, vocab].  -inf and NaN have no probability (the result of a filter, say); +inf counts

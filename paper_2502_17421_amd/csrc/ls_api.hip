@@ -120,6 +120,8 @@ Workspace layout(const ls_desc &d, const SplitPlan &plan)
 
 }  // namespace
 
+int32_t single_launch_polls() { return g_spin_polls; }
+
 namespace {
 
 constexpr int kMaxDevices = 64;

@@ -155,6 +155,9 @@ struct WholeCall {
     int32_t in_parts;             // rows leave as parts, also those of a single split
 };
 
+// What ls_set_single_launch_polls has set; negative: the default of each entry point.
+int32_t single_launch_polls();
+
 // Compute units of the current device.
 inline int compute_units()
 {

@@ -15,12 +15,16 @@ struct SampleArgs {
     float *logprobs;
     int64_t t_stride[2], d_stride[2];
     int32_t batch, n_tree, vocab, with_replacement;
-    int32_t slices;  // pieces of the vocabulary
+    int32_t slice, slices;  // entries of a slice of the vocabulary, and their number
+    int32_t spin_limit;     // polls before a workgroup gives up on its group
+    uint64_t *records;
 };
 constexpr int kSampleThreads = 512;
-constexpr int kSampleSlice = kSampleThreads * 16;  // entries of a piece
-constexpr int kSampleSlices = 64;                  // at most
-static_assert(kSampleSlice * kSampleSlices == LS_MAX_VOCAB, "every vocabulary fits");
+constexpr int kSampleSlices = 64;  // at most
+static_assert(kSampleThreads * 16 * kSampleSlices == LS_MAX_VOCAB, "every vocabulary fits");
+inline int sample_slice(int vocab) { return vocab <= kSampleThreads * 8 * kSampleSlices ? kSampleThreads * 8 : kSampleThreads * 16; }
+// A state word and two records a slice, of 64 bytes each, per sequence; none where a sequence has one slice
+inline size_t sample_record_bytes(int batch, int slices) { return slices > 1 ? (size_t)batch * (2 * slices + 1) * 64 : 0; }
 hipError_t launch_tree_sample(const SampleArgs &a, int target_dtype, int draft_dtype, hipStream_t stream);
 
 // holder[page]: what the new tables hold it for: kNobody, kFull (some request, as a full page), or the lowest request that goes on in it.

@@ -5,6 +5,8 @@ namespace ls {
 
 namespace {
 
+constexpr int kDefaultSamplePolls = 20000;  // about 20 ms
+
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool known(int dtype) { return dtype == LS_BF16 || dtype == LS_F16 || dtype == LS_F32; }
 inline size_t up(size_t v) { return (v + 255) / 256 * 256; }
@@ -24,7 +26,17 @@ int validate(const ls_sample_desc *d)
     return LS_OK;
 }
 
-size_t sample_bytes(const ls_sample_desc &) { return 256; }
+int slices_of(const ls_sample_desc &d)
+{
+    const int slice = sample_slice(d.vocab);
+    return (d.vocab + slice - 1) / slice;
+}
+
+size_t sample_bytes(const ls_sample_desc &d)
+{
+    const size_t n = up(sample_record_bytes(d.batch, slices_of(d)));
+    return n ? n : 256;
+}
 
 int validate(const ls_page_desc *d)
 {
@@ -119,7 +131,9 @@ int ls_tree_accept_sampled(const ls_sample_desc *desc, const int32_t *parents, c
     a.path = accept_path, a.len = accept_len, a.next = next_token, a.logprobs = logprobs, a.err_flag = err_flag;
     for (int i = 0; i < 2; ++i) a.t_stride[i] = desc->target_stride[i], a.d_stride[i] = desc->draft_stride[i];
     a.batch = desc->batch, a.n_tree = desc->n_tree, a.vocab = desc->vocab, a.with_replacement = desc->with_replacement != 0;
-    a.slices = (desc->vocab + kSampleSlice - 1) / kSampleSlice;
+    a.slice = sample_slice(desc->vocab), a.slices = slices_of(*desc);
+    a.records = (uint64_t *)workspace;
+    a.spin_limit = single_launch_polls() < 0 ? kDefaultSamplePolls : single_launch_polls();
     return launch_tree_sample(a, desc->target_dtype, desc->draft_dtype, (hipStream_t)stream) == hipSuccess ? LS_OK : LS_ERR_HIP;
 }
 

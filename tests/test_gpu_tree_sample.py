@@ -314,3 +314,30 @@ def test_the_tokens_are_distributed_as_the_targets(with_replacement):
     p = torch.softmax(target.double(), 0)
     share = torch.bincount(first.long(), minlength=v).double() / n
     assert ((share - p).abs() <= 5 * (p * (1 - p) / n).sqrt()).all(), (share, p)
+
+
+@pytest.fixture
+def nobody_waits():
+    ls.ls_set_single_launch_polls(0)
+    yield
+    ls.ls_set_single_launch_polls(-1)
+
+
+@pytest.mark.parametrize("draft,with_replacement", [("bf16", False), ("f32", True), (None, False)])
+def test_walks_alone_give_the_same_bits(nobody_waits, draft, with_replacement):
+    """Workgroups that give up on their group at once: one of them does all of the sequence, with the same sums."""
+    c = Case(91, 9, 33, 50021, draft=draft, with_replacement=with_replacement, temperature=[0.0] + [0.8] * 8)
+    alone = {k: v.clone() for k, v in c.run().items()}
+    c.check()
+    ls.ls_set_single_launch_polls(-1)
+    assert all(torch.equal(v, alone[k]) for k, v in c.run().items())
+
+
+@pytest.mark.parametrize("polls", [1, 2, 3, 5, 9])
+def test_walks_given_up_on_the_way(nobody_waits, polls):
+    """Few polls: some groups get to the end, some do not, and both may write."""
+    ls.ls_set_single_launch_polls(polls)
+    c = Case(93, 60, 9, 30011, on_path=0.9)
+    for _ in range(3):
+        c.run()
+        c.check()
