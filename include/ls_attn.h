@@ -585,7 +585,7 @@ int ls_sample_workspace_bytes(const ls_sample_desc *desc, size_t *bytes_out);
  *   parents, draft_tokens  DEVICE int32[batch, n_tree], as for ls_tree_accept_greedy; a child whose token is outside
  *                     [0, vocab) is passed over
  *   target_logits     DEVICE target_dtype [batch, n_tree, vocab].  -inf and NaN have no probability (the result of a filter, say); +inf counts
- *                     as the largest finite number.
+ *                     as the largest finite number of the type.
  *   draft_logits      DEVICE draft_dtype [batch, n_tree, vocab], or NULL: all tokens were chosen.  Rows of leaves may be anything.
  *   temperature       DEVICE float[batch]; 0: greedy, as ls_tree_accept_greedy with the likeliest tokens, the lowest of equal ones
  *   draft_temperature DEVICE float[batch] or NULL: as temperature; 0: that sequence's tokens were chosen

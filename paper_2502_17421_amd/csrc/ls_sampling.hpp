@@ -21,8 +21,16 @@ struct SampleArgs {
 };
 constexpr int kSampleThreads = 512;
 constexpr int kSampleSlices = 64;  // at most
-static_assert(kSampleThreads * 16 * kSampleSlices == LS_MAX_VOCAB, "every vocabulary fits");
-inline int sample_slice(int vocab) { return vocab <= kSampleThreads * 8 * kSampleSlices ? kSampleThreads * 8 : kSampleThreads * 16; }
+static_assert(kSampleThreads * 32 * kSampleSlices >= LS_MAX_VOCAB, "every vocabulary fits");
+// 8, 16 or 32 entries a thread: as few as the card has room for, two workgroups a compute unit
+inline int sample_slice(int batch, int vocab, int compute_units)
+{
+    for (int slice = kSampleThreads * 8; slice < kSampleThreads * 32; slice *= 2) {
+        const int slices = (vocab + slice - 1) / slice;
+        if (slices <= kSampleSlices && (slices == 1 || (int64_t)batch * slices <= 2 * compute_units)) return slice;
+    }
+    return kSampleThreads * 32;
+}
 // A state word and two records a slice, of 64 bytes each, per sequence; none where a sequence has one slice
 inline size_t sample_record_bytes(int batch, int slices) { return slices > 1 ? (size_t)batch * (2 * slices + 1) * 64 : 0; }
 hipError_t launch_tree_sample(const SampleArgs &a, int target_dtype, int draft_dtype, hipStream_t stream);

@@ -28,7 +28,7 @@ int validate(const ls_sample_desc *d)
 
 int slices_of(const ls_sample_desc &d)
 {
-    const int slice = sample_slice(d.vocab);
+    const int slice = sample_slice(d.batch, d.vocab, compute_units());
     return (d.vocab + slice - 1) / slice;
 }
 
@@ -131,7 +131,7 @@ int ls_tree_accept_sampled(const ls_sample_desc *desc, const int32_t *parents, c
     a.path = accept_path, a.len = accept_len, a.next = next_token, a.logprobs = logprobs, a.err_flag = err_flag;
     for (int i = 0; i < 2; ++i) a.t_stride[i] = desc->target_stride[i], a.d_stride[i] = desc->draft_stride[i];
     a.batch = desc->batch, a.n_tree = desc->n_tree, a.vocab = desc->vocab, a.with_replacement = desc->with_replacement != 0;
-    a.slice = sample_slice(desc->vocab), a.slices = slices_of(*desc);
+    a.slice = sample_slice(desc->batch, desc->vocab, compute_units()), a.slices = slices_of(*desc);
     a.records = (uint64_t *)workspace;
     a.spin_limit = single_launch_polls() < 0 ? kDefaultSamplePolls : single_launch_polls();
     return launch_tree_sample(a, desc->target_dtype, desc->draft_dtype, (hipStream_t)stream) == hipSuccess ? LS_OK : LS_ERR_HIP;

@@ -33,49 +33,85 @@ constexpr int WAVES = NT / kWave;
 constexpr int kNone = INT32_MAX;
 template <int N> using Const = std::integral_constant<int, N>;
 
-// 2^y for y <= 0, to 1e-14 of its value: the Taylor series of exp(f ln 2), |f| <= 1/2, whose first term left out is
-// (ln 2 / 2)^12 / 12! = 6e-15.
+// 2^y for y <= 0, to 4e-14 of its value: y = n + f, |f| <= 1/2, and 2^f = 1 + f g(f) with the polynomial g of degree 8 that meets
+// (2^f - 1) / f at the zeros of the Chebyshev polynomial of degree 9.  Less than 2^-1074, and NaN, give 0.
 __device__ __forceinline__ double exp2_of(double y)
 {
-    y = y > -1100.0 ? y : -1100.0;  // 0 after the last step
+    y = __builtin_fmax(y, -1100.0);
     const double n = __builtin_rint(y), f = y - n;
-    double r = 4.4455382718708116e-10;   // ln2^11 / 11!
-    r = __builtin_fma(r, f, 7.0549116208011233e-09);
-    r = __builtin_fma(r, f, 1.0178086009239699e-07);
-    r = __builtin_fma(r, f, 1.3215486790144309e-06);
-    r = __builtin_fma(r, f, 1.5252733804059841e-05);
-    r = __builtin_fma(r, f, 1.5403530393381610e-04);
-    r = __builtin_fma(r, f, 1.3333558146428443e-03);
-    r = __builtin_fma(r, f, 9.6181291076284772e-03);
-    r = __builtin_fma(r, f, 5.5504108664821580e-02);
-    r = __builtin_fma(r, f, 2.4022650695910072e-01);
-    r = __builtin_fma(r, f, 6.9314718055994531e-01);
+    double r = 1.0203121047189341e-07;
+    r = __builtin_fma(r, f, 1.3255224879317324e-06);
+    r = __builtin_fma(r, f, 1.525268684635191e-05);
+    r = __builtin_fma(r, f, 1.540345585244999e-04);
+    r = __builtin_fma(r, f, 1.3333558179042969e-03);
+    r = __builtin_fma(r, f, 9.618129159402565e-03);
+    r = __builtin_fma(r, f, 5.5504108664760424e-02);
+    r = __builtin_fma(r, f, 2.402265069581299e-01);
+    r = __builtin_fma(r, f, 6.931471805599453e-01);
     r = __builtin_fma(r, f, 1.0);
     return __builtin_ldexp(r, (int)n);
 }
 
-// exp(logit - top) at a temperature; heat = log2(e) / temperature
-__device__ __forceinline__ double weight(float logit, float top, double heat)
+// exp((logit - top) / temperature), heat = log2(e) / temperature; 0 for -inf and NaN, also where top is -inf
+__device__ __forceinline__ double weight(float logit, double top, double heat) { return exp2_of(((double)logit - top) * heat); }
+
+// The largest finite number of a type, which +inf counts as
+template <typename T> constexpr float kLargest = std::is_same_v<T, half_t> ? 65504.f : sizeof(T) == 4 ? FLT_MAX : 3.38953139e38f;
+template <typename T> __device__ __forceinline__ float entry_of(const T *row, int at)
 {
-    return logit == -INFINITY ? 0.0 : exp2_of(((double)logit - (double)top) * heat);
+    const float x = Elem<T>::load(row + at);
+    return x > kLargest<T> ? kLargest<T> : x;
 }
 
-__device__ __forceinline__ float cleaned(float x) { return x != x ? -INFINITY : (x > FLT_MAX ? FLT_MAX : x); }
-
-template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Run {
-    T x[8];
+// Eight entries of a row as they are stored
+template <typename T> struct Run {
+    static constexpr int WORDS = 2 * sizeof(T);
+    uint32_t w[WORDS];
+    __device__ __forceinline__ float entry(int e) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        const uint32_t u = w[e / 2];
+        if constexpr (std::is_same_v<T, half_t>) return half_to_float((uint16_t)(e & 1 ? u >> 16 : u));
+        else return __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
+    }
+    __device__ __forceinline__ void set(int e, bool set, uint32_t bits)
+    {
+        if constexpr (sizeof(T) == 4) w[e] = set ? bits : w[e];
+        else w[e / 2] = set ? (e & 1 ? (w[e / 2] & 0xffffu) | bits << 16 : (w[e / 2] & 0xffff0000u) | bits) : w[e / 2];
+    }
+    // Entries are unpacked anew from here on, and not kept apart: the compiler would hold all of them, and all the exponentials that it can start with them.
+    __device__ __forceinline__ void stay_packed()
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) asm volatile("" : "+v"(w[i]));
+    }
+    static constexpr uint32_t kMinusInf = sizeof(T) == 4 ? 0xff800000u : std::is_same_v<T, half_t> ? 0xfc00u : 0xff80u;
+    static constexpr uint32_t kLargestBits = sizeof(T) == 4 ? 0x7f7fffffu : std::is_same_v<T, half_t> ? 0x7bffu : 0x7f7fu;
+};
+struct __attribute__((packed, aligned(2))) Words16 {
+    uint32_t w[4];
+};
+struct __attribute__((packed, aligned(4))) Words32 {
+    uint32_t w[8];
 };
 
-// Entries at .. at + 7 of a row
-template <typename T> __device__ __forceinline__ void load_run(const T *row, int at, int vocab, float (&x)[8])
+// Entries at .. at + 7 of a row; -inf behind its end
+template <typename T> __device__ __forceinline__ void load_run(const T *row, int at, int vocab, Run<T> &x)
 {
     if (at + 8 <= vocab) {
-        const Run<T> r = *(const Run<T> *)(row + at);
+        const auto r = *(const std::conditional_t<sizeof(T) == 4, Words32, Words16> *)(row + at);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = cleaned(Elem<T>::load(&r.x[e]));
+        for (int i = 0; i < Run<T>::WORDS; ++i) x.w[i] = r.w[i];
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = at + e < vocab ? cleaned(Elem<T>::load(row + at + e)) : -INFINITY;
+        for (int i = 0; i < Run<T>::WORDS; ++i) x.w[i] = Run<T>::kMinusInf * (sizeof(T) == 4 ? 1u : 0x10001u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (at + e < vocab) {
+                const T v = row[at + e];
+                if constexpr (sizeof(T) == 4) x.set(e, true, __float_as_uint(v));
+                else x.set(e, true, *(const uint16_t *)&v);
+            }
     }
 }
 
@@ -113,6 +149,11 @@ __device__ __forceinline__ double uniform(double x)
     return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 |
                                           (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
 }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
 __device__ __forceinline__ double lanes_sum(double x) { return of_lane(lanes_scan(x), 63); }
 __device__ __forceinline__ float lanes_max(float x)
 {
@@ -127,14 +168,19 @@ __device__ __forceinline__ float lanes_max(float x)
     step(Const<0x143>{}, Const<0xc>{});
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
-__device__ __forceinline__ int lanes_min(int v)
+__device__ __forceinline__ int lanes_min(int x)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        const int y = __shfl_xor(v, off, kWave);
-        v = y < v ? y : v;
-    }
-    return v;
+    auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+        const int y = from_lane<decltype(ctrl)::value, decltype(rows)::value>(x, kNone);
+        x = y < x ? y : x;
+    };
+    step(Const<0x111>{}, Const<0xf>{});
+    step(Const<0x112>{}, Const<0xf>{});
+    step(Const<0x114>{}, Const<0xf>{});
+    step(Const<0x118>{}, Const<0xf>{});
+    step(Const<0x142>{}, Const<0xa>{});
+    step(Const<0x143>{}, Const<0xc>{});
+    return __builtin_amdgcn_readlane(x, 63);
 }
 
 // What the workgroups of a group tell each other: per exchange a record each, of 32-bit words with the exchange's number in the upper half
@@ -188,20 +234,33 @@ sample_clear_kernel(uint64_t *words, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = 0;
 }
 
+// f(run, entry) for a thread's entries, in order, four of them in flight together
+template <typename R, int RUNS, typename F> __device__ __forceinline__ void each(R (&runs)[RUNS], const F &f)
+{
+#pragma unroll
+    for (int r = 0; r < RUNS; ++r) {
+        runs[r].stay_packed();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f(r, e);
+            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
 // The walk is a sequence of passes over a slice (over all of them, one after the other, where a workgroup is alone): the weights of a node's
 // rows and their sums; the sums of max(p - a q, 0) after a refusal; the search for the next token.
 enum Pass { kRows, kResidual, kDraw };
 
 template <typename TT, typename TD, int EPT>
-__global__ void __launch_bounds__(NT, EPT == 8 ? 2 : 2)
+__global__ void __launch_bounds__(NT, 4)
 tree_sample_kernel(SampleArgs a)
 {
     constexpr int RUNS = EPT / 8;  // a thread's entries: runs of 8, the lanes' runs side by side; a wave's are contiguous
     constexpr int SLICE = NT * EPT;
     static_assert(LS_MAX_TREE <= NT, "a thread per node");
-    __shared__ int32_t tok[LS_MAX_TREE], path[LS_MAX_TREE];
-    __shared__ float accept_u[LS_MAX_TREE];
-    __shared__ double kid_p[LS_MAX_TREE], kid_q[LS_MAX_TREE], kid_logit[LS_MAX_TREE];
+    __shared__ int32_t tok[LS_MAX_TREE], path[LS_MAX_TREE], has_kids[LS_MAX_TREE];
+    __shared__ float accept_u[LS_MAX_TREE], kid_x[LS_MAX_TREE], kid_y[LS_MAX_TREE];  // kid: logits of both models
     __shared__ double new_logit[LS_MAX_TREE], new_total[LS_MAX_TREE];  // of the new tokens: logit / temperature below the largest, and the sum of the weights
     __shared__ uint64_t kid_mask[LS_MAX_TREE / kWave];
     __shared__ float wave_top[2][WAVES];
@@ -211,16 +270,15 @@ tree_sample_kernel(SampleArgs a)
     __shared__ float part_top[2][kSampleSlices];
     __shared__ double part_sum[2][kSampleSlices];
     __shared__ int32_t part_best[kSampleSlices];
-    __shared__ int32_t first_sh, last_sh, heard_sh[2];
+    __shared__ int32_t first_sh, heard_sh[2];
 
-    const int b = (int)(blockIdx.x / (uint32_t)a.slices), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int b = (int)(blockIdx.x / (uint32_t)a.slices), tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     Exchange ex;
     ex.slices = a.slices, ex.slice = (int)(blockIdx.x % (uint32_t)a.slices), ex.spin_limit = a.spin_limit, ex.number = 0;
     ex.state = a.records + (int64_t)b * (2 * a.slices + 1) * kRecordWords;
     ex.records = ex.state + kRecordWords;
     bool alone = false;  // this workgroup does all slices
     const bool told = a.slices > 1;
-    if (told && __syncthreads_or(tid == 0 && __hip_atomic_load(ex.state, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0)) return;
     const TT *target = (const TT *)a.target + b * a.t_stride[0];
     const TD *draft = (const TD *)a.draft + (a.draft ? b * a.d_stride[0] : 0);
 
@@ -229,13 +287,21 @@ tree_sample_kernel(SampleArgs a)
     int my_parent = -1, my_tok = -1, bad = 0;
     if (is_node) {
         my_parent = a.parents[(int64_t)b * a.n_tree + tid];
-        if (my_parent < -1 || my_parent >= tid) bad = 1, my_parent = -1;
-        my_tok = tok[tid] = a.draft_tokens[(int64_t)b * a.n_tree + tid];
+        my_tok = a.draft_tokens[(int64_t)b * a.n_tree + tid];
         accept_u[tid] = a.accept_uniforms[(int64_t)b * a.n_tree + tid];
+        tok[tid] = my_tok;
         path[tid] = tid == 0 ? 0 : -1;
+        has_kids[tid] = 0;
+        if (my_parent < -1 || my_parent >= tid) bad = 1, my_parent = -1;
         if ((uint32_t)my_tok >= (uint32_t)a.vocab) my_parent = -1;  // nobody's child
     }
-    int err = __syncthreads_or(bad) ? 1 : 0;
+    if (tid == 0) heard_sh[0] = 0, heard_sh[1] = told && __hip_atomic_load(ex.state, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
+    __syncthreads();
+    if (bad) heard_sh[0] = 1;
+    if (my_parent >= 0) has_kids[my_parent] = 1;
+    __syncthreads();
+    int err = uniform(heard_sh[0]);
+    if (uniform(heard_sh[1])) return;  // somebody walks alone already
 
     float temp = a.temperature[b], draft_temp = a.draft_temperature ? a.draft_temperature[b] : temp;
     if (!(temp >= 0.f && temp <= FLT_MAX)) err |= 2, temp = 0.f;
@@ -249,25 +315,29 @@ tree_sample_kernel(SampleArgs a)
     int cur = 0, len = 1, next = -1;
     int writer = 0;                     // the slice whose workgroup draws the token and writes the outputs
     bool inner = false;                 // the node has children, and what they were drawn from counts
-    bool scaled = false;                // p and q are probabilities, and not weights relative to the wave's largest entries
-    float wt = 0.f, wq = 0.f;           // these entries
+    float wt = 0.f, wq = 0.f;           // the wave's largest entries
     float top = 0.f, draft_top = 0.f;   // the largest of the rows
-    double total = 0, draft_total = 0;  // sums of the weights relative to them
+    double total = 0, per_total = 0, per_draft_total = 0;  // sum of the weights relative to it; inverse sums
+    double part = 0;                    // lane i: slice i's share of `mass`
     double taken = 0, mass = 1, left = 1;  // a, S, W
     double rest = 0;                    // what the sum has to pass in the writer's slice
-    int refused = 0;                    // the children before this node have been
-    double p[EPT], q[EPT];
+    int refused = 0, removed = 0;       // the children before these nodes have been refused, and taken out of the rows
+    Run<TT> x[RUNS];
+    Run<TD> y[RUNS];
 
     const int own = wave * (kWave * EPT) + lane * 8;  // this thread's first entry in a slice
 
     while (true) {
+        float my_x = -INFINITY, my_y = -INFINITY;  // this thread's node is a child: its token's logits
+        const bool kid = my_parent == cur && tid > cur;
         if (pass == kRows) {
-            const uint64_t kids = __ballot(my_parent == cur && tid > cur);
-            if (lane == 0) kid_mask[wave] = kids;
-            inner = __syncthreads_or(kids != 0) && drawn;
+            inner = drawn && uniform(has_kids[cur]);
+            if (kid) {
+                my_x = entry_of(target + cur * a.t_stride[1], my_tok);
+                if (inner) my_y = entry_of(draft + cur * a.d_stride[1], my_tok);
+            }
             taken = 0, mass = left = 1;
             refused = 0;
-            scaled = false;
         }
         ++ex.number;
         bool heard = true;
@@ -277,7 +347,6 @@ tree_sample_kernel(SampleArgs a)
             if (pass == kRows || alone) {
                 const TT *row = target + cur * a.t_stride[1];
                 const int at = slice * SLICE + own;
-                float x[RUNS][8], y[RUNS][8];
 #pragma unroll
                 for (int r = 0; r < RUNS; ++r) load_run(row, at + r * kWave * 8, a.vocab, x[r]);
                 if (inner) {
@@ -285,93 +354,108 @@ tree_sample_kernel(SampleArgs a)
 #pragma unroll
                     for (int r = 0; r < RUNS; ++r) load_run(drow, at + r * kWave * 8, a.vocab, y[r]);
                 }
-                float m = -INFINITY, mq = -INFINITY;
+                // the largest entries; +inf counts as the largest finite number (of its type), which is what it is from here on
+                auto largest = [&](auto &runs) __attribute__((always_inline)) {
+                    float m = -INFINITY;
 #pragma unroll
-                for (int r = 0; r < RUNS; ++r)
+                    for (int r = 0; r < RUNS; ++r) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) m = fmaxf(m, x[r][e]);
-                wt = lanes_max(m);
-                if (greedy) {
-                    int best = kNone;
-#pragma unroll
-                    for (int r = RUNS - 1; r >= 0; --r)
-#pragma unroll
-                        for (int e = 7; e >= 0; --e)
-                            if (x[r][e] == wt) best = at + r * kWave * 8 + e;
-                    best = wt > -INFINITY ? lanes_min(best) : kNone;
-                    if (lane == 0) wave_best[wave] = best;
-                }
-#pragma unroll
-                for (int r = 0; r < RUNS; ++r)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        p[r * 8 + e] = weight(x[r][e], wt, heat);
-                        if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                        for (int e = 0; e < 8; ++e) m = fmaxf(m, runs[r].entry(e));
+                        runs[r].stay_packed();
                     }
-                if (inner) {
+                    m = lanes_max(m);
+                    if (m == INFINITY) {
+                        m = -INFINITY;
 #pragma unroll
-                    for (int r = 0; r < RUNS; ++r)
+                        for (int r = 0; r < RUNS; ++r)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) mq = fmaxf(mq, y[r][e]);
-                    wq = lanes_max(mq);
-#pragma unroll
-                    for (int r = 0; r < RUNS; ++r)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            q[r * 8 + e] = weight(y[r][e], wq, draft_heat);
-                            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                        }
-                } else {
-                    wq = -INFINITY;
-#pragma unroll
-                    for (int e = 0; e < EPT; ++e) q[e] = 0.0;
-                }
+                            for (int e = 0; e < 8; ++e) {
+                                runs[r].set(e, runs[r].entry(e) == INFINITY, runs[r].kLargestBits);
+                                m = fmaxf(m, runs[r].entry(e));
+                            }
+                        m = lanes_max(m);
+                    }
+                    return m;
+                };
+                wt = largest(x);
+                wq = inner ? largest(y) : -INFINITY;
+                removed = 0;
             }
+            // refused tokens have no weight any more
             if (pass != kRows) {
-                // to probabilities, with the refused tokens at zero
-                const bool anew = alone || !scaled;
-                if (anew) {
-                    const double f = wt > -INFINITY ? exp2_of(((double)wt - top) * heat) / total : 0.0;
-                    const double fq = wq > -INFINITY ? exp2_of(((double)wq - draft_top) * draft_heat) / draft_total : 0.0;
-#pragma unroll
-                    for (int e = 0; e < EPT; ++e) {
-                        p[e] *= f;
-                        q[e] *= fq;
-                    }
-                    scaled = true;
-                }
-                for (int w = anew ? 0 : (refused - 1) / kWave; w * kWave < refused; ++w)
-                    for (uint64_t m = kid_mask[w]; m; m &= m - 1) {
+                for (int w = removed / kWave; w * kWave < refused; ++w)
+                    for (uint64_t m = uniform(kid_mask[w]); m; m &= m - 1) {
                         const int k = w * kWave + __builtin_ctzll(m);
                         if (k >= refused) break;
-                        const int at = tok[k] - (slice * SLICE + own);
+                        const int at = __builtin_amdgcn_readfirstlane(tok[k] - slice * SLICE - wave * (kWave * EPT));
+                        if (k < removed || (uint32_t)at >= (uint32_t)(kWave * EPT)) continue;
+                        const bool my_run = lane == (at >> 3) % kWave;
 #pragma unroll
-                        for (int e = 0; e < EPT; ++e)
-                            if (at == (e >> 3) * kWave * 8 + (e & 7)) p[e] = q[e] = 0.0;
+                        for (int r = 0; r < RUNS; ++r) {
+                            if (r != at / (8 * kWave)) continue;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                x[r].set(e, my_run && e == at % 8, x[r].kMinusInf);
+                                if (inner) y[r].set(e, my_run && e == at % 8, y[r].kMinusInf);
+                            }
+                        }
                     }
+                removed = refused;
             }
             if (pass == kDraw) break;
-            // sums over the thread, the wave, the slice (in waves 0 and 1), relative to the largest of the waves' tops; then to everybody
+            // sums over the thread, the wave, the slice (in waves 0 and 1); then to everybody
             double s = 0, sq = 0;
-#pragma unroll
-            for (int e = 0; e < EPT; ++e) {
-                const double r = p[e] - taken * q[e];
-                s += r > 0 ? r : 0.0;
-                sq += q[e];
+            if (pass == kRows) {  // of the weights relative to the wave's largest entries
+                each(x, [&](int r, int e) __attribute__((always_inline)) { s += weight(x[r].entry(e), wt, heat); });
+                if (inner) each(y, [&](int r, int e) __attribute__((always_inline)) { sq += weight(y[r].entry(e), wq, draft_heat); });
+            } else if (inner) {   // of max(p - a q, 0), and of q
+                const double takes = taken * per_draft_total;
+                each(x, [&](int r, int e) __attribute__((always_inline)) {
+                    if (e == 0) y[r].stay_packed();
+                    const double wx = weight(x[r].entry(e), top, heat), wy = weight(y[r].entry(e), draft_top, draft_heat);
+                    s += __builtin_fmax(__builtin_fma(-takes, wy, wx * per_total), 0.0);
+                    sq += wy;
+                });
+                sq *= per_draft_total;
+            } else {
+                each(x, [&](int r, int e) __attribute__((always_inline)) { s += weight(x[r].entry(e), top, heat); });
+                s *= per_total;
             }
             s = lanes_sum(s);
-            sq = lanes_sum(sq);
+            if (inner) sq = lanes_sum(sq);
+            if (greedy && pass == kRows) {
+                int best = kNone;
+                const int at = slice * SLICE + own;
+#pragma unroll
+                for (int r = RUNS - 1; r >= 0; --r)
+#pragma unroll
+                    for (int e = 7; e >= 0; --e)
+                        if (x[r].entry(e) == wt) best = at + r * kWave * 8 + e;
+                best = wt > -INFINITY ? lanes_min(best) : kNone;
+                if (lane == 0) wave_best[wave] = best;
+            }
             if (lane == 0) {
                 wave_top[0][wave] = wt, wave_sum[0][wave] = s;
                 wave_top[1][wave] = wq, wave_sum[1][wave] = sq;
             }
             __syncthreads();
+            if (pass == kRows) {
+                const uint64_t kids = __ballot(kid);
+                if (lane == 0) kid_mask[wave] = kids;
+                if (kid) kid_x[tid] = my_x, kid_y[tid] = my_y;
+            }
             if (wave == 0 || (wave == 1 && inner)) {
                 const bool mine = lane < WAVES;
-                const float m = mine ? (pass == kRows ? wave_top[wave][lane] : 0.f) : -INFINITY, mm = lanes_max(m);
-                const double part = m > -INFINITY ? wave_sum[wave][lane] * exp2_of(((double)m - mm) * (wave ? draft_heat : heat)) : 0.0;
-                const double sum = lanes_sum(part);
-                const int best = greedy && wave == 0 ? lanes_min(mine && m == mm ? wave_best[lane] : kNone) : kNone;
+                double sum = mine ? wave_sum[wave][lane] : 0.0;
+                float mm = 0.f;
+                int best = kNone;
+                if (pass == kRows) {
+                    const float m = mine ? wave_top[wave][lane] : -INFINITY;
+                    mm = lanes_max(m);
+                    sum *= weight(m, mm, wave ? draft_heat : heat);
+                    if (greedy) best = lanes_min(mine && m == mm ? wave_best[lane] : kNone);
+                }
+                sum = lanes_sum(sum);
                 if (alone || !told) {
                     if (lane == 0) {
                         part_top[wave][slice] = mm, part_sum[wave][slice] = sum;
@@ -392,7 +476,7 @@ tree_sample_kernel(SampleArgs a)
                 }
             }
             __syncthreads();
-            heard = heard_sh[0] && (!inner || heard_sh[1]);
+            heard = uniform(heard_sh[0]) && (!inner || uniform(heard_sh[1]));
         }
 
         if (!heard) {  // the first one to give up goes on alone, from the root
@@ -402,7 +486,7 @@ tree_sample_kernel(SampleArgs a)
                                                                 __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
-            if (!first_sh) return;
+            if (!uniform(first_sh)) return;
             alone = true;
             pass = kRows;
             cur = 0, len = 1;
@@ -412,80 +496,91 @@ tree_sample_kernel(SampleArgs a)
         }
 
         if (pass == kDraw) {
-            double s = 0;
+            // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
+            // that has any weight.
+            const double takes = inner ? taken * per_draft_total : 0.0;
+            auto residual = [&](const Run<TT> &of_p, const Run<TD> &of_q, int e) __attribute__((always_inline)) {
+                double v = weight(of_p.entry(e), top, heat) * per_total;
+                if (inner) v = __builtin_fmax(__builtin_fma(-takes, weight(of_q.entry(e), draft_top, draft_heat), v), 0.0);
+                return v;
+            };
+            double run[RUNS], all = 0;
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) {
-                const double r = p[e] - taken * q[e];
-                p[e] = r > 0 ? r : 0.0;
-                s += p[e];
-            }
-            s = lanes_sum(s);
-            if (lane == 0) wave_sum[0][wave] = s;
-            if (tid == 0) first_sh = kNone, last_sh = -1;
-            __syncthreads();
-            double before = 0;  // of the entries before this wave's, then before this run
-            for (int w = 0; w < wave; ++w) before += wave_sum[0][w];
-            int first = kNone, last = -1;
+            for (int r = 0; r < RUNS; ++r) run[r] = 0;
+            each(x, [&](int r, int e) __attribute__((always_inline)) {
+                if (e == 0 && inner) y[r].stay_packed();
+                run[r] += residual(x[r], y[r], e);
+            });
 #pragma unroll
             for (int r = 0; r < RUNS; ++r) {
-                double run = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) run += p[r * 8 + e];
-                const double upto = lanes_scan(run);
-                double c = before + (upto - run);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int v = writer * SLICE + own + r * kWave * 8 + e;
-                    c += p[r * 8 + e];
-                    if (p[r * 8 + e] > 0) {
-                        last = v;
-                        if (first == kNone && c > rest) first = v;
-                    }
-                }
-                before += of_lane(upto, 63);
+                run[r] = lanes_sum(run[r]);
+                all += run[r];
             }
-            if (first != kNone) atomicMin(&first_sh, first);
-            if (last >= 0) atomicMax(&last_sh, last);
+            if (lane == 0) wave_sum[0][wave] = all;
+            if (tid == 0) first_sh = -1;
             __syncthreads();
-            next = first_sh != kNone ? first_sh : last_sh;
+            double before = 0, upto = 0;  // of the entries before the wave's; before what has been looked at
+            int at_wave = -1;
+            bool passed = false;
+            for (int w = 0; w < WAVES && !passed; ++w) {
+                const double sum = uniform(wave_sum[0][w]);
+                if (sum > 0) at_wave = w, before = upto, passed = upto + sum > rest;
+                upto += sum;
+            }
+            if (wave == at_wave) {
+                upto = before;
+                passed = false;
+                int at_run = 0;
+                Run<TT> rx = x[0];
+                Run<TD> ry = y[0];
+#pragma unroll
+                for (int r = 0; r < RUNS; ++r) {
+                    if (run[r] > 0 && !passed) {
+                        rx = x[r], ry = y[r];
+                        at_run = r, before = upto, passed = upto + run[r] > rest;
+                    }
+                    upto += run[r];
+                }
+                double v[8], sum = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += v[e] = residual(rx, ry, e);
+                const double scan = lanes_scan(sum);
+                const uint64_t some = __ballot(sum > 0), over = __ballot(sum > 0 && before + scan > rest);
+                if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
+                    double c = before + (scan - sum);
+                    int place = 0;
+                    passed = false;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        c += v[e];
+                        if (v[e] > 0 && !passed) place = e, passed = c > rest;
+                    }
+                    first_sh = writer * SLICE + own + at_run * kWave * 8 + place;
+                }
+            }
+            __syncthreads();
+            next = uniform(first_sh);
             break;
         }
 
         // What the sums say
-        const double per_temp = 1.0 / (greedy ? 1.0 : (double)temp);
         const bool mine = lane < a.slices;
-        double part = mine ? part_sum[0][lane] : 0.0;
+        part = mine ? part_sum[0][lane] : 0.0;
         int best = kNone;
         if (pass == kRows) {
             const float m = mine ? part_top[0][lane] : -INFINITY;
             top = lanes_max(m);
-            part = m > -INFINITY ? part * exp2_of(((double)m - top) * heat) : 0.0;
+            part *= weight(m, top, heat);
             total = lanes_sum(part);
+            per_total = uniform(total > 0 ? 1.0 / total : 0.0);
             if (greedy && total > 0) best = lanes_min(mine && m == top ? part_best[lane] : kNone);
-            if (total > 0) part /= total;
+            part *= per_total;
             if (inner) {
                 const float mq = mine ? part_top[1][lane] : -INFINITY;
                 draft_top = lanes_max(mq);
-                draft_total = lanes_sum(mq > -INFINITY ? part_sum[1][lane] * exp2_of(((double)mq - draft_top) * draft_heat) : 0.0);
+                const double draft_total = lanes_sum(mine ? part_sum[1][lane] * weight(mq, draft_top, draft_heat) : 0.0);
+                per_draft_total = uniform(draft_total > 0 ? 1.0 / draft_total : 0.0);
             }
-            // the children's probabilities, each in its own thread; a token that comes again has been refused before
-            if (my_parent == cur && tid > cur) {
-                const float l = cleaned(Elem<TT>::load(target + cur * a.t_stride[1] + my_tok));
-                double px = total > 0 ? weight(l, top, heat) / total : 0.0, qx = 1.0;
-                kid_logit[tid] = ((double)l - top) * per_temp;
-                if (inner) {
-                    const float lq = cleaned(Elem<TD>::load(draft + cur * a.d_stride[1] + my_tok));
-                    qx = draft_total > 0 ? weight(lq, draft_top, draft_heat) / draft_total : 0.0;
-                }
-                for (int w = 0; w <= wave; ++w)
-                    for (uint64_t k = kid_mask[w]; k; k &= k - 1) {
-                        const int i = w * kWave + __builtin_ctzll(k);
-                        if (i >= tid) break;
-                        if (tok[i] == my_tok) px = 0.0, qx = inner ? 0.0 : 1.0;
-                    }
-                kid_p[tid] = px, kid_q[tid] = qx;
-            }
-            __syncthreads();
         }
         mass = lanes_sum(part);
         if (pass == kResidual && inner && !a.with_replacement) left = lanes_sum(mine ? part_sum[1][lane] : 0.0);
@@ -494,30 +589,38 @@ tree_sample_kernel(SampleArgs a)
         int found = -1;
         bool again = false;
         for (int w = refused / kWave; w < LS_MAX_TREE / kWave && found < 0 && !again; ++w) {
-            uint64_t m = kid_mask[w];
+            uint64_t m = uniform(kid_mask[w]);
             if (w == refused / kWave) m &= ~0ull << (refused % kWave);
             for (; m && found < 0 && !again; m &= m - 1) {
                 const int k = w * kWave + __builtin_ctzll(m);
-                const double px = kid_p[k], qx = kid_q[k], u = accept_u[k];
-                const bool ok = greedy ? tok[k] == best : (px - (inner ? taken * qx : 0.0)) * left > u * qx * mass;
-                if (ok) {
-                    found = k;
+                bool ok;
+                if (greedy) {
+                    ok = tok[k] == best;
                 } else {
-                    refused = k + 1;
-                    again = !greedy;
+                    const double px = weight(kid_x[k], top, heat) * per_total, u = accept_u[k];
+                    if (inner) {
+                        const double qx = weight(kid_y[k], draft_top, draft_heat) * per_draft_total;
+                        ok = (px - taken * qx) * left > u * qx * mass;
+                    } else {
+                        ok = px > u * mass;
+                    }
                 }
+                ok = uniform((int)ok);
+                if (ok) found = k;
+                else refused = k + 1, again = !greedy;
             }
         }
         if (found >= 0) {
-            if (tid == 0) path[len] = found, new_logit[len - 1] = kid_logit[found], new_total[len - 1] = total;
+            if (tid == 0) path[len] = found, new_logit[len - 1] = ((double)kid_x[found] - top) / (greedy ? 1.0 : (double)temp), new_total[len - 1] = total;
             ++len;
             cur = found;
             pass = kRows;
-            __syncthreads();  // children and parts are read before the next node's are written
             continue;
         }
         if (again) {
             if (inner) taken = uniform(left > 0 ? fmin(taken + mass / left, 1e300) : 1e300);  // (finite: q(v) = 0 stays out of it)
+            // the same token once more has no weight either
+            if (kid && tid >= refused && my_tok == tok[refused - 1]) kid_x[tid] = kid_y[tid] = -INFINITY;
             pass = kResidual;
             continue;
         }
@@ -537,7 +640,7 @@ tree_sample_kernel(SampleArgs a)
     }
     if (tid == 0) {
         if (next >= 0) {
-            const float l = cleaned(Elem<TT>::load(target + cur * a.t_stride[1] + next));
+            const float l = entry_of(target + cur * a.t_stride[1], next);
             new_logit[len - 1] = ((double)l - top) / (greedy ? 1.0 : (double)temp), new_total[len - 1] = total;
         } else {
             new_logit[len - 1] = -INFINITY, new_total[len - 1] = 1.0;
@@ -559,7 +662,8 @@ template <typename TT, typename TD> hipError_t launch_types(const SampleArgs &a,
 {
     const dim3 grid((uint32_t)a.batch * a.slices), block(NT);
     if (a.slice == NT * 8) hipLaunchKernelGGL((tree_sample_kernel<TT, TD, 8>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((tree_sample_kernel<TT, TD, 16>), grid, block, 0, stream, a);
+    else if (a.slice == NT * 16) hipLaunchKernelGGL((tree_sample_kernel<TT, TD, 16>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((tree_sample_kernel<TT, TD, 32>), grid, block, 0, stream, a);
     return hipGetLastError();
 }
 

@@ -5,11 +5,11 @@ import numpy as np
 FLT_MAX = float(np.finfo(np.float32).max)
 
 
-def softmax(row, temperature):
+def softmax(row, temperature, largest=FLT_MAX):
     """Weights and their sum to 1 (or all 0), and the log probabilities; -inf and NaN have none, +inf is the largest finite number."""
     x = np.asarray(row, dtype=np.longdouble).copy()
     x[np.isnan(x)] = -np.inf
-    x[x == np.inf] = FLT_MAX
+    x[x == np.inf] = largest
     top = x.max()
     if top == -np.inf:
         return np.zeros_like(x), np.full_like(x, -np.inf)
@@ -19,8 +19,9 @@ def softmax(row, temperature):
         return w / w.sum(), y - np.log(w.sum())
 
 
-def accept_sampled(parents, tokens, target, draft, temperature, draft_temperature, accept_u, sample_u, with_replacement):
-    """One sequence.  target, draft: arrays [n_tree, vocab] (draft None: chosen).  Returns path, next token, log probabilities, error."""
+def accept_sampled(parents, tokens, target, draft, temperature, draft_temperature, accept_u, sample_u, with_replacement,
+                   largest=(FLT_MAX, FLT_MAX)):
+    """One sequence.  target, draft: arrays [n_tree, vocab] (draft None: chosen); largest: finite number of their types.  Returns path, next token, log probabilities, error."""
     n, vocab = target.shape
     err, above = 0, list(parents)
     for i, p in enumerate(above):
@@ -36,7 +37,7 @@ def accept_sampled(parents, tokens, target, draft, temperature, draft_temperatur
     path, logs = [0], []
     while True:
         cur = path[-1]
-        p, log_p = softmax(target[cur], heats[0] or 1.0)
+        p, log_p = softmax(target[cur], heats[0] or 1.0, largest[0])
         if heats[0] == 0:
             best = int(np.argmax(p)) if p.any() else -1
             p = np.zeros_like(p)
@@ -44,7 +45,7 @@ def accept_sampled(parents, tokens, target, draft, temperature, draft_temperatur
                 p[best] = 1
         kids = [i for i in range(n) if above[i] == cur and i > cur and 0 <= tokens[i] < vocab]
         drawn = draft is not None and heats[0] > 0 and heats[1] > 0
-        q = softmax(draft[cur], heats[1])[0] if drawn and kids else None
+        q = softmax(draft[cur], heats[1], largest[1])[0] if drawn and kids else None
         found = None
         for k in kids:
             x = tokens[k]

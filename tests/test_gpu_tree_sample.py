@@ -68,7 +68,8 @@ class Case:
             drf = None if self.draft is None else self.draft[i].float().numpy()
             dt = None if self.draft_temperature is None else float(self.draft_temperature[i])
             p, t, lg, e = ref.accept_sampled(self.parents[i].tolist(), self.tokens[i].tolist(), self.target[i].float().numpy(), drf,
-                                             float(self.temperature[i]), dt, self.accept_u[i].tolist(), float(self.sample_u[i]), self.with_replacement)
+                                             float(self.temperature[i]), dt, self.accept_u[i].tolist(), float(self.sample_u[i]), self.with_replacement,
+                                             [torch.finfo((self.target if x is None else x).dtype).max for x in (self.target, self.draft)])
             path[i, :len(p)], logs[i, :len(lg)] = p, np.array(lg, dtype=np.float64)
             lens[i], nexts[i], errs[i] = len(p), t, e
         return {"path": path, "len": lens, "next": nexts, "err": errs, "logprobs": logs}
@@ -149,9 +150,10 @@ def test_greedy_is_the_greedy_acceptance():
 
 
 @pytest.mark.parametrize("with_replacement", [False, True])
-def test_filtered_logits(with_replacement):
+@pytest.mark.parametrize("target,draft", [("bf16", "f32"), ("f16", "f16"), ("f32", "bf16")])
+def test_filtered_logits(target, draft, with_replacement):
     """-inf, NaN, +inf and the type's lowest value: rows that a filter has left few tokens of, rows without any."""
-    c = Case(31, 12, 15, 9001, "bf16", "f32", with_replacement=with_replacement, kind="tree")
+    c = Case(31, 12, 15, 9001, target, draft, with_replacement=with_replacement, kind="tree")
     rng = np.random.default_rng(1)
     for b in range(12):
         for i in range(15):
@@ -169,6 +171,10 @@ def test_filtered_logits(with_replacement):
                 c.target[b, i] = -torch.inf if b % 2 else float("nan")
             elif what == 3:
                 c.target[b, i, 8888] = torch.inf
+                c.draft[b, i, 17 + i] = torch.inf
+                for k in range(1, 15):  # a child of that token
+                    if c.parents[b, k] == i and b % 2:
+                        c.tokens[b, k] = 8888
             elif what == 4:
                 c.draft[b, i] = -torch.inf
     c.target[3, 0] = -torch.inf
