@@ -33,27 +33,60 @@ constexpr int WAVES = NT / kWave;
 constexpr int kNone = INT32_MAX;
 template <int N> using Const = std::integral_constant<int, N>;
 
+// a b + c with c in scalar registers: for a constant c the compiler takes the form whose result is its third operand, and moves the constant there
+// before each of them.
+__device__ __forceinline__ double fma_scalar(double a, double b, double c)
+{
+    double d;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "s"(c));
+    return d;
+}
+
 // 2^y for y <= 0, to 4e-14 of its value: y = n + f, |f| <= 1/2, and 2^f = 1 + f g(f) with the polynomial g of degree 8 that meets
 // (2^f - 1) / f at the zeros of the Chebyshev polynomial of degree 9.  Less than 2^-1074, and NaN, give 0.
 __device__ __forceinline__ double exp2_of(double y)
 {
     y = __builtin_fmax(y, -1100.0);
     const double n = __builtin_rint(y), f = y - n;
-    double r = 1.0203121047189341e-07;
-    r = __builtin_fma(r, f, 1.3255224879317324e-06);
-    r = __builtin_fma(r, f, 1.525268684635191e-05);
-    r = __builtin_fma(r, f, 1.540345585244999e-04);
-    r = __builtin_fma(r, f, 1.3333558179042969e-03);
-    r = __builtin_fma(r, f, 9.618129159402565e-03);
-    r = __builtin_fma(r, f, 5.5504108664760424e-02);
-    r = __builtin_fma(r, f, 2.402265069581299e-01);
-    r = __builtin_fma(r, f, 6.931471805599453e-01);
+    double r = fma_scalar(f, 1.0203121047189341e-07, 1.3255224879317324e-06);
+    r = fma_scalar(r, f, 1.525268684635191e-05);
+    r = fma_scalar(r, f, 1.540345585244999e-04);
+    r = fma_scalar(r, f, 1.3333558179042969e-03);
+    r = fma_scalar(r, f, 9.618129159402565e-03);
+    r = fma_scalar(r, f, 5.5504108664760424e-02);
+    r = fma_scalar(r, f, 2.402265069581299e-01);
+    r = fma_scalar(r, f, 6.931471805599453e-01);
     r = __builtin_fma(r, f, 1.0);
     return __builtin_ldexp(r, (int)n);
 }
 
 // exp((logit - top) / temperature), heat = log2(e) / temperature; 0 for -inf and NaN, also where top is -inf
 __device__ __forceinline__ double weight(float logit, double top, double heat) { return exp2_of(((double)logit - top) * heat); }
+
+// The same of four logits, step by step, so that no step waits for the one before it.  (Left to itself the compiler takes one after the other, or starts
+// all of a thread's at once and runs out of registers.)
+__device__ __forceinline__ void weights(const float (&logit)[4], double top, double heat, double (&w)[4])
+{
+    double n[4], f[4];
+#define LS_STEP(...)                        \
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) __VA_ARGS__; \
+    __builtin_amdgcn_sched_barrier(0);
+    LS_STEP(f[i] = (double)logit[i] - top)
+    LS_STEP(f[i] = __builtin_fmax(f[i] * heat, -1100.0))
+    LS_STEP(n[i] = __builtin_rint(f[i]))
+    LS_STEP(f[i] = f[i] - n[i])
+    LS_STEP(w[i] = fma_scalar(f[i], 1.0203121047189341e-07, 1.3255224879317324e-06))
+    LS_STEP(w[i] = fma_scalar(w[i], f[i], 1.525268684635191e-05))
+    LS_STEP(w[i] = fma_scalar(w[i], f[i], 1.540345585244999e-04))
+    LS_STEP(w[i] = fma_scalar(w[i], f[i], 1.3333558179042969e-03))
+    LS_STEP(w[i] = fma_scalar(w[i], f[i], 9.618129159402565e-03))
+    LS_STEP(w[i] = fma_scalar(w[i], f[i], 5.5504108664760424e-02))
+    LS_STEP(w[i] = fma_scalar(w[i], f[i], 2.402265069581299e-01))
+    LS_STEP(w[i] = fma_scalar(w[i], f[i], 6.931471805599453e-01))
+    LS_STEP(w[i] = __builtin_fma(w[i], f[i], 1.0))
+    LS_STEP(w[i] = __builtin_ldexp(w[i], (int)n[i]))
+#undef LS_STEP
+}
 
 // The largest finite number of a type, which +inf counts as
 template <typename T> constexpr float kLargest = std::is_same_v<T, half_t> ? 65504.f : sizeof(T) == 4 ? FLT_MAX : 3.38953139e38f;
@@ -234,18 +267,59 @@ sample_clear_kernel(uint64_t *words, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = 0;
 }
 
-// f(run, entry) for a thread's entries, in order, four of them in flight together
-template <typename R, int RUNS, typename F> __device__ __forceinline__ void each(R (&runs)[RUNS], const F &f)
+// The kernel's arguments, read where they are needed: held in scalar registers from the start, as the compiler would have it, they
+// leave too few for the polynomial's coefficients, which then take vector registers.
+typedef const __attribute__((address_space(4))) SampleArgs *ArgsHere;
+__device__ __forceinline__ ArgsHere args_here()
+{
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return (ArgsHere)p;
+}
+
+// add(r, w): the weights of a thread's entries, in order, four at a time of run r
+template <typename R, int RUNS, typename F>
+__device__ __forceinline__ void each_four(R (&runs)[RUNS], double top, double heat, const F &add)
 {
 #pragma unroll
     for (int r = 0; r < RUNS; ++r) {
         runs[r].stay_packed();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f(r, e);
-            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        for (int h = 0; h < 8; h += 4) {
+            const float l[4] = {runs[r].entry(h), runs[r].entry(h + 1), runs[r].entry(h + 2), runs[r].entry(h + 3)};
+            double w[4];
+            weights(l, top, heat, w);
+            add(r, w);
         }
     }
+}
+// residual(r, v): max(p - a q, 0) of the same, and the weights of q
+template <typename P, typename Q, int RUNS, typename F>
+__device__ __forceinline__ void each_four(P (&x)[RUNS], Q (&y)[RUNS], double top, double heat, double draft_top, double draft_heat, double per_total,
+                                          double takes, const F &add)
+{
+#pragma unroll
+    for (int r = 0; r < RUNS; ++r) {
+        x[r].stay_packed();
+        y[r].stay_packed();
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+            const float l[4] = {x[r].entry(h), x[r].entry(h + 1), x[r].entry(h + 2), x[r].entry(h + 3)};
+            const float m[4] = {y[r].entry(h), y[r].entry(h + 1), y[r].entry(h + 2), y[r].entry(h + 3)};
+            double v[4], w[4];
+            weights(l, top, heat, v);
+            weights(m, draft_top, draft_heat, w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __builtin_fmax(__builtin_fma(-takes, w[i], v[i] * per_total), 0.0);
+            add(r, v, w);
+        }
+    }
+}
+// A sum that is worked out here, and not where it is used
+__device__ __forceinline__ void add_four(double &sum, const double (&w)[4])
+{
+    sum += (w[0] + w[1]) + (w[2] + w[3]);
+    asm volatile("" : "+v"(sum));
 }
 
 // The walk is a sequence of passes over a slice (over all of them, one after the other, where a workgroup is alone): the weights of a node's
@@ -254,8 +328,9 @@ enum Pass { kRows, kResidual, kDraw };
 
 template <typename TT, typename TD, int EPT>
 __global__ void __launch_bounds__(NT, 4)
-tree_sample_kernel(SampleArgs a)
+tree_sample_kernel(SampleArgs)
 {
+    const ArgsHere a = args_here();
     constexpr int RUNS = EPT / 8;  // a thread's entries: runs of 8, the lanes' runs side by side; a wave's are contiguous
     constexpr int SLICE = NT * EPT;
     static_assert(LS_MAX_TREE <= NT, "a thread per node");
@@ -272,28 +347,35 @@ tree_sample_kernel(SampleArgs a)
     __shared__ int32_t part_best[kSampleSlices];
     __shared__ int32_t first_sh, heard_sh[2];
 
-    const int b = (int)(blockIdx.x / (uint32_t)a.slices), tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int b = (int)(blockIdx.x / (uint32_t)a->slices), tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     Exchange ex;
-    ex.slices = a.slices, ex.slice = (int)(blockIdx.x % (uint32_t)a.slices), ex.spin_limit = a.spin_limit, ex.number = 0;
-    ex.state = a.records + (int64_t)b * (2 * a.slices + 1) * kRecordWords;
+    ex.slices = a->slices, ex.slice = (int)(blockIdx.x % (uint32_t)a->slices), ex.spin_limit = a->spin_limit, ex.number = 0;
+    ex.state = a->records + (int64_t)b * (2 * a->slices + 1) * kRecordWords;
     ex.records = ex.state + kRecordWords;
     bool alone = false;  // this workgroup does all slices
-    const bool told = a.slices > 1;
-    const TT *target = (const TT *)a.target + b * a.t_stride[0];
-    const TD *draft = (const TD *)a.draft + (a.draft ? b * a.d_stride[0] : 0);
+    const bool told = a->slices > 1;
+    // node's rows of logits
+    auto target_row = [&](int node) __attribute__((always_inline)) {
+        const ArgsHere h = args_here();
+        return (const TT *)h->target + b * h->t_stride[0] + node * h->t_stride[1];
+    };
+    auto draft_row = [&](int node) __attribute__((always_inline)) {
+        const ArgsHere h = args_here();
+        return (const TD *)h->draft + b * h->d_stride[0] + node * h->d_stride[1];
+    };
 
     // thread i has node i
-    const bool is_node = tid < a.n_tree;
+    const bool is_node = tid < a->n_tree;
     int my_parent = -1, my_tok = -1, bad = 0;
     if (is_node) {
-        my_parent = a.parents[(int64_t)b * a.n_tree + tid];
-        my_tok = a.draft_tokens[(int64_t)b * a.n_tree + tid];
-        accept_u[tid] = a.accept_uniforms[(int64_t)b * a.n_tree + tid];
+        my_parent = a->parents[(int64_t)b * a->n_tree + tid];
+        my_tok = a->draft_tokens[(int64_t)b * a->n_tree + tid];
+        accept_u[tid] = a->accept_uniforms[(int64_t)b * a->n_tree + tid];
         tok[tid] = my_tok;
         path[tid] = tid == 0 ? 0 : -1;
         has_kids[tid] = 0;
         if (my_parent < -1 || my_parent >= tid) bad = 1, my_parent = -1;
-        if ((uint32_t)my_tok >= (uint32_t)a.vocab) my_parent = -1;  // nobody's child
+        if ((uint32_t)my_tok >= (uint32_t)a->vocab) my_parent = -1;  // nobody's child
     }
     if (tid == 0) heard_sh[0] = 0, heard_sh[1] = told && __hip_atomic_load(ex.state, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
     __syncthreads();
@@ -303,11 +385,11 @@ tree_sample_kernel(SampleArgs a)
     int err = uniform(heard_sh[0]);
     if (uniform(heard_sh[1])) return;  // somebody walks alone already
 
-    float temp = a.temperature[b], draft_temp = a.draft_temperature ? a.draft_temperature[b] : temp;
+    float temp = a->temperature[b], draft_temp = a->draft_temperature ? a->draft_temperature[b] : temp;
     if (!(temp >= 0.f && temp <= FLT_MAX)) err |= 2, temp = 0.f;
     if (!(draft_temp >= 0.f && draft_temp <= FLT_MAX)) err |= 2, draft_temp = 0.f;
     const bool greedy = temp == 0.f;
-    const bool drawn = a.draft && !greedy && draft_temp > 0.f;
+    const bool drawn = a->draft && !greedy && draft_temp > 0.f;
     const double heat = uniform(1.4426950408889634074 / (greedy ? 1.0 : (double)temp));
     const double draft_heat = uniform(drawn ? 1.4426950408889634074 / (double)draft_temp : 0.0);
 
@@ -333,26 +415,26 @@ tree_sample_kernel(SampleArgs a)
         if (pass == kRows) {
             inner = drawn && uniform(has_kids[cur]);
             if (kid) {
-                my_x = entry_of(target + cur * a.t_stride[1], my_tok);
-                if (inner) my_y = entry_of(draft + cur * a.d_stride[1], my_tok);
+                my_x = entry_of(target_row(cur), my_tok);
+                if (inner) my_y = entry_of(draft_row(cur), my_tok);
             }
             taken = 0, mass = left = 1;
             refused = 0;
         }
         ++ex.number;
         bool heard = true;
-        int slice = alone ? 0 : ex.slice, end = alone ? a.slices : ex.slice + 1;
+        int slice = alone ? 0 : ex.slice, end = alone ? a->slices : ex.slice + 1;
         if (pass == kDraw) slice = writer, end = writer + 1;
         for (; slice < end && heard; ++slice) {
             if (pass == kRows || alone) {
-                const TT *row = target + cur * a.t_stride[1];
+                const TT *row = target_row(cur);
                 const int at = slice * SLICE + own;
 #pragma unroll
-                for (int r = 0; r < RUNS; ++r) load_run(row, at + r * kWave * 8, a.vocab, x[r]);
+                for (int r = 0; r < RUNS; ++r) load_run(row, at + r * kWave * 8, a->vocab, x[r]);
                 if (inner) {
-                    const TD *drow = draft + cur * a.d_stride[1];
+                    const TD *drow = draft_row(cur);
 #pragma unroll
-                    for (int r = 0; r < RUNS; ++r) load_run(drow, at + r * kWave * 8, a.vocab, y[r]);
+                    for (int r = 0; r < RUNS; ++r) load_run(drow, at + r * kWave * 8, a->vocab, y[r]);
                 }
                 // the largest entries; +inf counts as the largest finite number (of its type), which is what it is from here on
                 auto largest = [&](auto &runs) __attribute__((always_inline)) {
@@ -406,19 +488,14 @@ tree_sample_kernel(SampleArgs a)
             // sums over the thread, the wave, the slice (in waves 0 and 1); then to everybody
             double s = 0, sq = 0;
             if (pass == kRows) {  // of the weights relative to the wave's largest entries
-                each(x, [&](int r, int e) __attribute__((always_inline)) { s += weight(x[r].entry(e), wt, heat); });
-                if (inner) each(y, [&](int r, int e) __attribute__((always_inline)) { sq += weight(y[r].entry(e), wq, draft_heat); });
+                each_four(x, wt, heat, [&](int, const double (&w)[4]) __attribute__((always_inline)) { add_four(s, w); });
+                if (inner) each_four(y, wq, draft_heat, [&](int, const double (&w)[4]) __attribute__((always_inline)) { add_four(sq, w); });
             } else if (inner) {   // of max(p - a q, 0), and of q
-                const double takes = taken * per_draft_total;
-                each(x, [&](int r, int e) __attribute__((always_inline)) {
-                    if (e == 0) y[r].stay_packed();
-                    const double wx = weight(x[r].entry(e), top, heat), wy = weight(y[r].entry(e), draft_top, draft_heat);
-                    s += __builtin_fmax(__builtin_fma(-takes, wy, wx * per_total), 0.0);
-                    sq += wy;
-                });
+                each_four(x, y, top, heat, draft_top, draft_heat, per_total, taken * per_draft_total,
+                          [&](int, const double (&v)[4], const double (&w)[4]) __attribute__((always_inline)) { add_four(s, v), add_four(sq, w); });
                 sq *= per_draft_total;
             } else {
-                each(x, [&](int r, int e) __attribute__((always_inline)) { s += weight(x[r].entry(e), top, heat); });
+                each_four(x, top, heat, [&](int, const double (&w)[4]) __attribute__((always_inline)) { add_four(s, w); });
                 s *= per_total;
             }
             s = lanes_sum(s);
@@ -467,7 +544,7 @@ tree_sample_kernel(SampleArgs a)
                     ex.tell(wave, lane, lane == 0 ? __float_as_uint(mm) : lane == 1 ? (uint32_t)bits : lane == 2 ? (uint32_t)(bits >> 32) : (uint32_t)best);
                     uint32_t value[4];
                     const bool all = ex.hear(wave, lane, value);
-                    if (lane < a.slices) {
+                    if (lane < a->slices) {
                         part_top[wave][lane] = __uint_as_float(value[0]);
                         part_sum[wave][lane] = from_words(value[1], value[2]);
                         if (wave == 0) part_best[lane] = (int)value[3];
@@ -490,7 +567,7 @@ tree_sample_kernel(SampleArgs a)
             alone = true;
             pass = kRows;
             cur = 0, len = 1;
-            if (is_node) path[tid] = tid == 0 ? 0 : -1;
+            path[tid] = tid == 0 ? 0 : -1;
             __syncthreads();
             continue;
         }
@@ -499,21 +576,17 @@ tree_sample_kernel(SampleArgs a)
             // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
             // that has any weight.
             const double takes = inner ? taken * per_draft_total : 0.0;
-            auto residual = [&](const Run<TT> &of_p, const Run<TD> &of_q, int e) __attribute__((always_inline)) {
-                double v = weight(of_p.entry(e), top, heat) * per_total;
-                if (inner) v = __builtin_fmax(__builtin_fma(-takes, weight(of_q.entry(e), draft_top, draft_heat), v), 0.0);
-                return v;
-            };
             double run[RUNS], all = 0;
 #pragma unroll
             for (int r = 0; r < RUNS; ++r) run[r] = 0;
-            each(x, [&](int r, int e) __attribute__((always_inline)) {
-                if (e == 0 && inner) y[r].stay_packed();
-                run[r] += residual(x[r], y[r], e);
-            });
+            if (inner)
+                each_four(x, y, top, heat, draft_top, draft_heat, per_total, takes,
+                          [&](int r, const double (&v)[4], const double (&)[4]) __attribute__((always_inline)) { add_four(run[r], v); });
+            else
+                each_four(x, top, heat, [&](int r, const double (&w)[4]) __attribute__((always_inline)) { add_four(run[r], w); });
 #pragma unroll
             for (int r = 0; r < RUNS; ++r) {
-                run[r] = lanes_sum(run[r]);
+                run[r] = lanes_sum(inner ? run[r] : run[r] * per_total);
                 all += run[r];
             }
             if (lane == 0) wave_sum[0][wave] = all;
@@ -543,7 +616,24 @@ tree_sample_kernel(SampleArgs a)
                 }
                 double v[8], sum = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[e] = residual(rx, ry, e);
+                for (int h = 0; h < 8; h += 4) {
+                    const float l[4] = {rx.entry(h), rx.entry(h + 1), rx.entry(h + 2), rx.entry(h + 3)};
+                    double w[4];
+                    weights(l, top, heat, w);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[h + i] = w[i] * per_total;
+                }
+                if (inner)
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        const float l[4] = {ry.entry(h), ry.entry(h + 1), ry.entry(h + 2), ry.entry(h + 3)};
+                        double w[4];
+                        weights(l, draft_top, draft_heat, w);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[h + i] = __builtin_fmax(__builtin_fma(-takes, w[i], v[h + i]), 0.0);
+                    }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += v[e];
                 const double scan = lanes_scan(sum);
                 const uint64_t some = __ballot(sum > 0), over = __ballot(sum > 0 && before + scan > rest);
                 if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
@@ -564,7 +654,7 @@ tree_sample_kernel(SampleArgs a)
         }
 
         // What the sums say
-        const bool mine = lane < a.slices;
+        const bool mine = lane < a->slices;
         part = mine ? part_sum[0][lane] : 0.0;
         int best = kNone;
         if (pass == kRows) {
@@ -583,7 +673,7 @@ tree_sample_kernel(SampleArgs a)
             }
         }
         mass = lanes_sum(part);
-        if (pass == kResidual && inner && !a.with_replacement) left = lanes_sum(mine ? part_sum[1][lane] : 0.0);
+        if (pass == kResidual && inner && !args_here()->with_replacement) left = lanes_sum(mine ? part_sum[1][lane] : 0.0);
 
         // the children that have not been tried
         int found = -1;
@@ -628,7 +718,7 @@ tree_sample_kernel(SampleArgs a)
         if (greedy) {
             next = best == kNone ? -1 : best;
         } else if (mass > 0) {
-            const double upto = lanes_scan(part), point = (double)a.sample_uniforms[b] * mass;
+            const double upto = lanes_scan(part), point = (double)args_here()->sample_uniforms[b] * mass;
             const uint64_t passed = __ballot(part > 0 && upto > point), some = __ballot(part > 0);
             writer = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);
             rest = uniform(point - of_lane(upto - part, writer));
@@ -640,21 +730,23 @@ tree_sample_kernel(SampleArgs a)
     }
     if (tid == 0) {
         if (next >= 0) {
-            const float l = entry_of(target + cur * a.t_stride[1], next);
+            const float l = entry_of(target_row(cur), next);
             new_logit[len - 1] = ((double)l - top) / (greedy ? 1.0 : (double)temp), new_total[len - 1] = total;
         } else {
             new_logit[len - 1] = -INFINITY, new_total[len - 1] = 1.0;
             err |= 4;
         }
-        a.len[b] = len;
-        a.next[b] = next;
-        if (a.err_flag) a.err_flag[b] = err;
+        const ArgsHere h = args_here();
+        h->len[b] = len;
+        h->next[b] = next;
+        if (h->err_flag) h->err_flag[b] = err;
     }
     __syncthreads();
-    if (is_node) {
-        const int64_t at = (int64_t)b * a.n_tree + tid;
-        a.path[at] = path[tid];
-        if (a.logprobs) a.logprobs[at] = tid < len ? (float)(new_logit[tid] - log(new_total[tid])) : 0.f;
+    const ArgsHere h = args_here();
+    if (tid < h->n_tree) {
+        const int64_t at = (int64_t)b * h->n_tree + tid;
+        h->path[at] = path[tid];
+        if (h->logprobs) h->logprobs[at] = tid < len ? (float)(new_logit[tid] - log(new_total[tid])) : 0.f;
     }
 }
 
