@@ -17,22 +17,41 @@ struct SampleArgs {
     int32_t batch, n_tree, vocab, with_replacement;
     int32_t slice, slices;  // entries of a slice of the vocabulary, and their number
     int32_t spin_limit;     // polls before a workgroup gives up on its group
+    uint32_t call;          // a number of this call's own
     uint64_t *records;
 };
-constexpr int kSampleThreads = 512;
-constexpr int kSampleSlices = 64;  // at most
-static_assert(kSampleThreads * 32 * kSampleSlices >= LS_MAX_VOCAB, "every vocabulary fits");
-// 8, 16 or 32 entries a thread: as few as the card has room for, two workgroups a compute unit
-inline int sample_slice(int batch, int vocab, int compute_units)
+constexpr int kSampleThreads = 256;
+constexpr int kSampleSlices = 64;                   // at most
+constexpr int kSampleUnit = kSampleThreads * 8;     // entries: slices are multiples
+constexpr int kSampleLds = 156 * 1024;              // dynamic LDS, at most
+// 40 bytes for each node, nodes up to a multiple of 64; the entries of both rows
+inline int sample_lds_bytes(int n_tree, int slice, int target_bytes, int draft_bytes)
 {
-    for (int slice = kSampleThreads * 8; slice < kSampleThreads * 32; slice *= 2) {
-        const int slices = (vocab + slice - 1) / slice;
-        if (slices <= kSampleSlices && (slices == 1 || (int64_t)batch * slices <= 2 * compute_units)) return slice;
-    }
-    return kSampleThreads * 32;
+    return (n_tree + 63) / 64 * 64 * 40 + slice * (target_bytes + draft_bytes);
 }
-// A state word and two records a slice, of 64 bytes each, per sequence; none where a sequence has one slice
-inline size_t sample_record_bytes(int batch, int slices) { return slices > 1 ? (size_t)batch * (2 * slices + 1) * 64 : 0; }
+static_assert(512 * 40 + LS_MAX_VOCAB / kSampleSlices * 8 <= kSampleLds, "every vocabulary fits");
+// The smallest slices with which all workgroups of the call fit on the card at a time; if none do, the largest of which four fit on a compute unit.
+inline int sample_slice(int batch, int n_tree, int vocab, int target_bytes, int draft_bytes, int compute_units)
+{
+    int slice = kSampleUnit;
+    for (; slice < kSampleUnit * 32; slice += kSampleUnit) {
+        const int slices = (vocab + slice - 1) / slice;
+        if (slices > kSampleSlices) continue;
+        const int each = sample_lds_bytes(n_tree, slice, target_bytes, draft_bytes) + 3072;
+        int fit = 160 * 1024 / each;
+        fit = fit > 4 ? 4 : fit;  // by their registers
+        if (slices == 1 || (int64_t)batch * slices <= (int64_t)fit * compute_units) return slice;
+        if (sample_lds_bytes(n_tree, slice + kSampleUnit, target_bytes, draft_bytes) + 3072 > 40 * 1024) return slice;
+    }
+    return slice;
+}
+// State, marks and two records a slice, in 64-bit words, per sequence; none where a sequence has one slice
+inline size_t sample_record_bytes(int batch, int slices)
+{
+    return slices > 1 ? (size_t)batch * (8 + (slices + 7) / 8 * 8 + 16 * slices) * 8 : 0;
+}
+// A 32-bit number that other calls hardly ever have
+uint32_t new_call_number();
 hipError_t launch_tree_sample(const SampleArgs &a, int target_dtype, int draft_dtype, hipStream_t stream);
 
 // holder[page]: what the new tables hold it for: kNobody, kFull (some request, as a full page), or the lowest request that goes on in it.

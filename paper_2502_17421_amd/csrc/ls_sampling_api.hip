@@ -1,7 +1,21 @@
 // Host side of the entry points of sampled decoding (include/ls_attn.h): argument checks and dispatch.
 #include "ls_sampling.hpp"
 
+#include <unistd.h>
+
+#include <chrono>
+
 namespace ls {
+
+uint32_t new_call_number()
+{
+    // calls of this process count on from where the clock and the process number say; a mixing of all bits keeps neighbours apart
+    static std::atomic<uint64_t> count{(uint64_t)std::chrono::steady_clock::now().time_since_epoch().count() ^ (uint64_t)getpid() << 40};
+    uint64_t z = count.fetch_add(0x9e3779b97f4a7c15ull, std::memory_order_relaxed);
+    z = (z ^ z >> 30) * 0xbf58476d1ce4e5b9ull;
+    z = (z ^ z >> 27) * 0x94d049bb133111ebull;
+    return (uint32_t)(z ^ z >> 31);
+}
 
 namespace {
 
@@ -26,9 +40,14 @@ int validate(const ls_sample_desc *d)
     return LS_OK;
 }
 
+int slice_of(const ls_sample_desc &d)
+{
+    return sample_slice(d.batch, d.n_tree, d.vocab, is_16bit(d.target_dtype) ? 2 : 4, is_16bit(d.draft_dtype) ? 2 : 4, compute_units());
+}
+
 int slices_of(const ls_sample_desc &d)
 {
-    const int slice = sample_slice(d.batch, d.vocab, compute_units());
+    const int slice = slice_of(d);
     return (d.vocab + slice - 1) / slice;
 }
 
@@ -131,8 +150,8 @@ int ls_tree_accept_sampled(const ls_sample_desc *desc, const int32_t *parents, c
     a.path = accept_path, a.len = accept_len, a.next = next_token, a.logprobs = logprobs, a.err_flag = err_flag;
     for (int i = 0; i < 2; ++i) a.t_stride[i] = desc->target_stride[i], a.d_stride[i] = desc->draft_stride[i];
     a.batch = desc->batch, a.n_tree = desc->n_tree, a.vocab = desc->vocab, a.with_replacement = desc->with_replacement != 0;
-    a.slice = sample_slice(desc->batch, desc->vocab, compute_units()), a.slices = slices_of(*desc);
-    a.records = (uint64_t *)workspace;
+    a.slice = slice_of(*desc), a.slices = slices_of(*desc);
+    a.records = (uint64_t *)workspace, a.call = new_call_number();
     a.spin_limit = single_launch_polls() < 0 ? kDefaultSamplePolls : single_launch_polls();
     return launch_tree_sample(a, desc->target_dtype, desc->draft_dtype, (hipStream_t)stream) == hipSuccess ? LS_OK : LS_ERR_HIP;
 }

@@ -107,19 +107,11 @@ template <typename T> struct Run {
         if constexpr (std::is_same_v<T, half_t>) return half_to_float((uint16_t)(e & 1 ? u >> 16 : u));
         else return __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
     }
-    __device__ __forceinline__ void set(int e, bool set, uint32_t bits)
-    {
-        if constexpr (sizeof(T) == 4) w[e] = set ? bits : w[e];
-        else w[e / 2] = set ? (e & 1 ? (w[e / 2] & 0xffffu) | bits << 16 : (w[e / 2] & 0xffff0000u) | bits) : w[e / 2];
-    }
-    // Entries are unpacked anew from here on, and not kept apart: the compiler would hold all of them, and all the exponentials that it can start with them.
-    __device__ __forceinline__ void stay_packed()
+    __device__ __forceinline__ void four(int h, float (&l)[4]) const
     {
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) asm volatile("" : "+v"(w[i]));
+        for (int i = 0; i < 4; ++i) l[i] = entry(h + i);
     }
-    static constexpr uint32_t kMinusInf = sizeof(T) == 4 ? 0xff800000u : std::is_same_v<T, half_t> ? 0xfc00u : 0xff80u;
-    static constexpr uint32_t kLargestBits = sizeof(T) == 4 ? 0x7f7fffffu : std::is_same_v<T, half_t> ? 0x7bffu : 0x7f7fu;
 };
 struct __attribute__((packed, aligned(2))) Words16 {
     uint32_t w[4];
@@ -127,26 +119,37 @@ struct __attribute__((packed, aligned(2))) Words16 {
 struct __attribute__((packed, aligned(4))) Words32 {
     uint32_t w[8];
 };
-
-// Entries at .. at + 7 of a row; -inf behind its end
-template <typename T> __device__ __forceinline__ void load_run(const T *row, int at, int vocab, Run<T> &x)
+template <typename T> __device__ __forceinline__ Run<T> run_of_row(const T *at)  // (any alignment)
 {
-    if (at + 8 <= vocab) {
-        const auto r = *(const std::conditional_t<sizeof(T) == 4, Words32, Words16> *)(row + at);
+    Run<T> x;
+    const auto r = *(const std::conditional_t<sizeof(T) == 4, Words32, Words16> *)at;
 #pragma unroll
-        for (int i = 0; i < Run<T>::WORDS; ++i) x.w[i] = r.w[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < Run<T>::WORDS; ++i) x.w[i] = Run<T>::kMinusInf * (sizeof(T) == 4 ? 1u : 0x10001u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (at + e < vocab) {
-                const T v = row[at + e];
-                if constexpr (sizeof(T) == 4) x.set(e, true, __float_as_uint(v));
-                else x.set(e, true, *(const uint16_t *)&v);
-            }
-    }
+    for (int i = 0; i < Run<T>::WORDS; ++i) x.w[i] = r.w[i];
+    return x;
 }
+template <typename T> __device__ __forceinline__ Run<T> run_of_lds(const T *at)
+{
+    Run<T> x;
+#pragma unroll
+    for (int i = 0; i < Run<T>::WORDS; i += 4) {
+        const uint4 u = *(const uint4 *)((const uint32_t *)at + i);
+        x.w[i] = u.x, x.w[i + 1] = u.y, x.w[i + 2] = u.z, x.w[i + 3] = u.w;
+    }
+    return x;
+}
+template <typename T> __device__ __forceinline__ void run_to_lds(const Run<T> &x, T *at)
+{
+#pragma unroll
+    for (int i = 0; i < Run<T>::WORDS; i += 4) *(uint4 *)((uint32_t *)at + i) = make_uint4(x.w[i], x.w[i + 1], x.w[i + 2], x.w[i + 3]);
+}
+template <typename T> __device__ __forceinline__ T from_bits(uint32_t bits)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
+    else if constexpr (std::is_same_v<T, half_t>) return half_t{(uint16_t)bits};
+    else return (T)bits;
+}
+template <typename T> __device__ __forceinline__ T minus_inf() { return from_bits<T>(sizeof(T) == 4 ? 0xff800000u : std::is_same_v<T, half_t> ? 0xfc00u : 0xff80u); }
+template <typename T> __device__ __forceinline__ T largest_bits() { return from_bits<T>(sizeof(T) == 4 ? 0x7f7fffffu : std::is_same_v<T, half_t> ? 0x7bffu : 0x7f7fu); }
 
 // x of the lane that a DPP control names; `other` where there is none
 template <int CTRL, int ROWS> __device__ __forceinline__ int from_lane(int x, int other)
@@ -201,6 +204,25 @@ __device__ __forceinline__ float lanes_max(float x)
     step(Const<0x143>{}, Const<0xc>{});
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
+// The same over four neighbouring lanes, in all of these
+__device__ __forceinline__ double quad_sum(double x)
+{
+    x += from_lane<0xb1, 0xf>(x);
+    x += from_lane<0x4e, 0xf>(x);
+    return x;
+}
+__device__ __forceinline__ float quad_max(float x)
+{
+    x = fmaxf(x, __int_as_float(from_lane<0xb1, 0xf>(__float_as_int(x), __float_as_int(-INFINITY))));
+    return fmaxf(x, __int_as_float(from_lane<0x4e, 0xf>(__float_as_int(x), __float_as_int(-INFINITY))));
+}
+// 1 / x to the last bit or two, for x of the size of such sums
+__device__ __forceinline__ double inverse(double x)
+{
+    double r = __builtin_amdgcn_rcp(x);
+    r = __builtin_fma(__builtin_fma(-x, r, 1.0), r, r);
+    return __builtin_fma(__builtin_fma(-x, r, 1.0), r, r);
+}
 __device__ __forceinline__ int lanes_min(int x)
 {
     auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
@@ -216,56 +238,103 @@ __device__ __forceinline__ int lanes_min(int x)
     return __builtin_amdgcn_readlane(x, 63);
 }
 
-// What the workgroups of a group tell each other: per exchange a record each, of 32-bit words with the exchange's number in the upper half
-// of 64 bits.  A word is written and read at once, so its number says that its value is there, and no fence is needed; two sets of records
-// take turns, since nobody is at exchange n + 2 before everybody has read those of n.  The numbers start at 1 in records that
-// a kernel before this one has cleared.
+// What the workgroups of a group tell each other: per exchange a record each, half of it about p and half about q, of four 32-bit values with a
+// tag each in the upper half of 64 bits.  A word is written and read at once, so its tag says that its value is there, and no fence is needed; two
+// sets of records take turns, since nobody is at exchange n + 2 before everybody has read those of n.
+//
+// Tags are a number of the call's own plus that of the exchange, that of a half record's last word with a checksum of its values: what the workspace
+// held before does not pass for a record (with a chance of 2^-64).  A graph that is replayed has the same number again, so whoever writes the outputs
+// clears the records at the end, once the others have left their marks that they have read all they need.
+// (A kernel that cleared them beforehand took 5 us of each call.)
 //
 // The workgroups of a group are next to each other in the launch, so that all of the first group that is not done yet are on the card, or
 // will be when what else runs there is done.  No wait is unbounded all the same: who has polled spin_limit times gives up on
 // the group, and the first of them (the state word says so) walks the tree alone, slice after slice, with the same sums in the same order.
 // What it writes are the bits that the group writes if it gets to the end after all.
-constexpr int kRecordWords = 8;  // p: 0 largest entry, 1-2 sum, 3 where the largest is; q: 4 largest entry, 5-6 sum
+constexpr int kRecordWords = 8;  // of p: 0 largest entry, 1-2 sum, 3 where the largest is; 4-7 the same of q
+
+struct Half {
+    uint32_t value[4];
+    __device__ __forceinline__ uint32_t check() const
+    {
+        return value[0] ^ value[1] * 0x85ebca6bu ^ value[2] * 0xc2b2ae35u ^ value[3] * 0x27d4eb2fu;
+    }
+};
 
 struct Exchange {
-    uint64_t *records;  // [2][slices][kRecordWords]
-    uint64_t *state;    // 1: some workgroup walks alone
-    int slices, slice, spin_limit;
-    uint32_t number;
+    uint64_t *words;  // of the sequence: [8] state, [slices up to a multiple of 8] marks, [2][slices][kRecordWords] records
+    int slices, slice;
+    uint32_t call, number;
 
-    __device__ __forceinline__ uint64_t *record(int of) const { return records + ((number & 1) * slices + of) * kRecordWords; }
-    // lane i < 4 of wave 0 or 1 writes word 4 * wave + i
-    __device__ __forceinline__ void tell(int wave, int lane, uint32_t value) const
+    __device__ __forceinline__ uint64_t *marks() const { return words + 8; }
+    __device__ __forceinline__ uint64_t *record(int of) const
     {
-        if (lane < 4)
-            __hip_atomic_store(record(slice) + 4 * wave + lane, (uint64_t)number << 32 | value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return words + 8 + (slices + 7) / 8 * 8 + ((number & 1) * slices + of) * kRecordWords;
     }
-    // lane i reads the half record of slice i; false: given up
-    __device__ __forceinline__ bool hear(int wave, int lane, uint32_t (&value)[4]) const
+    __device__ __forceinline__ int n_words() const { return 8 + (slices + 7) / 8 * 8 + 2 * slices * kRecordWords; }
+    static __device__ __forceinline__ void put(uint64_t *at, uint64_t word)
     {
-        const uint64_t *from = record(lane < slices ? lane : 0) + 4 * wave;
+        __hip_atomic_store(at, word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    static __device__ __forceinline__ uint64_t get(const uint64_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+    __device__ __forceinline__ uint64_t taken() const { return (uint64_t)call << 32 | 1u; }
+    __device__ __forceinline__ bool somebody_alone() const { return get(words) == taken(); }
+    // true for the first one of the call
+    __device__ __forceinline__ bool go_alone() const
+    {
+        unsigned long long now = get(words);
+        while (now != taken())
+            if (__hip_atomic_compare_exchange_strong((unsigned long long *)words, &now, (unsigned long long)taken(), __ATOMIC_RELAXED,
+                                                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+                return true;
+        return false;
+    }
+    // lanes first .. first + 3 have the values of half `which`, lane by lane
+    __device__ __forceinline__ void tell(int which, int lane_of_four, uint32_t value, uint32_t check) const
+    {
+        const uint32_t tag = (call + number) ^ (lane_of_four == 3 ? check : 0u);
+        if (lane_of_four >= 0 && lane_of_four < 4) put(record(slice) + 4 * which + lane_of_four, (uint64_t)tag << 32 | value);
+    }
+    // lane i reads what slice i says (of q only if `both`); false: given up
+    __device__ __forceinline__ bool hear(int lane, bool both, int spin_limit, Half &p, Half &q) const
+    {
+        const uint64_t *from = record(lane < slices ? lane : 0);
+        const uint32_t tag = call + number;
         for (int poll = 0; poll < spin_limit; ++poll) {
+            uint64_t word[8] = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) word[i] = get(from + i);
+            if (both) {
+#pragma unroll
+                for (int i = 4; i < 8; ++i) word[i] = get(from + i);
+            }
             bool there = true;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint64_t word = __hip_atomic_load(from + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                value[i] = (uint32_t)word;
-                there &= (uint32_t)(word >> 32) == number;
+            for (int i = 0; i < 4; ++i) p.value[i] = (uint32_t)word[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) there &= (uint32_t)(word[i] >> 32) == (tag ^ (i == 3 ? p.check() : 0u));
+            if (both) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q.value[i] = (uint32_t)word[4 + i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) there &= (uint32_t)(word[4 + i] >> 32) == (tag ^ (i == 3 ? q.check() : 0u));
             }
             if (__all(there)) return true;
-            if ((poll & 15) == 15 && __hip_atomic_load(state, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0) return false;
+            if ((poll & 15) == 15 && somebody_alone()) return false;
         }
         return false;
+    }
+    __device__ __forceinline__ void leave_mark() const { put(marks() + slice, (uint64_t)call << 32 | 2u); }
+    // (by a wave) the others' marks are there, or it has been long enough: then they find nothing and walk alone
+    __device__ __forceinline__ void wait_for_marks(int lane, int spin_limit) const
+    {
+        for (int poll = 0; poll < spin_limit; ++poll)
+            if (__all(lane >= slices || lane == slice || get(marks() + lane) == ((uint64_t)call << 32 | 2u))) return;
     }
 };
 
 __device__ __forceinline__ double from_words(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
-
-__global__ void __launch_bounds__(256)
-sample_clear_kernel(uint64_t *words, int64_t n)
-{
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = 0;
-}
 
 // The kernel's arguments, read where they are needed: held in scalar registers from the start, as the compiler would have it, they
 // leave too few for the polynomial's coefficients, which then take vector registers.
@@ -277,485 +346,580 @@ __device__ __forceinline__ ArgsHere args_here()
     return (ArgsHere)p;
 }
 
-// add(r, w): the weights of a thread's entries, in order, four at a time of run r
-template <typename R, int RUNS, typename F>
-__device__ __forceinline__ void each_four(R (&runs)[RUNS], double top, double heat, const F &add)
-{
-#pragma unroll
-    for (int r = 0; r < RUNS; ++r) {
-        runs[r].stay_packed();
-#pragma unroll
-        for (int h = 0; h < 8; h += 4) {
-            const float l[4] = {runs[r].entry(h), runs[r].entry(h + 1), runs[r].entry(h + 2), runs[r].entry(h + 3)};
-            double w[4];
-            weights(l, top, heat, w);
-            add(r, w);
-        }
-    }
-}
-// residual(r, v): max(p - a q, 0) of the same, and the weights of q
-template <typename P, typename Q, int RUNS, typename F>
-__device__ __forceinline__ void each_four(P (&x)[RUNS], Q (&y)[RUNS], double top, double heat, double draft_top, double draft_heat, double per_total,
-                                          double takes, const F &add)
-{
-#pragma unroll
-    for (int r = 0; r < RUNS; ++r) {
-        x[r].stay_packed();
-        y[r].stay_packed();
-#pragma unroll
-        for (int h = 0; h < 8; h += 4) {
-            const float l[4] = {x[r].entry(h), x[r].entry(h + 1), x[r].entry(h + 2), x[r].entry(h + 3)};
-            const float m[4] = {y[r].entry(h), y[r].entry(h + 1), y[r].entry(h + 2), y[r].entry(h + 3)};
-            double v[4], w[4];
-            weights(l, top, heat, v);
-            weights(m, draft_top, draft_heat, w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __builtin_fmax(__builtin_fma(-takes, w[i], v[i] * per_total), 0.0);
-            add(r, v, w);
-        }
-    }
-}
-// A sum that is worked out here, and not where it is used
-__device__ __forceinline__ void add_four(double &sum, const double (&w)[4])
-{
-    sum += (w[0] + w[1]) + (w[2] + w[3]);
-    asm volatile("" : "+v"(sum));
-}
+__device__ __forceinline__ double sum_four(const double (&w)[4]) { return (w[0] + w[1]) + (w[2] + w[3]); }
 
 // The walk is a sequence of passes over a slice (over all of them, one after the other, where a workgroup is alone): the weights of a node's
-// rows and their sums; the sums of max(p - a q, 0) after a refusal; the search for the next token.
-enum Pass { kRows, kResidual, kDraw };
+// rows and their sums; the sums of max(p - a q, 0) after a refusal; the search for the next token.  Between two passes the first wave joins
+// the sums of the waves, exchanges them with the group, and decides what comes next (all of it in Walk, in LDS).
+enum Pass { kRows, kResidual, kDraw, kEnd, kGiveUp };
 
-template <typename TT, typename TD, int EPT>
+struct Walk {
+    int32_t pass, cur, len, next, writer;  // writer: the slice whose workgroup draws the token and writes the outputs
+    int32_t refused, removed;              // the children before these nodes have been refused, and taken out of the rows in registers
+    float top, draft_top;                  // the largest entries of the rows
+    double total;                          // the sum of the target's weights relative to its largest entry
+    double per_total, per_draft_total;     // inverse sums
+    double taken, mass, left;              // a, S, W
+    double rest;                           // what the sum has to pass in the writer's slice
+};
+
+template <typename TT, typename TD>
 __global__ void __launch_bounds__(NT, 4)
 tree_sample_kernel(SampleArgs)
 {
-    const ArgsHere a = args_here();
-    constexpr int RUNS = EPT / 8;  // a thread's entries: runs of 8, the lanes' runs side by side; a wave's are contiguous
-    constexpr int SLICE = NT * EPT;
-    static_assert(LS_MAX_TREE <= NT, "a thread per node");
-    __shared__ int32_t tok[LS_MAX_TREE], path[LS_MAX_TREE], has_kids[LS_MAX_TREE];
-    __shared__ float accept_u[LS_MAX_TREE], kid_x[LS_MAX_TREE], kid_y[LS_MAX_TREE];  // kid: logits of both models
-    __shared__ double new_logit[LS_MAX_TREE], new_total[LS_MAX_TREE];  // of the new tokens: logit / temperature below the largest, and the sum of the weights
+    constexpr int NODES = LS_MAX_TREE / NT;  // of a thread: tid, tid + NT
+    static_assert(WAVES == 4, "their sums are joined in four lanes");
+    // per node: token, path, first child, number for its acceptance, and (for children) the logits of both models; of the new tokens: logit / temperature
+    // below the largest, and the sum of the weights.  Then the slice's entries of both rows.
+    extern __shared__ __align__(16) uint8_t lds[];
     __shared__ uint64_t kid_mask[LS_MAX_TREE / kWave];
     __shared__ float wave_top[2][WAVES];
     __shared__ double wave_sum[2][WAVES];
     __shared__ int32_t wave_best[WAVES];
-    // of the slices: largest entry, sum of the weights relative to it, and where the largest of p is first; then the sums of max(p - a q, 0) and of q
+    // of the slices, where there is no group: largest entries, sums, and where the largest of p is first
     __shared__ float part_top[2][kSampleSlices];
     __shared__ double part_sum[2][kSampleSlices];
     __shared__ int32_t part_best[kSampleSlices];
-    __shared__ int32_t first_sh, heard_sh[2];
+    __shared__ Walk walk;
+    __shared__ int32_t flag_sh[2];
 
-    const int b = (int)(blockIdx.x / (uint32_t)a->slices), tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const ArgsHere a = args_here();
+    const int slices = a->slices, vocab = a->vocab;
+    const int b = (int)(blockIdx.x / (uint32_t)slices), thread = threadIdx.x, wave = uniform(thread >> 6);
+    int tid = thread;
     Exchange ex;
-    ex.slices = a->slices, ex.slice = (int)(blockIdx.x % (uint32_t)a->slices), ex.spin_limit = a->spin_limit, ex.number = 0;
-    ex.state = a->records + (int64_t)b * (2 * a->slices + 1) * kRecordWords;
-    ex.records = ex.state + kRecordWords;
-    bool alone = false;  // this workgroup does all slices
-    const bool told = a->slices > 1;
+    ex.slices = slices, ex.slice = (int)(blockIdx.x % (uint32_t)slices), ex.call = a->call, ex.number = 0;
+    ex.words = a->records + (int64_t)b * ex.n_words();
+    const int n_nodes = (a->n_tree + kWave - 1) / kWave * kWave, slice_size = a->slice;
+    double *const new_logit = (double *)lds, *const new_total = new_logit + n_nodes;
+    int32_t *const tok = (int32_t *)(new_total + n_nodes), *const path = tok + n_nodes, *const first_kid = path + n_nodes;
+    float *const accept_u = (float *)(first_kid + n_nodes), *const kid_x = accept_u + n_nodes, *const kid_y = kid_x + n_nodes;
+    TT *const x_lds = (TT *)(kid_y + n_nodes);
+    TD *const y_lds = (TD *)(x_lds + slice_size);
+    const bool told = slices > 1;
+    bool alone = !told;  // this workgroup does all slices
     // node's rows of logits
-    auto target_row = [&](int node) __attribute__((always_inline)) {
-        const ArgsHere h = args_here();
-        return (const TT *)h->target + b * h->t_stride[0] + node * h->t_stride[1];
+    const TT *const target = (const TT *)a->target + b * a->t_stride[0];
+    const TD *const draft = (const TD *)a->draft + (a->draft ? b * a->d_stride[0] : 0);
+    const int64_t t_node = a->t_stride[1], d_node = a->d_stride[1];
+    auto target_row = [&](int node) __attribute__((always_inline)) { return target + node * t_node; };
+    auto draft_row = [&](int node) __attribute__((always_inline)) { return draft + node * d_node; };
+    // Asks for a node's part of this slice, so that it is in the L2 when it is needed: what comes, a value a line, is thrown away.  (Not the first wave:
+    // what it reads of the others would wait for it.)
+    float touched[2] = {0.f, 0.f};
+    auto touch = [&](int node, bool both) __attribute__((always_inline)) {
+        const int line = tid - kWave, x_at = ex.slice * slice_size + line * (128 / (int)sizeof(TT)), y_at = ex.slice * slice_size + line * (128 / (int)sizeof(TD));
+        if (line < 0) return;
+        if (line < slice_size * (int)sizeof(TT) / 128 && x_at < vocab) touched[0] = Elem<TT>::load(target_row(node) + x_at);
+        if (both && line < slice_size * (int)sizeof(TD) / 128 && y_at < vocab) touched[1] = Elem<TD>::load(draft_row(node) + y_at);
     };
-    auto draft_row = [&](int node) __attribute__((always_inline)) {
-        const ArgsHere h = args_here();
-        return (const TD *)h->draft + b * h->d_stride[0] + node * h->d_stride[1];
-    };
+    auto throw_away = [&]() __attribute__((always_inline)) { asm volatile("" ::"v"(touched[0]), "v"(touched[1])); };
 
-    // thread i has node i
-    const bool is_node = tid < a->n_tree;
-    int my_parent = -1, my_tok = -1, bad = 0;
-    if (is_node) {
-        my_parent = a->parents[(int64_t)b * a->n_tree + tid];
-        my_tok = a->draft_tokens[(int64_t)b * a->n_tree + tid];
-        accept_u[tid] = a->accept_uniforms[(int64_t)b * a->n_tree + tid];
-        tok[tid] = my_tok;
-        path[tid] = tid == 0 ? 0 : -1;
-        has_kids[tid] = 0;
-        if (my_parent < -1 || my_parent >= tid) bad = 1, my_parent = -1;
-        if ((uint32_t)my_tok >= (uint32_t)a->vocab) my_parent = -1;  // nobody's child
+    int my_parent[NODES], my_tok[NODES];
+    float my_u[NODES];
+#pragma unroll
+    for (int n = 0; n < NODES; ++n) {
+        const int node = tid + n * NT;
+        const int64_t at = (int64_t)b * a->n_tree + node;
+        my_parent[n] = my_tok[n] = -1, my_u[n] = 0.f;
+        if (node < a->n_tree) my_parent[n] = a->parents[at], my_tok[n] = a->draft_tokens[at], my_u[n] = a->accept_uniforms[at];
     }
-    if (tid == 0) heard_sh[0] = 0, heard_sh[1] = told && __hip_atomic_load(ex.state, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
-    __syncthreads();
-    if (bad) heard_sh[0] = 1;
-    if (my_parent >= 0) has_kids[my_parent] = 1;
-    __syncthreads();
-    int err = uniform(heard_sh[0]);
-    if (uniform(heard_sh[1])) return;  // somebody walks alone already
-
     float temp = a->temperature[b], draft_temp = a->draft_temperature ? a->draft_temperature[b] : temp;
-    if (!(temp >= 0.f && temp <= FLT_MAX)) err |= 2, temp = 0.f;
-    if (!(draft_temp >= 0.f && draft_temp <= FLT_MAX)) err |= 2, draft_temp = 0.f;
+    touch(0, a->draft != nullptr);
+    bool bad = false;
+#pragma unroll
+    for (int n = 0; n < NODES; ++n) {
+        const int node = tid + n * NT;
+        if (node < n_nodes) path[node] = node == 0 ? 0 : -1, first_kid[node] = kNone, tok[node] = my_tok[n], accept_u[node] = my_u[n];
+        if (my_parent[n] < -1 || my_parent[n] >= node) bad = true, my_parent[n] = -1;
+        if ((uint32_t)my_tok[n] >= (uint32_t)vocab) my_parent[n] = -1;  // nobody's child
+    }
+    if (tid == 0) {
+        flag_sh[0] = 0, flag_sh[1] = told && ex.somebody_alone();
+        walk.pass = kRows, walk.cur = 0, walk.len = 1, walk.next = -1, walk.writer = 0;
+    }
+    __syncthreads();
+    if (bad) flag_sh[0] = 1;
+#pragma unroll
+    for (int n = 0; n < NODES; ++n)
+        if (my_parent[n] >= 0) atomicMin(&first_kid[my_parent[n]], tid + n * NT);
+    int err = 0;
+    if (!(temp >= 0.f && temp <= FLT_MAX)) err = 2, temp = 0.f;
+    if (!(draft_temp >= 0.f && draft_temp <= FLT_MAX)) err = 2, draft_temp = 0.f;
     const bool greedy = temp == 0.f;
     const bool drawn = a->draft && !greedy && draft_temp > 0.f;
-    const double heat = uniform(1.4426950408889634074 / (greedy ? 1.0 : (double)temp));
-    const double draft_heat = uniform(drawn ? 1.4426950408889634074 / (double)draft_temp : 0.0);
+    const double heat = 1.4426950408889634074 / (greedy ? 1.0 : (double)temp);
+    const double draft_heat = drawn ? 1.4426950408889634074 / (double)draft_temp : 0.0;
+    throw_away();
+    __syncthreads();
+    err |= uniform(flag_sh[0]);
+    if (uniform(flag_sh[1])) return;
 
-    Pass pass = kRows;
-    int cur = 0, len = 1, next = -1;
-    int writer = 0;                     // the slice whose workgroup draws the token and writes the outputs
-    bool inner = false;                 // the node has children, and what they were drawn from counts
-    float wt = 0.f, wq = 0.f;           // the wave's largest entries
-    float top = 0.f, draft_top = 0.f;   // the largest of the rows
-    double total = 0, per_total = 0, per_draft_total = 0;  // sum of the weights relative to it; inverse sums
-    double part = 0;                    // lane i: slice i's share of `mass`
-    double taken = 0, mass = 1, left = 1;  // a, S, W
-    double rest = 0;                    // what the sum has to pass in the writer's slice
-    int refused = 0, removed = 0;       // the children before these nodes have been refused, and taken out of the rows
-    Run<TT> x[RUNS];
-    Run<TD> y[RUNS];
-
-    const int own = wave * (kWave * EPT) + lane * 8;  // this thread's first entry in a slice
+    // A thread's entries: runs of 8, the lanes' runs side by side; a wave's are contiguous.  What a thread reads of its runs in LDS it has written itself.
+    const int wave_size = slice_size / WAVES, runs = wave_size / (kWave * 8);
 
     while (true) {
-        float my_x = -INFINITY, my_y = -INFINITY;  // this thread's node is a child: its token's logits
-        const bool kid = my_parent == cur && tid > cur;
-        if (pass == kRows) {
-            inner = drawn && uniform(has_kids[cur]);
-            if (kid) {
-                my_x = entry_of(target_row(cur), my_tok);
-                if (inner) my_y = entry_of(draft_row(cur), my_tok);
+        // (known anew in each turn: what can be worked out from it before the loop would take most of the registers)
+        asm volatile("" : "+v"(tid));
+        const int lane = tid & 63, own = wave * wave_size + lane * 8;
+        const int pass = uniform(walk.pass), cur = uniform(walk.cur);
+        if (pass == kEnd) break;
+        if (pass == kGiveUp) {  // the first one to give up goes on alone, from the root
+            __syncthreads();
+            if (tid == 0) {
+                flag_sh[0] = ex.go_alone();
+                walk.pass = kRows, walk.cur = 0, walk.len = 1, walk.next = -1, walk.writer = 0;
             }
-            taken = 0, mass = left = 1;
-            refused = 0;
+            for (int i = tid; i < n_nodes; i += NT) path[i] = i == 0 ? 0 : -1;
+            __syncthreads();
+            if (!uniform(flag_sh[0])) return;
+            alone = true;
+            continue;
         }
+        const int kid = uniform(first_kid[cur]);
+        const bool inner = drawn && kid != kNone;  // the node has children, and what they were drawn from counts
+        if (pass == kDraw && !alone && uniform(walk.writer) != ex.slice) {
+            if (tid == 0) ex.leave_mark();
+            return;
+        }
+        const float top = walk.top, draft_top = walk.draft_top;
+        const double per_total = walk.per_total, per_draft_total = walk.per_draft_total, takes = walk.taken * per_draft_total;
+        int slice = alone ? 0 : ex.slice, end = alone ? slices : ex.slice + 1;
+        if (pass == kDraw) slice = uniform(walk.writer), end = slice + 1;
         ++ex.number;
-        bool heard = true;
-        int slice = alone ? 0 : ex.slice, end = alone ? a->slices : ex.slice + 1;
-        if (pass == kDraw) slice = writer, end = writer + 1;
-        for (; slice < end && heard; ++slice) {
-            if (pass == kRows || alone) {
-                const TT *row = target_row(cur);
-                const int at = slice * SLICE + own;
+        float wt = -INFINITY, wq = -INFINITY;  // the wave's largest entries
+        for (; slice < end; ++slice) {
+            if (pass == kRows || (alone && told)) {
+                float my_x[NODES], my_y[NODES];
 #pragma unroll
-                for (int r = 0; r < RUNS; ++r) load_run(row, at + r * kWave * 8, a->vocab, x[r]);
-                if (inner) {
-                    const TD *drow = draft_row(cur);
-#pragma unroll
-                    for (int r = 0; r < RUNS; ++r) load_run(drow, at + r * kWave * 8, a->vocab, y[r]);
+                for (int n = 0; n < NODES; ++n) {
+                    my_x[n] = my_y[n] = -INFINITY;
+                    if (pass == kRows && my_parent[n] == cur) {
+                        my_x[n] = entry_of(target_row(cur), my_tok[n]);
+                        if (inner) my_y[n] = entry_of(draft_row(cur), my_tok[n]);
+                    }
                 }
-                // the largest entries; +inf counts as the largest finite number (of its type), which is what it is from here on
-                auto largest = [&](auto &runs) __attribute__((always_inline)) {
-                    float m = -INFINITY;
-#pragma unroll
-                    for (int r = 0; r < RUNS; ++r) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) m = fmaxf(m, runs[r].entry(e));
-                        runs[r].stay_packed();
+                const TT *row = target_row(cur);
+                const TD *drow = inner ? draft_row(cur) : nullptr;
+                float m = -INFINITY, mq = -INFINITY;
+                auto fetch = [&](auto *from, auto *to, int at, float &most) __attribute__((always_inline)) {  // entries behind the row's end, one by one
+                    using T = std::remove_reference_t<decltype(*to)>;
+#pragma unroll 1
+                    for (int e = 0; e < 8; ++e) {
+                        const T v = at + e < vocab ? from[at + e] : minus_inf<T>();
+                        to[e] = v;
+                        most = fmaxf(most, Elem<T>::load(&v));
                     }
-                    m = lanes_max(m);
-                    if (m == INFINITY) {
-                        m = -INFINITY;
-#pragma unroll
-                        for (int r = 0; r < RUNS; ++r)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                runs[r].set(e, runs[r].entry(e) == INFINITY, runs[r].kLargestBits);
-                                m = fmaxf(m, runs[r].entry(e));
-                            }
-                        m = lanes_max(m);
-                    }
-                    return m;
                 };
-                wt = largest(x);
-                wq = inner ? largest(y) : -INFINITY;
-                removed = 0;
+#pragma unroll 1
+                for (int r0 = 0; r0 < runs; r0 += 2) {
+                    Run<TT> x[2] = {};
+                    Run<TD> y[2] = {};
+                    const int at = slice * slice_size + own + r0 * kWave * 8;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (r0 + i < runs && at + i * kWave * 8 + 8 <= vocab) x[i] = run_of_row(row + at + i * kWave * 8);
+                    if (inner)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            if (r0 + i < runs && at + i * kWave * 8 + 8 <= vocab) y[i] = run_of_row(drow + at + i * kWave * 8);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (r0 + i < runs) {
+                            const int in = own + (r0 + i) * kWave * 8;
+                            if (at + i * kWave * 8 + 8 <= vocab) {
+                                run_to_lds(x[i], x_lds + in);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) m = fmaxf(m, x[i].entry(e));
+                            } else {
+                                fetch(row, x_lds + in, slice * slice_size + in, m);
+                            }
+                        }
+                    if (inner)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            if (r0 + i < runs) {
+                                const int in = own + (r0 + i) * kWave * 8;
+                                if (at + i * kWave * 8 + 8 <= vocab) {
+                                    run_to_lds(y[i], y_lds + in);
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) mq = fmaxf(mq, y[i].entry(e));
+                                } else {
+                                    fetch(drow, y_lds + in, slice * slice_size + in, mq);
+                                }
+                            }
+                }
+                // +inf counts as the largest finite number of its type, which is what it is from here on
+                auto whole = [&](auto *entries, float most) __attribute__((always_inline)) {
+                    using T = std::remove_reference_t<decltype(*entries)>;
+                    most = lanes_max(most);
+                    if (most != INFINITY) return most;
+                    most = -INFINITY;
+#pragma unroll 1
+                    for (int r = 0; r < runs; ++r)
+#pragma unroll 1
+                        for (int e = 0; e < 8; ++e) {
+                            T *const at = entries + own + r * kWave * 8 + e;
+                            if (Elem<T>::load(at) == INFINITY) *at = largest_bits<T>();
+                            most = fmaxf(most, Elem<T>::load(at));
+                        }
+                    return lanes_max(most);
+                };
+                wt = whole(x_lds, m);
+                wq = inner ? whole(y_lds, mq) : -INFINITY;
+                if (pass == kRows) {
+#pragma unroll
+                    for (int n = 0; n < NODES; ++n) {
+                        const bool is_kid = my_parent[n] == cur;
+                        const uint64_t kids = __ballot(is_kid);
+                        if (lane == 0) kid_mask[wave + n * WAVES] = kids;
+                        if (is_kid) kid_x[tid + n * NT] = my_x[n], kid_y[tid + n * NT] = my_y[n];
+                    }
+                    if (!alone && kid != kNone) touch(kid, drawn && uniform(first_kid[kid]) != kNone);
+                }
             }
             // refused tokens have no weight any more
             if (pass != kRows) {
-                for (int w = removed / kWave; w * kWave < refused; ++w)
-                    for (uint64_t m = uniform(kid_mask[w]); m; m &= m - 1) {
+                const int refused = uniform(walk.refused), removed = alone && told ? 0 : uniform(walk.removed);
+                for (int w = removed / kWave; w * kWave < refused; ++w) {
+                    uint64_t m = uniform(kid_mask[w]);
+                    if (w == removed / kWave) m &= ~0ull << (removed % kWave);
+                    for (; m; m &= m - 1) {
                         const int k = w * kWave + __builtin_ctzll(m);
                         if (k >= refused) break;
-                        const int at = __builtin_amdgcn_readfirstlane(tok[k] - slice * SLICE - wave * (kWave * EPT));
-                        if (k < removed || (uint32_t)at >= (uint32_t)(kWave * EPT)) continue;
-                        const bool my_run = lane == (at >> 3) % kWave;
-#pragma unroll
-                        for (int r = 0; r < RUNS; ++r) {
-                            if (r != at / (8 * kWave)) continue;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                x[r].set(e, my_run && e == at % 8, x[r].kMinusInf);
-                                if (inner) y[r].set(e, my_run && e == at % 8, y[r].kMinusInf);
-                            }
+                        const int at = tok[k] - slice * slice_size;
+                        if ((uint32_t)at < (uint32_t)slice_size && at / wave_size == wave && at / 8 % kWave == lane) {
+                            x_lds[at] = minus_inf<TT>();
+                            if (inner) y_lds[at] = minus_inf<TD>();
                         }
                     }
-                removed = refused;
+                }
             }
             if (pass == kDraw) break;
-            // sums over the thread, the wave, the slice (in waves 0 and 1); then to everybody
+            // sums over the thread and the wave: of the weights relative to the wave's largest entries, or of max(p - a q, 0) and of q
             double s = 0, sq = 0;
-            if (pass == kRows) {  // of the weights relative to the wave's largest entries
-                each_four(x, wt, heat, [&](int, const double (&w)[4]) __attribute__((always_inline)) { add_four(s, w); });
-                if (inner) each_four(y, wq, draft_heat, [&](int, const double (&w)[4]) __attribute__((always_inline)) { add_four(sq, w); });
-            } else if (inner) {   // of max(p - a q, 0), and of q
-                each_four(x, y, top, heat, draft_top, draft_heat, per_total, taken * per_draft_total,
-                          [&](int, const double (&v)[4], const double (&w)[4]) __attribute__((always_inline)) { add_four(s, v), add_four(sq, w); });
-                sq *= per_draft_total;
+            const bool residual = pass == kResidual;
+            const double x_top = residual ? top : wt, y_top = residual ? draft_top : wq, scale = residual ? per_total : 1.0;
+            if (inner) {
+                const double y_scale = residual ? takes : 0.0;
+#pragma unroll 1
+                for (int r = 0; r < runs; ++r) {
+                    const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
+                    const Run<TD> y = run_of_lds(y_lds + own + r * kWave * 8);
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        float l[4];
+                        double v[4], w[4];
+                        x.four(h, l);
+                        weights(l, x_top, heat, v);
+                        y.four(h, l);
+                        weights(l, y_top, draft_heat, w);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = __builtin_fmax(__builtin_fma(-y_scale, w[i], v[i] * scale), 0.0);
+                        s += sum_four(v);
+                        sq += sum_four(w);
+                    }
+                }
+                sq = lanes_sum(residual ? sq * per_draft_total : sq);
             } else {
-                each_four(x, top, heat, [&](int, const double (&w)[4]) __attribute__((always_inline)) { add_four(s, w); });
-                s *= per_total;
+#pragma unroll 1
+                for (int r = 0; r < runs; ++r) {
+                    const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        float l[4];
+                        double w[4];
+                        x.four(h, l);
+                        weights(l, x_top, heat, w);
+                        s += sum_four(w);
+                    }
+                }
+                s *= scale;
             }
             s = lanes_sum(s);
-            if (inner) sq = lanes_sum(sq);
-            if (greedy && pass == kRows) {
-                int best = kNone;
-                const int at = slice * SLICE + own;
-#pragma unroll
-                for (int r = RUNS - 1; r >= 0; --r)
-#pragma unroll
-                    for (int e = 7; e >= 0; --e)
-                        if (x[r].entry(e) == wt) best = at + r * kWave * 8 + e;
-                best = wt > -INFINITY ? lanes_min(best) : kNone;
-                if (lane == 0) wave_best[wave] = best;
-            }
-            if (lane == 0) {
-                wave_top[0][wave] = wt, wave_sum[0][wave] = s;
-                wave_top[1][wave] = wq, wave_sum[1][wave] = sq;
-            }
-            __syncthreads();
             if (pass == kRows) {
-                const uint64_t kids = __ballot(kid);
-                if (lane == 0) kid_mask[wave] = kids;
-                if (kid) kid_x[tid] = my_x, kid_y[tid] = my_y;
+                if (lane == 0) wave_top[0][wave] = wt, wave_top[1][wave] = wq;
+                if (greedy) {
+                    int best = kNone;
+#pragma unroll 1
+                    for (int r = runs - 1; r >= 0; --r) {
+                        const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
+#pragma unroll
+                        for (int e = 7; e >= 0; --e)
+                            if (x.entry(e) == wt) best = slice * slice_size + own + r * kWave * 8 + e;
+                    }
+                    best = wt > -INFINITY ? lanes_min(best) : kNone;
+                    if (lane == 0) wave_best[wave] = best;
+                }
             }
-            if (wave == 0 || (wave == 1 && inner)) {
-                const bool mine = lane < WAVES;
-                double sum = mine ? wave_sum[wave][lane] : 0.0;
+            if (lane == 0) wave_sum[0][wave] = s, wave_sum[1][wave] = sq;
+            __syncthreads();
+            if (wave == 0) {
+                // The waves' sums to the slice's: lanes 0 to 3 have p's, lanes 4 to 7 q's
+                const bool mine = lane < 2 * WAVES;
+                const int which = lane >> 2;
+                double sum = mine ? wave_sum[which][lane & 3] : 0.0;
                 float mm = 0.f;
                 int best = kNone;
                 if (pass == kRows) {
-                    const float m = mine ? wave_top[wave][lane] : -INFINITY;
-                    mm = lanes_max(m);
-                    sum *= weight(m, mm, wave ? draft_heat : heat);
-                    if (greedy) best = lanes_min(mine && m == mm ? wave_best[lane] : kNone);
+                    const float m = mine ? wave_top[which][lane & 3] : -INFINITY;
+                    mm = quad_max(m);
+                    sum *= weight(m, mm, which == 0 ? heat : draft_heat);
+                    if (greedy) best = lanes_min(lane < WAVES && m == mm ? wave_best[lane] : kNone);
                 }
-                sum = lanes_sum(sum);
-                if (alone || !told) {
-                    if (lane == 0) {
-                        part_top[wave][slice] = mm, part_sum[wave][slice] = sum;
-                        if (wave == 0) part_best[slice] = best;
-                        heard_sh[wave] = 1;
+                sum = quad_sum(sum);
+                Half p = {}, q = {};
+                if (alone) {
+                    if ((lane & 3) == 0 && mine) {
+                        part_top[which][slice] = mm, part_sum[which][slice] = sum;
+                        if (lane == 0) part_best[slice] = best;
                     }
+                    if (slice + 1 < end) goto next_slice;
                 } else {
                     const uint64_t bits = __builtin_bit_cast(uint64_t, sum);
-                    ex.tell(wave, lane, lane == 0 ? __float_as_uint(mm) : lane == 1 ? (uint32_t)bits : lane == 2 ? (uint32_t)(bits >> 32) : (uint32_t)best);
-                    uint32_t value[4];
-                    const bool all = ex.hear(wave, lane, value);
-                    if (lane < a->slices) {
-                        part_top[wave][lane] = __uint_as_float(value[0]);
-                        part_sum[wave][lane] = from_words(value[1], value[2]);
-                        if (wave == 0) part_best[lane] = (int)value[3];
+                    Half own_half = {{__float_as_uint(mm), (uint32_t)bits, (uint32_t)(bits >> 32), (uint32_t)best}};
+                    const int i = lane & 3;
+                    const uint32_t value = i == 0 ? own_half.value[0] : i == 1 ? own_half.value[1] : i == 2 ? own_half.value[2] : own_half.value[3];
+                    if (lane < (inner ? 8 : 4)) ex.tell(which, i, value, own_half.check());
+                    if (!ex.hear(lane, inner, args_here()->spin_limit, p, q)) {
+                        if (lane == 0) walk.pass = kGiveUp;
+                        goto next_slice;
                     }
-                    if (lane == 0) heard_sh[wave] = all;
                 }
-            }
-            __syncthreads();
-            heard = uniform(heard_sh[0]) && (!inner || uniform(heard_sh[1]));
-        }
-
-        if (!heard) {  // the first one to give up goes on alone, from the root
-            if (tid == 0) {
-                unsigned long long expected = 0;
-                first_sh = __hip_atomic_compare_exchange_strong((unsigned long long *)ex.state, &expected, 1ull, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                                                __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            if (!uniform(first_sh)) return;
-            alone = true;
-            pass = kRows;
-            cur = 0, len = 1;
-            path[tid] = tid == 0 ? 0 : -1;
-            __syncthreads();
-            continue;
-        }
-
-        if (pass == kDraw) {
-            // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
-            // that has any weight.
-            const double takes = inner ? taken * per_draft_total : 0.0;
-            double run[RUNS], all = 0;
-#pragma unroll
-            for (int r = 0; r < RUNS; ++r) run[r] = 0;
-            if (inner)
-                each_four(x, y, top, heat, draft_top, draft_heat, per_total, takes,
-                          [&](int r, const double (&v)[4], const double (&)[4]) __attribute__((always_inline)) { add_four(run[r], v); });
-            else
-                each_four(x, top, heat, [&](int r, const double (&w)[4]) __attribute__((always_inline)) { add_four(run[r], w); });
-#pragma unroll
-            for (int r = 0; r < RUNS; ++r) {
-                run[r] = lanes_sum(inner ? run[r] : run[r] * per_total);
-                all += run[r];
-            }
-            if (lane == 0) wave_sum[0][wave] = all;
-            if (tid == 0) first_sh = -1;
-            __syncthreads();
-            double before = 0, upto = 0;  // of the entries before the wave's; before what has been looked at
-            int at_wave = -1;
-            bool passed = false;
-            for (int w = 0; w < WAVES && !passed; ++w) {
-                const double sum = uniform(wave_sum[0][w]);
-                if (sum > 0) at_wave = w, before = upto, passed = upto + sum > rest;
-                upto += sum;
-            }
-            if (wave == at_wave) {
-                upto = before;
-                passed = false;
-                int at_run = 0;
-                Run<TT> rx = x[0];
-                Run<TD> ry = y[0];
-#pragma unroll
-                for (int r = 0; r < RUNS; ++r) {
-                    if (run[r] > 0 && !passed) {
-                        rx = x[r], ry = y[r];
-                        at_run = r, before = upto, passed = upto + run[r] > rest;
+                {
+                    // What the sums say
+                    const bool there = lane < slices;
+                    float m = -INFINITY, mq = -INFINITY;
+                    double part = 0, part_q = 0;
+                    int part_b = kNone;
+                    if (there) {
+                        m = alone ? part_top[0][lane] : __uint_as_float(p.value[0]);
+                        part = alone ? part_sum[0][lane] : from_words(p.value[1], p.value[2]);
+                        part_b = alone ? part_best[lane] : (int)p.value[3];
+                        if (inner) {
+                            mq = alone ? part_top[1][lane] : __uint_as_float(q.value[0]);
+                            part_q = alone ? part_sum[1][lane] : from_words(q.value[1], q.value[2]);
+                        }
                     }
-                    upto += run[r];
+                    double taken = 0, left = 1, pt = per_total, pd = per_draft_total;
+                    float t = top, dt = draft_top;
+                    int at_best = kNone, refused = 0;
+                    double mass = 1;
+                    if (pass == kRows) {  // (both rows, step by step together, also where there is no draft's)
+                        t = lanes_max(m), dt = lanes_max(mq);
+                        part *= weight(m, t, heat), part_q *= weight(mq, dt, draft_heat);
+                        const double total = lanes_sum(part), draft_total = lanes_sum(part_q);
+                        pt = inverse(total), pd = inverse(draft_total);
+                        pt = total > 0 ? pt : 0.0, pd = draft_total > 0 ? pd : 0.0;
+                        part *= pt;
+                        mass = total > 0 ? 1.0 : 0.0;
+                        if (greedy && total > 0) at_best = lanes_min(there && m == t ? part_b : kNone);
+                        if (lane == 0) walk.top = t, walk.draft_top = dt, walk.total = total, walk.per_total = pt, walk.per_draft_total = pd;
+                    } else {
+                        taken = walk.taken, refused = uniform(walk.refused);
+                        const double q_left = lanes_sum(part_q);
+                        mass = lanes_sum(part);
+                        if (inner && !args_here()->with_replacement) left = q_left;
+                    }
+
+                    // The children that have not been tried.  Of tokens that were chosen the refused ones' probabilities are taken off the sums as long
+                    // as much is left (then a pass over the rows makes the sums anew).
+                    int found = -1;
+                    bool again = false;
+                    const int len = uniform(walk.len);
+                    for (int w = refused / kWave; w * kWave < n_nodes && found < 0 && !again; ++w) {
+                        uint64_t k = uniform(kid_mask[w]);
+                        if (w == refused / kWave) k &= ~0ull << (refused % kWave);
+                        if (!k) continue;
+                        const int node = w * kWave + lane, my_token = tok[node];
+                        const double u = accept_u[node];
+                        const bool is_kid = k >> lane & 1;
+                        double px = weight(is_kid ? kid_x[node] : -INFINITY, t, heat) * pt, qx = weight(is_kid ? kid_y[node] : -INFINITY, dt, draft_heat) * pd;
+                        if (!inner) qx = 1.0;
+                        for (; k && found < 0 && !again; k &= k - 1) {
+                            const int i = __builtin_ctzll(k);
+                            const int token = __builtin_amdgcn_readlane(my_token, i);
+                            bool ok;
+                            if (greedy) ok = token == at_best;
+                            else ok = __ballot((px - (inner ? taken * qx : 0.0)) * left > u * qx * mass) >> i & 1;
+                            if (ok) {
+                                found = w * kWave + i;
+                                break;
+                            }
+                            refused = w * kWave + i + 1;
+                            if (greedy) continue;
+                            // the same token once more has no weight either
+                            const bool same = my_token == token;
+                            const double off = of_lane(px, i);
+                            px = same ? 0.0 : px;
+                            if (inner && same) qx = 0.0;
+                            for (int v = w; v * kWave < n_nodes; ++v)
+                                if (uniform(kid_mask[v]) >> lane & 1 && v * kWave + lane >= refused && tok[v * kWave + lane] == token)
+                                    kid_x[v * kWave + lane] = kid_y[v * kWave + lane] = -INFINITY;
+                            if (inner) {
+                                again = true;
+                            } else {
+                                mass -= off;
+                                if (token / slice_size == lane) part = __builtin_fmax(part - off, 0.0);
+                                again = mass < 0x1p-10;
+                            }
+                        }
+                    }
+                    int next_pass = kRows, writer = 0;
+                    if (found >= 0) {
+                        if (lane == 0) {
+                            path[len] = found;
+                            new_logit[len - 1] = ((double)kid_x[found] - t) / (greedy ? 1.0 : (double)temp), new_total[len - 1] = walk.total;
+                            walk.len = len + 1, walk.cur = found;
+                        }
+                    } else if (again) {
+                        if (inner && lane == 0) walk.taken = left > 0 ? fmin(taken + mass / left, 1e300) : 1e300;  // (finite: q(v) = 0 stays out of it)
+                        if (!inner && lane == 0) walk.taken = 0;
+                        next_pass = kResidual;
+                    } else {  // the path ends here
+                        next_pass = kEnd;
+                        int next = -1;
+                        double rest = 0;
+                        if (greedy) {
+                            next = at_best == kNone ? -1 : at_best;
+                        } else if (mass > 0) {
+                            const double upto = lanes_scan(part), point = (double)args_here()->sample_uniforms[b] * mass;
+                            const uint64_t passed = __ballot(part > 0 && upto > point), some = __ballot(part > 0);
+                            if (some) {
+                                writer = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);
+                                rest = point - of_lane(upto - part, writer);
+                                next_pass = kDraw;
+                            }
+                        }
+                        if (lane == 0) {
+                            walk.next = next, walk.rest = rest, walk.writer = writer;
+                            if (pass == kRows) walk.taken = 0;
+                        }
+                    }
+                    if (lane == 0) {
+                        walk.pass = next_pass;
+                        walk.removed = pass == kRows ? 0 : uniform(walk.refused);
+                        walk.refused = refused;
+                    }
                 }
-                double v[8], sum = 0;
+            next_slice:;
+            }
+            __syncthreads();
+            throw_away();
+        }
+        if (pass != kDraw) continue;
+
+        // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
+        // that has any weight.
+        const double rest = walk.rest;
+        // the residual's eight entries of a run, and their sum
+        auto residual_run = [&](int r, double (&v)[8]) __attribute__((always_inline)) {
+            const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                float l[4];
+                double w[4];
+                x.four(h, l);
+                weights(l, top, heat, w);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[h + i] = w[i] * per_total;
+            }
+            if (inner) {
+                const Run<TD> y = run_of_lds(y_lds + own + r * kWave * 8);
 #pragma unroll
                 for (int h = 0; h < 8; h += 4) {
-                    const float l[4] = {rx.entry(h), rx.entry(h + 1), rx.entry(h + 2), rx.entry(h + 3)};
+                    float l[4];
                     double w[4];
-                    weights(l, top, heat, w);
+                    y.four(h, l);
+                    weights(l, draft_top, draft_heat, w);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[h + i] = w[i] * per_total;
-                }
-                if (inner)
-#pragma unroll
-                    for (int h = 0; h < 8; h += 4) {
-                        const float l[4] = {ry.entry(h), ry.entry(h + 1), ry.entry(h + 2), ry.entry(h + 3)};
-                        double w[4];
-                        weights(l, draft_top, draft_heat, w);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[h + i] = __builtin_fmax(__builtin_fma(-takes, w[i], v[h + i]), 0.0);
-                    }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[e];
-                const double scan = lanes_scan(sum);
-                const uint64_t some = __ballot(sum > 0), over = __ballot(sum > 0 && before + scan > rest);
-                if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
-                    double c = before + (scan - sum);
-                    int place = 0;
-                    passed = false;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        c += v[e];
-                        if (v[e] > 0 && !passed) place = e, passed = c > rest;
-                    }
-                    first_sh = writer * SLICE + own + at_run * kWave * 8 + place;
+                    for (int i = 0; i < 4; ++i) v[h + i] = __builtin_fmax(__builtin_fma(-takes, w[i], v[h + i]), 0.0);
                 }
             }
-            __syncthreads();
-            next = uniform(first_sh);
-            break;
-        }
-
-        // What the sums say
-        const bool mine = lane < a->slices;
-        part = mine ? part_sum[0][lane] : 0.0;
-        int best = kNone;
-        if (pass == kRows) {
-            const float m = mine ? part_top[0][lane] : -INFINITY;
-            top = lanes_max(m);
-            part *= weight(m, top, heat);
-            total = lanes_sum(part);
-            per_total = uniform(total > 0 ? 1.0 / total : 0.0);
-            if (greedy && total > 0) best = lanes_min(mine && m == top ? part_best[lane] : kNone);
-            part *= per_total;
-            if (inner) {
-                const float mq = mine ? part_top[1][lane] : -INFINITY;
-                draft_top = lanes_max(mq);
-                const double draft_total = lanes_sum(mine ? part_sum[1][lane] * weight(mq, draft_top, draft_heat) : 0.0);
-                per_draft_total = uniform(draft_total > 0 ? 1.0 / draft_total : 0.0);
-            }
-        }
-        mass = lanes_sum(part);
-        if (pass == kResidual && inner && !args_here()->with_replacement) left = lanes_sum(mine ? part_sum[1][lane] : 0.0);
-
-        // the children that have not been tried
-        int found = -1;
-        bool again = false;
-        for (int w = refused / kWave; w < LS_MAX_TREE / kWave && found < 0 && !again; ++w) {
-            uint64_t m = uniform(kid_mask[w]);
-            if (w == refused / kWave) m &= ~0ull << (refused % kWave);
-            for (; m && found < 0 && !again; m &= m - 1) {
-                const int k = w * kWave + __builtin_ctzll(m);
-                bool ok;
-                if (greedy) {
-                    ok = tok[k] == best;
-                } else {
-                    const double px = weight(kid_x[k], top, heat) * per_total, u = accept_u[k];
-                    if (inner) {
-                        const double qx = weight(kid_y[k], draft_top, draft_heat) * per_draft_total;
-                        ok = (px - taken * qx) * left > u * qx * mass;
-                    } else {
-                        ok = px > u * mass;
-                    }
-                }
-                ok = uniform((int)ok);
-                if (ok) found = k;
-                else refused = k + 1, again = !greedy;
-            }
-        }
-        if (found >= 0) {
-            if (tid == 0) path[len] = found, new_logit[len - 1] = ((double)kid_x[found] - top) / (greedy ? 1.0 : (double)temp), new_total[len - 1] = total;
-            ++len;
-            cur = found;
-            pass = kRows;
-            continue;
-        }
-        if (again) {
-            if (inner) taken = uniform(left > 0 ? fmin(taken + mass / left, 1e300) : 1e300);  // (finite: q(v) = 0 stays out of it)
-            // the same token once more has no weight either
-            if (kid && tid >= refused && my_tok == tok[refused - 1]) kid_x[tid] = kid_y[tid] = -INFINITY;
-            pass = kResidual;
-            continue;
-        }
-        // the path ends here
-        if (greedy) {
-            next = best == kNone ? -1 : best;
-        } else if (mass > 0) {
-            const double upto = lanes_scan(part), point = (double)args_here()->sample_uniforms[b] * mass;
-            const uint64_t passed = __ballot(part > 0 && upto > point), some = __ballot(part > 0);
-            writer = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);
-            rest = uniform(point - of_lane(upto - part, writer));
-            pass = kDraw;
-        }
-        if (!alone && writer != ex.slice) return;
-        if (pass != kDraw) break;
+            double sum = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += v[e];
+            return sum;
+        };
+        double v[8], all = 0;
+#pragma unroll 1
+        for (int r = 0; r < runs; ++r) all += lanes_sum(residual_run(r, v));
+        if (lane == 0) wave_sum[0][wave] = all;
         __syncthreads();
+        double before = 0, upto = 0;  // of the entries before the wave's; before what has been looked at
+        int at_wave = -1;
+        bool passed = false;
+        for (int w = 0; w < WAVES && !passed; ++w) {
+            const double sum = uniform(wave_sum[0][w]);
+            if (sum > 0) at_wave = w, before = upto, passed = upto + sum > rest;
+            upto += sum;
+        }
+        if (wave == at_wave) {
+            upto = before;
+            passed = false;
+            int at_run = 0;
+#pragma unroll 1
+            for (int r = 0; r < runs && !passed; ++r) {
+                const double sum = lanes_sum(residual_run(r, v));
+                if (sum > 0) at_run = r, before = upto, passed = upto + sum > rest;
+                upto += sum;
+            }
+            const double sum = residual_run(at_run, v), scan = lanes_scan(sum);
+            const uint64_t some = __ballot(sum > 0), over = __ballot(sum > 0 && before + scan > rest);
+            if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
+                double c = before + (scan - sum);
+                int place = 0;
+                passed = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    c += v[e];
+                    if (v[e] > 0 && !passed) place = e, passed = c > rest;
+                }
+                walk.next = uniform(walk.writer) * slice_size + own + at_run * kWave * 8 + place;
+            }
+        }
+        __syncthreads();
+        break;
     }
+
+    // The outputs
+    const ArgsHere h = args_here();
+    if (!alone && uniform(walk.writer) != ex.slice) {
+        if (tid == 0) ex.leave_mark();
+        return;
+    }
+    const int len = uniform(walk.len), next = uniform(walk.next);
     if (tid == 0) {
         if (next >= 0) {
-            const float l = entry_of(target_row(cur), next);
-            new_logit[len - 1] = ((double)l - top) / (greedy ? 1.0 : (double)temp), new_total[len - 1] = total;
+            new_logit[len - 1] = ((double)entry_of(target_row(walk.cur), next) - walk.top) / (greedy ? 1.0 : (double)temp);
+            new_total[len - 1] = walk.total;
         } else {
             new_logit[len - 1] = -INFINITY, new_total[len - 1] = 1.0;
             err |= 4;
         }
-        const ArgsHere h = args_here();
         h->len[b] = len;
         h->next[b] = next;
         if (h->err_flag) h->err_flag[b] = err;
     }
     __syncthreads();
-    const ArgsHere h = args_here();
-    if (tid < h->n_tree) {
-        const int64_t at = (int64_t)b * h->n_tree + tid;
-        h->path[at] = path[tid];
-        if (h->logprobs) h->logprobs[at] = tid < len ? (float)(new_logit[tid] - log(new_total[tid])) : 0.f;
+    for (int i = tid; i < h->n_tree; i += NT) {
+        const int64_t at = (int64_t)b * h->n_tree + i;
+        h->path[at] = path[i];
+        if (h->logprobs) h->logprobs[at] = i < len ? (float)(new_logit[i] - log(new_total[i])) : 0.f;
     }
+    if (!told) return;
+    if (wave == 0 && !alone) ex.wait_for_marks(tid, h->spin_limit);
+    __syncthreads();
+    for (int i = tid; i < ex.n_words(); i += NT) Exchange::put(ex.words + i, 0);
 }
 
 template <typename TT, typename TD> hipError_t launch_types(const SampleArgs &a, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)a.batch * a.slices), block(NT);
-    if (a.slice == NT * 8) hipLaunchKernelGGL((tree_sample_kernel<TT, TD, 8>), grid, block, 0, stream, a);
-    else if (a.slice == NT * 16) hipLaunchKernelGGL((tree_sample_kernel<TT, TD, 16>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((tree_sample_kernel<TT, TD, 32>), grid, block, 0, stream, a);
+    const int bytes = sample_lds_bytes(a.n_tree, a.slice, sizeof(TT), a.draft ? sizeof(TD) : 0);
+    static std::atomic<uint64_t> allowed{0};
+    const hipError_t e = allow_dynamic_lds((const void *)tree_sample_kernel<TT, TD>, kSampleLds, allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((tree_sample_kernel<TT, TD>), dim3((uint32_t)a.batch * a.slices), dim3(NT), bytes, stream, a);
     return hipGetLastError();
 }
 
@@ -770,11 +934,6 @@ template <typename TT> hipError_t launch_for(const SampleArgs &a, int draft_dtyp
 
 hipError_t launch_tree_sample(const SampleArgs &a, int target_dtype, int draft_dtype, hipStream_t stream)
 {
-    if (a.slices > 1) {
-        const int64_t words = (int64_t)sample_record_bytes(a.batch, a.slices) / 8;
-        const int64_t groups = (words + 255) / 256;
-        hipLaunchKernelGGL(sample_clear_kernel, dim3(groups < 1024 ? groups : 1024), dim3(256), 0, stream, a.records, words);
-    }
     if (!a.draft) draft_dtype = target_dtype;
     if (target_dtype == LS_F32) return launch_for<float>(a, draft_dtype, stream);
     if (target_dtype == LS_F16) return launch_for<half_t>(a, draft_dtype, stream);
