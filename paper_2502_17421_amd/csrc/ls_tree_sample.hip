@@ -31,6 +31,7 @@ namespace {
 constexpr int NT = kSampleThreads;
 constexpr int WAVES = NT / kWave;
 constexpr int kNone = INT32_MAX;
+constexpr int RUN = 4;  // entries that a thread takes at a time
 template <int N> using Const = std::integral_constant<int, N>;
 
 // a b + c with c in scalar registers: for a constant c the compiler takes the form whose result is its third operand, and moves the constant there
@@ -63,13 +64,13 @@ __device__ __forceinline__ double exp2_of(double y)
 // exp((logit - top) / temperature), heat = log2(e) / temperature; 0 for -inf and NaN, also where top is -inf
 __device__ __forceinline__ double weight(float logit, double top, double heat) { return exp2_of(((double)logit - top) * heat); }
 
-// The same of four logits, step by step, so that no step waits for the one before it.  (Left to itself the compiler takes one after the other, or starts
+// The same of a run, step by step, so that no step waits for the one before it.  (Left to itself the compiler takes one after the other, or starts
 // all of a thread's at once and runs out of registers.)
-__device__ __forceinline__ void weights(const float (&logit)[4], double top, double heat, double (&w)[4])
+__device__ __forceinline__ void weights(const float (&logit)[RUN], double top, double heat, double (&w)[RUN])
 {
-    double n[4], f[4];
+    double n[RUN], f[RUN];
 #define LS_STEP(...)                        \
-    _Pragma("unroll") for (int i = 0; i < 4; ++i) __VA_ARGS__; \
+    _Pragma("unroll") for (int i = 0; i < RUN; ++i) __VA_ARGS__; \
     __builtin_amdgcn_sched_barrier(0);
     LS_STEP(f[i] = (double)logit[i] - top)
     LS_STEP(f[i] = __builtin_fmax(f[i] * heat, -1100.0))
@@ -96,10 +97,10 @@ template <typename T> __device__ __forceinline__ float entry_of(const T *row, in
     return x > kLargest<T> ? kLargest<T> : x;
 }
 
-// Eight entries of a row as they are stored
+// Four entries of a row as they are stored
 template <typename T> struct Run {
-    static constexpr int WORDS = 2 * sizeof(T);
-    uint32_t w[WORDS];
+    static constexpr int WORDS = RUN * sizeof(T) / 4;
+    alignas(16) uint32_t w[WORDS];
     __device__ __forceinline__ float entry(int e) const
     {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
@@ -107,17 +108,17 @@ template <typename T> struct Run {
         if constexpr (std::is_same_v<T, half_t>) return half_to_float((uint16_t)(e & 1 ? u >> 16 : u));
         else return __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
     }
-    __device__ __forceinline__ void four(int h, float (&l)[4]) const
+    __device__ __forceinline__ void entries(float (&l)[RUN]) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) l[i] = entry(h + i);
+        for (int e = 0; e < RUN; ++e) l[e] = entry(e);
     }
 };
 struct __attribute__((packed, aligned(2))) Words16 {
-    uint32_t w[4];
+    uint32_t w[2];
 };
 struct __attribute__((packed, aligned(4))) Words32 {
-    uint32_t w[8];
+    uint32_t w[4];
 };
 template <typename T> __device__ __forceinline__ Run<T> run_of_row(const T *at)  // (any alignment)
 {
@@ -130,17 +131,14 @@ template <typename T> __device__ __forceinline__ Run<T> run_of_row(const T *at) 
 template <typename T> __device__ __forceinline__ Run<T> run_of_lds(const T *at)
 {
     Run<T> x;
-#pragma unroll
-    for (int i = 0; i < Run<T>::WORDS; i += 4) {
-        const uint4 u = *(const uint4 *)((const uint32_t *)at + i);
-        x.w[i] = u.x, x.w[i + 1] = u.y, x.w[i + 2] = u.z, x.w[i + 3] = u.w;
-    }
+    using W = std::conditional_t<sizeof(T) == 4, uint4, uint2>;
+    *(W *)x.w = *(const W *)at;
     return x;
 }
 template <typename T> __device__ __forceinline__ void run_to_lds(const Run<T> &x, T *at)
 {
-#pragma unroll
-    for (int i = 0; i < Run<T>::WORDS; i += 4) *(uint4 *)((uint32_t *)at + i) = make_uint4(x.w[i], x.w[i + 1], x.w[i + 2], x.w[i + 3]);
+    using W = std::conditional_t<sizeof(T) == 4, uint4, uint2>;
+    *(W *)at = *(const W *)x.w;
 }
 template <typename T> __device__ __forceinline__ T from_bits(uint32_t bits)
 {
@@ -204,17 +202,23 @@ __device__ __forceinline__ float lanes_max(float x)
     step(Const<0x143>{}, Const<0xc>{});
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
-// The same over four neighbouring lanes, in all of these
-__device__ __forceinline__ double quad_sum(double x)
+// The same over eight neighbouring lanes, in all of these: of the lane next to it, of two lanes on, of the other four
+__device__ __forceinline__ double eight_sum(double x)
 {
     x += from_lane<0xb1, 0xf>(x);
     x += from_lane<0x4e, 0xf>(x);
+    x += from_lane<0x141, 0xf>(x);
     return x;
 }
-__device__ __forceinline__ float quad_max(float x)
+__device__ __forceinline__ float eight_max(float x)
 {
-    x = fmaxf(x, __int_as_float(from_lane<0xb1, 0xf>(__float_as_int(x), __float_as_int(-INFINITY))));
-    return fmaxf(x, __int_as_float(from_lane<0x4e, 0xf>(__float_as_int(x), __float_as_int(-INFINITY))));
+    auto step = [&](auto ctrl) __attribute__((always_inline)) {
+        x = fmaxf(x, __int_as_float(from_lane<decltype(ctrl)::value, 0xf>(__float_as_int(x), __float_as_int(-INFINITY))));
+    };
+    step(Const<0xb1>{});
+    step(Const<0x4e>{});
+    step(Const<0x141>{});
+    return x;
 }
 // 1 / x to the last bit or two, for x of the size of such sums
 __device__ __forceinline__ double inverse(double x)
@@ -346,7 +350,7 @@ __device__ __forceinline__ ArgsHere args_here()
     return (ArgsHere)p;
 }
 
-__device__ __forceinline__ double sum_four(const double (&w)[4]) { return (w[0] + w[1]) + (w[2] + w[3]); }
+__device__ __forceinline__ double sum_of(const double (&w)[RUN]) { return (w[0] + w[1]) + (w[2] + w[3]); }
 
 // The walk is a sequence of passes over a slice (over all of them, one after the other, where a workgroup is alone): the weights of a node's
 // rows and their sums; the sums of max(p - a q, 0) after a refusal; the search for the next token.  Between two passes the first wave joins
@@ -368,7 +372,7 @@ __global__ void __launch_bounds__(NT, 4)
 tree_sample_kernel(SampleArgs)
 {
     constexpr int NODES = LS_MAX_TREE / NT;  // of a thread: tid, tid + NT
-    static_assert(WAVES == 4, "their sums are joined in four lanes");
+    static_assert(WAVES == 8, "their sums are joined in eight lanes");
     // per node: token, path, first child, number for its acceptance, and (for children) the logits of both models; of the new tokens: logit / temperature
     // below the largest, and the sum of the weights.  Then the slice's entries of both rows.
     extern __shared__ __align__(16) uint8_t lds[];
@@ -404,17 +408,6 @@ tree_sample_kernel(SampleArgs)
     const int64_t t_node = a->t_stride[1], d_node = a->d_stride[1];
     auto target_row = [&](int node) __attribute__((always_inline)) { return target + node * t_node; };
     auto draft_row = [&](int node) __attribute__((always_inline)) { return draft + node * d_node; };
-    // Asks for a node's part of this slice, so that it is in the L2 when it is needed: what comes, a value a line, is thrown away.  (Not the first wave:
-    // what it reads of the others would wait for it.)
-    float touched[2] = {0.f, 0.f};
-    auto touch = [&](int node, bool both) __attribute__((always_inline)) {
-        const int line = tid - kWave, x_at = ex.slice * slice_size + line * (128 / (int)sizeof(TT)), y_at = ex.slice * slice_size + line * (128 / (int)sizeof(TD));
-        if (line < 0) return;
-        if (line < slice_size * (int)sizeof(TT) / 128 && x_at < vocab) touched[0] = Elem<TT>::load(target_row(node) + x_at);
-        if (both && line < slice_size * (int)sizeof(TD) / 128 && y_at < vocab) touched[1] = Elem<TD>::load(draft_row(node) + y_at);
-    };
-    auto throw_away = [&]() __attribute__((always_inline)) { asm volatile("" ::"v"(touched[0]), "v"(touched[1])); };
-
     int my_parent[NODES], my_tok[NODES];
     float my_u[NODES];
 #pragma unroll
@@ -425,7 +418,6 @@ tree_sample_kernel(SampleArgs)
         if (node < a->n_tree) my_parent[n] = a->parents[at], my_tok[n] = a->draft_tokens[at], my_u[n] = a->accept_uniforms[at];
     }
     float temp = a->temperature[b], draft_temp = a->draft_temperature ? a->draft_temperature[b] : temp;
-    touch(0, a->draft != nullptr);
     bool bad = false;
 #pragma unroll
     for (int n = 0; n < NODES; ++n) {
@@ -450,18 +442,17 @@ tree_sample_kernel(SampleArgs)
     const bool drawn = a->draft && !greedy && draft_temp > 0.f;
     const double heat = 1.4426950408889634074 / (greedy ? 1.0 : (double)temp);
     const double draft_heat = drawn ? 1.4426950408889634074 / (double)draft_temp : 0.0;
-    throw_away();
     __syncthreads();
     err |= uniform(flag_sh[0]);
     if (uniform(flag_sh[1])) return;
 
-    // A thread's entries: runs of 8, the lanes' runs side by side; a wave's are contiguous.  What a thread reads of its runs in LDS it has written itself.
-    const int wave_size = slice_size / WAVES, runs = wave_size / (kWave * 8);
+    // A thread's entries: runs of 4, the lanes' runs side by side; a wave's are contiguous.  What a thread reads of its runs in LDS it has written itself.
+    const int wave_size = slice_size / WAVES, runs = wave_size / (kWave * RUN);
 
     while (true) {
         // (known anew in each turn: what can be worked out from it before the loop would take most of the registers)
         asm volatile("" : "+v"(tid));
-        const int lane = tid & 63, own = wave * wave_size + lane * 8;
+        const int lane = tid & 63, own = wave * wave_size + lane * RUN;
         const int pass = uniform(walk.pass), cur = uniform(walk.cur);
         if (pass == kEnd) break;
         if (pass == kGiveUp) {  // the first one to give up goes on alone, from the root
@@ -488,9 +479,59 @@ tree_sample_kernel(SampleArgs)
         if (pass == kDraw) slice = uniform(walk.writer), end = slice + 1;
         ++ex.number;
         float wt = -INFINITY, wq = -INFINITY;  // the wave's largest entries
+        float my_x[NODES], my_y[NODES];        // logits of nodes that are children, read after the rows: those are waited for first
         for (; slice < end; ++slice) {
             if (pass == kRows || (alone && told)) {
-                float my_x[NODES], my_y[NODES];
+                const TT *row = target_row(cur);
+                const TD *drow = inner ? draft_row(cur) : nullptr;
+                float m = -INFINITY, mq = -INFINITY;
+                auto fetch = [&](auto *from, auto *to, int at, float &most) __attribute__((always_inline)) {  // entries behind the row's end, one by one
+                    using T = std::remove_reference_t<decltype(*to)>;
+#pragma unroll 1
+                    for (int e = 0; e < RUN; ++e) {
+                        const T v = at + e < vocab ? from[at + e] : minus_inf<T>();
+                        to[e] = v;
+                        most = fmaxf(most, Elem<T>::load(&v));
+                    }
+                };
+#pragma unroll 1
+                for (int r0 = 0; r0 < runs; r0 += 4) {
+                    Run<TT> x[4] = {};
+                    Run<TD> y[4] = {};
+                    const int at = slice * slice_size + own + r0 * kWave * RUN;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (r0 + i < runs && at + i * kWave * RUN + RUN <= vocab) x[i] = run_of_row(row + at + i * kWave * RUN);
+                    if (inner)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (r0 + i < runs && at + i * kWave * RUN + RUN <= vocab) y[i] = run_of_row(drow + at + i * kWave * RUN);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (r0 + i < runs) {
+                            const int in = own + (r0 + i) * kWave * RUN;
+                            if (at + i * kWave * RUN + RUN <= vocab) {
+                                run_to_lds(x[i], x_lds + in);
+#pragma unroll
+                                for (int e = 0; e < RUN; ++e) m = fmaxf(m, x[i].entry(e));
+                            } else {
+                                fetch(row, x_lds + in, slice * slice_size + in, m);
+                            }
+                        }
+                    if (inner)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (r0 + i < runs) {
+                                const int in = own + (r0 + i) * kWave * RUN;
+                                if (at + i * kWave * RUN + RUN <= vocab) {
+                                    run_to_lds(y[i], y_lds + in);
+#pragma unroll
+                                    for (int e = 0; e < RUN; ++e) mq = fmaxf(mq, y[i].entry(e));
+                                } else {
+                                    fetch(drow, y_lds + in, slice * slice_size + in, mq);
+                                }
+                            }
+                }
 #pragma unroll
                 for (int n = 0; n < NODES; ++n) {
                     my_x[n] = my_y[n] = -INFINITY;
@@ -498,56 +539,6 @@ tree_sample_kernel(SampleArgs)
                         my_x[n] = entry_of(target_row(cur), my_tok[n]);
                         if (inner) my_y[n] = entry_of(draft_row(cur), my_tok[n]);
                     }
-                }
-                const TT *row = target_row(cur);
-                const TD *drow = inner ? draft_row(cur) : nullptr;
-                float m = -INFINITY, mq = -INFINITY;
-                auto fetch = [&](auto *from, auto *to, int at, float &most) __attribute__((always_inline)) {  // entries behind the row's end, one by one
-                    using T = std::remove_reference_t<decltype(*to)>;
-#pragma unroll 1
-                    for (int e = 0; e < 8; ++e) {
-                        const T v = at + e < vocab ? from[at + e] : minus_inf<T>();
-                        to[e] = v;
-                        most = fmaxf(most, Elem<T>::load(&v));
-                    }
-                };
-#pragma unroll 1
-                for (int r0 = 0; r0 < runs; r0 += 2) {
-                    Run<TT> x[2] = {};
-                    Run<TD> y[2] = {};
-                    const int at = slice * slice_size + own + r0 * kWave * 8;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (r0 + i < runs && at + i * kWave * 8 + 8 <= vocab) x[i] = run_of_row(row + at + i * kWave * 8);
-                    if (inner)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            if (r0 + i < runs && at + i * kWave * 8 + 8 <= vocab) y[i] = run_of_row(drow + at + i * kWave * 8);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (r0 + i < runs) {
-                            const int in = own + (r0 + i) * kWave * 8;
-                            if (at + i * kWave * 8 + 8 <= vocab) {
-                                run_to_lds(x[i], x_lds + in);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) m = fmaxf(m, x[i].entry(e));
-                            } else {
-                                fetch(row, x_lds + in, slice * slice_size + in, m);
-                            }
-                        }
-                    if (inner)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            if (r0 + i < runs) {
-                                const int in = own + (r0 + i) * kWave * 8;
-                                if (at + i * kWave * 8 + 8 <= vocab) {
-                                    run_to_lds(y[i], y_lds + in);
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e) mq = fmaxf(mq, y[i].entry(e));
-                                } else {
-                                    fetch(drow, y_lds + in, slice * slice_size + in, mq);
-                                }
-                            }
                 }
                 // +inf counts as the largest finite number of its type, which is what it is from here on
                 auto whole = [&](auto *entries, float most) __attribute__((always_inline)) {
@@ -558,8 +549,8 @@ tree_sample_kernel(SampleArgs)
 #pragma unroll 1
                     for (int r = 0; r < runs; ++r)
 #pragma unroll 1
-                        for (int e = 0; e < 8; ++e) {
-                            T *const at = entries + own + r * kWave * 8 + e;
+                        for (int e = 0; e < RUN; ++e) {
+                            T *const at = entries + own + r * kWave * RUN + e;
                             if (Elem<T>::load(at) == INFINITY) *at = largest_bits<T>();
                             most = fmaxf(most, Elem<T>::load(at));
                         }
@@ -567,16 +558,6 @@ tree_sample_kernel(SampleArgs)
                 };
                 wt = whole(x_lds, m);
                 wq = inner ? whole(y_lds, mq) : -INFINITY;
-                if (pass == kRows) {
-#pragma unroll
-                    for (int n = 0; n < NODES; ++n) {
-                        const bool is_kid = my_parent[n] == cur;
-                        const uint64_t kids = __ballot(is_kid);
-                        if (lane == 0) kid_mask[wave + n * WAVES] = kids;
-                        if (is_kid) kid_x[tid + n * NT] = my_x[n], kid_y[tid + n * NT] = my_y[n];
-                    }
-                    if (!alone && kid != kNone) touch(kid, drawn && uniform(first_kid[kid]) != kNone);
-                }
             }
             // refused tokens have no weight any more
             if (pass != kRows) {
@@ -588,7 +569,7 @@ tree_sample_kernel(SampleArgs)
                         const int k = w * kWave + __builtin_ctzll(m);
                         if (k >= refused) break;
                         const int at = tok[k] - slice * slice_size;
-                        if ((uint32_t)at < (uint32_t)slice_size && at / wave_size == wave && at / 8 % kWave == lane) {
+                        if ((uint32_t)at < (uint32_t)slice_size && at / wave_size == wave && at / RUN % kWave == lane) {
                             x_lds[at] = minus_inf<TT>();
                             if (inner) y_lds[at] = minus_inf<TD>();
                         }
@@ -598,44 +579,40 @@ tree_sample_kernel(SampleArgs)
             if (pass == kDraw) break;
             // sums over the thread and the wave: of the weights relative to the wave's largest entries, or of max(p - a q, 0) and of q
             double s = 0, sq = 0;
-            const bool residual = pass == kResidual;
-            const double x_top = residual ? top : wt, y_top = residual ? draft_top : wq, scale = residual ? per_total : 1.0;
-            if (inner) {
-                const double y_scale = residual ? takes : 0.0;
+            auto sum_weights = [&](const auto *entries, double most, double h) __attribute__((always_inline)) {
+                double sum = 0;
 #pragma unroll 1
                 for (int r = 0; r < runs; ++r) {
-                    const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
-                    const Run<TD> y = run_of_lds(y_lds + own + r * kWave * 8);
-#pragma unroll
-                    for (int h = 0; h < 8; h += 4) {
-                        float l[4];
-                        double v[4], w[4];
-                        x.four(h, l);
-                        weights(l, x_top, heat, v);
-                        y.four(h, l);
-                        weights(l, y_top, draft_heat, w);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = __builtin_fmax(__builtin_fma(-y_scale, w[i], v[i] * scale), 0.0);
-                        s += sum_four(v);
-                        sq += sum_four(w);
-                    }
+                    float l[RUN];
+                    double w[RUN];
+                    run_of_lds(entries + own + r * kWave * RUN).entries(l);
+                    weights(l, most, h, w);
+                    sum += sum_of(w);
                 }
-                sq = lanes_sum(residual ? sq * per_draft_total : sq);
+                return sum;
+            };
+            if (pass == kRows) {
+                s = sum_weights(x_lds, wt, heat);
+                if (inner) sq = sum_weights(y_lds, wq, draft_heat);
+            } else if (inner) {
+#pragma unroll 1
+                for (int r = 0; r < runs; ++r) {
+                    float l[RUN];
+                    double v[RUN], w[RUN];
+                    run_of_lds(x_lds + own + r * kWave * RUN).entries(l);
+                    weights(l, top, heat, v);
+                    run_of_lds(y_lds + own + r * kWave * RUN).entries(l);
+                    weights(l, draft_top, draft_heat, w);
+#pragma unroll
+                    for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e] * per_total), 0.0);
+                    s += sum_of(v);
+                    sq += sum_of(w);
+                }
+                sq *= per_draft_total;
             } else {
-#pragma unroll 1
-                for (int r = 0; r < runs; ++r) {
-                    const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
-#pragma unroll
-                    for (int h = 0; h < 8; h += 4) {
-                        float l[4];
-                        double w[4];
-                        x.four(h, l);
-                        weights(l, x_top, heat, w);
-                        s += sum_four(w);
-                    }
-                }
-                s *= scale;
+                s = sum_weights(x_lds, top, heat) * per_total;
             }
+            if (inner) sq = lanes_sum(sq);
             s = lanes_sum(s);
             if (pass == kRows) {
                 if (lane == 0) wave_top[0][wave] = wt, wave_top[1][wave] = wq;
@@ -643,34 +620,43 @@ tree_sample_kernel(SampleArgs)
                     int best = kNone;
 #pragma unroll 1
                     for (int r = runs - 1; r >= 0; --r) {
-                        const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
+                        const Run<TT> x = run_of_lds(x_lds + own + r * kWave * RUN);
 #pragma unroll
-                        for (int e = 7; e >= 0; --e)
-                            if (x.entry(e) == wt) best = slice * slice_size + own + r * kWave * 8 + e;
+                        for (int e = RUN - 1; e >= 0; --e)
+                            if (x.entry(e) == wt) best = slice * slice_size + own + r * kWave * RUN + e;
                     }
                     best = wt > -INFINITY ? lanes_min(best) : kNone;
                     if (lane == 0) wave_best[wave] = best;
                 }
             }
             if (lane == 0) wave_sum[0][wave] = s, wave_sum[1][wave] = sq;
+            if (pass == kRows) {
+#pragma unroll
+                for (int n = 0; n < NODES; ++n) {
+                    const bool is_kid = my_parent[n] == cur;
+                    const uint64_t kids = __ballot(is_kid);
+                    if (lane == 0) kid_mask[wave + n * WAVES] = kids;
+                    if (is_kid) kid_x[tid + n * NT] = my_x[n], kid_y[tid + n * NT] = my_y[n];
+                }
+            }
             __syncthreads();
             if (wave == 0) {
-                // The waves' sums to the slice's: lanes 0 to 3 have p's, lanes 4 to 7 q's
+                // The waves' sums to the slice's: lanes 0 to 7 have p's, lanes 8 to 15 q's
                 const bool mine = lane < 2 * WAVES;
-                const int which = lane >> 2;
-                double sum = mine ? wave_sum[which][lane & 3] : 0.0;
+                const int which = lane >> 3;
+                double sum = mine ? wave_sum[which][lane & 7] : 0.0;
                 float mm = 0.f;
                 int best = kNone;
                 if (pass == kRows) {
-                    const float m = mine ? wave_top[which][lane & 3] : -INFINITY;
-                    mm = quad_max(m);
+                    const float m = mine ? wave_top[which][lane & 7] : -INFINITY;
+                    mm = eight_max(m);
                     sum *= weight(m, mm, which == 0 ? heat : draft_heat);
                     if (greedy) best = lanes_min(lane < WAVES && m == mm ? wave_best[lane] : kNone);
                 }
-                sum = quad_sum(sum);
+                sum = eight_sum(sum);
                 Half p = {}, q = {};
                 if (alone) {
-                    if ((lane & 3) == 0 && mine) {
+                    if ((lane & 7) == 0 && mine) {
                         part_top[which][slice] = mm, part_sum[which][slice] = sum;
                         if (lane == 0) part_best[slice] = best;
                     }
@@ -678,9 +664,9 @@ tree_sample_kernel(SampleArgs)
                 } else {
                     const uint64_t bits = __builtin_bit_cast(uint64_t, sum);
                     Half own_half = {{__float_as_uint(mm), (uint32_t)bits, (uint32_t)(bits >> 32), (uint32_t)best}};
-                    const int i = lane & 3;
+                    const int i = lane & 7;
                     const uint32_t value = i == 0 ? own_half.value[0] : i == 1 ? own_half.value[1] : i == 2 ? own_half.value[2] : own_half.value[3];
-                    if (lane < (inner ? 8 : 4)) ex.tell(which, i, value, own_half.check());
+                    if (lane < (inner ? 16 : 8)) ex.tell(which, i, value, own_half.check());
                     if (!ex.hear(lane, inner, args_here()->spin_limit, p, q)) {
                         if (lane == 0) walk.pass = kGiveUp;
                         goto next_slice;
@@ -805,77 +791,73 @@ tree_sample_kernel(SampleArgs)
             next_slice:;
             }
             __syncthreads();
-            throw_away();
         }
         if (pass != kDraw) continue;
 
         // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
         // that has any weight.
         const double rest = walk.rest;
-        // the residual's eight entries of a run, and their sum
-        auto residual_run = [&](int r, double (&v)[8]) __attribute__((always_inline)) {
-            const Run<TT> x = run_of_lds(x_lds + own + r * kWave * 8);
+        // the residual's entries of a run, and their sum
+        auto residual_run = [&](int r, double (&v)[RUN]) __attribute__((always_inline)) {
+            float l[RUN];
+            run_of_lds(x_lds + own + r * kWave * RUN).entries(l);
+            weights(l, top, heat, v);
 #pragma unroll
-            for (int h = 0; h < 8; h += 4) {
-                float l[4];
-                double w[4];
-                x.four(h, l);
-                weights(l, top, heat, w);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[h + i] = w[i] * per_total;
-            }
+            for (int e = 0; e < RUN; ++e) v[e] *= per_total;
             if (inner) {
-                const Run<TD> y = run_of_lds(y_lds + own + r * kWave * 8);
+                double w[RUN];
+                run_of_lds(y_lds + own + r * kWave * RUN).entries(l);
+                weights(l, draft_top, draft_heat, w);
 #pragma unroll
-                for (int h = 0; h < 8; h += 4) {
-                    float l[4];
-                    double w[4];
-                    y.four(h, l);
-                    weights(l, draft_top, draft_heat, w);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[h + i] = __builtin_fmax(__builtin_fma(-takes, w[i], v[h + i]), 0.0);
-                }
+                for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e]), 0.0);
             }
-            double sum = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[e];
-            return sum;
+            return sum_of(v);
         };
-        double v[8], all = 0;
+        double v[RUN], sum = 0;
+        {
+            double all = 0;
 #pragma unroll 1
-        for (int r = 0; r < runs; ++r) all += lanes_sum(residual_run(r, v));
-        if (lane == 0) wave_sum[0][wave] = all;
+            for (int r = 0; r < runs; ++r) all += sum = residual_run(r, v);
+            all = lanes_sum(all);
+            if (lane == 0) wave_sum[0][wave] = all;
+        }
         __syncthreads();
         double before = 0, upto = 0;  // of the entries before the wave's; before what has been looked at
         int at_wave = -1;
         bool passed = false;
-        for (int w = 0; w < WAVES && !passed; ++w) {
-            const double sum = uniform(wave_sum[0][w]);
-            if (sum > 0) at_wave = w, before = upto, passed = upto + sum > rest;
-            upto += sum;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const double of_wave = uniform(wave_sum[0][w]);
+            if (of_wave > 0 && !passed) at_wave = w, before = upto, passed = upto + of_wave > rest;
+            upto += of_wave;
         }
         if (wave == at_wave) {
+            // runs in turn, until one passes; where roundings let none, the last that has any weight
             upto = before;
-            passed = false;
-            int at_run = 0;
+            int last_run = -1;
 #pragma unroll 1
-            for (int r = 0; r < runs && !passed; ++r) {
-                const double sum = lanes_sum(residual_run(r, v));
-                if (sum > 0) at_run = r, before = upto, passed = upto + sum > rest;
-                upto += sum;
-            }
-            const double sum = residual_run(at_run, v), scan = lanes_scan(sum);
-            const uint64_t some = __ballot(sum > 0), over = __ballot(sum > 0 && before + scan > rest);
-            if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
-                double c = before + (scan - sum);
-                int place = 0;
-                passed = false;
+            for (int r = 0;; ++r) {
+                const bool again = r == runs;
+                if (again) r = last_run, upto = before;
+                if (again || runs > 1) sum = residual_run(r, v);
+                const double scan = lanes_scan(sum), of_run = of_lane(scan, 63);
+                if (!again && of_run > 0) last_run = r, before = upto;
+                const uint64_t over = __ballot(sum > 0 && upto + scan > rest), some = __ballot(sum > 0);
+                if (over || again) {
+                    if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
+                        double c = upto + (scan - sum);
+                        int place = 0;
+                        passed = false;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    c += v[e];
-                    if (v[e] > 0 && !passed) place = e, passed = c > rest;
+                        for (int e = 0; e < RUN; ++e) {
+                            c += v[e];
+                            if (v[e] > 0 && !passed) place = e, passed = c > rest;
+                        }
+                        walk.next = uniform(walk.writer) * slice_size + own + r * kWave * RUN + place;
+                    }
+                    break;
                 }
-                walk.next = uniform(walk.writer) * slice_size + own + at_run * kWave * 8 + place;
+                upto += of_run;
             }
         }
         __syncthreads();
@@ -902,13 +884,13 @@ tree_sample_kernel(SampleArgs)
         if (h->err_flag) h->err_flag[b] = err;
     }
     __syncthreads();
+    if (told && !alone && wave == WAVES - 1) ex.wait_for_marks(tid & 63, h->spin_limit);
     for (int i = tid; i < h->n_tree; i += NT) {
         const int64_t at = (int64_t)b * h->n_tree + i;
         h->path[at] = path[i];
         if (h->logprobs) h->logprobs[at] = i < len ? (float)(new_logit[i] - log(new_total[i])) : 0.f;
     }
     if (!told) return;
-    if (wave == 0 && !alone) ex.wait_for_marks(tid, h->spin_limit);
     __syncthreads();
     for (int i = tid; i < ex.n_words(); i += NT) Exchange::put(ex.words + i, 0);
 }
