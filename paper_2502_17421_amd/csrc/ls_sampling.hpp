@@ -66,7 +66,8 @@ struct ForkArgs {
 };
 hipError_t launch_page_fork(const ForkArgs &a, hipStream_t stream);
 
-// used: a bit per page; before[word]: pages in use before the 64 of a word; head: their number, and those of them below it.
+constexpr int kParts = 8;
+// used: a bit per page, or kParts times, each of some requests' pages; before[word]: pages in use before the 64 of a word; head: their number, and those of them below it.
 struct CompactArgs {
     const int32_t *pages_held, *block_table;
     int32_t *new_block_table, *free_pages, *new_free_count, *n_copies;

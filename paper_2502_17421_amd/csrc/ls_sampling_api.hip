@@ -90,7 +90,7 @@ CompactWorkspace compact_layout(const ls_page_desc &d)
     CompactWorkspace w;
     w.before = 256;  // after the counts
     w.used = w.before + up(words * 4);
-    w.total = w.used + up(words * 8);
+    w.total = w.used + up(words * 8 * kParts);
     return w;
 }
 
