@@ -14,7 +14,13 @@ A verification round over a speculation tree:
 
     cache.plan(most_accepted)                                       # room for the longest path
     for layer ...: cache.rotate_tree(...); cache.verify(...)        # ls_rope, ls_hybrid_tree_attn_paged
+    cache.accept(...)                                               # at a temperature: ls_tree_accept_sampled
     cache.commit(layers, ...)                                       # ls_kv_commit_paged; surplus pages go back with the next plan
+
+Several continuations of a prompt, beams, requests that go back to earlier rows:
+
+    cache.fork(sources)                                             # ls_page_fork, ls_page_copy: full pages are shared
+    cache.compact()                                                 # ls_page_compact, ls_page_copy: pages in use to the front of the pool
 
 Everything runs on torch's current stream and nothing waits for the GPU: lengths, tables and the number of free pages stay on
 the device, so a step can be recorded into a graph and replayed, other steps in between.
@@ -44,6 +50,8 @@ class PagedCache:
         self._next_lens = ints(batch)
         self.slots = self.positions = None
         self._buffers = {}
+        self._next_table = None   # of forks and compactions
+        self._n_copies = ints(1)
 
     def _buffer(self, name, size, dtype=torch.uint8):
         """`size` elements or more.  A recorded step goes on using the buffers it was recorded with, so one that a larger step outgrows is
@@ -56,8 +64,52 @@ class PagedCache:
     # ---- the requests' lengths
 
     def release(self, request):
-        """The request has ended: its pages go back with the next plan (its new length must be 0 or a new request's)."""
-        self.kv_lens[request] = 0
+        """The request has ended: its pages go back with the next plan (its new length must be 0 or a new request's).  Where requests may
+        share pages, by a fork: at once, those that nobody else holds."""
+        if self._next_table is None:
+            self.kv_lens[request] = 0
+            return
+        sources = torch.arange(self.batch, dtype=torch.int32, device=self.kv_lens.device)
+        sources[request] = -1
+        self.fork(sources)
+
+    # ---- requests that share pages
+
+    def _tables(self):
+        if self._next_table is None:
+            self._next_table = torch.zeros_like(self.block_table)
+        return self._next_table
+
+    def _move_rows(self, copies):
+        desc = ls.make_copy_desc(self.k_pages, self.v_pages, copies.shape[0])
+        ls.ls_page_copy(desc, copies, self._n_copies, self.k_pages, self.v_pages)
+
+    def fork(self, sources, keep_lens=None):
+        """Request b goes on from the rows (the first keep_lens[b]) of request sources[b], -1: from none, as they are now; int32 [batch], device.
+        Full pages are shared, of a page filled in part every request but one gets a copy, and pages that nobody holds any more are free
+        at once.  err: 1 where no page was left for the copy (the request then ends with its full pages), 2 for sources or lengths that are none."""
+        for x in (sources,) if keep_lens is None else (sources, keep_lens):
+            if x.shape != self.kv_lens.shape or x.dtype != torch.int32:
+                raise ValueError(f"sources, keep_lens: int32 [{self.batch}]")
+        desc = ls.make_page_desc(self.block_table, 0, self.page_size, self.n_pages)
+        copies = self._buffer("fork copies", 4 * self.batch, torch.int32)[:4 * self.batch].view(-1, 4)
+        ls.ls_page_fork(desc, sources, keep_lens, self.kv_lens, self.pages_held, self.block_table, self.free_pages, self.free_count, self._tables(),
+                        self._next_lens, self._next_held, self._next_free, copies, self._n_copies, self.err,
+                        self._buffer("fork", ls.ls_page_fork_workspace_bytes(desc)))
+        self._move_rows(copies)
+        for kept, made in ((self.block_table, self._next_table), (self.kv_lens, self._next_lens), (self.pages_held, self._next_held),
+                           (self.free_count, self._next_free)):
+            kept.copy_(made)
+
+    def compact(self):
+        """The pages in use to the front of the pool: afterwards they are 0 .. n_pages - free_count - 1."""
+        desc = ls.make_page_desc(self.block_table, 0, self.page_size, self.n_pages)
+        n = self.n_pages // 2 + 1
+        copies = self._buffer("compact copies", 4 * n, torch.int32)[:4 * n].view(-1, 4)
+        ls.ls_page_compact(desc, self.pages_held, self.block_table, self._tables(), self.free_pages, self.free_count, copies, self._n_copies,
+                           self._buffer("compact", ls.ls_page_compact_workspace_bytes(desc)))
+        self._move_rows(copies)
+        self.block_table.copy_(self._next_table)
 
     def plan(self, new_lens, n_tokens=0):
         """Pages for new_lens (int32 [batch], device) more rows of each request; with n_tokens, the packed tokens' slots and
@@ -122,6 +174,14 @@ class PagedCache:
         ls.ls_hybrid_tree_attn_paged(desc, q, kp, vp, self.block_table, self.page_size, self.kv_lens, k_tree, v_tree, parents, out, lse,
                                      ws)
 
+    def accept(self, parents, draft_tokens, target_logits, draft_logits, temperature, accept_uniforms, sample_uniforms, accept_path,
+               accept_len, next_token, logprobs=None, err=None, draft_temperature=None, with_replacement=False):
+        """Acceptance of the drafted trees at a temperature, from given random numbers; draft_logits None: the drafted tokens were chosen."""
+        desc = ls.make_sample_desc(target_logits, draft_logits, with_replacement)
+        ws = self._buffer("sample", ls.ls_sample_workspace_bytes(desc))
+        ls.ls_tree_accept_sampled(desc, parents, draft_tokens, target_logits, draft_logits, temperature, draft_temperature, accept_uniforms,
+                                  sample_uniforms, accept_path, accept_len, next_token, logprobs, err, ws)
+
     def commit(self, k_trees, v_trees, accept_path, accept_len):
         """k_trees, v_trees: a tensor per layer.  The accepted rows go into the pages and count as cached, as far as the pages reach that
         the plan before gave the request: a request it refused commits nothing, a path beyond its pages ends with them.  err is then
@@ -185,6 +245,23 @@ def main():
     report(f"accepted {accepted.tolist()}")
     cache.release(1)
     step([1, 0, 500], 1006)
+    # the third request goes on in two ways: its tree is drawn by a draft model and verified at a temperature, in each of them
+    cache.fork(ints([0, 2, 2]))
+    report("forked")
+    cache.plan(ints([4, 4, 4]))
+    vocab, uniforms = 32000, torch.rand((3, 6), device="cuda")
+    target = 4 * randn(3, 6, vocab)
+    draft = target + 0.5 * randn(3, 6, vocab)
+    tokens = torch.zeros_like(parents)
+    for node, above in ((1, 0), (3, 1), (5, 3), (2, 0), (4, 1)):  # (independent draws)
+        tokens[:, node] = torch.multinomial(torch.softmax(draft[:, above].float(), -1), 1)[:, 0].to(torch.int32)
+    logprobs = torch.empty((3, 6), device="cuda")
+    cache.accept(parents, tokens, target, draft, torch.ones(3, device="cuda"), uniforms, torch.rand(3, device="cuda"), path, accepted, following,
+                 logprobs, err, with_replacement=True)
+    cache.commit(k_trees, v_trees, path, accepted)
+    report(f"accepted at a temperature {accepted.tolist()}")
+    cache.compact()
+    report("compacted")
 
 
 if __name__ == "__main__":
