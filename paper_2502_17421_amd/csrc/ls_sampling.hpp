@@ -20,7 +20,7 @@ struct SampleArgs {
     uint32_t call;          // a number of this call's own
     uint64_t *records;
 };
-constexpr int kSampleThreads = 512;
+constexpr int kSampleThreads = 256;
 constexpr int kSampleSlices = 64;                   // at most
 constexpr int kSampleUnit = kSampleThreads * 4;     // entries: slices are multiples
 constexpr int kSampleLds = 156 * 1024;              // dynamic LDS, at most
@@ -30,18 +30,18 @@ inline int sample_lds_bytes(int n_tree, int slice, int target_bytes, int draft_b
     return (n_tree + 63) / 64 * 64 * 40 + slice * (target_bytes + draft_bytes);
 }
 static_assert(512 * 40 + LS_MAX_VOCAB / kSampleSlices * 8 <= kSampleLds, "every vocabulary fits");
-// The smallest slices with which all workgroups of the call fit on the card at a time; if none do, the largest of which two fit on a compute unit.
+// The smallest slices with which all workgroups of the call fit on the card at a time; if none do, the largest of which four fit on a compute unit.
 inline int sample_slice(int batch, int n_tree, int vocab, int target_bytes, int draft_bytes, int compute_units)
 {
     int slice = kSampleUnit;
-    for (; slice < kSampleUnit * 32; slice += kSampleUnit) {
+    for (; slice < kSampleUnit * 64; slice += kSampleUnit) {
         const int slices = (vocab + slice - 1) / slice;
         if (slices > kSampleSlices) continue;
         const int each = sample_lds_bytes(n_tree, slice, target_bytes, draft_bytes) + 3072;
         int fit = 160 * 1024 / each;
-        fit = fit > 2 ? 2 : fit;  // by their registers
+        fit = fit > 4 ? 4 : fit;  // by their registers
         if (slices == 1 || (int64_t)batch * slices <= (int64_t)fit * compute_units) return slice;
-        if (sample_lds_bytes(n_tree, slice + kSampleUnit, target_bytes, draft_bytes) + 3072 > 80 * 1024) return slice;
+        if (sample_lds_bytes(n_tree, slice + kSampleUnit, target_bytes, draft_bytes) + 3072 > 40 * 1024) return slice;
     }
     return slice;
 }

@@ -188,36 +188,49 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x)
 {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
-__device__ __forceinline__ double lanes_sum(double x) { return of_lane(lanes_scan(x), 63); }
+// Sums and largest values of all lanes: rotations within rows of 16, then the four rows'
+template <int BY> __device__ __forceinline__ int rotated(int x)  // by BY lanes of the row
+{
+    return __builtin_amdgcn_update_dpp(x, x, 0x120 + BY, 0xf, 0xf, false);
+}
+template <int BY> __device__ __forceinline__ double rotated(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)rotated<BY>((int)(u >> 32)) << 32 | (uint32_t)rotated<BY>((int)u));
+}
+__device__ __forceinline__ double lanes_sum(double x)
+{
+    x += rotated<8>(x);
+    x += rotated<4>(x);
+    x += rotated<2>(x);
+    x += rotated<1>(x);
+    return (of_lane(x, 0) + of_lane(x, 16)) + (of_lane(x, 32) + of_lane(x, 48));
+}
 __device__ __forceinline__ float lanes_max(float x)
 {
-    auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
-        x = fmaxf(x, __int_as_float(from_lane<decltype(ctrl)::value, decltype(rows)::value>(__float_as_int(x), __float_as_int(-INFINITY))));
-    };
-    step(Const<0x111>{}, Const<0xf>{});
-    step(Const<0x112>{}, Const<0xf>{});
-    step(Const<0x114>{}, Const<0xf>{});
-    step(Const<0x118>{}, Const<0xf>{});
-    step(Const<0x142>{}, Const<0xa>{});
-    step(Const<0x143>{}, Const<0xc>{});
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+    x = fmaxf(x, __int_as_float(rotated<8>(__float_as_int(x))));
+    x = fmaxf(x, __int_as_float(rotated<4>(__float_as_int(x))));
+    x = fmaxf(x, __int_as_float(rotated<2>(__float_as_int(x))));
+    x = fmaxf(x, __int_as_float(rotated<1>(__float_as_int(x))));
+    auto row = [&](int lane) __attribute__((always_inline)) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); };
+    return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
 }
-// The same over eight neighbouring lanes, in all of these: of the lane next to it, of two lanes on, of the other four
-__device__ __forceinline__ double eight_sum(double x)
+// The same over WAVES neighbouring lanes, in all of these: of the lane next to it, of two lanes on, of the other four
+__device__ __forceinline__ double waves_sum(double x)
 {
     x += from_lane<0xb1, 0xf>(x);
     x += from_lane<0x4e, 0xf>(x);
-    x += from_lane<0x141, 0xf>(x);
+    if constexpr (WAVES == 8) x += from_lane<0x141, 0xf>(x);
     return x;
 }
-__device__ __forceinline__ float eight_max(float x)
+__device__ __forceinline__ float waves_max(float x)
 {
     auto step = [&](auto ctrl) __attribute__((always_inline)) {
         x = fmaxf(x, __int_as_float(from_lane<decltype(ctrl)::value, 0xf>(__float_as_int(x), __float_as_int(-INFINITY))));
     };
     step(Const<0xb1>{});
     step(Const<0x4e>{});
-    step(Const<0x141>{});
+    if constexpr (WAVES == 8) step(Const<0x141>{});
     return x;
 }
 // 1 / x to the last bit or two, for x of the size of such sums
@@ -359,7 +372,7 @@ enum Pass { kRows, kResidual, kDraw, kEnd, kGiveUp };
 
 struct Walk {
     int32_t pass, cur, len, next, writer;  // writer: the slice whose workgroup draws the token and writes the outputs
-    int32_t refused, removed;              // the children before these nodes have been refused, and taken out of the rows in registers
+    int32_t refused, removed, newest;      // the children before these nodes have been refused, and taken out of the rows in LDS; the last one's token
     float top, draft_top;                  // the largest entries of the rows
     double total;                          // the sum of the target's weights relative to its largest entry
     double per_total, per_draft_total;     // inverse sums
@@ -372,7 +385,7 @@ __global__ void __launch_bounds__(NT, 4)
 tree_sample_kernel(SampleArgs)
 {
     constexpr int NODES = LS_MAX_TREE / NT;  // of a thread: tid, tid + NT
-    static_assert(WAVES == 8, "their sums are joined in eight lanes");
+    static_assert(WAVES == 4 || WAVES == 8, "their sums are joined in as many lanes");
     // per node: token, path, first child, number for its acceptance, and (for children) the logits of both models; of the new tokens: logit / temperature
     // below the largest, and the sum of the weights.  Then the slice's entries of both rows.
     extern __shared__ __align__(16) uint8_t lds[];
@@ -385,7 +398,7 @@ tree_sample_kernel(SampleArgs)
     __shared__ double part_sum[2][kSampleSlices];
     __shared__ int32_t part_best[kSampleSlices];
     __shared__ Walk walk;
-    __shared__ int32_t flag_sh[2];
+    __shared__ int32_t flag_sh;
 
     const ArgsHere a = args_here();
     const int slices = a->slices, vocab = a->vocab;
@@ -427,11 +440,11 @@ tree_sample_kernel(SampleArgs)
         if ((uint32_t)my_tok[n] >= (uint32_t)vocab) my_parent[n] = -1;  // nobody's child
     }
     if (tid == 0) {
-        flag_sh[0] = 0, flag_sh[1] = told && ex.somebody_alone();
+        flag_sh = 0;
         walk.pass = kRows, walk.cur = 0, walk.len = 1, walk.next = -1, walk.writer = 0;
     }
     __syncthreads();
-    if (bad) flag_sh[0] = 1;
+    if (bad) flag_sh = 1;
 #pragma unroll
     for (int n = 0; n < NODES; ++n)
         if (my_parent[n] >= 0) atomicMin(&first_kid[my_parent[n]], tid + n * NT);
@@ -443,8 +456,7 @@ tree_sample_kernel(SampleArgs)
     const double heat = 1.4426950408889634074 / (greedy ? 1.0 : (double)temp);
     const double draft_heat = drawn ? 1.4426950408889634074 / (double)draft_temp : 0.0;
     __syncthreads();
-    err |= uniform(flag_sh[0]);
-    if (uniform(flag_sh[1])) return;
+    err |= uniform(flag_sh);
 
     // A thread's entries: runs of 4, the lanes' runs side by side; a wave's are contiguous.  What a thread reads of its runs in LDS it has written itself.
     const int wave_size = slice_size / WAVES, runs = wave_size / (kWave * RUN);
@@ -458,12 +470,12 @@ tree_sample_kernel(SampleArgs)
         if (pass == kGiveUp) {  // the first one to give up goes on alone, from the root
             __syncthreads();
             if (tid == 0) {
-                flag_sh[0] = ex.go_alone();
+                flag_sh = ex.go_alone();
                 walk.pass = kRows, walk.cur = 0, walk.len = 1, walk.next = -1, walk.writer = 0;
             }
             for (int i = tid; i < n_nodes; i += NT) path[i] = i == 0 ? 0 : -1;
             __syncthreads();
-            if (!uniform(flag_sh[0])) return;
+            if (!uniform(flag_sh)) return;
             alone = true;
             continue;
         }
@@ -479,7 +491,8 @@ tree_sample_kernel(SampleArgs)
         if (pass == kDraw) slice = uniform(walk.writer), end = slice + 1;
         ++ex.number;
         float wt = -INFINITY, wq = -INFINITY;  // the wave's largest entries
-        float my_x[NODES], my_y[NODES];        // logits of nodes that are children, read after the rows: those are waited for first
+        TT my_x[NODES];                        // logits of nodes that are children, as they are stored: asked for after the rows, and first looked at
+        TD my_y[NODES];                        // when the sums of these are done
         for (; slice < end; ++slice) {
             if (pass == kRows || (alone && told)) {
                 const TT *row = target_row(cur);
@@ -534,10 +547,10 @@ tree_sample_kernel(SampleArgs)
                 }
 #pragma unroll
                 for (int n = 0; n < NODES; ++n) {
-                    my_x[n] = my_y[n] = -INFINITY;
+                    my_x[n] = minus_inf<TT>(), my_y[n] = minus_inf<TD>();
                     if (pass == kRows && my_parent[n] == cur) {
-                        my_x[n] = entry_of(target_row(cur), my_tok[n]);
-                        if (inner) my_y[n] = entry_of(draft_row(cur), my_tok[n]);
+                        my_x[n] = target_row(cur)[my_tok[n]];
+                        if (inner) my_y[n] = draft_row(cur)[my_tok[n]];
                     }
                 }
                 // +inf counts as the largest finite number of its type, which is what it is from here on
@@ -561,17 +574,25 @@ tree_sample_kernel(SampleArgs)
             }
             // refused tokens have no weight any more
             if (pass != kRows) {
-                const int refused = uniform(walk.refused), removed = alone && told ? 0 : uniform(walk.removed);
-                for (int w = removed / kWave; w * kWave < refused; ++w) {
-                    uint64_t m = uniform(kid_mask[w]);
-                    if (w == removed / kWave) m &= ~0ull << (removed % kWave);
-                    for (; m; m &= m - 1) {
-                        const int k = w * kWave + __builtin_ctzll(m);
-                        if (k >= refused) break;
-                        const int at = tok[k] - slice * slice_size;
-                        if ((uint32_t)at < (uint32_t)slice_size && at / wave_size == wave && at / RUN % kWave == lane) {
-                            x_lds[at] = minus_inf<TT>();
-                            if (inner) y_lds[at] = minus_inf<TD>();
+                auto remove = [&](int token) __attribute__((always_inline)) {
+                    const int at = token - slice * slice_size, in_wave = at - wave * wave_size;
+                    if ((uint32_t)in_wave < (uint32_t)wave_size && in_wave / RUN % kWave == lane) {
+                        x_lds[at] = minus_inf<TT>();
+                        if (inner) y_lds[at] = minus_inf<TD>();
+                    }
+                };
+                const bool anew = alone && told;  // (the rows have been read again)
+                if (pass == kResidual && inner && !anew) {
+                    remove(walk.newest);
+                } else {
+                    const int refused = uniform(walk.refused), removed = anew ? 0 : uniform(walk.removed);
+                    for (int w = removed / kWave; w * kWave < refused; ++w) {
+                        uint64_t m = uniform(kid_mask[w]);
+                        if (w == removed / kWave) m &= ~0ull << (removed % kWave);
+                        for (; m; m &= m - 1) {
+                            const int k = w * kWave + __builtin_ctzll(m);
+                            if (k >= refused) break;
+                            remove(tok[k]);
                         }
                     }
                 }
@@ -636,27 +657,27 @@ tree_sample_kernel(SampleArgs)
                     const bool is_kid = my_parent[n] == cur;
                     const uint64_t kids = __ballot(is_kid);
                     if (lane == 0) kid_mask[wave + n * WAVES] = kids;
-                    if (is_kid) kid_x[tid + n * NT] = my_x[n], kid_y[tid + n * NT] = my_y[n];
+                    if (is_kid) kid_x[tid + n * NT] = entry_of(&my_x[n], 0), kid_y[tid + n * NT] = entry_of(&my_y[n], 0);
                 }
             }
             __syncthreads();
             if (wave == 0) {
-                // The waves' sums to the slice's: lanes 0 to 7 have p's, lanes 8 to 15 q's
+                // The waves' sums to the slice's: the first WAVES lanes have p's, the next ones q's
                 const bool mine = lane < 2 * WAVES;
-                const int which = lane >> 3;
-                double sum = mine ? wave_sum[which][lane & 7] : 0.0;
+                const int which = lane / WAVES;
+                double sum = mine ? wave_sum[which][lane % WAVES] : 0.0;
                 float mm = 0.f;
                 int best = kNone;
                 if (pass == kRows) {
-                    const float m = mine ? wave_top[which][lane & 7] : -INFINITY;
-                    mm = eight_max(m);
+                    const float m = mine ? wave_top[which][lane % WAVES] : -INFINITY;
+                    mm = waves_max(m);
                     sum *= weight(m, mm, which == 0 ? heat : draft_heat);
                     if (greedy) best = lanes_min(lane < WAVES && m == mm ? wave_best[lane] : kNone);
                 }
-                sum = eight_sum(sum);
+                sum = waves_sum(sum);
                 Half p = {}, q = {};
                 if (alone) {
-                    if ((lane & 7) == 0 && mine) {
+                    if (lane % WAVES == 0 && mine) {
                         part_top[which][slice] = mm, part_sum[which][slice] = sum;
                         if (lane == 0) part_best[slice] = best;
                     }
@@ -664,9 +685,9 @@ tree_sample_kernel(SampleArgs)
                 } else {
                     const uint64_t bits = __builtin_bit_cast(uint64_t, sum);
                     Half own_half = {{__float_as_uint(mm), (uint32_t)bits, (uint32_t)(bits >> 32), (uint32_t)best}};
-                    const int i = lane & 7;
+                    const int i = lane % WAVES;
                     const uint32_t value = i == 0 ? own_half.value[0] : i == 1 ? own_half.value[1] : i == 2 ? own_half.value[2] : own_half.value[3];
-                    if (lane < (inner ? 16 : 8)) ex.tell(which, i, value, own_half.check());
+                    if (lane < (inner ? 2 : 1) * WAVES) ex.tell(which, i, value, own_half.check());
                     if (!ex.hear(lane, inner, args_here()->spin_limit, p, q)) {
                         if (lane == 0) walk.pass = kGiveUp;
                         goto next_slice;
@@ -689,7 +710,7 @@ tree_sample_kernel(SampleArgs)
                     }
                     double taken = 0, left = 1, pt = per_total, pd = per_draft_total;
                     float t = top, dt = draft_top;
-                    int at_best = kNone, refused = 0;
+                    int at_best = kNone, refused = 0, newest = -1;
                     double mass = 1;
                     if (pass == kRows) {  // (both rows, step by step together, also where there is no draft's)
                         t = lanes_max(m), dt = lanes_max(mq);
@@ -732,7 +753,7 @@ tree_sample_kernel(SampleArgs)
                                 found = w * kWave + i;
                                 break;
                             }
-                            refused = w * kWave + i + 1;
+                            refused = w * kWave + i + 1, newest = token;
                             if (greedy) continue;
                             // the same token once more has no weight either
                             const bool same = my_token == token;
@@ -746,7 +767,7 @@ tree_sample_kernel(SampleArgs)
                                 again = true;
                             } else {
                                 mass -= off;
-                                if (token / slice_size == lane) part = __builtin_fmax(part - off, 0.0);
+                                if ((uint32_t)(token - lane * slice_size) < (uint32_t)slice_size) part = __builtin_fmax(part - off, 0.0);
                                 again = mass < 0x1p-10;
                             }
                         }
@@ -785,7 +806,7 @@ tree_sample_kernel(SampleArgs)
                     if (lane == 0) {
                         walk.pass = next_pass;
                         walk.removed = pass == kRows ? 0 : uniform(walk.refused);
-                        walk.refused = refused;
+                        walk.refused = refused, walk.newest = newest;
                     }
                 }
             next_slice:;
