@@ -353,6 +353,19 @@ struct Exchange {
 
 __device__ __forceinline__ double from_words(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
 
+// A value that the compiler takes for a new one: it works out what follows from it where that is needed, and not before a loop for all its
+// turns, where it would hold it in registers or even scratch.
+__device__ __forceinline__ int here(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ int here_scalar(int x)
+{
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
 // The kernel's arguments, read where they are needed: held in scalar registers from the start, as the compiler would have it, they
 // leave too few for the polynomial's coefficients, which then take vector registers.
 typedef const __attribute__((address_space(4))) SampleArgs *ArgsHere;
@@ -380,14 +393,28 @@ struct Walk {
     double rest;                           // what the sum has to pass in the writer's slice
 };
 
+// What there is per node in LDS: of the new tokens, logit / temperature below the largest, and the sum of the weights; token, path, first child,
+// number for its acceptance, and (for children) the logits of both models
+struct NodeArrays {
+    uint8_t *lds;
+    int n;
+    __device__ __forceinline__ double *new_logit() const { return (double *)lds; }
+    __device__ __forceinline__ double *new_total() const { return (double *)lds + n; }
+    __device__ __forceinline__ int32_t *tok() const { return (int32_t *)lds + 4 * n; }
+    __device__ __forceinline__ int32_t *path() const { return (int32_t *)lds + 5 * n; }
+    __device__ __forceinline__ int32_t *first_kid() const { return (int32_t *)lds + 6 * n; }
+    __device__ __forceinline__ float *accept_u() const { return (float *)lds + 7 * n; }
+    __device__ __forceinline__ float *kid_x() const { return (float *)lds + 8 * n; }
+    __device__ __forceinline__ float *kid_y() const { return (float *)lds + 9 * n; }
+};
+
 template <typename TT, typename TD>
 __global__ void __launch_bounds__(NT, 4)
 tree_sample_kernel(SampleArgs)
 {
     constexpr int NODES = LS_MAX_TREE / NT;  // of a thread: tid, tid + NT
     static_assert(WAVES == 4 || WAVES == 8, "their sums are joined in as many lanes");
-    // per node: token, path, first child, number for its acceptance, and (for children) the logits of both models; of the new tokens: logit / temperature
-    // below the largest, and the sum of the weights.  Then the slice's entries of both rows.
+    // what there is per node, then the slice's entries of both rows
     extern __shared__ __align__(16) uint8_t lds[];
     __shared__ uint64_t kid_mask[LS_MAX_TREE / kWave];
     __shared__ float wave_top[2][WAVES];
@@ -402,16 +429,15 @@ tree_sample_kernel(SampleArgs)
 
     const ArgsHere a = args_here();
     const int slices = a->slices, vocab = a->vocab;
-    const int b = (int)(blockIdx.x / (uint32_t)slices), thread = threadIdx.x, wave = uniform(thread >> 6);
-    int tid = thread;
+    const int b = (int)(blockIdx.x / (uint32_t)slices), tid = threadIdx.x, wave = uniform(tid >> 6);
     Exchange ex;
     ex.slices = slices, ex.slice = (int)(blockIdx.x % (uint32_t)slices), ex.call = a->call, ex.number = 0;
     ex.words = a->records + (int64_t)b * ex.n_words();
     const int n_nodes = (a->n_tree + kWave - 1) / kWave * kWave, slice_size = a->slice;
-    double *const new_logit = (double *)lds, *const new_total = new_logit + n_nodes;
-    int32_t *const tok = (int32_t *)(new_total + n_nodes), *const path = tok + n_nodes, *const first_kid = path + n_nodes;
-    float *const accept_u = (float *)(first_kid + n_nodes), *const kid_x = accept_u + n_nodes, *const kid_y = kid_x + n_nodes;
-    TT *const x_lds = (TT *)(kid_y + n_nodes);
+    const NodeArrays nodes_lds{lds, n_nodes};
+    int32_t *const tok = nodes_lds.tok(), *const path = nodes_lds.path(), *const first_kid = nodes_lds.first_kid();
+    float *const kid_x = nodes_lds.kid_x(), *const kid_y = nodes_lds.kid_y();
+    TT *const x_lds = (TT *)(lds + n_nodes * 40);
     TD *const y_lds = (TD *)(x_lds + slice_size);
     const bool told = slices > 1;
     bool alone = !told;  // this workgroup does all slices
@@ -435,7 +461,7 @@ tree_sample_kernel(SampleArgs)
 #pragma unroll
     for (int n = 0; n < NODES; ++n) {
         const int node = tid + n * NT;
-        if (node < n_nodes) path[node] = node == 0 ? 0 : -1, first_kid[node] = kNone, tok[node] = my_tok[n], accept_u[node] = my_u[n];
+        if (node < n_nodes) path[node] = node == 0 ? 0 : -1, first_kid[node] = kNone, tok[node] = my_tok[n], nodes_lds.accept_u()[node] = my_u[n];
         if (my_parent[n] < -1 || my_parent[n] >= node) bad = true, my_parent[n] = -1;
         if ((uint32_t)my_tok[n] >= (uint32_t)vocab) my_parent[n] = -1;  // nobody's child
     }
@@ -462,9 +488,7 @@ tree_sample_kernel(SampleArgs)
     const int wave_size = slice_size / WAVES, runs = wave_size / (kWave * RUN);
 
     while (true) {
-        // (known anew in each turn: what can be worked out from it before the loop would take most of the registers)
-        asm volatile("" : "+v"(tid));
-        const int lane = tid & 63, own = wave * wave_size + lane * RUN;
+        const int lane = here(tid) & 63, own = wave * wave_size + lane * RUN;
         const int pass = uniform(walk.pass), cur = uniform(walk.cur);
         if (pass == kEnd) break;
         if (pass == kGiveUp) {  // the first one to give up goes on alone, from the root
@@ -494,6 +518,7 @@ tree_sample_kernel(SampleArgs)
         TT my_x[NODES];                        // logits of nodes that are children, as they are stored: asked for after the rows, and first looked at
         TD my_y[NODES];                        // when the sums of these are done
         for (; slice < end; ++slice) {
+            const int lane = here(tid) & 63, own = wave * wave_size + lane * RUN;
             if (pass == kRows || (alone && told)) {
                 const TT *row = target_row(cur);
                 const TD *drow = inner ? draft_row(cur) : nullptr;
@@ -662,6 +687,12 @@ tree_sample_kernel(SampleArgs)
             }
             __syncthreads();
             if (wave == 0) {
+                const int lane = here(tid) & 63, slices = here_scalar(ex.slices), n_nodes = here_scalar(nodes_lds.n);  // (what follows from
+                // them is not worked out before, for every pass and wave)
+                const NodeArrays here_lds{lds, n_nodes};
+                int32_t *const tok = here_lds.tok(), *const path = here_lds.path();
+                float *const accept_u = here_lds.accept_u(), *const kid_x = here_lds.kid_x(), *const kid_y = here_lds.kid_y();
+                double *const new_logit = here_lds.new_logit(), *const new_total = here_lds.new_total();
                 // The waves' sums to the slice's: the first WAVES lanes have p's, the next ones q's
                 const bool mine = lane < 2 * WAVES;
                 const int which = lane / WAVES;
@@ -892,6 +923,7 @@ tree_sample_kernel(SampleArgs)
         return;
     }
     const int len = uniform(walk.len), next = uniform(walk.next);
+    double *const new_logit = nodes_lds.new_logit(), *const new_total = nodes_lds.new_total();
     if (tid == 0) {
         if (next >= 0) {
             new_logit[len - 1] = ((double)entry_of(target_row(walk.cur), next) - walk.top) / (greedy ? 1.0 : (double)temp);
