@@ -24,12 +24,12 @@ constexpr int kSampleThreads = 256;
 constexpr int kSampleSlices = 64;                   // at most
 constexpr int kSampleUnit = kSampleThreads * 4;     // entries: slices are multiples
 constexpr int kSampleLds = 156 * 1024;              // dynamic LDS, at most
-// 40 bytes for each node, nodes up to a multiple of 64; the entries of both rows
+constexpr int kSampleNode = 40;                     // bytes of LDS for each node, nodes up to a multiple of 64; then the entries of both rows
 inline int sample_lds_bytes(int n_tree, int slice, int target_bytes, int draft_bytes)
 {
-    return (n_tree + 63) / 64 * 64 * 40 + slice * (target_bytes + draft_bytes);
+    return (n_tree + 63) / 64 * 64 * kSampleNode + slice * (target_bytes + draft_bytes);
 }
-static_assert(512 * 40 + LS_MAX_VOCAB / kSampleSlices * 8 <= kSampleLds, "every vocabulary fits");
+static_assert(LS_MAX_TREE * kSampleNode + LS_MAX_VOCAB / kSampleSlices * 8 <= kSampleLds, "every vocabulary fits");
 // The smallest slices with which all workgroups of the call fit on the card at a time; if none do, the largest of which four fit on a compute unit.
 inline int sample_slice(int batch, int n_tree, int vocab, int target_bytes, int draft_bytes, int compute_units)
 {

@@ -393,20 +393,14 @@ struct Walk {
     double rest;                           // what the sum has to pass in the writer's slice
 };
 
-// What there is per node in LDS: of the new tokens, logit / temperature below the largest, and the sum of the weights; token, path, first child,
-// number for its acceptance, and (for children) the logits of both models
-struct NodeArrays {
-    uint8_t *lds;
-    int n;
-    __device__ __forceinline__ double *new_logit() const { return (double *)lds; }
-    __device__ __forceinline__ double *new_total() const { return (double *)lds + n; }
-    __device__ __forceinline__ int32_t *tok() const { return (int32_t *)lds + 4 * n; }
-    __device__ __forceinline__ int32_t *path() const { return (int32_t *)lds + 5 * n; }
-    __device__ __forceinline__ int32_t *first_kid() const { return (int32_t *)lds + 6 * n; }
-    __device__ __forceinline__ float *accept_u() const { return (float *)lds + 7 * n; }
-    __device__ __forceinline__ float *kid_x() const { return (float *)lds + 8 * n; }
-    __device__ __forceinline__ float *kid_y() const { return (float *)lds + 9 * n; }
+// What there is per node in LDS.  new_: of the path's n-th token in node n, logit / temperature below the largest, and the sum of the weights.  kid_: the logits
+// of both models at a child's token.
+struct Node {
+    double new_logit, new_total;
+    int32_t tok, path, first_kid;
+    float accept_u, kid_x, kid_y;
 };
+static_assert(sizeof(Node) == kSampleNode, "what the launch reserves");
 
 template <typename TT, typename TD>
 __global__ void __launch_bounds__(NT, 4)
@@ -434,13 +428,10 @@ tree_sample_kernel(SampleArgs)
     ex.slices = slices, ex.slice = (int)(blockIdx.x % (uint32_t)slices), ex.call = a->call, ex.number = 0;
     ex.words = a->records + (int64_t)b * ex.n_words();
     const int n_nodes = (a->n_tree + kWave - 1) / kWave * kWave, slice_size = a->slice;
-    const NodeArrays nodes_lds{lds, n_nodes};
-    int32_t *const tok = nodes_lds.tok(), *const path = nodes_lds.path(), *const first_kid = nodes_lds.first_kid();
-    float *const kid_x = nodes_lds.kid_x(), *const kid_y = nodes_lds.kid_y();
-    TT *const x_lds = (TT *)(lds + n_nodes * 40);
+    Node *const nodes = (Node *)lds;
+    TT *const x_lds = (TT *)(nodes + n_nodes);
     TD *const y_lds = (TD *)(x_lds + slice_size);
     const bool told = slices > 1;
-    bool alone = !told;  // this workgroup does all slices
     // node's rows of logits
     const TT *const target = (const TT *)a->target + b * a->t_stride[0];
     const TD *const draft = (const TD *)a->draft + (a->draft ? b * a->d_stride[0] : 0);
@@ -461,7 +452,7 @@ tree_sample_kernel(SampleArgs)
 #pragma unroll
     for (int n = 0; n < NODES; ++n) {
         const int node = tid + n * NT;
-        if (node < n_nodes) path[node] = node == 0 ? 0 : -1, first_kid[node] = kNone, tok[node] = my_tok[n], nodes_lds.accept_u()[node] = my_u[n];
+        if (node < n_nodes) nodes[node] = {0.0, 0.0, my_tok[n], node == 0 ? 0 : -1, kNone, my_u[n], 0.f, 0.f};
         if (my_parent[n] < -1 || my_parent[n] >= node) bad = true, my_parent[n] = -1;
         if ((uint32_t)my_tok[n] >= (uint32_t)vocab) my_parent[n] = -1;  // nobody's child
     }
@@ -473,7 +464,7 @@ tree_sample_kernel(SampleArgs)
     if (bad) flag_sh = 1;
 #pragma unroll
     for (int n = 0; n < NODES; ++n)
-        if (my_parent[n] >= 0) atomicMin(&first_kid[my_parent[n]], tid + n * NT);
+        if (my_parent[n] >= 0) atomicMin(&nodes[my_parent[n]].first_kid, tid + n * NT);
     int err = 0;
     if (!(temp >= 0.f && temp <= FLT_MAX)) err = 2, temp = 0.f;
     if (!(draft_temp >= 0.f && draft_temp <= FLT_MAX)) err = 2, draft_temp = 0.f;
@@ -487,39 +478,32 @@ tree_sample_kernel(SampleArgs)
     // A thread's entries: runs of 4, the lanes' runs side by side; a wave's are contiguous.  What a thread reads of its runs in LDS it has written itself.
     const int wave_size = slice_size / WAVES, runs = wave_size / (kWave * RUN);
 
+    // The walk, over this workgroup's slice of each row, or over all of them.  false: given up
+    auto walk_tree = [&](auto by_itself) __attribute__((always_inline)) {
+    constexpr bool ALONE = decltype(by_itself)::value;
+    int pass = kEnd;
     while (true) {
         const int lane = here(tid) & 63, own = wave * wave_size + lane * RUN;
-        const int pass = uniform(walk.pass), cur = uniform(walk.cur);
-        if (pass == kEnd) break;
-        if (pass == kGiveUp) {  // the first one to give up goes on alone, from the root
-            __syncthreads();
-            if (tid == 0) {
-                flag_sh = ex.go_alone();
-                walk.pass = kRows, walk.cur = 0, walk.len = 1, walk.next = -1, walk.writer = 0;
-            }
-            for (int i = tid; i < n_nodes; i += NT) path[i] = i == 0 ? 0 : -1;
-            __syncthreads();
-            if (!uniform(flag_sh)) return;
-            alone = true;
-            continue;
-        }
-        const int kid = uniform(first_kid[cur]);
+        const bool summed = pass == kResidual;
+        const int cur = uniform(walk.cur);
+        pass = uniform(walk.pass);
+        if (pass == kEnd) return true;
+        if (pass == kGiveUp) return false;
+        const int kid = uniform(nodes[cur].first_kid);
         const bool inner = drawn && kid != kNone;  // the node has children, and what they were drawn from counts
-        if (pass == kDraw && !alone && uniform(walk.writer) != ex.slice) {
-            if (tid == 0) ex.leave_mark();
-            return;
-        }
+        if (!ALONE && pass == kDraw && uniform(walk.writer) != ex.slice) return true;
         const float top = walk.top, draft_top = walk.draft_top;
         const double per_total = walk.per_total, per_draft_total = walk.per_draft_total, takes = walk.taken * per_draft_total;
-        int slice = alone ? 0 : ex.slice, end = alone ? slices : ex.slice + 1;
-        if (pass == kDraw) slice = uniform(walk.writer), end = slice + 1;
+        int slice = ALONE ? 0 : ex.slice;
+        const int end = ALONE ? slices : slice + 1;
+        if (ALONE && pass == kDraw) slice = uniform(walk.writer);
         ++ex.number;
         float wt = -INFINITY, wq = -INFINITY;  // the wave's largest entries
         TT my_x[NODES];                        // logits of nodes that are children, as they are stored: asked for after the rows, and first looked at
         TD my_y[NODES];                        // when the sums of these are done
-        for (; slice < end; ++slice) {
+        do {
             const int lane = here(tid) & 63, own = wave * wave_size + lane * RUN;
-            if (pass == kRows || (alone && told)) {
+            if (pass == kRows || ALONE) {
                 const TT *row = target_row(cur);
                 const TD *drow = inner ? draft_row(cur) : nullptr;
                 float m = -INFINITY, mq = -INFINITY;
@@ -606,18 +590,18 @@ tree_sample_kernel(SampleArgs)
                         if (inner) y_lds[at] = minus_inf<TD>();
                     }
                 };
-                const bool anew = alone && told;  // (the rows have been read again)
-                if (pass == kResidual && inner && !anew) {
+                if (pass == kResidual && inner && !ALONE) {
                     remove(walk.newest);
                 } else {
-                    const int refused = uniform(walk.refused), removed = anew ? 0 : uniform(walk.removed);
+                    const int refused = uniform(walk.refused), removed = ALONE ? 0 :  // (the rows have been read again)
+                        uniform(walk.removed);
                     for (int w = removed / kWave; w * kWave < refused; ++w) {
                         uint64_t m = uniform(kid_mask[w]);
                         if (w == removed / kWave) m &= ~0ull << (removed % kWave);
                         for (; m; m &= m - 1) {
                             const int k = w * kWave + __builtin_ctzll(m);
                             if (k >= refused) break;
-                            remove(tok[k]);
+                            remove(nodes[k].tok);
                         }
                     }
                 }
@@ -682,17 +666,13 @@ tree_sample_kernel(SampleArgs)
                     const bool is_kid = my_parent[n] == cur;
                     const uint64_t kids = __ballot(is_kid);
                     if (lane == 0) kid_mask[wave + n * WAVES] = kids;
-                    if (is_kid) kid_x[tid + n * NT] = entry_of(&my_x[n], 0), kid_y[tid + n * NT] = entry_of(&my_y[n], 0);
+                    if (is_kid) nodes[tid + n * NT].kid_x = entry_of(&my_x[n], 0), nodes[tid + n * NT].kid_y = entry_of(&my_y[n], 0);
                 }
             }
             __syncthreads();
             if (wave == 0) {
-                const int lane = here(tid) & 63, slices = here_scalar(ex.slices), n_nodes = here_scalar(nodes_lds.n);  // (what follows from
-                // them is not worked out before, for every pass and wave)
-                const NodeArrays here_lds{lds, n_nodes};
-                int32_t *const tok = here_lds.tok(), *const path = here_lds.path();
-                float *const accept_u = here_lds.accept_u(), *const kid_x = here_lds.kid_x(), *const kid_y = here_lds.kid_y();
-                double *const new_logit = here_lds.new_logit(), *const new_total = here_lds.new_total();
+                const int lane = here(tid) & 63, slices = here_scalar(ex.slices);  // (what follows from them is not worked out before,
+                // for every pass and wave)
                 // The waves' sums to the slice's: the first WAVES lanes have p's, the next ones q's
                 const bool mine = lane < 2 * WAVES;
                 const int which = lane / WAVES;
@@ -707,7 +687,7 @@ tree_sample_kernel(SampleArgs)
                 }
                 sum = waves_sum(sum);
                 Half p = {}, q = {};
-                if (alone) {
+                if (ALONE) {
                     if (lane % WAVES == 0 && mine) {
                         part_top[which][slice] = mm, part_sum[which][slice] = sum;
                         if (lane == 0) part_best[slice] = best;
@@ -718,10 +698,16 @@ tree_sample_kernel(SampleArgs)
                     Half own_half = {{__float_as_uint(mm), (uint32_t)bits, (uint32_t)(bits >> 32), (uint32_t)best}};
                     const int i = lane % WAVES;
                     const uint32_t value = i == 0 ? own_half.value[0] : i == 1 ? own_half.value[1] : i == 2 ? own_half.value[2] : own_half.value[3];
-                    if (lane < (inner ? 2 : 1) * WAVES) ex.tell(which, i, value, own_half.check());
-                    if (!ex.hear(lane, inner, args_here()->spin_limit, p, q)) {
-                        if (lane == 0) walk.pass = kGiveUp;
-                        goto next_slice;
+                    if (told) {
+                        if (lane < (inner ? 2 : 1) * WAVES) ex.tell(which, i, value, own_half.check());
+                        if (!ex.hear(lane, inner, args_here()->spin_limit, p, q)) {
+                            if (lane == 0) walk.pass = kGiveUp;
+                            goto next_slice;
+                        }
+                    } else {
+                        p = own_half;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) q.value[k] = (uint32_t)__builtin_amdgcn_readlane((int)own_half.value[k], WAVES);
                     }
                 }
                 {
@@ -731,12 +717,12 @@ tree_sample_kernel(SampleArgs)
                     double part = 0, part_q = 0;
                     int part_b = kNone;
                     if (there) {
-                        m = alone ? part_top[0][lane] : __uint_as_float(p.value[0]);
-                        part = alone ? part_sum[0][lane] : from_words(p.value[1], p.value[2]);
-                        part_b = alone ? part_best[lane] : (int)p.value[3];
+                        m = ALONE ? part_top[0][lane] : __uint_as_float(p.value[0]);
+                        part = ALONE ? part_sum[0][lane] : from_words(p.value[1], p.value[2]);
+                        part_b = ALONE ? part_best[lane] : (int)p.value[3];
                         if (inner) {
-                            mq = alone ? part_top[1][lane] : __uint_as_float(q.value[0]);
-                            part_q = alone ? part_sum[1][lane] : from_words(q.value[1], q.value[2]);
+                            mq = ALONE ? part_top[1][lane] : __uint_as_float(q.value[0]);
+                            part_q = ALONE ? part_sum[1][lane] : from_words(q.value[1], q.value[2]);
                         }
                     }
                     double taken = 0, left = 1, pt = per_total, pd = per_draft_total;
@@ -769,10 +755,10 @@ tree_sample_kernel(SampleArgs)
                         uint64_t k = uniform(kid_mask[w]);
                         if (w == refused / kWave) k &= ~0ull << (refused % kWave);
                         if (!k) continue;
-                        const int node = w * kWave + lane, my_token = tok[node];
-                        const double u = accept_u[node];
+                        const int node = w * kWave + lane, my_token = nodes[node].tok;
+                        const double u = nodes[node].accept_u;
                         const bool is_kid = k >> lane & 1;
-                        double px = weight(is_kid ? kid_x[node] : -INFINITY, t, heat) * pt, qx = weight(is_kid ? kid_y[node] : -INFINITY, dt, draft_heat) * pd;
+                        double px = weight(is_kid ? nodes[node].kid_x : -INFINITY, t, heat) * pt, qx = weight(is_kid ? nodes[node].kid_y : -INFINITY, dt, draft_heat) * pd;
                         if (!inner) qx = 1.0;
                         for (; k && found < 0 && !again; k &= k - 1) {
                             const int i = __builtin_ctzll(k);
@@ -791,9 +777,10 @@ tree_sample_kernel(SampleArgs)
                             const double off = of_lane(px, i);
                             px = same ? 0.0 : px;
                             if (inner && same) qx = 0.0;
-                            for (int v = w; v * kWave < n_nodes; ++v)
-                                if (uniform(kid_mask[v]) >> lane & 1 && v * kWave + lane >= refused && tok[v * kWave + lane] == token)
-                                    kid_x[v * kWave + lane] = kid_y[v * kWave + lane] = -INFINITY;
+                            for (int v = w; v * kWave < n_nodes; ++v) {
+                                Node &other = nodes[v * kWave + lane];
+                                if (uniform(kid_mask[v]) >> lane & 1 && v * kWave + lane >= refused && other.tok == token) other.kid_x = other.kid_y = -INFINITY;
+                            }
                             if (inner) {
                                 again = true;
                             } else {
@@ -806,8 +793,8 @@ tree_sample_kernel(SampleArgs)
                     int next_pass = kRows, writer = 0;
                     if (found >= 0) {
                         if (lane == 0) {
-                            path[len] = found;
-                            new_logit[len - 1] = ((double)kid_x[found] - t) / (greedy ? 1.0 : (double)temp), new_total[len - 1] = walk.total;
+                            nodes[len].path = found;
+                            nodes[len - 1].new_logit = ((double)nodes[found].kid_x - t) / (greedy ? 1.0 : (double)temp), nodes[len - 1].new_total = walk.total;
                             walk.len = len + 1, walk.cur = found;
                         }
                     } else if (again) {
@@ -843,7 +830,7 @@ tree_sample_kernel(SampleArgs)
             next_slice:;
             }
             __syncthreads();
-        }
+        } while (ALONE && ++slice < end);
         if (pass != kDraw) continue;
 
         // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
@@ -866,7 +853,8 @@ tree_sample_kernel(SampleArgs)
             return sum_of(v);
         };
         double v[RUN], sum = 0;
-        {
+        const bool sums_there = !ALONE && summed && inner;  // (those of the pass before)
+        if (!sums_there) {
             double all = 0;
 #pragma unroll 1
             for (int r = 0; r < runs; ++r) all += sum = residual_run(r, v);
@@ -891,7 +879,7 @@ tree_sample_kernel(SampleArgs)
             for (int r = 0;; ++r) {
                 const bool again = r == runs;
                 if (again) r = last_run, upto = before;
-                if (again || runs > 1) sum = residual_run(r, v);
+                if (again || runs > 1 || sums_there) sum = residual_run(r, v);
                 const double scan = lanes_scan(sum), of_run = of_lane(scan, 63);
                 if (!again && of_run > 0) last_run = r, before = upto;
                 const uint64_t over = __ballot(sum > 0 && upto + scan > rest), some = __ballot(sum > 0);
@@ -913,7 +901,22 @@ tree_sample_kernel(SampleArgs)
             }
         }
         __syncthreads();
-        break;
+        return true;
+    }
+    };
+
+    bool alone = false;
+    if (!walk_tree(std::false_type{})) {  // the first one to give up goes on alone, from the root
+        __syncthreads();
+        if (tid == 0) {
+            flag_sh = ex.go_alone();
+            walk.pass = kRows, walk.cur = 0, walk.len = 1, walk.next = -1, walk.writer = 0;
+        }
+        for (int i = tid; i < n_nodes; i += NT) nodes[i].path = i == 0 ? 0 : -1;
+        __syncthreads();
+        if (!uniform(flag_sh)) return;
+        alone = true;
+        walk_tree(std::true_type{});
     }
 
     // The outputs
@@ -923,13 +926,12 @@ tree_sample_kernel(SampleArgs)
         return;
     }
     const int len = uniform(walk.len), next = uniform(walk.next);
-    double *const new_logit = nodes_lds.new_logit(), *const new_total = nodes_lds.new_total();
     if (tid == 0) {
         if (next >= 0) {
-            new_logit[len - 1] = ((double)entry_of(target_row(walk.cur), next) - walk.top) / (greedy ? 1.0 : (double)temp);
-            new_total[len - 1] = walk.total;
+            nodes[len - 1].new_logit = ((double)entry_of(target_row(walk.cur), next) - walk.top) / (greedy ? 1.0 : (double)temp);
+            nodes[len - 1].new_total = walk.total;
         } else {
-            new_logit[len - 1] = -INFINITY, new_total[len - 1] = 1.0;
+            nodes[len - 1].new_logit = -INFINITY, nodes[len - 1].new_total = 1.0;
             err |= 4;
         }
         h->len[b] = len;
@@ -940,8 +942,8 @@ tree_sample_kernel(SampleArgs)
     if (told && !alone && wave == WAVES - 1) ex.wait_for_marks(tid & 63, h->spin_limit);
     for (int i = tid; i < h->n_tree; i += NT) {
         const int64_t at = (int64_t)b * h->n_tree + i;
-        h->path[at] = path[i];
-        if (h->logprobs) h->logprobs[at] = i < len ? (float)(new_logit[i] - log(new_total[i])) : 0.f;
+        h->path[at] = nodes[i].path;
+        if (h->logprobs) h->logprobs[at] = i < len ? (float)(nodes[i].new_logit - log(nodes[i].new_total)) : 0.f;
     }
     if (!told) return;
     __syncthreads();
