@@ -393,7 +393,7 @@ struct Walk {
     double rest;                           // what the sum has to pass in the writer's slice
 };
 
-// What there is per node in LDS.  new_: of the path's n-th token in node n, logit / temperature below the largest, and the sum of the weights.  kid_: the logits
+// What there is per node in LDS.  new_: of the path's n-th token in node n, its logit less the largest, and the sum of the weights.  kid_: the logits
 // of both models at a child's token.
 struct Node {
     double new_logit, new_total;
@@ -423,9 +423,9 @@ tree_sample_kernel(SampleArgs)
 
     const ArgsHere a = args_here();
     const int slices = a->slices, vocab = a->vocab;
-    const int b = (int)(blockIdx.x / (uint32_t)slices), tid = threadIdx.x, wave = uniform(tid >> 6);
+    const int b = blockIdx.y, tid = threadIdx.x, wave = uniform(tid >> 6);
     Exchange ex;
-    ex.slices = slices, ex.slice = (int)(blockIdx.x % (uint32_t)slices), ex.call = a->call, ex.number = 0;
+    ex.slices = slices, ex.slice = blockIdx.x, ex.call = a->call, ex.number = 0;
     ex.words = a->records + (int64_t)b * ex.n_words();
     const int n_nodes = (a->n_tree + kWave - 1) / kWave * kWave, slice_size = a->slice;
     Node *const nodes = (Node *)lds;
@@ -794,7 +794,7 @@ tree_sample_kernel(SampleArgs)
                     if (found >= 0) {
                         if (lane == 0) {
                             nodes[len].path = found;
-                            nodes[len - 1].new_logit = ((double)nodes[found].kid_x - t) / (greedy ? 1.0 : (double)temp), nodes[len - 1].new_total = walk.total;
+                            nodes[len - 1].new_logit = (double)nodes[found].kid_x - t, nodes[len - 1].new_total = walk.total;
                             walk.len = len + 1, walk.cur = found;
                         }
                     } else if (again) {
@@ -928,7 +928,7 @@ tree_sample_kernel(SampleArgs)
     const int len = uniform(walk.len), next = uniform(walk.next);
     if (tid == 0) {
         if (next >= 0) {
-            nodes[len - 1].new_logit = ((double)entry_of(target_row(walk.cur), next) - walk.top) / (greedy ? 1.0 : (double)temp);
+            nodes[len - 1].new_logit = (double)entry_of(target_row(walk.cur), next) - walk.top;
             nodes[len - 1].new_total = walk.total;
         } else {
             nodes[len - 1].new_logit = -INFINITY, nodes[len - 1].new_total = 1.0;
@@ -943,7 +943,7 @@ tree_sample_kernel(SampleArgs)
     for (int i = tid; i < h->n_tree; i += NT) {
         const int64_t at = (int64_t)b * h->n_tree + i;
         h->path[at] = nodes[i].path;
-        if (h->logprobs) h->logprobs[at] = i < len ? (float)(nodes[i].new_logit - log(nodes[i].new_total)) : 0.f;
+        if (h->logprobs) h->logprobs[at] = i < len ? (float)(nodes[i].new_logit / (greedy ? 1.0 : (double)temp) - log(nodes[i].new_total)) : 0.f;
     }
     if (!told) return;
     __syncthreads();
@@ -956,7 +956,7 @@ template <typename TT, typename TD> hipError_t launch_types(const SampleArgs &a,
     static std::atomic<uint64_t> allowed{0};
     const hipError_t e = allow_dynamic_lds((const void *)tree_sample_kernel<TT, TD>, kSampleLds, allowed);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((tree_sample_kernel<TT, TD>), dim3((uint32_t)a.batch * a.slices), dim3(NT), bytes, stream, a);
+    hipLaunchKernelGGL((tree_sample_kernel<TT, TD>), dim3(a.slices, a.batch), dim3(NT), bytes, stream, a);
     return hipGetLastError();
 }
 

@@ -93,6 +93,21 @@ def test_vocabularies(vocab, with_replacement):
     c.check()
 
 
+@pytest.mark.parametrize("target,draft", [("bf16", "bf16"), ("f16", "f32"), ("f32", "f16")])
+@pytest.mark.parametrize("vocab", [3, 50, 1021, 4096, 50257])
+def test_nan_that_signals(target, draft, vocab):
+    """NaN of any bits has no probability, wherever it stands: in front of the largest entries, behind them, at a row's end."""
+    c = Case(vocab, 3, 9, vocab, target=target, draft=draft)
+    for x in (c.target, c.draft):
+        bits = {torch.bfloat16: (0x7f81, 0xff81 - 0x10000), torch.float16: (0x7c01, 0xfc01 - 0x10000), torch.float32: (0x7f800001, 0xff800001 - (1 << 32))}[x.dtype]
+        whole = x.view(torch.int32 if x.dtype == torch.float32 else torch.int16)
+        whole[..., 1::3] = bits[0]
+        whole[..., 4::6] = bits[1]
+        whole[1, ..., -1] = bits[1]
+    c.run()
+    c.check()
+
+
 @pytest.mark.parametrize("target,draft", [(t, d) for t in DT for d in (*DT, None)])
 def test_types(target, draft):
     c = Case(3, 4, 24, 10007, target, draft)
