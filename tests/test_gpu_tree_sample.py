@@ -131,6 +131,40 @@ def test_batches(batch, vocab):
     c.check()
 
 
+def test_more_groups_than_there_is_room_for():
+    """1500 sequences of several workgroups each, in float: many rounds of the card."""
+    c = Case(6, 1500, 2, 20011, "f32", "f32", spread=4.0, noise=0.7)
+    assert ls.ls_sample_workspace_bytes(ls.make_sample_desc(c.target, c.draft)) > 1500 * 64
+    c.run()
+    c.check()
+
+
+def test_the_largest_batch():
+    """65535 sequences: the bits of two calls of half of them each, and the reference for the first and the last."""
+    c = Case(7, 64, 3, 11, kind="star")
+    b, most = 64, 65535
+    for name in ("parents", "target", "draft", "tokens", "temperature"):
+        x = getattr(c, name)
+        setattr(c, name, x.repeat(most // b + 1, *(1,) * (x.dim() - 1))[:most].contiguous())
+    gen = torch.Generator().manual_seed(7)
+    c.accept_u, c.sample_u = torch.rand((most, 3), generator=gen), torch.rand(most, generator=gen)
+    out = {k: v.clone() for k, v in c.run().items()}
+    names = ("parents", "target", "draft", "tokens", "temperature", "accept_u", "sample_u")
+    full = {name: getattr(c, name) for name in names}
+
+    def rows(lo, hi):
+        for name in names:
+            setattr(c, name, full[name][lo:hi])
+
+    for lo, hi in ((0, 32768), (32768, most)):
+        rows(lo, hi)
+        for k, v in c.run().items():
+            assert torch.equal(out[k][lo:hi], v), k
+    for lo, hi in ((0, 100), (most - 100, most)):
+        rows(lo, hi)
+        c.check(got={k: v[lo:hi] for k, v in out.items()})
+
+
 def test_the_largest_vocabulary():
     c = Case(5, 1, 3, ls.LS_MAX_VOCAB, "f16", "f16", kind="star")
     c.run()
@@ -313,6 +347,35 @@ def test_recorded_into_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         c.check()
+
+
+def test_graphs_that_share_a_workspace():
+    """Two recorded calls of different sizes, replayed in turns over one workspace, with calls of their own in between."""
+    cases = [Case(83, 5, 20, 40009), Case(84, 9, 7, 90001, "f32", "f16", on_path=0.8)]
+    for c in cases:
+        c.run()
+    shared = torch.full((max(c.args[-1].numel() for c in cases),), 0xff, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for c in cases:
+        c.args[-1] = shared
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            ls.ls_tree_accept_sampled(*c.args)
+    rng = np.random.default_rng(3)
+    for turn in range(6):
+        for c, graph in zip(cases, graphs):
+            c.accept_u = torch.from_numpy(rng.random(c.accept_u.shape, dtype=np.float32))
+            c.args[7].copy_(c.accept_u)
+            for v in c.out.values():
+                v.fill_(9)
+            if turn % 3 == 2:
+                ls.ls_tree_accept_sampled(*c.args)
+            else:
+                graph.replay()
+        torch.cuda.synchronize()
+        for c in cases:
+            c.check()
 
 
 @pytest.mark.parametrize("with_replacement", [False, True])
