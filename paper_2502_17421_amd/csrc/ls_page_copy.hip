@@ -2,7 +2,8 @@
 //
 // Bound by HBM: every byte is read once and written once.  A workgroup takes a (copy, layer, K or V) at a time, whose rows are one contiguous piece
 // (rows token after token, or all rows of a page of heads side by side), a piece per head, or rows by themselves; four 16-byte loads a lane are in
-// flight before the first is stored.  900 whole pages of 16 rows through 8 layers of 8 heads of 128, 944 MB read and written: 187 us, 5.06 TB/s (a large copy by torch: 5.03).  Stores go past the caches: 150 part pages through 16 layers 30 us, else 37.
+// flight before the first is stored.  900 whole pages of 16 rows through 8 layers of 8 heads of 128, 944 MB read and written: 187 us, 5.05 TB/s (a
+// large copy by torch: 5.03).  Stores go past the caches: 150 part pages through 16 layers 30 us, else 37.
 #include "ls_sampling.hpp"
 
 namespace ls {

@@ -1,4 +1,9 @@
 // Block tables of requests that share pages: forks, and compaction of the pool.
+//
+// The tables are small (256 requests of 271 pages: 280 KB, 0.1 us at the rate of a copy); what bounds both is launches that wait for each other, 3.8 us each, and within
+// a launch round trips to the tables.  So there are as few launches as the sizes allow: forks of up to 64 requests take one (64 samples of 8 prompts: 9.8 us; in four launches
+// 13.6), larger ones four (256 beams 16.7 us), compaction one (64 requests in a pool of 40000 pages 8.6 us; in four 15.2) or two (512 requests, 262144 pages: 16.1; in
+// four 22.2).
 #include "ls_sampling.hpp"
 
 namespace ls {

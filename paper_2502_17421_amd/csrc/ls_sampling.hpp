@@ -20,7 +20,7 @@ struct SampleArgs {
     uint32_t call;          // a number of this call's own
     uint64_t *records;
 };
-constexpr int kSampleThreads = 256;
+constexpr int kSampleThreads = 256;  // (48 chains over 128256: 95 us, with 512 threads 108)
 constexpr int kSampleSlices = 64;                   // at most
 constexpr int kSampleUnit = kSampleThreads * 4;     // entries: slices are multiples
 constexpr int kSampleLds = 156 * 1024;              // dynamic LDS, at most
@@ -30,18 +30,22 @@ inline int sample_lds_bytes(int n_tree, int slice, int target_bytes, int draft_b
     return (n_tree + 63) / 64 * 64 * kSampleNode + slice * (target_bytes + draft_bytes);
 }
 static_assert(LS_MAX_TREE * kSampleNode + LS_MAX_VOCAB / kSampleSlices * 8 <= kSampleLds, "every vocabulary fits");
+constexpr int kSampleOtherLds = 3 * 1024;  // beside it, at most
 // The smallest slices with which all workgroups of the call fit on the card at a time; if none do, the largest of which four fit on a compute unit.
+// One chain of 3 tokens over 32000: 19.0 us, with slices of twice the size 20.9; 96 of them 44, with no more than two workgroups on a compute unit 55.  Where not all
+// fit (bf16, chains of 3 over 128256, 128 of them; of 2 over 32000, 300 of them) four on a compute unit take 137 and 77 us, two 172 and 123, eight with slices of half
+// the size 205 and 95.
 inline int sample_slice(int batch, int n_tree, int vocab, int target_bytes, int draft_bytes, int compute_units)
 {
     int slice = kSampleUnit;
     for (; slice < kSampleUnit * 64; slice += kSampleUnit) {
         const int slices = (vocab + slice - 1) / slice;
         if (slices > kSampleSlices) continue;
-        const int each = sample_lds_bytes(n_tree, slice, target_bytes, draft_bytes) + 3072;
+        const int each = sample_lds_bytes(n_tree, slice, target_bytes, draft_bytes) + kSampleOtherLds;
         int fit = 160 * 1024 / each;
         fit = fit > 4 ? 4 : fit;  // by their registers
         if (slices == 1 || (int64_t)batch * slices <= (int64_t)fit * compute_units) return slice;
-        if (sample_lds_bytes(n_tree, slice + kSampleUnit, target_bytes, draft_bytes) + 3072 > 40 * 1024) return slice;
+        if (sample_lds_bytes(n_tree, slice + kSampleUnit, target_bytes, draft_bytes) + kSampleOtherLds > 40 * 1024) return slice;
     }
     return slice;
 }

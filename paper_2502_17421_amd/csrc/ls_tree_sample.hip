@@ -16,8 +16,17 @@
 // Everything is in 64 bits: the border between two neighbouring tokens in a cumulated sum over 150 thousand of them is missed by 32 bits about
 // once in a hundred draws.
 //
-// A sequence belongs to a group of workgroups, one per slice of the vocabulary, which walk its tree together: each keeps its slice of p and q
-// in registers, tells the others its sums, and decides what all of them decide from all sums in the same order.  See Exchange.
+// A sequence belongs to a group of workgroups, one per slice of the vocabulary, which walk its tree together: each reads its slice of both rows into
+// LDS, as they are stored (weights as doubles would take four times the room, and let one workgroup on a compute unit where these let four), and works out the weights
+// anew in each pass over it; it tells the others its sums, and the first wave of each decides what all of them decide, from all sums in the
+// same order.  See Exchange.
+//
+// What bounds it: one request and few trees, the passes' chain: each waits for a row (1 us), its sums, the others' sums (1 us) and the decision (1.5 us).
+// One request, 22 nodes of 32000 in half: 22.7 us (one workgroup by itself 189).  Four beam trees of 69 nodes of 32000 in float 22.9.  Many requests, the
+// weights: 18 instructions of 64 bits each, 2 ns for a wave on a SIMD, and waits that four workgroups on a compute unit do not all cover.  48 chains of 5 tokens over 128256
+// in bf16: 87 us, of which the vector ALUs are busy 45 % (107 MB: 21 us at the rate of a copy); 16 trees over 152064: 69 us.
+// Tried, and not faster than the form of the time: the next child's rows asked for ahead (chains 95.0 us for 93.4), two polls in flight (16 trees 73.5 for
+// 69.8), eight weights of a thread at a time (chains 116 for 98).
 #include <float.h>
 
 #include <type_traits>
@@ -480,429 +489,429 @@ tree_sample_kernel(SampleArgs)
 
     // The walk, over this workgroup's slice of each row, or over all of them.  false: given up
     auto walk_tree = [&](auto by_itself) __attribute__((always_inline)) {
-    constexpr bool ALONE = decltype(by_itself)::value;
-    int pass = kEnd;
-    while (true) {
-        const int lane = here(tid) & 63, own = wave * wave_size + lane * RUN;
-        const bool summed = pass == kResidual;
-        const int cur = uniform(walk.cur);
-        pass = uniform(walk.pass);
-        if (pass == kEnd) return true;
-        if (pass == kGiveUp) return false;
-        const int kid = uniform(nodes[cur].first_kid);
-        const bool inner = drawn && kid != kNone;  // the node has children, and what they were drawn from counts
-        if (!ALONE && pass == kDraw && uniform(walk.writer) != ex.slice) return true;
-        const float top = walk.top, draft_top = walk.draft_top;
-        const double per_total = walk.per_total, per_draft_total = walk.per_draft_total, takes = walk.taken * per_draft_total;
-        int slice = ALONE ? 0 : ex.slice;
-        const int end = ALONE ? slices : slice + 1;
-        if (ALONE && pass == kDraw) slice = uniform(walk.writer);
-        ++ex.number;
-        float wt = -INFINITY, wq = -INFINITY;  // the wave's largest entries
-        TT my_x[NODES];                        // logits of nodes that are children, as they are stored: asked for after the rows, and first looked at
-        TD my_y[NODES];                        // when the sums of these are done
-        do {
+        constexpr bool ALONE = decltype(by_itself)::value;
+        int pass = kEnd;
+        while (true) {
             const int lane = here(tid) & 63, own = wave * wave_size + lane * RUN;
-            if (pass == kRows || ALONE) {
-                const TT *row = target_row(cur);
-                const TD *drow = inner ? draft_row(cur) : nullptr;
-                float m = -INFINITY, mq = -INFINITY;
-                auto fetch = [&](auto *from, auto *to, int at, float &most) __attribute__((always_inline)) {  // entries behind the row's end, one by one
-                    using T = std::remove_reference_t<decltype(*to)>;
+            const bool summed = pass == kResidual;
+            const int cur = uniform(walk.cur);
+            pass = uniform(walk.pass);
+            if (pass == kEnd) return true;
+            if (pass == kGiveUp) return false;
+            const int kid = uniform(nodes[cur].first_kid);
+            const bool inner = drawn && kid != kNone;  // the node has children, and what they were drawn from counts
+            if (!ALONE && pass == kDraw && uniform(walk.writer) != ex.slice) return true;
+            const float top = walk.top, draft_top = walk.draft_top;
+            const double per_total = walk.per_total, per_draft_total = walk.per_draft_total, takes = walk.taken * per_draft_total;
+            int slice = ALONE ? 0 : ex.slice;
+            const int end = ALONE ? slices : slice + 1;
+            if (ALONE && pass == kDraw) slice = uniform(walk.writer);
+            ++ex.number;
+            float wt = -INFINITY, wq = -INFINITY;  // the wave's largest entries
+            TT my_x[NODES];                        // logits of nodes that are children, as they are stored: asked for after the rows, and first looked at
+            TD my_y[NODES];                        // when the sums of these are done
+            do {
+                const int lane = here(tid) & 63, own = wave * wave_size + lane * RUN;
+                if (pass == kRows || ALONE) {
+                    const TT *row = target_row(cur);
+                    const TD *drow = inner ? draft_row(cur) : nullptr;
+                    float m = -INFINITY, mq = -INFINITY;
+                    auto fetch = [&](auto *from, auto *to, int at, float &most) __attribute__((always_inline)) {  // entries behind the row's end, one by one
+                        using T = std::remove_reference_t<decltype(*to)>;
 #pragma unroll 1
-                    for (int e = 0; e < RUN; ++e) {
-                        const T v = at + e < vocab ? from[at + e] : minus_inf<T>();
-                        to[e] = v;
-                        most = fmaxf(most, Elem<T>::load(&v));
-                    }
-                };
+                        for (int e = 0; e < RUN; ++e) {
+                            const T v = at + e < vocab ? from[at + e] : minus_inf<T>();
+                            to[e] = v;
+                            most = fmaxf(most, Elem<T>::load(&v));
+                        }
+                    };
 #pragma unroll 1
-                for (int r0 = 0; r0 < runs; r0 += 4) {
-                    Run<TT> x[4] = {};
-                    Run<TD> y[4] = {};
-                    const int at = slice * slice_size + own + r0 * kWave * RUN;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (r0 + i < runs && at + i * kWave * RUN + RUN <= vocab) x[i] = run_of_row(row + at + i * kWave * RUN);
-                    if (inner)
+                    for (int r0 = 0; r0 < runs; r0 += 4) {
+                        Run<TT> x[4] = {};
+                        Run<TD> y[4] = {};
+                        const int at = slice * slice_size + own + r0 * kWave * RUN;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (r0 + i < runs && at + i * kWave * RUN + RUN <= vocab) y[i] = run_of_row(drow + at + i * kWave * RUN);
+                            if (r0 + i < runs && at + i * kWave * RUN + RUN <= vocab) x[i] = run_of_row(row + at + i * kWave * RUN);
+                        if (inner)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (r0 + i < runs) {
-                            const int in = own + (r0 + i) * kWave * RUN;
-                            if (at + i * kWave * RUN + RUN <= vocab) {
-                                run_to_lds(x[i], x_lds + in);
-#pragma unroll
-                                for (int e = 0; e < RUN; ++e) m = fmaxf(m, x[i].entry(e));
-                            } else {
-                                fetch(row, x_lds + in, slice * slice_size + in, m);
-                            }
-                        }
-                    if (inner)
+                            for (int i = 0; i < 4; ++i)
+                                if (r0 + i < runs && at + i * kWave * RUN + RUN <= vocab) y[i] = run_of_row(drow + at + i * kWave * RUN);
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             if (r0 + i < runs) {
                                 const int in = own + (r0 + i) * kWave * RUN;
                                 if (at + i * kWave * RUN + RUN <= vocab) {
-                                    run_to_lds(y[i], y_lds + in);
+                                    run_to_lds(x[i], x_lds + in);
 #pragma unroll
-                                    for (int e = 0; e < RUN; ++e) mq = fmaxf(mq, y[i].entry(e));
+                                    for (int e = 0; e < RUN; ++e) m = fmaxf(m, x[i].entry(e));
                                 } else {
-                                    fetch(drow, y_lds + in, slice * slice_size + in, mq);
+                                    fetch(row, x_lds + in, slice * slice_size + in, m);
                                 }
                             }
-                }
+                        if (inner)
 #pragma unroll
-                for (int n = 0; n < NODES; ++n) {
-                    my_x[n] = minus_inf<TT>(), my_y[n] = minus_inf<TD>();
-                    if (pass == kRows && my_parent[n] == cur) {
-                        my_x[n] = target_row(cur)[my_tok[n]];
-                        if (inner) my_y[n] = draft_row(cur)[my_tok[n]];
+                            for (int i = 0; i < 4; ++i)
+                                if (r0 + i < runs) {
+                                    const int in = own + (r0 + i) * kWave * RUN;
+                                    if (at + i * kWave * RUN + RUN <= vocab) {
+                                        run_to_lds(y[i], y_lds + in);
+#pragma unroll
+                                        for (int e = 0; e < RUN; ++e) mq = fmaxf(mq, y[i].entry(e));
+                                    } else {
+                                        fetch(drow, y_lds + in, slice * slice_size + in, mq);
+                                    }
+                                }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NODES; ++n) {
+                        my_x[n] = minus_inf<TT>(), my_y[n] = minus_inf<TD>();
+                        if (pass == kRows && my_parent[n] == cur) {
+                            my_x[n] = target_row(cur)[my_tok[n]];
+                            if (inner) my_y[n] = draft_row(cur)[my_tok[n]];
+                        }
+                    }
+                    // +inf counts as the largest finite number of its type, which is what it is from here on
+                    auto whole = [&](auto *entries, float most) __attribute__((always_inline)) {
+                        using T = std::remove_reference_t<decltype(*entries)>;
+                        most = lanes_max(most);
+                        if (most != INFINITY) return most;
+                        most = -INFINITY;
+#pragma unroll 1
+                        for (int r = 0; r < runs; ++r)
+#pragma unroll 1
+                            for (int e = 0; e < RUN; ++e) {
+                                T *const at = entries + own + r * kWave * RUN + e;
+                                if (Elem<T>::load(at) == INFINITY) *at = largest_bits<T>();
+                                most = fmaxf(most, Elem<T>::load(at));
+                            }
+                        return lanes_max(most);
+                    };
+                    wt = whole(x_lds, m);
+                    wq = inner ? whole(y_lds, mq) : -INFINITY;
+                }
+                // refused tokens have no weight any more
+                if (pass != kRows) {
+                    auto remove = [&](int token) __attribute__((always_inline)) {
+                        const int at = token - slice * slice_size, in_wave = at - wave * wave_size;
+                        if ((uint32_t)in_wave < (uint32_t)wave_size && in_wave / RUN % kWave == lane) {
+                            x_lds[at] = minus_inf<TT>();
+                            if (inner) y_lds[at] = minus_inf<TD>();
+                        }
+                    };
+                    if (pass == kResidual && inner && !ALONE) {
+                        remove(walk.newest);
+                    } else {
+                        const int refused = uniform(walk.refused), removed = ALONE ? 0 :  // (the rows have been read again)
+                            uniform(walk.removed);
+                        for (int w = removed / kWave; w * kWave < refused; ++w) {
+                            uint64_t m = uniform(kid_mask[w]);
+                            if (w == removed / kWave) m &= ~0ull << (removed % kWave);
+                            for (; m; m &= m - 1) {
+                                const int k = w * kWave + __builtin_ctzll(m);
+                                if (k >= refused) break;
+                                remove(nodes[k].tok);
+                            }
+                        }
                     }
                 }
-                // +inf counts as the largest finite number of its type, which is what it is from here on
-                auto whole = [&](auto *entries, float most) __attribute__((always_inline)) {
-                    using T = std::remove_reference_t<decltype(*entries)>;
-                    most = lanes_max(most);
-                    if (most != INFINITY) return most;
-                    most = -INFINITY;
+                if (pass == kDraw) break;
+                // sums over the thread and the wave: of the weights relative to the wave's largest entries, or of max(p - a q, 0) and of q
+                double s = 0, sq = 0;
+                auto sum_weights = [&](const auto *entries, double most, double h) __attribute__((always_inline)) {
+                    double sum = 0;
 #pragma unroll 1
-                    for (int r = 0; r < runs; ++r)
-#pragma unroll 1
-                        for (int e = 0; e < RUN; ++e) {
-                            T *const at = entries + own + r * kWave * RUN + e;
-                            if (Elem<T>::load(at) == INFINITY) *at = largest_bits<T>();
-                            most = fmaxf(most, Elem<T>::load(at));
-                        }
-                    return lanes_max(most);
-                };
-                wt = whole(x_lds, m);
-                wq = inner ? whole(y_lds, mq) : -INFINITY;
-            }
-            // refused tokens have no weight any more
-            if (pass != kRows) {
-                auto remove = [&](int token) __attribute__((always_inline)) {
-                    const int at = token - slice * slice_size, in_wave = at - wave * wave_size;
-                    if ((uint32_t)in_wave < (uint32_t)wave_size && in_wave / RUN % kWave == lane) {
-                        x_lds[at] = minus_inf<TT>();
-                        if (inner) y_lds[at] = minus_inf<TD>();
+                    for (int r = 0; r < runs; ++r) {
+                        float l[RUN];
+                        double w[RUN];
+                        run_of_lds(entries + own + r * kWave * RUN).entries(l);
+                        weights(l, most, h, w);
+                        sum += sum_of(w);
                     }
+                    return sum;
                 };
-                if (pass == kResidual && inner && !ALONE) {
-                    remove(walk.newest);
+                if (pass == kRows) {
+                    s = sum_weights(x_lds, wt, heat);
+                    if (inner) sq = sum_weights(y_lds, wq, draft_heat);
+                } else if (inner) {
+#pragma unroll 1
+                    for (int r = 0; r < runs; ++r) {
+                        float l[RUN];
+                        double v[RUN], w[RUN];
+                        run_of_lds(x_lds + own + r * kWave * RUN).entries(l);
+                        weights(l, top, heat, v);
+                        run_of_lds(y_lds + own + r * kWave * RUN).entries(l);
+                        weights(l, draft_top, draft_heat, w);
+#pragma unroll
+                        for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e] * per_total), 0.0);
+                        s += sum_of(v);
+                        sq += sum_of(w);
+                    }
+                    sq *= per_draft_total;
                 } else {
-                    const int refused = uniform(walk.refused), removed = ALONE ? 0 :  // (the rows have been read again)
-                        uniform(walk.removed);
-                    for (int w = removed / kWave; w * kWave < refused; ++w) {
-                        uint64_t m = uniform(kid_mask[w]);
-                        if (w == removed / kWave) m &= ~0ull << (removed % kWave);
-                        for (; m; m &= m - 1) {
-                            const int k = w * kWave + __builtin_ctzll(m);
-                            if (k >= refused) break;
-                            remove(nodes[k].tok);
+                    s = sum_weights(x_lds, top, heat) * per_total;
+                }
+                if (inner) sq = lanes_sum(sq);
+                s = lanes_sum(s);
+                if (pass == kRows) {
+                    if (lane == 0) wave_top[0][wave] = wt, wave_top[1][wave] = wq;
+                    if (greedy) {
+                        int best = kNone;
+#pragma unroll 1
+                        for (int r = runs - 1; r >= 0; --r) {
+                            const Run<TT> x = run_of_lds(x_lds + own + r * kWave * RUN);
+#pragma unroll
+                            for (int e = RUN - 1; e >= 0; --e)
+                                if (x.entry(e) == wt) best = slice * slice_size + own + r * kWave * RUN + e;
                         }
+                        best = wt > -INFINITY ? lanes_min(best) : kNone;
+                        if (lane == 0) wave_best[wave] = best;
                     }
                 }
-            }
-            if (pass == kDraw) break;
-            // sums over the thread and the wave: of the weights relative to the wave's largest entries, or of max(p - a q, 0) and of q
-            double s = 0, sq = 0;
-            auto sum_weights = [&](const auto *entries, double most, double h) __attribute__((always_inline)) {
-                double sum = 0;
-#pragma unroll 1
-                for (int r = 0; r < runs; ++r) {
-                    float l[RUN];
-                    double w[RUN];
-                    run_of_lds(entries + own + r * kWave * RUN).entries(l);
-                    weights(l, most, h, w);
-                    sum += sum_of(w);
+                if (lane == 0) wave_sum[0][wave] = s, wave_sum[1][wave] = sq;
+                if (pass == kRows) {
+#pragma unroll
+                    for (int n = 0; n < NODES; ++n) {
+                        const bool is_kid = my_parent[n] == cur;
+                        const uint64_t kids = __ballot(is_kid);
+                        if (lane == 0) kid_mask[wave + n * WAVES] = kids;
+                        if (is_kid) nodes[tid + n * NT].kid_x = entry_of(&my_x[n], 0), nodes[tid + n * NT].kid_y = entry_of(&my_y[n], 0);
+                    }
                 }
-                return sum;
-            };
-            if (pass == kRows) {
-                s = sum_weights(x_lds, wt, heat);
-                if (inner) sq = sum_weights(y_lds, wq, draft_heat);
-            } else if (inner) {
-#pragma unroll 1
-                for (int r = 0; r < runs; ++r) {
-                    float l[RUN];
-                    double v[RUN], w[RUN];
-                    run_of_lds(x_lds + own + r * kWave * RUN).entries(l);
-                    weights(l, top, heat, v);
+                __syncthreads();
+                if (wave == 0) {
+                    const int lane = here(tid) & 63, slices = here_scalar(ex.slices);  // (what follows from them is not worked out before,
+                    // for every pass and wave)
+                    // The waves' sums to the slice's: the first WAVES lanes have p's, the next ones q's
+                    const bool mine = lane < 2 * WAVES;
+                    const int which = lane / WAVES;
+                    double sum = mine ? wave_sum[which][lane % WAVES] : 0.0;
+                    float mm = 0.f;
+                    int best = kNone;
+                    if (pass == kRows) {
+                        const float m = mine ? wave_top[which][lane % WAVES] : -INFINITY;
+                        mm = waves_max(m);
+                        sum *= weight(m, mm, which == 0 ? heat : draft_heat);
+                        if (greedy) best = lanes_min(lane < WAVES && m == mm ? wave_best[lane] : kNone);
+                    }
+                    sum = waves_sum(sum);
+                    Half p = {}, q = {};
+                    if (ALONE) {
+                        if (lane % WAVES == 0 && mine) {
+                            part_top[which][slice] = mm, part_sum[which][slice] = sum;
+                            if (lane == 0) part_best[slice] = best;
+                        }
+                        if (slice + 1 < end) goto next_slice;
+                    } else {
+                        const uint64_t bits = __builtin_bit_cast(uint64_t, sum);
+                        Half own_half = {{__float_as_uint(mm), (uint32_t)bits, (uint32_t)(bits >> 32), (uint32_t)best}};
+                        const int i = lane % WAVES;
+                        const uint32_t value = i == 0 ? own_half.value[0] : i == 1 ? own_half.value[1] : i == 2 ? own_half.value[2] : own_half.value[3];
+                        if (told) {
+                            if (lane < (inner ? 2 : 1) * WAVES) ex.tell(which, i, value, own_half.check());
+                            if (!ex.hear(lane, inner, args_here()->spin_limit, p, q)) {
+                                if (lane == 0) walk.pass = kGiveUp;
+                                goto next_slice;
+                            }
+                        } else {
+                            p = own_half;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) q.value[k] = (uint32_t)__builtin_amdgcn_readlane((int)own_half.value[k], WAVES);
+                        }
+                    }
+                    {
+                        // What the sums say
+                        const bool there = lane < slices;
+                        float m = -INFINITY, mq = -INFINITY;
+                        double part = 0, part_q = 0;
+                        int part_b = kNone;
+                        if (there) {
+                            m = ALONE ? part_top[0][lane] : __uint_as_float(p.value[0]);
+                            part = ALONE ? part_sum[0][lane] : from_words(p.value[1], p.value[2]);
+                            part_b = ALONE ? part_best[lane] : (int)p.value[3];
+                            if (inner) {
+                                mq = ALONE ? part_top[1][lane] : __uint_as_float(q.value[0]);
+                                part_q = ALONE ? part_sum[1][lane] : from_words(q.value[1], q.value[2]);
+                            }
+                        }
+                        double taken = 0, left = 1, pt = per_total, pd = per_draft_total;
+                        float t = top, dt = draft_top;
+                        int at_best = kNone, refused = 0, newest = -1;
+                        double mass = 1;
+                        if (pass == kRows) {  // (both rows, step by step together, also where there is no draft's)
+                            t = lanes_max(m), dt = lanes_max(mq);
+                            part *= weight(m, t, heat), part_q *= weight(mq, dt, draft_heat);
+                            const double total = lanes_sum(part), draft_total = lanes_sum(part_q);
+                            pt = inverse(total), pd = inverse(draft_total);
+                            pt = total > 0 ? pt : 0.0, pd = draft_total > 0 ? pd : 0.0;
+                            part *= pt;
+                            mass = total > 0 ? 1.0 : 0.0;
+                            if (greedy && total > 0) at_best = lanes_min(there && m == t ? part_b : kNone);
+                            if (lane == 0) walk.top = t, walk.draft_top = dt, walk.total = total, walk.per_total = pt, walk.per_draft_total = pd;
+                        } else {
+                            taken = walk.taken, refused = uniform(walk.refused);
+                            const double q_left = lanes_sum(part_q);
+                            mass = lanes_sum(part);
+                            if (inner && !args_here()->with_replacement) left = q_left;
+                        }
+
+                        // The children that have not been tried.  Of tokens that were chosen the refused ones' probabilities are taken off the sums as long
+                        // as much is left (then a pass over the rows makes the sums anew).
+                        int found = -1;
+                        bool again = false;
+                        const int len = uniform(walk.len);
+                        for (int w = refused / kWave; w * kWave < n_nodes && found < 0 && !again; ++w) {
+                            uint64_t k = uniform(kid_mask[w]);
+                            if (w == refused / kWave) k &= ~0ull << (refused % kWave);
+                            if (!k) continue;
+                            const int node = w * kWave + lane, my_token = nodes[node].tok;
+                            const double u = nodes[node].accept_u;
+                            const bool is_kid = k >> lane & 1;
+                            double px = weight(is_kid ? nodes[node].kid_x : -INFINITY, t, heat) * pt, qx = weight(is_kid ? nodes[node].kid_y : -INFINITY, dt, draft_heat) * pd;
+                            if (!inner) qx = 1.0;
+                            for (; k && found < 0 && !again; k &= k - 1) {
+                                const int i = __builtin_ctzll(k);
+                                const int token = __builtin_amdgcn_readlane(my_token, i);
+                                bool ok;
+                                if (greedy) ok = token == at_best;
+                                else ok = __ballot((px - (inner ? taken * qx : 0.0)) * left > u * qx * mass) >> i & 1;
+                                if (ok) {
+                                    found = w * kWave + i;
+                                    break;
+                                }
+                                refused = w * kWave + i + 1, newest = token;
+                                if (greedy) continue;
+                                // the same token once more has no weight either
+                                const bool same = my_token == token;
+                                const double off = of_lane(px, i);
+                                px = same ? 0.0 : px;
+                                if (inner && same) qx = 0.0;
+                                for (int v = w; v * kWave < n_nodes; ++v) {
+                                    Node &other = nodes[v * kWave + lane];
+                                    if (uniform(kid_mask[v]) >> lane & 1 && v * kWave + lane >= refused && other.tok == token) other.kid_x = other.kid_y = -INFINITY;
+                                }
+                                if (inner) {
+                                    again = true;
+                                } else {
+                                    mass -= off;
+                                    if ((uint32_t)(token - lane * slice_size) < (uint32_t)slice_size) part = __builtin_fmax(part - off, 0.0);
+                                    again = mass < 0x1p-10;
+                                }
+                            }
+                        }
+                        int next_pass = kRows, writer = 0;
+                        if (found >= 0) {
+                            if (lane == 0) {
+                                nodes[len].path = found;
+                                nodes[len - 1].new_logit = (double)nodes[found].kid_x - t, nodes[len - 1].new_total = walk.total;
+                                walk.len = len + 1, walk.cur = found;
+                            }
+                        } else if (again) {
+                            if (inner && lane == 0) walk.taken = left > 0 ? fmin(taken + mass / left, 1e300) : 1e300;  // (finite: q(v) = 0 stays out of it)
+                            if (!inner && lane == 0) walk.taken = 0;
+                            next_pass = kResidual;
+                        } else {  // the path ends here
+                            next_pass = kEnd;
+                            int next = -1;
+                            double rest = 0;
+                            if (greedy) {
+                                next = at_best == kNone ? -1 : at_best;
+                            } else if (mass > 0) {
+                                const double upto = lanes_scan(part), point = (double)args_here()->sample_uniforms[b] * mass;
+                                const uint64_t passed = __ballot(part > 0 && upto > point), some = __ballot(part > 0);
+                                if (some) {
+                                    writer = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);
+                                    rest = point - of_lane(upto - part, writer);
+                                    next_pass = kDraw;
+                                }
+                            }
+                            if (lane == 0) {
+                                walk.next = next, walk.rest = rest, walk.writer = writer;
+                                if (pass == kRows) walk.taken = 0;
+                            }
+                        }
+                        if (lane == 0) {
+                            walk.pass = next_pass;
+                            walk.removed = pass == kRows ? 0 : uniform(walk.refused);
+                            walk.refused = refused, walk.newest = newest;
+                        }
+                    }
+                next_slice:;
+                }
+                __syncthreads();
+            } while (ALONE && ++slice < end);
+            if (pass != kDraw) continue;
+
+            // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
+            // that has any weight.
+            const double rest = walk.rest;
+            // the residual's entries of a run, and their sum
+            auto residual_run = [&](int r, double (&v)[RUN]) __attribute__((always_inline)) {
+                float l[RUN];
+                run_of_lds(x_lds + own + r * kWave * RUN).entries(l);
+                weights(l, top, heat, v);
+#pragma unroll
+                for (int e = 0; e < RUN; ++e) v[e] *= per_total;
+                if (inner) {
+                    double w[RUN];
                     run_of_lds(y_lds + own + r * kWave * RUN).entries(l);
                     weights(l, draft_top, draft_heat, w);
 #pragma unroll
-                    for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e] * per_total), 0.0);
-                    s += sum_of(v);
-                    sq += sum_of(w);
+                    for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e]), 0.0);
                 }
-                sq *= per_draft_total;
-            } else {
-                s = sum_weights(x_lds, top, heat) * per_total;
-            }
-            if (inner) sq = lanes_sum(sq);
-            s = lanes_sum(s);
-            if (pass == kRows) {
-                if (lane == 0) wave_top[0][wave] = wt, wave_top[1][wave] = wq;
-                if (greedy) {
-                    int best = kNone;
+                return sum_of(v);
+            };
+            double v[RUN], sum = 0;
+            const bool sums_there = !ALONE && summed && inner;  // (those of the pass before)
+            if (!sums_there) {
+                double all = 0;
 #pragma unroll 1
-                    for (int r = runs - 1; r >= 0; --r) {
-                        const Run<TT> x = run_of_lds(x_lds + own + r * kWave * RUN);
-#pragma unroll
-                        for (int e = RUN - 1; e >= 0; --e)
-                            if (x.entry(e) == wt) best = slice * slice_size + own + r * kWave * RUN + e;
-                    }
-                    best = wt > -INFINITY ? lanes_min(best) : kNone;
-                    if (lane == 0) wave_best[wave] = best;
-                }
+                for (int r = 0; r < runs; ++r) all += sum = residual_run(r, v);
+                all = lanes_sum(all);
+                if (lane == 0) wave_sum[0][wave] = all;
             }
-            if (lane == 0) wave_sum[0][wave] = s, wave_sum[1][wave] = sq;
-            if (pass == kRows) {
+            __syncthreads();
+            double before = 0, upto = 0;  // of the entries before the wave's; before what has been looked at
+            int at_wave = -1;
+            bool passed = false;
 #pragma unroll
-                for (int n = 0; n < NODES; ++n) {
-                    const bool is_kid = my_parent[n] == cur;
-                    const uint64_t kids = __ballot(is_kid);
-                    if (lane == 0) kid_mask[wave + n * WAVES] = kids;
-                    if (is_kid) nodes[tid + n * NT].kid_x = entry_of(&my_x[n], 0), nodes[tid + n * NT].kid_y = entry_of(&my_y[n], 0);
+            for (int w = 0; w < WAVES; ++w) {
+                const double of_wave = uniform(wave_sum[0][w]);
+                if (of_wave > 0 && !passed) at_wave = w, before = upto, passed = upto + of_wave > rest;
+                upto += of_wave;
+            }
+            if (wave == at_wave) {
+                // runs in turn, until one passes; where roundings let none, the last that has any weight
+                upto = before;
+                int last_run = -1;
+#pragma unroll 1
+                for (int r = 0;; ++r) {
+                    const bool again = r == runs;
+                    if (again) r = last_run, upto = before;
+                    if (again || runs > 1 || sums_there) sum = residual_run(r, v);
+                    const double scan = lanes_scan(sum), of_run = of_lane(scan, 63);
+                    if (!again && of_run > 0) last_run = r, before = upto;
+                    const uint64_t over = __ballot(sum > 0 && upto + scan > rest), some = __ballot(sum > 0);
+                    if (over || again) {
+                        if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
+                            double c = upto + (scan - sum);
+                            int place = 0;
+                            passed = false;
+#pragma unroll
+                            for (int e = 0; e < RUN; ++e) {
+                                c += v[e];
+                                if (v[e] > 0 && !passed) place = e, passed = c > rest;
+                            }
+                            walk.next = uniform(walk.writer) * slice_size + own + r * kWave * RUN + place;
+                        }
+                        break;
+                    }
+                    upto += of_run;
                 }
             }
             __syncthreads();
-            if (wave == 0) {
-                const int lane = here(tid) & 63, slices = here_scalar(ex.slices);  // (what follows from them is not worked out before,
-                // for every pass and wave)
-                // The waves' sums to the slice's: the first WAVES lanes have p's, the next ones q's
-                const bool mine = lane < 2 * WAVES;
-                const int which = lane / WAVES;
-                double sum = mine ? wave_sum[which][lane % WAVES] : 0.0;
-                float mm = 0.f;
-                int best = kNone;
-                if (pass == kRows) {
-                    const float m = mine ? wave_top[which][lane % WAVES] : -INFINITY;
-                    mm = waves_max(m);
-                    sum *= weight(m, mm, which == 0 ? heat : draft_heat);
-                    if (greedy) best = lanes_min(lane < WAVES && m == mm ? wave_best[lane] : kNone);
-                }
-                sum = waves_sum(sum);
-                Half p = {}, q = {};
-                if (ALONE) {
-                    if (lane % WAVES == 0 && mine) {
-                        part_top[which][slice] = mm, part_sum[which][slice] = sum;
-                        if (lane == 0) part_best[slice] = best;
-                    }
-                    if (slice + 1 < end) goto next_slice;
-                } else {
-                    const uint64_t bits = __builtin_bit_cast(uint64_t, sum);
-                    Half own_half = {{__float_as_uint(mm), (uint32_t)bits, (uint32_t)(bits >> 32), (uint32_t)best}};
-                    const int i = lane % WAVES;
-                    const uint32_t value = i == 0 ? own_half.value[0] : i == 1 ? own_half.value[1] : i == 2 ? own_half.value[2] : own_half.value[3];
-                    if (told) {
-                        if (lane < (inner ? 2 : 1) * WAVES) ex.tell(which, i, value, own_half.check());
-                        if (!ex.hear(lane, inner, args_here()->spin_limit, p, q)) {
-                            if (lane == 0) walk.pass = kGiveUp;
-                            goto next_slice;
-                        }
-                    } else {
-                        p = own_half;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) q.value[k] = (uint32_t)__builtin_amdgcn_readlane((int)own_half.value[k], WAVES);
-                    }
-                }
-                {
-                    // What the sums say
-                    const bool there = lane < slices;
-                    float m = -INFINITY, mq = -INFINITY;
-                    double part = 0, part_q = 0;
-                    int part_b = kNone;
-                    if (there) {
-                        m = ALONE ? part_top[0][lane] : __uint_as_float(p.value[0]);
-                        part = ALONE ? part_sum[0][lane] : from_words(p.value[1], p.value[2]);
-                        part_b = ALONE ? part_best[lane] : (int)p.value[3];
-                        if (inner) {
-                            mq = ALONE ? part_top[1][lane] : __uint_as_float(q.value[0]);
-                            part_q = ALONE ? part_sum[1][lane] : from_words(q.value[1], q.value[2]);
-                        }
-                    }
-                    double taken = 0, left = 1, pt = per_total, pd = per_draft_total;
-                    float t = top, dt = draft_top;
-                    int at_best = kNone, refused = 0, newest = -1;
-                    double mass = 1;
-                    if (pass == kRows) {  // (both rows, step by step together, also where there is no draft's)
-                        t = lanes_max(m), dt = lanes_max(mq);
-                        part *= weight(m, t, heat), part_q *= weight(mq, dt, draft_heat);
-                        const double total = lanes_sum(part), draft_total = lanes_sum(part_q);
-                        pt = inverse(total), pd = inverse(draft_total);
-                        pt = total > 0 ? pt : 0.0, pd = draft_total > 0 ? pd : 0.0;
-                        part *= pt;
-                        mass = total > 0 ? 1.0 : 0.0;
-                        if (greedy && total > 0) at_best = lanes_min(there && m == t ? part_b : kNone);
-                        if (lane == 0) walk.top = t, walk.draft_top = dt, walk.total = total, walk.per_total = pt, walk.per_draft_total = pd;
-                    } else {
-                        taken = walk.taken, refused = uniform(walk.refused);
-                        const double q_left = lanes_sum(part_q);
-                        mass = lanes_sum(part);
-                        if (inner && !args_here()->with_replacement) left = q_left;
-                    }
-
-                    // The children that have not been tried.  Of tokens that were chosen the refused ones' probabilities are taken off the sums as long
-                    // as much is left (then a pass over the rows makes the sums anew).
-                    int found = -1;
-                    bool again = false;
-                    const int len = uniform(walk.len);
-                    for (int w = refused / kWave; w * kWave < n_nodes && found < 0 && !again; ++w) {
-                        uint64_t k = uniform(kid_mask[w]);
-                        if (w == refused / kWave) k &= ~0ull << (refused % kWave);
-                        if (!k) continue;
-                        const int node = w * kWave + lane, my_token = nodes[node].tok;
-                        const double u = nodes[node].accept_u;
-                        const bool is_kid = k >> lane & 1;
-                        double px = weight(is_kid ? nodes[node].kid_x : -INFINITY, t, heat) * pt, qx = weight(is_kid ? nodes[node].kid_y : -INFINITY, dt, draft_heat) * pd;
-                        if (!inner) qx = 1.0;
-                        for (; k && found < 0 && !again; k &= k - 1) {
-                            const int i = __builtin_ctzll(k);
-                            const int token = __builtin_amdgcn_readlane(my_token, i);
-                            bool ok;
-                            if (greedy) ok = token == at_best;
-                            else ok = __ballot((px - (inner ? taken * qx : 0.0)) * left > u * qx * mass) >> i & 1;
-                            if (ok) {
-                                found = w * kWave + i;
-                                break;
-                            }
-                            refused = w * kWave + i + 1, newest = token;
-                            if (greedy) continue;
-                            // the same token once more has no weight either
-                            const bool same = my_token == token;
-                            const double off = of_lane(px, i);
-                            px = same ? 0.0 : px;
-                            if (inner && same) qx = 0.0;
-                            for (int v = w; v * kWave < n_nodes; ++v) {
-                                Node &other = nodes[v * kWave + lane];
-                                if (uniform(kid_mask[v]) >> lane & 1 && v * kWave + lane >= refused && other.tok == token) other.kid_x = other.kid_y = -INFINITY;
-                            }
-                            if (inner) {
-                                again = true;
-                            } else {
-                                mass -= off;
-                                if ((uint32_t)(token - lane * slice_size) < (uint32_t)slice_size) part = __builtin_fmax(part - off, 0.0);
-                                again = mass < 0x1p-10;
-                            }
-                        }
-                    }
-                    int next_pass = kRows, writer = 0;
-                    if (found >= 0) {
-                        if (lane == 0) {
-                            nodes[len].path = found;
-                            nodes[len - 1].new_logit = (double)nodes[found].kid_x - t, nodes[len - 1].new_total = walk.total;
-                            walk.len = len + 1, walk.cur = found;
-                        }
-                    } else if (again) {
-                        if (inner && lane == 0) walk.taken = left > 0 ? fmin(taken + mass / left, 1e300) : 1e300;  // (finite: q(v) = 0 stays out of it)
-                        if (!inner && lane == 0) walk.taken = 0;
-                        next_pass = kResidual;
-                    } else {  // the path ends here
-                        next_pass = kEnd;
-                        int next = -1;
-                        double rest = 0;
-                        if (greedy) {
-                            next = at_best == kNone ? -1 : at_best;
-                        } else if (mass > 0) {
-                            const double upto = lanes_scan(part), point = (double)args_here()->sample_uniforms[b] * mass;
-                            const uint64_t passed = __ballot(part > 0 && upto > point), some = __ballot(part > 0);
-                            if (some) {
-                                writer = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);
-                                rest = point - of_lane(upto - part, writer);
-                                next_pass = kDraw;
-                            }
-                        }
-                        if (lane == 0) {
-                            walk.next = next, walk.rest = rest, walk.writer = writer;
-                            if (pass == kRows) walk.taken = 0;
-                        }
-                    }
-                    if (lane == 0) {
-                        walk.pass = next_pass;
-                        walk.removed = pass == kRows ? 0 : uniform(walk.refused);
-                        walk.refused = refused, walk.newest = newest;
-                    }
-                }
-            next_slice:;
-            }
-            __syncthreads();
-        } while (ALONE && ++slice < end);
-        if (pass != kDraw) continue;
-
-        // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
-        // that has any weight.
-        const double rest = walk.rest;
-        // the residual's entries of a run, and their sum
-        auto residual_run = [&](int r, double (&v)[RUN]) __attribute__((always_inline)) {
-            float l[RUN];
-            run_of_lds(x_lds + own + r * kWave * RUN).entries(l);
-            weights(l, top, heat, v);
-#pragma unroll
-            for (int e = 0; e < RUN; ++e) v[e] *= per_total;
-            if (inner) {
-                double w[RUN];
-                run_of_lds(y_lds + own + r * kWave * RUN).entries(l);
-                weights(l, draft_top, draft_heat, w);
-#pragma unroll
-                for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e]), 0.0);
-            }
-            return sum_of(v);
-        };
-        double v[RUN], sum = 0;
-        const bool sums_there = !ALONE && summed && inner;  // (those of the pass before)
-        if (!sums_there) {
-            double all = 0;
-#pragma unroll 1
-            for (int r = 0; r < runs; ++r) all += sum = residual_run(r, v);
-            all = lanes_sum(all);
-            if (lane == 0) wave_sum[0][wave] = all;
+            return true;
         }
-        __syncthreads();
-        double before = 0, upto = 0;  // of the entries before the wave's; before what has been looked at
-        int at_wave = -1;
-        bool passed = false;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const double of_wave = uniform(wave_sum[0][w]);
-            if (of_wave > 0 && !passed) at_wave = w, before = upto, passed = upto + of_wave > rest;
-            upto += of_wave;
-        }
-        if (wave == at_wave) {
-            // runs in turn, until one passes; where roundings let none, the last that has any weight
-            upto = before;
-            int last_run = -1;
-#pragma unroll 1
-            for (int r = 0;; ++r) {
-                const bool again = r == runs;
-                if (again) r = last_run, upto = before;
-                if (again || runs > 1 || sums_there) sum = residual_run(r, v);
-                const double scan = lanes_scan(sum), of_run = of_lane(scan, 63);
-                if (!again && of_run > 0) last_run = r, before = upto;
-                const uint64_t over = __ballot(sum > 0 && upto + scan > rest), some = __ballot(sum > 0);
-                if (over || again) {
-                    if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
-                        double c = upto + (scan - sum);
-                        int place = 0;
-                        passed = false;
-#pragma unroll
-                        for (int e = 0; e < RUN; ++e) {
-                            c += v[e];
-                            if (v[e] > 0 && !passed) place = e, passed = c > rest;
-                        }
-                        walk.next = uniform(walk.writer) * slice_size + own + r * kWave * RUN + place;
-                    }
-                    break;
-                }
-                upto += of_run;
-            }
-        }
-        __syncthreads();
-        return true;
-    }
     };
 
     bool alone = false;
