@@ -221,7 +221,10 @@ def test_a_large_pool():
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, torch.float16])
 @pytest.mark.parametrize("layers,heads,page_size,d,layout", [(1, 1, 1, 8, "head"), (2, 8, 16, 128, "head"), (3, 4, 32, 64, "token"), (1, 32, 16, 128, "token"),
-                                                            (2, 3, 24, 40, "head"), (4, 5, 16, 72, "gaps"), (1, 2, 256, 512, "head")])
+                                                            (2, 3, 24, 40, "head"), (4, 5, 16, 72, "gaps"), (1, 2, 256, 512, "head"),
+                                                            # pages that several workgroups take shares of
+                                                            (2, 7, 72, 136, "head"), (2, 7, 72, 136, "token"), (1, 7, 72, 136, "gaps"), (2, 7, 72, 136, "wide"),
+                                                            (3, 8, 128, 128, "head"), (1, 3, 16, 64, "wide")])
 @pytest.mark.parametrize("n", [0, 1, 9, 60])
 def test_copies(dtype, layers, heads, page_size, d, layout, n):
     rng = np.random.default_rng(n + page_size)
@@ -231,6 +234,9 @@ def test_copies(dtype, layers, heads, page_size, d, layout, n):
     if layout == "token":
         make_ = make
         make = lambda: make_().transpose(2, 3).contiguous().transpose(2, 3)  # noqa: E731
+    elif layout == "wide":  # rows token after token, of more heads than these
+        make = lambda: torch.randint(-30000, 30000, (layers, pages, page_size, heads + 1, d * dtype.itemsize // 2), dtype=torch.int16,  # noqa: E731
+                                     device="cuda").view(dtype)[:, :, :, :heads].transpose(2, 3)
     elif layout == "gaps":  # rows further apart than they are long
         make = lambda: torch.randint(-30000, 30000, (layers, pages, heads, page_size + 1, (d + 8) * dtype.itemsize // 2), dtype=torch.int16,  # noqa: E731
                                      device="cuda").view(dtype)[:, :, :, :page_size, :d]
