@@ -224,12 +224,11 @@ __device__ __forceinline__ float lanes_max(float x)
     auto row = [&](int lane) __attribute__((always_inline)) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); };
     return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
 }
-// The same over WAVES neighbouring lanes, in all of these: of the lane next to it, of two lanes on, of the other four
+// The same over WAVES neighbouring lanes, in all of these: of the lane next to it, of two lanes on
 __device__ __forceinline__ double waves_sum(double x)
 {
     x += from_lane<0xb1, 0xf>(x);
     x += from_lane<0x4e, 0xf>(x);
-    if constexpr (WAVES == 8) x += from_lane<0x141, 0xf>(x);
     return x;
 }
 __device__ __forceinline__ float waves_max(float x)
@@ -239,7 +238,6 @@ __device__ __forceinline__ float waves_max(float x)
     };
     step(Const<0xb1>{});
     step(Const<0x4e>{});
-    if constexpr (WAVES == 8) step(Const<0x141>{});
     return x;
 }
 // 1 / x to the last bit or two, for x of the size of such sums
@@ -416,7 +414,7 @@ __global__ void __launch_bounds__(NT, 4)
 tree_sample_kernel(SampleArgs)
 {
     constexpr int NODES = LS_MAX_TREE / NT;  // of a thread: tid, tid + NT
-    static_assert(WAVES == 4 || WAVES == 8, "their sums are joined in as many lanes");
+    static_assert(WAVES == 4, "their sums are joined in as many lanes");
     // what there is per node, then the slice's entries of both rows
     extern __shared__ __align__(16) uint8_t lds[];
     __shared__ uint64_t kid_mask[LS_MAX_TREE / kWave];
