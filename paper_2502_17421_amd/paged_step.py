@@ -50,8 +50,9 @@ class PagedCache:
         self._next_lens = ints(batch)
         self.slots = self.positions = None
         self._buffers = {}
-        self._next_table = None   # of forks and compactions
+        self._next_table = torch.zeros_like(self.block_table)  # of forks and compactions
         self._n_copies = ints(1)
+        self._may_share = False  # a fork or compaction has run, or has been recorded
 
     def _buffer(self, name, size, dtype=torch.uint8):
         """`size` elements or more.  A recorded step goes on using the buffers it was recorded with, so one that a larger step outgrows is
@@ -65,20 +66,25 @@ class PagedCache:
 
     def release(self, request):
         """The request has ended: its pages go back with the next plan (its new length must be 0 or a new request's).  Where requests may
-        share pages, by a fork: at once, those that nobody else holds."""
-        if self._next_table is None:
-            self.kv_lens[request] = 0
+        share pages, by a fork: at once, those that nobody else holds; so too in a recording, which may be replayed after a fork."""
+        if not self._may_share and not self._recording():
+            self._set(self.kv_lens, request, 0)
             return
         sources = torch.arange(self.batch, dtype=torch.int32, device=self.kv_lens.device)
-        sources[request] = -1
+        self._set(sources, request, -1)
         self.fork(sources)
 
     # ---- requests that share pages
 
-    def _tables(self):
-        if self._next_table is None:
-            self._next_table = torch.zeros_like(self.block_table)
-        return self._next_table
+    @staticmethod
+    def _set(x, request, value):
+        if type(request) is int:
+            x[request].fill_(value)  # (an assignment brings the value from the host, which a recording refuses)
+        else:
+            x[request] = value
+
+    def _recording(self):
+        return self.kv_lens.is_cuda and torch.cuda.is_current_stream_capturing()
 
     def _move_rows(self, copies):
         desc = ls.make_copy_desc(self.k_pages, self.v_pages, copies.shape[0])
@@ -91,9 +97,10 @@ class PagedCache:
         for x in (sources,) if keep_lens is None else (sources, keep_lens):
             if x.shape != self.kv_lens.shape or x.dtype != torch.int32:
                 raise ValueError(f"sources, keep_lens: int32 [{self.batch}]")
+        self._may_share = True
         desc = ls.make_page_desc(self.block_table, 0, self.page_size, self.n_pages)
         copies = self._buffer("fork copies", 4 * self.batch, torch.int32)[:4 * self.batch].view(-1, 4)
-        ls.ls_page_fork(desc, sources, keep_lens, self.kv_lens, self.pages_held, self.block_table, self.free_pages, self.free_count, self._tables(),
+        ls.ls_page_fork(desc, sources, keep_lens, self.kv_lens, self.pages_held, self.block_table, self.free_pages, self.free_count, self._next_table,
                         self._next_lens, self._next_held, self._next_free, copies, self._n_copies, self.err,
                         self._buffer("fork", ls.ls_page_fork_workspace_bytes(desc)))
         self._move_rows(copies)
@@ -103,10 +110,11 @@ class PagedCache:
 
     def compact(self):
         """The pages in use to the front of the pool: afterwards they are 0 .. n_pages - free_count - 1."""
+        self._may_share = True
         desc = ls.make_page_desc(self.block_table, 0, self.page_size, self.n_pages)
         n = self.n_pages // 2 + 1
         copies = self._buffer("compact copies", 4 * n, torch.int32)[:4 * n].view(-1, 4)
-        ls.ls_page_compact(desc, self.pages_held, self.block_table, self._tables(), self.free_pages, self.free_count, copies, self._n_copies,
+        ls.ls_page_compact(desc, self.pages_held, self.block_table, self._next_table, self.free_pages, self.free_count, copies, self._n_copies,
                            self._buffer("compact", ls.ls_page_compact_workspace_bytes(desc)))
         self._move_rows(copies)
         self.block_table.copy_(self._next_table)
