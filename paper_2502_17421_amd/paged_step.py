@@ -22,6 +22,8 @@ Several continuations of a prompt, beams, requests that go back to earlier rows:
     cache.fork(sources)                                             # ls_page_fork, ls_page_copy: full pages are shared
     cache.compact()                                                 # ls_page_compact, ls_page_copy: pages in use to the front of the pool
 
+A fork ends a step that has been planned and not kept or committed yet; a release does not, nor does a compaction, but for the slots.
+
 Everything runs on torch's current stream and nothing waits for the GPU: lengths, tables and the number of free pages stay on
 the device, so a step can be recorded into a graph and replayed, other steps in between.
 `python -m paper_2502_17421_amd.paged_step` runs three requests through both.
@@ -52,7 +54,10 @@ class PagedCache:
         self._buffers = {}
         self._next_table = torch.zeros_like(self.block_table)  # of forks and compactions
         self._n_copies = ints(1)
+        self._fork_err = ints(batch)
         self._may_share = False  # a fork or compaction has run, or has been recorded
+        self._ended = False      # a fork has ended the last plan
+        self._recorded = False   # a plan has been recorded: replays are plans that nothing here sees
 
     def _buffer(self, name, size, dtype=torch.uint8):
         """`size` elements or more.  A recorded step goes on using the buffers it was recorded with, so one that a larger step outgrows is
@@ -66,13 +71,17 @@ class PagedCache:
 
     def release(self, request):
         """The request has ended: its pages go back with the next plan (its new length must be 0 or a new request's).  Where requests may
-        share pages, by a fork: at once, those that nobody else holds; so too in a recording, which may be replayed after a fork."""
+        share pages, by a fork: at once, those that nobody else holds; so too in a recording, which may be replayed after a fork.
+        In a step that has been planned it counts as refused from now on (err is 1); the others go on with the pages they were given."""
+        for x, value in ((self.kv_lens, 0), (self.total_lens, 0), (self.err, 1)):
+            self._set(x, request, value)
         if not self._may_share and not self._recording():
-            self._set(self.kv_lens, request, 0)
             return
-        sources = torch.arange(self.batch, dtype=torch.int32, device=self.kv_lens.device)
+        # (what ls_page_fork does with requests whose source is none: they keep all they hold, and what was reserved for a step)
+        sources = torch.full_like(self.kv_lens, -2)
         self._set(sources, request, -1)
-        self.fork(sources)
+        self._next_table.copy_(self.block_table)
+        self._fork(sources, None, self._fork_err)
 
     # ---- requests that share pages
 
@@ -90,26 +99,34 @@ class PagedCache:
         desc = ls.make_copy_desc(self.k_pages, self.v_pages, copies.shape[0])
         ls.ls_page_copy(desc, copies, self._n_copies, self.k_pages, self.v_pages)
 
-    def fork(self, sources, keep_lens=None):
-        """Request b goes on from the rows (the first keep_lens[b]) of request sources[b], -1: from none, as they are now; int32 [batch], device.
-        Full pages are shared, of a page filled in part every request but one gets a copy, and pages that nobody holds any more are free
-        at once.  err: 1 where no page was left for the copy (the request then ends with its full pages), 2 for sources or lengths that are none."""
-        for x in (sources,) if keep_lens is None else (sources, keep_lens):
-            if x.shape != self.kv_lens.shape or x.dtype != torch.int32:
-                raise ValueError(f"sources, keep_lens: int32 [{self.batch}]")
+    def _fork(self, sources, keep_lens, err):
         self._may_share = True
         desc = ls.make_page_desc(self.block_table, 0, self.page_size, self.n_pages)
         copies = self._buffer("fork copies", 4 * self.batch, torch.int32)[:4 * self.batch].view(-1, 4)
         ls.ls_page_fork(desc, sources, keep_lens, self.kv_lens, self.pages_held, self.block_table, self.free_pages, self.free_count, self._next_table,
-                        self._next_lens, self._next_held, self._next_free, copies, self._n_copies, self.err,
+                        self._next_lens, self._next_held, self._next_free, copies, self._n_copies, err,
                         self._buffer("fork", ls.ls_page_fork_workspace_bytes(desc)))
-        self._move_rows(copies)
         for kept, made in ((self.block_table, self._next_table), (self.kv_lens, self._next_lens), (self.pages_held, self._next_held),
                            (self.free_count, self._next_free)):
             kept.copy_(made)
+        return copies
+
+    def fork(self, sources, keep_lens=None):
+        """Request b goes on from the rows (the first keep_lens[b]) of request sources[b], -1: from none, as they are now; int32 [batch], device.
+        Full pages are shared, of a page filled in part every request but one gets a copy, and pages that nobody holds any more are free
+        at once, those that a plan reserved among them: the step is over, and what comes next has to be planned.
+        err: 1 where no page was left for the copy (the request then ends with its full pages), 2 for sources or lengths that are none."""
+        for x in (sources,) if keep_lens is None else (sources, keep_lens):
+            if x.shape != self.kv_lens.shape or x.dtype != torch.int32:
+                raise ValueError(f"sources, keep_lens: int32 [{self.batch}]")
+        self._move_rows(self._fork(sources, keep_lens, self.err))
+        self.slots = self.positions = None
+        self.total_lens.copy_(self.kv_lens)  # (of a recorded plan: nothing is new)
+        self._ended = True
 
     def compact(self):
-        """The pages in use to the front of the pool: afterwards they are 0 .. n_pages - free_count - 1."""
+        """The pages in use to the front of the pool: afterwards they are 0 .. n_pages - free_count - 1.  Rows of a step that are still to be
+        written have to be planned again."""
         self._may_share = True
         desc = ls.make_page_desc(self.block_table, 0, self.page_size, self.n_pages)
         n = self.n_pages // 2 + 1
@@ -118,6 +135,7 @@ class PagedCache:
                            self._buffer("compact", ls.ls_page_compact_workspace_bytes(desc)))
         self._move_rows(copies)
         self.block_table.copy_(self._next_table)
+        self.slots = self.positions = None  # (they say where the pages were)
 
     def plan(self, new_lens, n_tokens=0):
         """Pages for new_lens (int32 [batch], device) more rows of each request; with n_tokens, the packed tokens' slots and
@@ -125,6 +143,7 @@ class PagedCache:
         if new_lens.shape != self.kv_lens.shape or new_lens.dtype != torch.int32:
             raise ValueError(f"new_lens: int32 [{self.batch}]")
         self.slots = self.positions = None
+        self._ended, self._recorded = False, self._recorded or self._recording()
         if n_tokens:
             self.slots = self._buffer("slots", n_tokens, torch.int32)[:n_tokens]
             self.positions = self._buffer("positions", n_tokens, torch.int32)[:n_tokens].view(1, n_tokens)
@@ -135,8 +154,13 @@ class PagedCache:
         self.pages_held.copy_(self._next_held)
         self.free_count.copy_(self._next_free)
 
+    def _check_plan(self):
+        if self._ended and not self._recorded and not self._recording():
+            raise RuntimeError("a fork has ended the step: it has to be planned again")
+
     def keep_new(self):
         """The step's rows have been written: they count as cached (refused requests stay as they were)."""
+        self._check_plan()
         self.kv_lens.copy_(torch.where(self.err == 0, self.total_lens, self.kv_lens))
 
     # ---- new tokens, packed: q [n_tokens, heads, head_dim], k and v [n_tokens, kv heads, head_dim]
@@ -147,7 +171,7 @@ class PagedCache:
         kp, vp = self.k_pages[layer], self.v_pages[layer]
         n = q.shape[0]
         if self.slots is None or n > self.slots.shape[0] or n > positions.shape[1]:
-            raise ValueError("more tokens than were planned")
+            raise ValueError("more tokens than were planned (a fork or a compaction takes the slots away)")
         if q_out.shape != q.shape or not k.shape == v.shape == (n, kp.shape[1], kp.shape[3]):
             raise ValueError("q_out: the shape of q; k and v: [tokens, kv heads, head_dim] for the same tokens")
         if not q.dtype == k.dtype == v.dtype == q_out.dtype == kp.dtype:
@@ -194,6 +218,7 @@ class PagedCache:
         """k_trees, v_trees: a tensor per layer.  The accepted rows go into the pages and count as cached, as far as the pages reach that
         the plan before gave the request: a request it refused commits nothing, a path beyond its pages ends with them.  err is then
         1 (or what it was) for requests of which not all rows were committed."""
+        self._check_plan()
         room = self.pages_held * self.page_size - self.kv_lens
         fits = torch.where(self.err == 0, torch.minimum(accept_len, room), 0)
         for layer, (k_tree, v_tree) in enumerate(zip(k_trees, v_trees)):

@@ -1,9 +1,10 @@
-"""Requests of paged_step.PagedCache that end, on the CPU with plain stand-ins for the device calls: recordings that are replayed later."""
+"""Requests of paged_step.PagedCache that end, on the CPU with plain stand-ins for the device calls: in recordings that are replayed later, and
+in a step that has been planned; forks and compactions there."""
 import pytest
 import torch
 
 from paper_2502_17421_amd import paged_step
-from test_paged_cache import filled_cache, ints, plain_calls, request_rows  # noqa: F401  (plain_calls: fixture)
+from test_paged_cache import filled_cache, ints, plain_calls, trees  # noqa: F401  (plain_calls: fixture)
 from test_paged_cache_fork import contents, plain_forks, same  # noqa: F401  (plain_forks: fixture)
 
 
@@ -48,3 +49,97 @@ def test_a_release_recorded_before_a_fork_and_replayed_after_it(plain_forks, rec
         check_pages(cache)
     assert cache.kv_lens.tolist() == [20, 40, 20] and not set(tables(cache)[0]) & set(tables(cache)[1])
     assert same(contents(cache)[1], before[1]) and same(contents(cache)[2], before[2])
+
+
+@pytest.mark.parametrize("forked", [False, True])
+def test_a_release_in_a_planned_step_leaves_the_others_their_pages(plain_forks, forked):  # noqa: F811
+    cache = filled_cache([40, 16, 1], 9)
+    if forked:
+        cache.fork(ints([0, 1, 2]))
+    before = contents(cache)
+    cache.plan(ints([20, 3, 0]), 23)
+    planned, slots = tables(cache)[0], cache.slots.clone()
+    assert len(planned) == 4
+    cache.release(1)
+    assert tables(cache)[0] == planned and cache.err.tolist() == [0, 1, 0] and torch.equal(cache.slots, slots)
+    cache.keep_new()
+    assert cache.kv_lens.tolist() == [60, 0, 1]
+    check_pages(cache)
+    now = contents(cache)
+    assert torch.equal(now[0][0][:, :, :40], before[0][0]) and same(now[2], before[2])
+    cache.plan(ints([0, 70, 0]))
+    cache.keep_new()
+    assert cache.err.tolist() == [0, 1, 0] and cache.kv_lens.tolist() == [60, 0, 1]  # (four pages are free, five wanted)
+    cache.plan(ints([0, 60, 0]))
+    cache.keep_new()
+    assert cache.err.tolist() == [0, 0, 0] and cache.kv_lens.tolist() == [60, 60, 1]
+    check_pages(cache)
+
+
+@pytest.mark.parametrize("forked", [False, True])
+def test_a_release_between_plan_and_commit(plain_forks, forked):  # noqa: F811
+    """One request ends, one was refused: the others' paths are committed whole, the two commit nothing."""
+    cache = filled_cache([15, 14, 16, 30], 8)
+    if forked:
+        cache.fork(ints([0, 1, 2, 3]))
+    cache.plan(ints([4, 4, 4, 4]))  # nine pages
+    assert cache.err.tolist() == [0, 0, 0, 1]
+    cache.release(1)
+    path = ints([[0, 1, 2, 3, 4, 5]] * 4)
+    k_trees, v_trees = trees(4, 6)
+    cache.commit(k_trees, v_trees, path, ints([4, 4, 4, 4]))
+    assert cache.kv_lens.tolist() == [19, 0, 20, 30] and cache.err.tolist() == [0, 1, 0, 1]
+    check_pages(cache)
+    for b in (0, 2):
+        for now, tree in zip(contents(cache)[b], (k_trees, v_trees)):
+            assert torch.equal(now[:, :, -4:], torch.stack([x[b][:, :4] for x in tree]))
+
+
+def test_a_fork_ends_a_planned_step(plain_forks):  # noqa: F811
+    cache = filled_cache([40, 16, 1], 12)
+    cache.plan(ints([20, 3, 0]), 23)
+    cache.fork(ints([0, 0, 2]))
+    lens, made = cache.kv_lens.tolist(), tables(cache)
+    assert lens == [40, 40, 1] and cache.slots is None and cache.positions is None
+    k_trees, v_trees = trees(3, 6)
+    x = torch.zeros((23, 2, 64))
+    for call in (cache.keep_new, lambda: cache.commit(k_trees, v_trees, ints([[0, 1, 2, 3, 4, 5]] * 3), ints([1, 1, 1])),
+                 lambda: cache.write(0, x, x, x, None, x, positions=torch.zeros((1, 23), dtype=torch.int32))):
+        with pytest.raises((RuntimeError, ValueError)):
+            call()
+    assert cache.kv_lens.tolist() == lens and tables(cache) == made and cache.err.tolist() == [0, 0, 0]
+    check_pages(cache)
+    cache.plan(ints([20, 3, 0]), 23)
+    cache.keep_new()
+    assert cache.kv_lens.tolist() == [60, 43, 1]
+    check_pages(cache)
+
+
+def test_a_fork_ends_a_step_whose_plan_was_recorded(plain_forks, monkeypatch):  # noqa: F811
+    """Whether its replay came before the fork or after it nobody can tell on the host: nothing is new until it has."""
+    cache = filled_cache([40, 16, 1], 12)
+    with monkeypatch.context() as m:
+        m.setattr(paged_step.PagedCache, "_recording", lambda self: True, raising=False)
+        cache.plan(ints([20, 3, 0]), 23)
+    cache.fork(ints([0, 0, 2]))
+    cache.keep_new()
+    assert cache.kv_lens.tolist() == [40, 40, 1]
+    check_pages(cache)
+
+
+def test_a_compaction_in_a_planned_step(plain_forks):  # noqa: F811
+    """Rows that have been written move along and are kept; slots of rows that have not are gone."""
+    cache = filled_cache([40, 16, 1], 30)
+    cache.release(0)
+    cache.plan(ints([0, 0, 20]), 20)
+    rows = cache.slots.long()
+    for x in (cache.k_pages, cache.v_pages):
+        x[:, rows // 16, :, rows % 16] = torch.randn((20, 2, 2, 64))
+    want = [[x[:, tables(cache)[b]].transpose(1, 2).flatten(2, 3)[:, :, :n].clone() for x in (cache.k_pages, cache.v_pages)]
+            for b, n in ((1, 16), (2, 21))]
+    cache.compact()
+    assert cache.slots is None and cache.positions is None
+    cache.keep_new()
+    assert cache.kv_lens.tolist() == [0, 16, 21] and cache.err.tolist() == [0, 0, 0]
+    check_pages(cache)
+    assert all(same(x, y) for x, y in zip(contents(cache)[1:], want))
