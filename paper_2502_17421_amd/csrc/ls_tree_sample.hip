@@ -397,7 +397,7 @@ struct Walk {
     double total;                          // the sum of the target's weights relative to its largest entry
     double per_total, per_draft_total;     // inverse sums
     double taken, mass, left;              // a, S, W
-    double rest;                           // what the sum has to pass in the writer's slice
+    double rest;                           // what the sum (of weights times the inverse sum) has to pass in the writer's slice
 };
 
 // What there is per node in LDS.  new_: of the path's n-th token in node n, its logit less the largest, and the sum of the weights.  kid_: the logits
@@ -753,6 +753,8 @@ tree_sample_kernel(SampleArgs)
                             if (inner && !args_here()->with_replacement) left = q_left;
                         }
 
+                        const double whole = part;
+
                         // The children that have not been tried.  Of tokens that were chosen the refused ones' probabilities are taken off the sums as long
                         // as much is left (then a pass over the rows makes the sums anew).
                         int found = -1;
@@ -797,6 +799,10 @@ tree_sample_kernel(SampleArgs)
                                 }
                             }
                         }
+                        // Sums that say whether a slice has any weight at all: those made after the refusals, of the weights that the draw looks at.  What a refusal
+                        // has been taken off may be a rounding of nothing, or nothing where something is left; and sums relative to other entries may be the
+                        // least numbers there are without any weight being one.
+                        const bool fresh = pass == kResidual && refused == uniform(walk.refused);
                         int next_pass = kRows, writer = 0;
                         if (found >= 0) {
                             if (lane == 0) {
@@ -820,7 +826,8 @@ tree_sample_kernel(SampleArgs)
                                 if (some) {
                                     writer = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);
                                     rest = point - of_lane(upto - part, writer);
-                                    next_pass = kDraw;
+                                    const bool unsure = __any(part < whole * 0x1p-32) || of_lane(part, writer) < 0x1p-900;
+                                    next_pass = fresh || !unsure ? kDraw : kResidual;
                                 }
                             }
                             if (lane == 0) {
@@ -841,21 +848,19 @@ tree_sample_kernel(SampleArgs)
             if (pass != kDraw) continue;
 
             // The first entry at which the sum of max(p - a q, 0) passes `rest`: its wave, run, lane, place.  Where roundings let none pass, the last one
-            // that has any weight.
-            const double rest = walk.rest;
-            // the residual's entries of a run, and their sum
+            // that has any weight.  Of the target's weights alone, which are summed as they are: a product with the inverse sum could round the least of them to 0.
+            const double rest = inner ? walk.rest : walk.rest * walk.total;
+            // the entries of a run, and their sum
             auto residual_run = [&](int r, double (&v)[RUN]) __attribute__((always_inline)) {
                 float l[RUN];
                 run_of_lds(x_lds + own + r * kWave * RUN).entries(l);
                 weights(l, top, heat, v);
-#pragma unroll
-                for (int e = 0; e < RUN; ++e) v[e] *= per_total;
                 if (inner) {
                     double w[RUN];
                     run_of_lds(y_lds + own + r * kWave * RUN).entries(l);
                     weights(l, draft_top, draft_heat, w);
 #pragma unroll
-                    for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e]), 0.0);
+                    for (int e = 0; e < RUN; ++e) v[e] = __builtin_fmax(__builtin_fma(-takes, w[e], v[e] * per_total), 0.0);
                 }
                 return sum_of(v);
             };
