@@ -750,7 +750,8 @@ tree_sample_kernel(SampleArgs)
                             taken = walk.taken, refused = uniform(walk.refused);
                             const double q_left = lanes_sum(part_q);
                             mass = lanes_sum(part);
-                            if (inner && !args_here()->with_replacement) left = q_left;
+                            // (a draft whose tokens have all been refused has q = 0 for the others: 1 in place of the 0 that would hide it)
+                            if (inner && !args_here()->with_replacement) left = q_left > 0 ? q_left : 1.0;
                         }
 
                         const double whole = part;
@@ -811,7 +812,7 @@ tree_sample_kernel(SampleArgs)
                                 walk.len = len + 1, walk.cur = found;
                             }
                         } else if (again) {
-                            if (inner && lane == 0) walk.taken = left > 0 ? fmin(taken + mass / left, 1e300) : 1e300;  // (finite: q(v) = 0 stays out of it)
+                            if (inner && lane == 0) walk.taken = fmin(taken + mass / left, 1e300);  // (finite: q(v) = 0 stays out of it)
                             if (!inner && lane == 0) walk.taken = 0;
                             next_pass = kResidual;
                         } else {  // the path ends here

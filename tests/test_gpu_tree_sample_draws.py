@@ -1,5 +1,5 @@
-"""Acceptance of drafted trees where a slice of the vocabulary has nothing left, or next to nothing: against the definition in more than 64 bits, by groups of
-workgroups and by workgroups alone."""
+"""Acceptance of drafted trees where a slice of the vocabulary, or the draft's distribution, has nothing left, or next to nothing: against the definition
+in more than 64 bits, by groups of workgroups and by workgroups alone."""
 import numpy as np
 import pytest
 import torch
@@ -71,3 +71,25 @@ def test_a_slice_of_the_least_weights_there_are(walks):
     got = {k: v.cpu() for k, v in c.run().items()}
     assert (got["err"] == 0).all() and (got["len"] == 1).all()
     assert ((got["next"] < 2000) & (got["next"] >= 0) | (got["next"] == 31000)).all(), got["next"]
+
+
+@pytest.mark.parametrize("with_replacement", [False, True])
+@pytest.mark.parametrize("vocab", [4, 9001, 50257])
+def test_children_behind_a_draft_that_is_used_up(walks, vocab, with_replacement):
+    """Drafts of one token, and of two, with three children: those that the draft cannot have drawn have q = 0, and are accepted if they have any
+    probability, in whatever order they come."""
+    orders = [(0, 1, 2), (1, 0, 2), (1, 2, 0), (0, 2, 1), (3, 0, 1), (0, 3, 1)]
+    c = Case(13, 12, 4, vocab, "f32", "f32", kind="star", with_replacement=with_replacement, temperature=[1.0] * 12)
+    at = np.array([0, 1, 2, 3]) if vocab == 4 else np.array([17, vocab // 3, vocab // 2, vocab - 5])
+    c.target[:] = -torch.inf
+    for b in range(12):
+        drawn = 1 + b // 6
+        c.target[b][:, torch.from_numpy(at[:3])] = torch.tensor([0.0, 0.1, -0.2])  # the last token has none
+        c.draft[b] = -torch.inf
+        c.draft[b][:, torch.from_numpy(at[:drawn])] = torch.tensor([0.4, 0.0])[:drawn]
+        c.tokens[b, 1:] = torch.from_numpy(at[list(orders[b % 6])].astype(np.int32))
+    for u in (0.9, 0.5, 1 - 2.0 ** -24):
+        c.accept_u[:] = u
+        c.run()
+        want = c.check()
+        assert (want["len"] == 2).any()
