@@ -800,10 +800,6 @@ tree_sample_kernel(SampleArgs)
                                 }
                             }
                         }
-                        // Sums that say whether a slice has any weight at all: those made after the refusals, of the weights that the draw looks at.  What a refusal
-                        // has been taken off may be a rounding of nothing, or nothing where something is left; and sums relative to other entries may be the
-                        // least numbers there are without any weight being one.
-                        const bool fresh = pass == kResidual && refused == uniform(walk.refused);
                         int next_pass = kRows, writer = 0;
                         if (found >= 0) {
                             if (lane == 0) {
@@ -827,8 +823,12 @@ tree_sample_kernel(SampleArgs)
                                 if (some) {
                                     writer = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);
                                     rest = point - of_lane(upto - part, writer);
-                                    const bool unsure = __any(part < whole * 0x1p-32) || of_lane(part, writer) < 0x1p-900;
-                                    next_pass = fresh || !unsure ? kDraw : kResidual;
+                                    next_pass = kDraw;
+                                    // Whether a slice has any weight at all is said by sums that are made after the refusals, of the weights that the draw looks
+                                    // at (what is left of a sum that a refusal has been taken off may be a rounding of nothing, or 0 where something is left;
+                                    // sums relative to other entries may be the least numbers there are without any weight being one).
+                                    const bool made = pass == kResidual && refused == uniform(walk.refused);
+                                    if (!inner && !made && (__any(part < whole * 0x1p-32) || of_lane(part, writer) < 0x1p-900)) next_pass = kResidual;
                                 }
                             }
                             if (lane == 0) {
