@@ -17,7 +17,7 @@ struct SampleArgs {
     int32_t batch, n_tree, vocab, with_replacement;
     int32_t slice, slices;  // entries of a slice of the vocabulary, and their number
     int32_t spin_limit;     // polls before a workgroup gives up on its group
-    uint32_t call;          // a number of this call's own
+    uint64_t call;          // a number of this call's own, not 0
     uint64_t *records;
 };
 constexpr int kSampleThreads = 256;  // (48 chains over 128256: 95 us, with 512 threads 108)
@@ -49,13 +49,13 @@ inline int sample_slice(int batch, int n_tree, int vocab, int target_bytes, int 
     }
     return slice;
 }
-// State, marks and two records a slice, in 64-bit words, per sequence; none where a sequence has one slice
+// State and count, and two records a slice, in 64-bit words, per sequence; none where a sequence has one slice
 inline size_t sample_record_bytes(int batch, int slices)
 {
-    return slices > 1 ? (size_t)batch * (8 + (slices + 7) / 8 * 8 + 16 * slices) * 8 : 0;
+    return slices > 1 ? (size_t)batch * (8 + 16 * slices) * 8 : 0;
 }
-// A 32-bit number that other calls hardly ever have
-uint32_t new_call_number();
+// A 64-bit number that no other call of this process has, others' hardly ever; not 0
+uint64_t new_call_number();
 hipError_t launch_tree_sample(const SampleArgs &a, int target_dtype, int draft_dtype, hipStream_t stream);
 
 // holder[page]: what the new tables hold it for: kNobody, kFull (some request, as a full page), or the lowest request that goes on in it.

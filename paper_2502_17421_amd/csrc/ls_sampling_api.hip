@@ -7,14 +7,15 @@
 
 namespace ls {
 
-uint32_t new_call_number()
+uint64_t new_call_number()
 {
     // calls of this process count on from where the clock and the process number say; a mixing of all bits keeps neighbours apart
     static std::atomic<uint64_t> count{(uint64_t)std::chrono::steady_clock::now().time_since_epoch().count() ^ (uint64_t)getpid() << 40};
     uint64_t z = count.fetch_add(0x9e3779b97f4a7c15ull, std::memory_order_relaxed);
     z = (z ^ z >> 30) * 0xbf58476d1ce4e5b9ull;
     z = (z ^ z >> 27) * 0x94d049bb133111ebull;
-    return (uint32_t)(z ^ z >> 31);
+    z ^= z >> 31;
+    return z ? z : 1;
 }
 
 namespace {
