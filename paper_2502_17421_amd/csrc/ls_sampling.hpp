@@ -49,10 +49,10 @@ inline int sample_slice(int batch, int n_tree, int vocab, int target_bytes, int 
     }
     return slice;
 }
-// State and count, and two records a slice, in 64-bit words, per sequence; none where a sequence has one slice
+// State, marks and two records a slice, in 64-bit words, per sequence; none where a sequence has one slice
 inline size_t sample_record_bytes(int batch, int slices)
 {
-    return slices > 1 ? (size_t)batch * (8 + 16 * slices) * 8 : 0;
+    return slices > 1 ? (size_t)batch * (8 + (slices + 7) / 8 * 8 + 16 * slices) * 8 : 0;
 }
 // A 64-bit number that no other call of this process has, others' hardly ever; not 0
 uint64_t new_call_number();

@@ -266,19 +266,20 @@ __device__ __forceinline__ int lanes_min(int x)
 // tag each in the upper half of 64 bits.  A word is written and read at once, so its tag says that its value is there, and no fence is needed; two
 // sets of records take turns, since nobody is at exchange n + 2 before everybody has read those of n.
 //
-// Tags follow from a 64-bit number of the call's own, from a count in the workspace, and from the number of the exchange; that of a half record's last word
-// from a checksum of its values too.  What the workspace held before does not pass for a record: of another call with a chance of 2^-64; of the same call
-// replayed by a graph, whose number is the same, because of the count.  Whoever has written a sequence's outputs adds 1 to its count, so every launch leaves another
-// one than it found, and another one than anybody in it has read: who reads a count works with those who read the same, and whichever of them ends the walk, or the
-// one that they have left it to, adds to it later.  So records are never cleared, and one that comes late, from a workgroup that has been given up, can stay.
-// (Clearing them at the end, when everybody had left a mark, let such a one stay for the next replay to take.  A kernel that cleared them beforehand took 5 us of
-// each call.)
+// Tags are the halves of a 64-bit number of the call's own, in turns, plus the number of the exchange; that of a half record's last word with a checksum of its
+// values.  What the workspace held before does not pass for a record (with a chance of 2^-64).  A graph that is replayed has the same number again, so no record
+// may be there when a launch ends:
+// - Whoever writes the outputs clears all records at the end, once the others have left their marks that they have read all they need.
+// - Whoever gives up on the group clears its own first of all, so that what it has told late does not stay.
+// That is enough.  A workgroup that gets to the end with the group, and does not write, has heard the others in its last exchange after it has told them.  If
+// the writer got there too, it has heard this one, and clears it.  If not, it gave up in that same exchange, and its record was heard before it cleared it; whoever
+// walked alone for it cleared everything after that.  (Marks may stay, of late ones.  They let the writer of a replay clear too early; who has not
+// read by then gives up and walks alone.)  A kernel that cleared the records beforehand took 5 us of each call.
 //
 // The workgroups of a group are next to each other in the launch, so that all of the first group that is not done yet are on the card, or
 // will be when what else runs there is done.  No wait is unbounded all the same: who has polled spin_limit times gives up on
 // the group, and the first of them (the state word says so) walks the tree alone, slice after slice, with the same sums in the same order.
-// What it writes are the bits that the group writes if it gets to the end after all.  At the end it takes its word off the state first and adds to the count
-// afterwards: who has still read the word has read the count before.
+// What it writes are the bits that the group writes if it gets to the end after all.
 constexpr int kRecordWords = 8;  // of p: 0 largest entry, 1-2 sum, 3 where the largest is; 4-7 the same of q
 
 struct Half {
@@ -290,22 +291,23 @@ struct Half {
 };
 
 struct Exchange {
-    uint64_t *words;  // of the sequence: [8] state, count; [2][slices][kRecordWords] records
+    uint64_t *words;  // of the sequence: [8] state, [slices up to a multiple of 8] marks, [2][slices][kRecordWords] records
     int slices, slice;
     uint64_t call;
-    uint32_t even, odd, number;  // tags of even and of odd words, less the number of the exchange
+    uint32_t number;
 
-    __device__ __forceinline__ uint64_t *record(int of) const { return words + 8 + ((number & 1) * slices + of) * kRecordWords; }
+    __device__ __forceinline__ uint64_t *marks() const { return words + 8; }
+    __device__ __forceinline__ uint64_t *record(int of) const
+    {
+        return words + 8 + (slices + 7) / 8 * 8 + ((number & 1) * slices + of) * kRecordWords;
+    }
+    __device__ __forceinline__ int n_words() const { return 8 + (slices + 7) / 8 * 8 + 2 * slices * kRecordWords; }
     static __device__ __forceinline__ void put(uint64_t *at, uint64_t word)
     {
         __hip_atomic_store(at, word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     static __device__ __forceinline__ uint64_t get(const uint64_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-    __device__ __forceinline__ void start(uint64_t count)
-    {
-        even = (uint32_t)call + (uint32_t)count * 0x9e3779b1u, odd = (uint32_t)(call >> 32) + (uint32_t)count * 0x85ebca77u;
-    }
     __device__ __forceinline__ bool somebody_alone() const { return get(words) == call; }
     // true for the first one of the call
     __device__ __forceinline__ bool go_alone() const
@@ -317,26 +319,24 @@ struct Exchange {
                 return true;
         return false;
     }
-    // by one thread
-    __device__ __forceinline__ void end(bool alone) const
-    {
-        if (alone) {
-            put(words, 0);
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-        }
-        __hip_atomic_fetch_add((unsigned long long *)words + 1, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
     // lanes first .. first + 3 have the values of half `which`, lane by lane
     __device__ __forceinline__ void tell(int which, int lane_of_four, uint32_t value, uint32_t check) const
     {
-        const uint32_t t = ((lane_of_four & 1 ? odd : even) + number) ^ (lane_of_four == 3 ? check : 0u);
-        if (lane_of_four >= 0 && lane_of_four < 4) put(record(slice) + 4 * which + lane_of_four, (uint64_t)t << 32 | value);
+        const uint32_t tag = ((lane_of_four & 1 ? (uint32_t)(call >> 32) : (uint32_t)call) + number) ^ (lane_of_four == 3 ? check : 0u);
+        if (lane_of_four >= 0 && lane_of_four < 4) put(record(slice) + 4 * which + lane_of_four, (uint64_t)tag << 32 | value);
+    }
+    // (by the lanes that have told it) this workgroup's records, before anything that follows
+    __device__ __forceinline__ void take_back(int lane) const
+    {
+        uint64_t *const mine = words + 8 + (slices + 7) / 8 * 8 + slice * kRecordWords + lane;
+        if (lane < kRecordWords) put(mine, 0), put(mine + slices * kRecordWords, 0);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
     }
     // lane i reads what slice i says (of q only if `both`); false: given up
     __device__ __forceinline__ bool hear(int lane, bool both, int spin_limit, Half &p, Half &q) const
     {
         const uint64_t *from = record(lane < slices ? lane : 0);
-        const uint32_t t = even + number, t_odd = odd + number;
+        const uint32_t tag = (uint32_t)call + number, odd_tag = (uint32_t)(call >> 32) + number;
         for (int poll = 0; poll < spin_limit; ++poll) {
             uint64_t word[8] = {};
 #pragma unroll
@@ -349,17 +349,24 @@ struct Exchange {
 #pragma unroll
             for (int i = 0; i < 4; ++i) p.value[i] = (uint32_t)word[i];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) there &= (uint32_t)(word[i] >> 32) == ((i & 1 ? t_odd : t) ^ (i == 3 ? p.check() : 0u));
+            for (int i = 0; i < 4; ++i) there &= (uint32_t)(word[i] >> 32) == ((i & 1 ? odd_tag : tag) ^ (i == 3 ? p.check() : 0u));
             if (both) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) q.value[i] = (uint32_t)word[4 + i];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) there &= (uint32_t)(word[4 + i] >> 32) == ((i & 1 ? t_odd : t) ^ (i == 3 ? q.check() : 0u));
+                for (int i = 0; i < 4; ++i) there &= (uint32_t)(word[4 + i] >> 32) == ((i & 1 ? odd_tag : tag) ^ (i == 3 ? q.check() : 0u));
             }
             if (__all(there)) return true;
             if ((poll & 15) == 15 && somebody_alone()) return false;
         }
         return false;
+    }
+    __device__ __forceinline__ void leave_mark() const { put(marks() + slice, call); }
+    // (by a wave) the others' marks are there, or it has been long enough: then they find nothing and walk alone
+    __device__ __forceinline__ void wait_for_marks(int lane, int spin_limit) const
+    {
+        for (int poll = 0; poll < spin_limit; ++poll)
+            if (__all(lane >= slices || lane == slice || get(marks() + lane) == call)) return;
     }
 };
 
@@ -438,7 +445,7 @@ tree_sample_kernel(SampleArgs)
     const int b = blockIdx.y, tid = threadIdx.x, wave = uniform(tid >> 6);
     Exchange ex;
     ex.slices = slices, ex.slice = blockIdx.x, ex.call = a->call, ex.number = 0;
-    ex.words = a->records + (int64_t)b * (8 + 2 * slices * kRecordWords);
+    ex.words = a->records + (int64_t)b * ex.n_words();
     const int n_nodes = (a->n_tree + kWave - 1) / kWave * kWave, slice_size = a->slice;
     Node *const nodes = (Node *)lds;
     TT *const x_lds = (TT *)(nodes + n_nodes);
@@ -459,7 +466,6 @@ tree_sample_kernel(SampleArgs)
         my_parent[n] = my_tok[n] = -1, my_u[n] = 0.f;
         if (node < a->n_tree) my_parent[n] = a->parents[at], my_tok[n] = a->draft_tokens[at], my_u[n] = a->accept_uniforms[at];
     }
-    const uint64_t count = told ? Exchange::get(ex.words + 1) : 0;
     float temp = a->temperature[b], draft_temp = a->draft_temperature ? a->draft_temperature[b] : temp;
     bool bad = false;
 #pragma unroll
@@ -487,7 +493,6 @@ tree_sample_kernel(SampleArgs)
     const double draft_heat = drawn ? 1.4426950408889634074 / (double)draft_temp : 0.0;
     __syncthreads();
     err |= uniform(flag_sh);
-    ex.start(uniform(count));
 
     // A thread's entries: runs of 4, the lanes' runs side by side; a wave's are contiguous.  What a thread reads of its runs in LDS it has written itself.
     const int wave_size = slice_size / WAVES, runs = wave_size / (kWave * RUN);
@@ -927,6 +932,7 @@ tree_sample_kernel(SampleArgs)
 
     bool alone = false;
     if (!walk_tree(std::false_type{})) {  // the first one to give up goes on alone, from the root
+        if (wave == 0) ex.take_back(tid);
         __syncthreads();
         if (tid == 0) {
             flag_sh = ex.go_alone();
@@ -941,7 +947,10 @@ tree_sample_kernel(SampleArgs)
 
     // The outputs
     const ArgsHere h = args_here();
-    if (!alone && uniform(walk.writer) != ex.slice) return;
+    if (!alone && uniform(walk.writer) != ex.slice) {
+        if (tid == 0) ex.leave_mark();
+        return;
+    }
     const int len = uniform(walk.len), next = uniform(walk.next);
     if (tid == 0) {
         if (next >= 0) {
@@ -956,12 +965,15 @@ tree_sample_kernel(SampleArgs)
         if (h->err_flag) h->err_flag[b] = err;
     }
     __syncthreads();
+    if (told && !alone && wave == WAVES - 1) ex.wait_for_marks(tid & 63, h->spin_limit);
     for (int i = tid; i < h->n_tree; i += NT) {
         const int64_t at = (int64_t)b * h->n_tree + i;
         h->path[at] = nodes[i].path;
         if (h->logprobs) h->logprobs[at] = i < len ? (float)(nodes[i].new_logit / (greedy ? 1.0 : (double)temp) - log(nodes[i].new_total)) : 0.f;
     }
-    if (told && tid == 0) ex.end(alone);
+    if (!told) return;
+    __syncthreads();
+    for (int i = tid; i < ex.n_words(); i += NT) Exchange::put(ex.words + i, 0);
 }
 
 template <typename TT, typename TD> hipError_t launch_types(const SampleArgs &a, hipStream_t stream)
