@@ -101,19 +101,73 @@ template <typename... A> struct Typed<int (*)(A...)> {
     }
 };
 
+// Whether the tensors of a call are what its descriptor says; false: a Python error is set.  (Other objects with a data_ptr() are taken as they are.)
+bool refuse(const char *name, const char *expected, int64_t batch, int64_t each)
+{
+    if (each == 1) PyErr_Format(PyExc_ValueError, "%s: expected %s [%lld], contiguous, beside the logits", name, expected, (long long)batch);
+    else PyErr_Format(PyExc_ValueError, "%s: expected %s [%lld, %lld], contiguous, beside the logits", name, expected, (long long)batch, (long long)each);
+    return false;
+}
+bool entries_fit(PyObject *obj, const char *name, at::ScalarType type, int64_t batch, int64_t each, const at::Tensor *beside)
+{
+    if (obj == Py_None || !THPVariable_Check(obj)) return true;
+    const at::Tensor &x = THPVariable_Unpack(obj);
+    if (x.scalar_type() == type && x.numel() == batch * each && (!beside || x.get_device() == beside->get_device()) && x.is_contiguous() &&
+        (each == 1 || x.dim() < 2 || x.size(-1) == each))
+        return true;
+    return refuse(name, type == at::kInt ? "int32" : "float32", batch, each);
+}
+bool logits_fit(PyObject *obj, const char *name, int32_t dtype, const int64_t *stride, const ls_sample_desc &d, const at::Tensor *beside)
+{
+    if (obj == Py_None || !THPVariable_Check(obj)) return true;
+    const at::Tensor &x = THPVariable_Unpack(obj);
+    const at::ScalarType type = dtype == LS_BF16 ? at::kBFloat16 : dtype == LS_F16 ? at::kHalf : at::kFloat;
+    if (x.scalar_type() == type && x.dim() == 3 && x.size(0) == d.batch && x.size(1) == d.n_tree && x.size(2) == d.vocab && (!beside || x.get_device() == beside->get_device()) &&
+        (d.vocab == 1 || x.stride(2) == 1) && (d.batch == 1 || x.stride(0) == stride[0]) && (d.n_tree == 1 || x.stride(1) == stride[1]))
+        return true;
+    PyErr_Format(PyExc_ValueError, "%s: not the tensor that the descriptor was made for", name);
+    return false;
+}
+bool sampled_fits(PyObject *const *args)
+{
+    const ls_sample_desc *d = nullptr;
+    if (!convert(args[0], d, false)) return false;
+    try {
+        const at::Tensor *const beside = THPVariable_Check(args[3]) ? &THPVariable_Unpack(args[3]) : nullptr;
+        const struct {
+            int at;
+            const char *name;
+            at::ScalarType type;
+            int64_t each;
+        } entries[] = {{1, "parents", at::kInt, d->n_tree}, {2, "draft_tokens", at::kInt, d->n_tree}, {5, "temperature", at::kFloat, 1},
+                       {6, "draft_temperature", at::kFloat, 1}, {7, "accept_uniforms", at::kFloat, d->n_tree}, {8, "sample_uniforms", at::kFloat, 1},
+                       {9, "accept_path", at::kInt, d->n_tree}, {10, "accept_len", at::kInt, 1}, {11, "next_token", at::kInt, 1},
+                       {12, "logprobs", at::kFloat, d->n_tree}, {13, "err_flag", at::kInt, 1}};
+        for (const auto &e : entries)
+            if (!entries_fit(args[e.at], e.name, e.type, d->batch, e.each, beside)) return false;
+        return logits_fit(args[3], "target_logits", d->target_dtype, d->target_stride, *d, beside) &&
+               logits_fit(args[4], "draft_logits", d->draft_dtype, d->draft_stride, *d, beside);
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_ValueError, e.what());
+        return false;
+    }
+}
+
 struct Entry {
     const char *name;
     Invoke invoke;
     int count;
+    bool (*fits)(PyObject *const *);
 };
-#define LS_ENTRY(NAME) {#NAME, &Typed<decltype(&NAME)>::invoke, Typed<decltype(&NAME)>::count}
+#define LS_CHECKED_ENTRY(NAME, FITS) {#NAME, &Typed<decltype(&NAME)>::invoke, Typed<decltype(&NAME)>::count, FITS}
+#define LS_ENTRY(NAME) LS_CHECKED_ENTRY(NAME, nullptr)
 const Entry kEntries[] = {
     LS_ENTRY(ls_hybrid_tree_attn), LS_ENTRY(ls_hybrid_tree_attn_single), LS_ENTRY(ls_hybrid_tree_attn_static),
     LS_ENTRY(ls_hybrid_tree_attn_fused), LS_ENTRY(ls_hybrid_tree_attn_paged), LS_ENTRY(ls_workspace_init),
     LS_ENTRY(ls_cache_attn), LS_ENTRY(ls_cache_attn_paged), LS_ENTRY(ls_build_tree_mask), LS_ENTRY(ls_prefix_attn_splitkv),
     LS_ENTRY(ls_tree_attn_masked), LS_ENTRY(ls_lse_merge), LS_ENTRY(ls_tree_accept_greedy), LS_ENTRY(ls_kv_commit),
     LS_ENTRY(ls_kv_commit_paged), LS_ENTRY(ls_page_plan), LS_ENTRY(ls_rope), LS_ENTRY(ls_rope_store_paged),
-    LS_ENTRY(ls_chunk_attn_paged), LS_ENTRY(ls_tree_accept_sampled), LS_ENTRY(ls_page_fork), LS_ENTRY(ls_page_compact),
+    LS_ENTRY(ls_chunk_attn_paged), LS_CHECKED_ENTRY(ls_tree_accept_sampled, sampled_fits), LS_ENTRY(ls_page_fork), LS_ENTRY(ls_page_compact),
     LS_ENTRY(ls_page_copy),
 };
 
@@ -133,6 +187,7 @@ PyObject *caller_call(PyObject *self, PyObject *const *args, size_t nargsf, PyOb
         PyErr_Format(PyExc_TypeError, "%s takes %d positional arguments", c->entry->name, c->entry->count);
         return nullptr;
     }
+    if (c->entry->fits && !c->addresses && !c->entry->fits(args)) return nullptr;
     return c->entry->invoke(c->fn, args, c->addresses);
 }
 
