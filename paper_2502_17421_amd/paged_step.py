@@ -67,6 +67,11 @@ class PagedCache:
             kept.append(torch.empty(max([size] + [2 * x.numel() for x in kept]), dtype=dtype, device=self.k_pages.device))
         return kept[-1]
 
+    def _check_ints(self, names, *given):
+        for x in given:
+            if x.shape != self.kv_lens.shape or x.dtype != torch.int32 or x.device != self.kv_lens.device or not x.is_contiguous():
+                raise ValueError(f"{names}: int32 [{self.batch}], contiguous, on the cache's device")
+
     # ---- the requests' lengths
 
     def release(self, request):
@@ -116,9 +121,7 @@ class PagedCache:
         Full pages are shared, of a page filled in part every request but one gets a copy, and pages that nobody holds any more are free
         at once, those that a plan reserved among them: the step is over, and what comes next has to be planned.
         err: 1 where no page was left for the copy (the request then ends with its full pages), 2 for sources or lengths that are none."""
-        for x in (sources,) if keep_lens is None else (sources, keep_lens):
-            if x.shape != self.kv_lens.shape or x.dtype != torch.int32:
-                raise ValueError(f"sources, keep_lens: int32 [{self.batch}]")
+        self._check_ints("sources, keep_lens", *((sources,) if keep_lens is None else (sources, keep_lens)))
         self._move_rows(self._fork(sources, keep_lens, self.err))
         self.slots = self.positions = None
         self.total_lens.copy_(self.kv_lens)  # (of a recorded plan: nothing is new)
@@ -140,8 +143,7 @@ class PagedCache:
     def plan(self, new_lens, n_tokens=0):
         """Pages for new_lens (int32 [batch], device) more rows of each request; with n_tokens, the packed tokens' slots and
         positions as well.  err says which requests were refused (they keep what they have)."""
-        if new_lens.shape != self.kv_lens.shape or new_lens.dtype != torch.int32:
-            raise ValueError(f"new_lens: int32 [{self.batch}]")
+        self._check_ints("new_lens", new_lens)
         self.slots = self.positions = None
         self._ended, self._recorded = False, self._recorded or self._recording()
         if n_tokens:

@@ -143,3 +143,16 @@ def test_a_compaction_in_a_planned_step(plain_forks):  # noqa: F811
     assert cache.kv_lens.tolist() == [0, 16, 21] and cache.err.tolist() == [0, 0, 0]
     check_pages(cache)
     assert all(same(x, y) for x, y in zip(contents(cache)[1:], want))
+
+
+def test_forks_and_plans_refuse_columns_and_other_devices(plain_forks):  # noqa: F811
+    """A column of a table of beams is not one number after the other, which is what is read."""
+    cache = filled_cache([40, 16, 1], 12)
+    table = ints([[0, 2], [0, 2], [1, 2]])
+    for sources, keep in ((table[:, 0], None), (table[:, 0].contiguous(), table[:, 1]), (table[:, 0].contiguous().to("meta"), None)):
+        with pytest.raises(ValueError):
+            cache.fork(sources, keep)
+        with pytest.raises(ValueError):
+            cache.plan(sources if keep is None else keep)
+    cache.fork(table[:, 0].contiguous())
+    assert cache.kv_lens.tolist() == [40, 40, 16]
