@@ -559,7 +559,7 @@ typedef struct {
     int32_t n_tree;            /* 1 .. LS_MAX_TREE */
     int32_t vocab;             /* 1 .. LS_MAX_VOCAB */
     int32_t target_dtype;      /* ls_dtype of the target's logits */
-    int32_t draft_dtype;       /* ls_dtype of the draft's logits (any where there are none) */
+    int32_t draft_dtype;       /* ls_dtype of the draft's logits (any of them where there are none) */
     int32_t with_replacement;  /* 0: the children of a node are different tokens, drawn one after the other without those before;
                                   else independent draws, in which a token may come twice */
     int64_t target_stride[2], draft_stride[2];  /* elements, (sequence, node); rows need no alignment but their elements' */
@@ -578,8 +578,9 @@ int ls_sample_workspace_bytes(const ls_sample_desc *desc, size_t *bytes_out);
  * positive part of p - q and, without replacement, q loses x and is normalised again.  If no child is accepted (a leaf has none) the path ends,
  * and the next token is drawn from p: the first one at which the cumulated probability passes sample_uniforms times their sum.
  * Tokens that were chosen and not drawn (the likeliest ones of a beam) have q(x) = 1: accepted if accept_uniforms[i] < p(x), else p loses x.
- * All arithmetic on probabilities is in 64 bits; a
- * token whose weight is below 2^-1074 of the likeliest one's has none.  Only the rows of nodes that the path reaches are read, of a last node that is a leaf the target's alone.
+ * (Where q(x) is 0: if p(x) > 0.)
+ * All arithmetic on probabilities is in 64 bits, their exponentials are right to 4e-14 of their value (some 44 bits); a
+ * token whose weight is below 2^-1074 of the likeliest one's has none, below 2^-1000 it may have none.  Only the rows of nodes that the path reaches are read, of a last node that is a leaf the target's alone.
  * A sequence's vocabulary is dealt to several workgroups, which wait for each other's sums, a bounded number of polls
  * (ls_set_single_launch_polls); one that waits longer walks its tree alone.  The results have the same bits either way.
  *   parents, draft_tokens  DEVICE int32[batch, n_tree], as for ls_tree_accept_greedy; a child whose token is outside

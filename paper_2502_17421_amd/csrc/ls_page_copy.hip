@@ -13,7 +13,8 @@ namespace {
 constexpr int NT = 256;
 constexpr int BATCH = 4;
 constexpr int kGroups = 16384;  // a unit each, up to so many (900 pages: 187 us, with 2048 groups that take several 195)
-// Fewer pages than kUnits are cut into shares of kLeast bytes or more: 32 of 1 MB 27.7 -> 12.6 us, 654 of up to 512 KB 81 -> 71, 1600 of up to 256 KB 102 -> 97 (shares of
+// Fewer pages than kUnits, by max_copies, which the host knows (a bound far above n_copies leaves each page in one piece),
+// are cut into shares of kLeast bytes or more: 32 of 1 MB 27.7 -> 12.6 us, 654 of up to 512 KB 81 -> 71, 1600 of up to 256 KB 102 -> 97 (shares of
 // 16 KB for any number of pages: 1280 of up to 64 KB 34.7 -> 39).
 constexpr int kUnits = 8192, kLeast = 16 * 1024;
 

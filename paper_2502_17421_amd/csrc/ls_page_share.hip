@@ -619,7 +619,8 @@ compact_one_kernel(CompactArgs a, bool parts)
 
 constexpr int kOneLds = 156 * 1024;
 // Up to these one workgroup (fork), or each (compaction), goes through the tables.  Forks of 64 requests with 250 pages each: 12.5 us, in four
-// launches 15.6; 500 pages 18.8 and 16.8; 128 requests with 60 pages 16.1 and 14.9.
+// launches 15.6; 128 requests with 60 pages 16.1 and 14.9.  The host knows the tables' width and not what is held: of 64 requests with a width of 500, one launch takes
+// 9.8 us and four 13.6 where 8 of them hold as much (prompts that become samples), but 18.8 and 16.8 where all do.  The limit is for the former.
 constexpr int kForkRequests = 64;
 constexpr int64_t kForkCells = 1 << 15, kCompactCells = 1 << 16;
 constexpr int kCompactRequests = 128;  // 512 requests with 125 pages: each on its own 16.4 us, by parts 10.8; 64 with 500: 9.3 and 10.8

@@ -20,7 +20,7 @@ struct SampleArgs {
     uint64_t call;          // a number of this call's own, not 0
     uint64_t *records;
 };
-constexpr int kSampleThreads = 256;  // (48 chains over 128256: 95 us, with 512 threads 108)
+constexpr int kSampleThreads = 256;  // (48 chains over 128256, in the form of the time: 95 us, with 512 threads 108)
 constexpr int kSampleSlices = 64;                   // at most
 constexpr int kSampleUnit = kSampleThreads * 4;     // entries: slices are multiples
 constexpr int kSampleLds = 156 * 1024;              // dynamic LDS, at most
@@ -31,7 +31,8 @@ inline int sample_lds_bytes(int n_tree, int slice, int target_bytes, int draft_b
 }
 static_assert(LS_MAX_TREE * kSampleNode + LS_MAX_VOCAB / kSampleSlices * 8 <= kSampleLds, "every vocabulary fits");
 constexpr int kSampleOtherLds = 3 * 1024;  // beside it, at most
-// The smallest slices with which all workgroups of the call fit on the card at a time; if none do, the largest of which four fit on a compute unit.
+// The smallest slices with which all workgroups of the call fit on the card at a time; if none do, the largest of which four fit on a compute unit.  (Tokens that were
+// chosen have no draft's row in LDS, but the descriptor does not say so: for them the slices are smaller than they could be.)
 // One chain of 3 tokens over 32000: 19.0 us, with slices of twice the size 20.9; 96 of them 44, with no more than two workgroups on a compute unit 55.  Where not all
 // fit (bf16, chains of 3 over 128256, 128 of them; of 2 over 32000, 300 of them) four on a compute unit take 137 and 77 us, two 172 and 123, eight with slices of half
 // the size 205 and 95.

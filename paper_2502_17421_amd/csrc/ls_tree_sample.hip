@@ -22,9 +22,11 @@
 // same order.  See Exchange.
 //
 // What bounds it: one request and few trees, the passes' chain: each waits for a row (1 us), its sums, the others' sums (1 us) and the decision (1.5 us).
-// One request, 22 nodes of 32000 in half: 22.7 us (one workgroup by itself 189).  Four beam trees of 69 nodes of 32000 in float 22.9.  Many requests, the
-// weights: 18 instructions of 64 bits each, 2 ns for a wave on a SIMD, and waits that four workgroups on a compute unit do not all cover.  48 chains of 5 tokens over 128256
-// in bf16: 87 us, of which the vector ALUs are busy 45 % (107 MB: 21 us at the rate of a copy); 16 trees over 152064: 69 us.
+// One request, 22 nodes of 32000 in half: 22 to 28 us by how far its path goes (one workgroup by itself 189).  Four beam trees of 69 nodes of 32000 in float 17 to 23.
+// Many requests, the weights: 18 instructions of 64 bits each, 2 ns for a wave on a SIMD, and waits that four workgroups on a compute unit do not all cover.  48 chains
+// of 5 tokens over 128256 in bf16: 87 to 91 us, of which the vector ALUs are busy 45 to 50 (107 MB: 21 us at the rate of a copy); 16 trees over 152064: 58 to 73 us.  The walk
+// of a group and that of a workgroup alone are code of their own, from one source; together they spill 75 to 80 scalar registers, into lanes of vector
+// registers and never to memory.
 // Tried, and not faster than the form of the time: the next child's rows asked for ahead (chains 95.0 us for 93.4), two polls in flight (16 trees 73.5 for
 // 69.8), eight weights of a thread at a time (chains 116 for 98).
 #include <float.h>
